@@ -304,6 +304,176 @@ GRAFT_API int graft_commit_accepted(graft_ctx *ctx, int32_t batch, const int32_t
                                     int64_t dst_batch_stride, int64_t dst_row_stride,
                                     graft_stream_t stream);
 
+/* ------------------------------------------------------------------------ */
+/* The verifier's step around a draft block: attention of the block over the   */
+/* cache, the sampled walk, and the cache's rows (plain or quantised).          */
+/* ------------------------------------------------------------------------ */
+
+/* Element types of the calls below. */
+#define GRAFT_F32 0
+#define GRAFT_BF16 1
+#define GRAFT_F16 2
+#define GRAFT_E4M3 3   /* 8 bits: sign, 4 exponent bits (bias 7), 3 of the fraction; no
+                          infinities, 0x7F and 0xFF are NaN; largest 448 */
+
+/* Rows of heads in strided memory: element (plane, b, row, head, i) is
+ * data[plane * plane_stride + b * batch_stride + row * row_stride + head *
+ * head_stride + i], strides in elements, unit stride along i < head_dim.  data
+ * is 16-byte aligned and every stride is non-negative and a multiple of 16
+ * bytes.  E4M3 rows have one scale a (plane, b, row, head), a byte s at the
+ * scale strides (in bytes) that stands for 2^(s - 127): the numbers are code *
+ * 2^(s - 127).  scale and its strides are ignored for other types. */
+typedef struct {
+    void *data;
+    int64_t plane_stride, batch_stride, row_stride, head_stride;
+    uint8_t *scale;
+    int64_t scale_plane_stride, scale_batch_stride, scale_row_stride, scale_head_stride;
+} graft_rows;
+
+/* Attention of a draft block.  Sequence b has S_b = n_nodes[b] + (with_root != 0)
+ * slots: slot 0 is the root (the last committed token, whose key and value are
+ * not in the cache yet) with with_root != 0, and the tree's nodes follow in
+ * canonical order.  Every slot attends to
+ *   - the shared prefix, rows 0 .. shared_len - 1, the same for the whole batch;
+ *   - the sequence's own cache, rows 0 .. cache_len[b] - 1;
+ *   - the block's slots it sees: a node sees itself, its ancestors (bit j of
+ *     mask row i, as graft_build_tree writes it) and the root; the root sees
+ *     itself.  With mask NULL the block is a chain: slot j <= i.
+ * Query head h reads key/value head h / (q_heads / kv_heads):
+ *   out[b, i, h] = sum_j p_j v_j,  p = softmax_j(scale q_i . k_j),
+ *   lse[b, i, h] = log sum_j exp(scale q_i . k_j)  (natural logarithm).
+ * A slot that sees nothing gets zeros and an lse of -inf.  Keys and values of
+ * slots it does not see never reach it, whatever they hold.  Rows of out and
+ * lse from slot S_b on are left as they were.
+ * Sums and softmax statistics are fp32; the probabilities are rounded to dtype
+ * for the product with v.  The result is the same bits for the same arguments.
+ * Plane strides are ignored. */
+typedef struct {
+    int32_t batch;               /* 1..max_batch */
+    int32_t slots;               /* rows of q, k, v, out a sequence: 1..max_nodes + 1 with a
+                                    root, 1..max_nodes without */
+    int32_t with_root;
+    int32_t q_heads, kv_heads;   /* q_heads a multiple of kv_heads, at most 1024 */
+    int32_t head_dim;            /* a multiple of 16, 16..128 */
+    int32_t dtype;               /* q, k, v, out: GRAFT_BF16 or GRAFT_F16 */
+    int32_t cache_dtype;         /* cache and shared prefix: dtype, or GRAFT_E4M3 with BF16 */
+    float scale;                 /* finite, > 0 */
+    graft_rows q, k, v;          /* [batch, slots, q_heads or kv_heads, head_dim] */
+    const int32_t *n_nodes;      /* [batch] */
+    const uint64_t *mask;        /* [batch, max_nodes, ceil(max_nodes/64)] or NULL (chain) */
+    graft_rows cache_k, cache_v; /* [batch, cache_rows, kv_heads, head_dim]; cache_rows 0: none */
+    int32_t cache_rows;
+    const int32_t *cache_len;    /* [batch] (ignored when cache_rows is 0) */
+    graft_rows shared_k, shared_v; /* [shared_len, kv_heads, head_dim]; shared_len 0: none */
+    int32_t shared_len;
+    graft_rows out;              /* [batch, slots, q_heads, head_dim]; no overlap with inputs */
+    float *lse;                  /* [batch, slots, q_heads] or NULL */
+    void *workspace;             /* 16-byte aligned, graft_tree_attention_workspace bytes */
+    int64_t workspace_bytes;
+} graft_attention;
+
+/* *bytes (host) receives the workspace that graft_tree_attention needs for
+ * these sizes (pointers in *a are not looked at); it may be 0. */
+GRAFT_API int graft_tree_attention_workspace(graft_ctx *ctx, const graft_attention *a /* host */,
+                                             int64_t *bytes /* host */);
+
+/* The attention above on `stream`.  The workspace belongs to the call until its
+ * work is done: calls that may overlap (other streams, other captured graphs)
+ * need workspaces of their own.  It needs no clearing.  n_nodes[b] outside 0 ..
+ * slots - with_root and cache_len[b] outside 0 .. cache_rows are clamped and
+ * reported by graft_get_device_status. */
+GRAFT_API int graft_tree_attention(graft_ctx *ctx, const graft_attention *a /* host */,
+                                   graft_stream_t stream);
+
+/* The target model's logits for the sampled walk.  Row of the root of sequence
+ * b: root + b * root_stride; of node i < node_rows: node + b *
+ * node_batch_stride + i * node_row_stride; vocab elements each, strides in
+ * elements, any alignment that the type has. */
+typedef struct {
+    int32_t dtype;               /* GRAFT_F32, GRAFT_BF16 or GRAFT_F16 */
+    const void *root;
+    int64_t root_stride;
+    const void *node;            /* may be NULL with node_rows 0 */
+    int64_t node_batch_stride, node_row_stride;
+    int32_t node_rows;           /* 0..max_nodes; nodes from there on are not part of the tree */
+    const float *temperature;    /* [batch] or NULL (1) */
+    const double *uniform;       /* [batch, L + 1] random numbers in [0, 1) */
+} graft_target_logits;
+
+/* *bytes (host) receives the workspace of graft_accept_sampled. */
+GRAFT_API int graft_accept_sampled_workspace(graft_ctx *ctx, int32_t batch,
+                                             int64_t *bytes /* host */);
+
+/* The sampled acceptance walk: graft_accept with tokens drawn from the target
+ * model.  At the root, and at every node the walk reaches, a token is drawn from
+ * p(v) = e_v / sum e, e_v = exp((z_v - max z) / T), with the level's random
+ * number u = uniform[b, level]:
+ *   x = min{v : sum_{w <= v} e_w > u sum e}
+ * (u outside [0, 1) gives the first or last token of positive probability, a NaN
+ * the last); T = 0 takes the largest logit, ties to the lowest index.  A child
+ * of the node with token x is accepted and the walk goes on there; else x is the
+ * bonus token.  The tree is a function of the drafter's logits, not drawn from
+ * them, so this keeps the target's distribution: it is the acceptance test
+ * against p with the residual drawn after a refusal, in one step.
+ * The exponentials and sums are fp64 (fp32 sums would move the borders between
+ * tokens by more than rare tokens are wide).  The uniforms are fp64 as well: an
+ * fp32 draw has 2^24 values, and rarer tokens would never be drawn.
+ * -inf (masked) and NaN logits have probability 0, +inf ones share it equally.  A
+ * row without a token of positive probability ends the walk with bonus -1.
+ * n_nodes, tokens, parents, acc_len, acc_nodes, bonus and update_history are as
+ * in graft_accept (children are listed after their parents); logp [batch, L + 1]
+ * or NULL receives log p of every token taken, the bonus last, and 0 after it.
+ * Rows without a token, and temperatures that are negative or NaN (taken as 0),
+ * are reported by graft_get_device_status.  The workspace (16-byte aligned)
+ * belongs to the call until its work is done and needs no clearing. */
+GRAFT_API int graft_accept_sampled(graft_ctx *ctx, int32_t batch, const int32_t *n_nodes,
+                                   const int32_t *tokens, const int32_t *parents,
+                                   const graft_target_logits *target /* host */, int32_t *acc_len,
+                                   int32_t *acc_nodes, int32_t *bonus, float *logp,
+                                   int32_t update_history, void *workspace,
+                                   int64_t workspace_bytes, graft_stream_t stream);
+
+/* Rows moved between a block (or a prompt) and a cache. */
+typedef struct {
+    int32_t batch;               /* 1..max_batch */
+    int32_t n_planes;            /* e.g. layers x {key, value} */
+    int32_t heads, head_dim;     /* head_dim a multiple of 16, 16..128 */
+    int32_t src_dtype, dst_dtype;
+    graft_rows src, dst;         /* [n_planes, batch, src_rows or dst_rows, heads, head_dim] */
+    int32_t src_rows, dst_rows;
+    const int32_t *n_rows;       /* [batch] rows to move (listed ones, with a list) */
+    const int32_t *start;        /* [batch] first cache row, or NULL (0) */
+    const int32_t *list;         /* graft_cache_write: [batch, list_len] source rows, or NULL:
+                                    0 .. n_rows[b] - 1 */
+    int32_t list_len;
+    int32_t with_root;           /* graft_cache_write with a list: source row 0 (the root) goes
+                                    first, and list entries are tree nodes, at source rows
+                                    entry + 1; n_rows does not count the root */
+} graft_cache_move;
+
+/* Appends rows to a cache: row i of what is moved goes to cache row start[b] +
+ * i.  With list = acc_nodes, list_len = L and n_rows = acc_len of the walk this
+ * commits the accepted path (with_root: and the root) of a block; without a
+ * list it stores a prompt.  n_rows is clamped to 0 .. list_len, or 0 .. src_rows.
+ * Source and cache types: GRAFT_BF16 or GRAFT_F16 to the same (a copy), or
+ * GRAFT_BF16 to GRAFT_E4M3: a (row, head) gets the scale 2^e, e the smallest
+ * integer >= -118 with max |x| <= 448 * 2^e over its finite numbers, and the codes
+ * nearest to x / 2^e, ties to even (the division is exact).  Infinities become
+ * the largest code, NaN stays NaN; at e = 120 codes end at 240, so that every
+ * value is finite in fp32 and exact in bf16.
+ * Rows whose source row is outside 0 .. src_rows - 1 or whose cache row is
+ * outside 0 .. dst_rows - 1 are skipped and reported by graft_get_device_status.
+ * src and dst must not overlap. */
+GRAFT_API int graft_cache_write(graft_ctx *ctx, const graft_cache_move *m /* host */,
+                                graft_stream_t stream);
+
+/* Reads rows start[b] .. start[b] + n_rows[b] - 1 of a GRAFT_E4M3 cache (src)
+ * back as GRAFT_BF16 or GRAFT_F32 numbers, to rows 0 .. n_rows[b] - 1 of dst.
+ * Exact in both types.  n_rows is clamped to 0 .. dst_rows; rows outside the cache are
+ * skipped and reported.  list and with_root are not used (NULL and 0). */
+GRAFT_API int graft_cache_read(graft_ctx *ctx, const graft_cache_move *m /* host */,
+                               graft_stream_t stream);
+
 /* Synchronizes `stream` and reports data errors the kernels detected since
  * the last call (token ids outside [0, V), for example): GRAFT_OK or
  * GRAFT_ERR_DEVICE_DATA; the flag is then cleared. */

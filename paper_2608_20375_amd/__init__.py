@@ -12,7 +12,7 @@ import os
 
 import torch
 
-__all__ = ["Context", "TreeBuffers", "TdesTrainer", "TdesHyper", "saba_fit", "read_stream", "lib",
+__all__ = ["Context", "QuantRows", "TreeBuffers", "TdesTrainer", "TdesHyper", "saba_fit", "read_stream", "lib",
            "library_path", "GraftError", "EXPORTED_SYMBOLS"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -26,7 +26,9 @@ EXPORTED_SYMBOLS = (
     "graft_synth_node_targets", "graft_profile_begin", "graft_profile_end", "graft_status_string", "graft_last_error",
     "graft_mask_to_bias", "graft_commit_accepted", "graft_tdes_create", "graft_tdes_destroy",
     "graft_tdes_param_count", "graft_tdes_step", "graft_tdes_device_status", "graft_saba_fit",
-    "graft_read_stream",
+    "graft_read_stream", "graft_tree_attention", "graft_tree_attention_workspace",
+    "graft_accept_sampled", "graft_accept_sampled_workspace", "graft_cache_write",
+    "graft_cache_read",
 )
 
 READ_STREAM_SINK_WORDS = 4096
@@ -108,6 +110,39 @@ class Targets(C.Structure):
                 ("target_depth", C.c_void_p)]
 
 
+class Rows(C.Structure):
+    _fields_ = ([("data", C.c_void_p)]
+                + [(n + "_stride", C.c_int64) for n in ("plane", "batch", "row", "head")]
+                + [("scale", C.c_void_p)]
+                + [("scale_%s_stride" % n, C.c_int64) for n in ("plane", "batch", "row", "head")])
+
+
+class Attention(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("slots", C.c_int32), ("with_root", C.c_int32),
+                ("q_heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int32), ("cache_dtype", C.c_int32), ("scale", C.c_float),
+                ("q", Rows), ("k", Rows), ("v", Rows), ("n_nodes", C.c_void_p),
+                ("mask", C.c_void_p), ("cache_k", Rows), ("cache_v", Rows),
+                ("cache_rows", C.c_int32), ("cache_len", C.c_void_p), ("shared_k", Rows),
+                ("shared_v", Rows), ("shared_len", C.c_int32), ("out", Rows), ("lse", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
+
+
+class TargetLogits(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("root", C.c_void_p), ("root_stride", C.c_int64),
+                ("node", C.c_void_p), ("node_batch_stride", C.c_int64),
+                ("node_row_stride", C.c_int64), ("node_rows", C.c_int32),
+                ("temperature", C.c_void_p), ("uniform", C.c_void_p)]
+
+
+class CacheMove(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("n_planes", C.c_int32), ("heads", C.c_int32),
+                ("head_dim", C.c_int32), ("src_dtype", C.c_int32), ("dst_dtype", C.c_int32),
+                ("src", Rows), ("dst", Rows), ("src_rows", C.c_int32), ("dst_rows", C.c_int32),
+                ("n_rows", C.c_void_p), ("start", C.c_void_p), ("list", C.c_void_p),
+                ("list_len", C.c_int32), ("with_root", C.c_int32)]
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -152,6 +187,13 @@ def lib():
                                      C.POINTER(C.c_float), C.POINTER(C.c_float),
                                      C.POINTER(C.c_double), vp]
         L.graft_read_stream.argtypes = [vp, C.c_int64, vp, vp]
+        L.graft_tree_attention_workspace.argtypes = [vp, C.POINTER(Attention), C.POINTER(i64)]
+        L.graft_tree_attention.argtypes = [vp, C.POINTER(Attention), vp]
+        L.graft_accept_sampled_workspace.argtypes = [vp, i32, C.POINTER(i64)]
+        L.graft_accept_sampled.argtypes = [vp, i32, vp, vp, vp, C.POINTER(TargetLogits), vp, vp,
+                                           vp, vp, i32, vp, i64, vp]
+        L.graft_cache_write.argtypes = [vp, C.POINTER(CacheMove), vp]
+        L.graft_cache_read.argtypes = [vp, C.POINTER(CacheMove), vp]
         L.graft_status_string.argtypes = [C.c_int]
         L.graft_status_string.restype = C.c_char_p
         L.graft_last_error.argtypes = []
@@ -163,7 +205,9 @@ def lib():
                   "graft_synth_node_targets", "graft_profile_begin", "graft_profile_end",
                   "graft_mask_to_bias", "graft_commit_accepted", "graft_tdes_create",
                   "graft_tdes_step", "graft_tdes_device_status", "graft_saba_fit",
-                  "graft_read_stream"):
+                  "graft_read_stream", "graft_tree_attention", "graft_tree_attention_workspace",
+                  "graft_accept_sampled", "graft_accept_sampled_workspace", "graft_cache_write",
+                  "graft_cache_read"):
             getattr(L, n).restype = C.c_int
         _lib = L
     return _lib
@@ -233,6 +277,68 @@ def _check(status: int, where: str):
         raise GraftError(status, where)
 
 
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+class QuantRows:
+    """Quantised key/value rows: codes [..., rows, heads, head_dim] (e4m3: uint8 or
+    float8_e4m3fn) and scales [..., rows, heads] (uint8, s stands for 2^(s - 127)),
+    the numbers being code * 2^(s - 127).  Indexing takes views of both."""
+
+    __slots__ = ("codes", "scales")
+
+    def __init__(self, codes, scales):
+        for name, t in (("codes", codes), ("scales", scales)):
+            if not isinstance(t, torch.Tensor):
+                raise TypeError("%s must be a torch tensor" % name)
+        if codes.dtype not in (torch.uint8, torch.float8_e4m3fn) or scales.dtype != torch.uint8:
+            raise TypeError("codes must be uint8 or float8_e4m3fn and scales uint8")
+        if codes.dim() < 3 or codes.shape[:-1] != scales.shape:
+            raise ValueError("scales must be codes' shape without its last extent, got %s and %s"
+                             % (list(codes.shape), list(scales.shape)))
+        if codes.device != scales.device:
+            raise ValueError("codes and scales must be on one device")
+        self.codes, self.scales = codes, scales
+
+    @classmethod
+    def empty(cls, *shape, device=None):
+        """Unwritten rows of shape [..., rows, heads, head_dim]."""
+        dev = device or torch.device("cuda", torch.cuda.current_device())
+        return cls(torch.empty(shape, dtype=torch.uint8, device=dev),
+                   torch.empty(shape[:-1], dtype=torch.uint8, device=dev))
+
+    @property
+    def shape(self):
+        return self.codes.shape
+
+    @property
+    def device(self):
+        return self.codes.device
+
+    def __getitem__(self, index):
+        """A view by leading indices: codes[index], scales[index]."""
+        return QuantRows(self.codes[index], self.scales[index])
+
+
+def _strides(t, names):
+    """Element strides of t's leading extents by name; 0 where there is one entry."""
+    return {n: (t.stride(i) if t.shape[i] > 1 else 0) for i, n in enumerate(names)}
+
+
+def _rows(t, names, name):
+    """graft_rows of a tensor or QuantRows whose extents are names + head_dim."""
+    data = t.codes if isinstance(t, QuantRows) else t
+    if data.stride(-1) != 1 and data.shape[-1] > 1:
+        raise ValueError("%s must have unit stride along its last dimension" % name)
+    r = Rows(data=data.data_ptr(),
+             **{n + "_stride": s for n, s in _strides(data, names).items()})
+    if isinstance(t, QuantRows):
+        r.scale = t.scales.data_ptr()
+        for n, s in _strides(t.scales, names).items():
+            setattr(r, "scale_%s_stride" % n, s)
+    return r
+
+
 class TreeBuffers:
     """Preallocated outputs of one build_tree call (torch tensors on the device)."""
 
@@ -284,6 +390,7 @@ class Context:
         _check(L.graft_create(C.byref(self.dims), C.byref(h)), "graft_create")
         self._h = h
         self._keep = []
+        self._device = torch.cuda.current_device()
 
     def close(self):
         if getattr(self, "_h", None):
@@ -559,6 +666,245 @@ class Context:
             ss[0] * es, ss[1] * es, ss[2] * es, ds[0] * es, ds[1] * es, ds[2] * es, _stream()),
             "graft_commit_accepted")
         return dst
+
+    def _here(self, **tensors):
+        """Raises unless every tensor given is on the context's device and that is the
+        current one."""
+        for name, t in tensors.items():
+            if t is None:
+                continue
+            if not isinstance(t, (torch.Tensor, QuantRows)) or t.device.type != "cuda":
+                raise TypeError("%s must be a CUDA (HIP) tensor" % name)
+            if t.device.index != self._device:
+                raise ValueError("%s is on device %s, the context on device %d"
+                                 % (name, t.device.index, self._device))
+        if torch.cuda.current_device() != self._device:
+            raise ValueError("the context's device %d is not the current one" % self._device)
+
+    def _kv_pair(self, pair, name, lead, heads, dim, dtype):
+        """(rows, type) of a key and a value tensor or QuantRows; lead: the extents in
+        front of heads, None for any."""
+        if not isinstance(pair, (tuple, list)) or len(pair) != 2:
+            raise ValueError("%s must be a pair of keys and values" % name)
+        kinds = set()
+        for t in pair:
+            if not isinstance(t, (torch.Tensor, QuantRows)):
+                raise TypeError("%s must hold tensors or QuantRows" % name)
+            s = list(t.shape)
+            if (len(s) != len(lead) + 2 or s[-2:] != [heads, dim]
+                    or any(w is not None and a < w for a, w in zip(s, lead))):
+                raise ValueError("%s must be [%s, %d, %d], got %s" % (
+                    name, ", ".join("rows" if w is None else ">=%d" % w for w in lead), heads, dim, s))
+            quant = isinstance(t, QuantRows)
+            if not quant and t.dtype != dtype:
+                raise TypeError("%s must be %s or QuantRows, got %s" % (name, dtype, t.dtype))
+            kinds.add(quant)
+        if len(kinds) != 1 or pair[0].shape[len(lead) - 1] != pair[1].shape[len(lead) - 1]:
+            raise ValueError("%s: keys and values must agree in type and rows" % name)
+        return pair[0].shape[len(lead) - 1], kinds.pop()
+
+    def tree_attention(self, q, k, v, n_nodes, mask=None, cache=None, cache_len=None, shared=None,
+                       scale=None, with_root=False, out=None, lse=None, workspace=None):
+        """Attention of a draft block (graft_tree_attention): q [batch, slots, q_heads, dim],
+        k and v [batch, slots, kv_heads, dim], bfloat16 or float16; slot 0 is the root with
+        with_root, the tree's nodes follow.  mask [batch, max_nodes, words] int64 as
+        build_tree writes it, or None for a chain.  cache: a pair of [batch, rows,
+        kv_heads, dim] keys and values, tensors of q's type or QuantRows (bfloat16 only),
+        of which sequence b has cache_len[b] rows; shared: a pair of [rows, kv_heads, dim]
+        of the cache's type that every sequence sees.  scale defaults to dim ** -0.5.
+        Writes out (allocated as zeros when None) up to each sequence's slots and, when
+        given, lse [batch, slots, q_heads] float32; returns out.  workspace: uint8, at
+        least tree_attention_workspace bytes; allocated when None."""
+        a, out, keep = self._attention(q, k, v, n_nodes, mask, cache, cache_len, shared, scale,
+                                       with_root, out, lse)
+        L = lib()
+        need = C.c_int64()
+        _check(L.graft_tree_attention_workspace(self._h, C.byref(a), C.byref(need)),
+               "graft_tree_attention_workspace")
+        workspace = self._workspace(workspace, need.value, q.device)
+        if workspace is not None:
+            a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
+        _check(L.graft_tree_attention(self._h, C.byref(a), _stream()), "graft_tree_attention")
+        return out
+
+    def tree_attention_workspace(self, q, k, v, n_nodes, mask=None, cache=None, cache_len=None,
+                                 shared=None, scale=None, with_root=False, out=None, lse=None):
+        """Bytes of workspace that tree_attention needs for these arguments."""
+        a, _, _ = self._attention(q, k, v, n_nodes, mask, cache, cache_len, shared, scale,
+                                  with_root, out, lse)
+        need = C.c_int64()
+        _check(lib().graft_tree_attention_workspace(self._h, C.byref(a), C.byref(need)),
+               "graft_tree_attention_workspace")
+        return need.value
+
+    def _workspace(self, workspace, need, device):
+        if workspace is None:
+            return torch.empty(need, dtype=torch.uint8, device=device) if need else None
+        if (not isinstance(workspace, torch.Tensor) or workspace.dtype != torch.uint8
+                or workspace.dim() != 1 or not workspace.is_contiguous() or workspace.numel() < need):
+            raise ValueError("workspace must be a contiguous uint8 vector of at least %d bytes" % need)
+        self._here(workspace=workspace)
+        return workspace
+
+    def _attention(self, q, k, v, n_nodes, mask, cache, cache_len, shared, scale, with_root, out,
+                   lse):
+        for name, t in (("q", q), ("k", k), ("v", v)):
+            if not isinstance(t, torch.Tensor) or t.dim() != 4 or min(t.shape) < 1:
+                raise ValueError("%s must be [batch, slots, heads, dim]" % name)
+        B, S, Hq, D = q.shape
+        H, N = k.shape[2], self.dims.max_nodes
+        _need(k, "k", B, S, H, D)
+        _need(v, "v", B, S, H, D)
+        _need(n_nodes, "n_nodes", B)
+        _need(mask, "mask", (B,), N, (N + 63) // 64)
+        _need(cache_len, "cache_len", B)
+        _need(out, "out", B, S, Hq, D)
+        _need(lse, "lse", B, S, Hq)
+        if n_nodes is None:
+            raise ValueError("n_nodes is required")
+        if q.dtype not in (torch.bfloat16, torch.float16):
+            raise TypeError("q must be bfloat16 or float16")
+        for name, t in (("k", k), ("v", v), ("out", out)):
+            if t is not None and t.dtype != q.dtype:
+                raise TypeError("%s must be %s" % (name, q.dtype))
+        a = Attention(batch=B, slots=S, with_root=1 if with_root else 0, q_heads=Hq, kv_heads=H,
+                      head_dim=D, dtype=_DTYPES[q.dtype], cache_dtype=_DTYPES[q.dtype],
+                      scale=float(D ** -0.5 if scale is None else scale))
+        kinds = set()
+        if cache is not None:
+            if cache_len is None:
+                raise ValueError("a cache needs cache_len")
+            a.cache_rows, quant = self._kv_pair(cache, "cache", (B, None), H, D, q.dtype)
+            kinds.add(quant)
+        if shared is not None:
+            a.shared_len, quant = self._kv_pair(shared, "shared", (None,), H, D, q.dtype)
+            kinds.add(quant)
+        if len(kinds) > 1:
+            raise ValueError("cache and shared must be of one type")
+        if True in kinds:
+            a.cache_dtype = 3
+        self._here(q=q, k=k, v=v, n_nodes=n_nodes, mask=mask, cache_len=cache_len, out=out, lse=lse,
+                   **({"cache keys": cache[0], "cache values": cache[1]} if cache is not None else {}),
+                   **({"shared keys": shared[0], "shared values": shared[1]}
+                      if shared is not None else {}))
+        if out is None:
+            out = torch.zeros_like(q, memory_format=torch.contiguous_format)
+        a.q, a.k, a.v, a.out = (_rows(t, ("batch", "row", "head"), n)
+                                for t, n in ((q, "q"), (k, "k"), (v, "v"), (out, "out")))
+        if a.cache_rows:
+            a.cache_k, a.cache_v = (_rows(t, ("batch", "row", "head"), "cache") for t in cache)
+        if a.shared_len:
+            a.shared_k, a.shared_v = (_rows(t, ("row", "head"), "shared") for t in shared)
+        a.n_nodes = _ptr(n_nodes, torch.int32, "n_nodes")
+        a.mask = _ptr(mask, torch.int64, "mask")
+        a.cache_len = _ptr(cache_len, torch.int32, "cache_len")
+        a.lse = _ptr(lse, torch.float32, "lse")
+        return a, out, None
+
+    def accept_sampled(self, n_nodes, tokens, parents, root_logits, node_logits, uniform,
+                       temperature=None, update_history=False, acc_len=None, acc_nodes=None,
+                       bonus=None, logp=None, workspace=None):
+        """The sampled acceptance walk (graft_accept_sampled).  root_logits [batch, V] and
+        node_logits [batch, rows, V] of the target model: float32, bfloat16 or float16,
+        unit stride along V (row 0 and rows 1.. of a block's logits, say); nodes from
+        `rows` on are not part of the tree.  uniform [batch, L + 1] float64 in [0, 1);
+        temperature [batch] float32, 0 for the largest logit, or None for 1.  Returns
+        (acc_len, acc_nodes, bonus, logp [batch, L + 1] of the tokens taken)."""
+        dm = self.dims
+        batch = _batch_of(n_nodes, "n_nodes")
+        L, N, V = dm.num_pos, dm.max_nodes, dm.vocab
+        _need(n_nodes, "n_nodes", batch)
+        _need(tokens, "tokens", (batch,), N)
+        _need(parents, "parents", (batch,), N)
+        _need(root_logits, "root_logits", (batch,), V)
+        _need(node_logits, "node_logits", (batch,), (0,), V)
+        _need(uniform, "uniform", (batch,), L + 1)
+        _need(temperature, "temperature", (batch,))
+        _need(acc_len, "acc_len", (batch,))
+        _need(acc_nodes, "acc_nodes", (batch,), L)
+        _need(bonus, "bonus", (batch,))
+        _need(logp, "logp", (batch,), L + 1)
+        if root_logits is None or node_logits is None or uniform is None:
+            raise ValueError("root_logits, node_logits and uniform are required")
+        if root_logits.dtype not in _DTYPES or node_logits.dtype != root_logits.dtype:
+            raise TypeError("logits must both be float32, bfloat16 or float16")
+        for name, t in (("root_logits", root_logits), ("node_logits", node_logits)):
+            if V > 1 and t.stride(-1) != 1:
+                raise ValueError("%s must have unit stride along V" % name)
+        self._here(n_nodes=n_nodes, tokens=tokens, parents=parents, root_logits=root_logits,
+                   node_logits=node_logits, uniform=uniform, temperature=temperature,
+                   acc_len=acc_len, acc_nodes=acc_nodes, bonus=bonus, logp=logp)
+        dev = n_nodes.device
+        i32 = dict(dtype=torch.int32, device=dev)
+        acc_len = torch.empty(batch, **i32) if acc_len is None else acc_len
+        acc_nodes = torch.empty(batch, L, **i32) if acc_nodes is None else acc_nodes
+        bonus = torch.empty(batch, **i32) if bonus is None else bonus
+        logp = torch.empty(batch, L + 1, dtype=torch.float32, device=dev) if logp is None else logp
+        rows = min(node_logits.shape[1], N)
+        t = TargetLogits(_DTYPES[root_logits.dtype], root_logits.data_ptr(), root_logits.stride(0),
+                         node_logits.data_ptr() if rows else None, node_logits.stride(0),
+                         node_logits.stride(1) if rows > 1 else 0, rows,
+                         _ptr(temperature, torch.float32, "temperature"),
+                         _ptr(uniform, torch.float64, "uniform"))
+        lib_ = lib()
+        need = C.c_int64()
+        _check(lib_.graft_accept_sampled_workspace(self._h, batch, C.byref(need)),
+               "graft_accept_sampled_workspace")
+        workspace = self._workspace(workspace, need.value, dev)
+        _check(lib_.graft_accept_sampled(
+            self._h, batch, _ptr(n_nodes, torch.int32, "n_nodes"), _ptr(tokens, torch.int32, "tokens"),
+            _ptr(parents, torch.int32, "parents"), C.byref(t), _ptr(acc_len, torch.int32, "acc_len"),
+            _ptr(acc_nodes, torch.int32, "acc_nodes"), _ptr(bonus, torch.int32, "bonus"),
+            _ptr(logp, torch.float32, "logp"), 1 if update_history else 0, workspace.data_ptr(),
+            workspace.numel(), _stream()), "graft_accept_sampled")
+        return acc_len, acc_nodes, bonus, logp
+
+    def _move(self, src, dst, n_rows, start, rows, with_root):
+        for name, t in (("src", src), ("dst", dst)):
+            if not isinstance(t, (torch.Tensor, QuantRows)):
+                raise TypeError("%s must be a tensor or QuantRows" % name)
+            if len(t.shape) != 5 or min(t.shape) < 1:
+                raise ValueError("%s must be [planes, batch, rows, heads, dim], got %s"
+                                 % (name, list(t.shape)))
+        batch = _batch_of(n_rows, "n_rows")
+        _need(n_rows, "n_rows", batch)
+        _need(start, "start", (batch,))
+        _need(rows, "rows", (batch,), (1,))
+        P, _, _, H, D = src.shape
+        for name, t in (("src", src), ("dst", dst)):
+            if t.shape[0] != P or t.shape[1] < batch or tuple(t.shape[3:]) != (H, D):
+                raise ValueError("%s must be [%d, >=%d, rows, %d, %d], got %s"
+                                 % (name, P, batch, H, D, list(t.shape)))
+        self._here(src=src, dst=dst, n_rows=n_rows, start=start, rows=rows)
+        kind = lambda t: 3 if isinstance(t, QuantRows) else _DTYPES.get(t.dtype, -1)
+        names = ("plane", "batch", "row", "head")
+        return CacheMove(batch, P, H, D, kind(src), kind(dst), _rows(src, names, "src"),
+                         _rows(dst, names, "dst"), src.shape[2], dst.shape[2],
+                         _ptr(n_rows, torch.int32, "n_rows"), _ptr(start, torch.int32, "start"),
+                         _ptr(rows, torch.int32, "rows"), 0 if rows is None else rows.shape[1],
+                         1 if with_root else 0)
+
+    def cache_write(self, dst, src, n_rows, rows=None, start=None, with_root=False):
+        """Appends rows of src [planes, batch, rows, heads, dim] to the cache dst of the same
+        form (graft_cache_write): a tensor of src's type (a copy), or QuantRows (src
+        bfloat16).  rows [batch, entries] lists source rows (None: 0 .. n_rows - 1); with
+        with_root its entries are tree nodes, at source rows entry + 1, and source row 0 is
+        written first.  The first row written is cache row start[b] (None: 0)."""
+        m = self._move(src, dst, n_rows, start, rows, with_root)
+        _check(lib().graft_cache_write(self._h, C.byref(m), _stream()), "graft_cache_write")
+        return dst
+
+    def cache_read(self, src, n_rows, start=None, out=None, dtype=torch.bfloat16):
+        """Rows start[b] .. start[b] + n_rows[b] - 1 of the QuantRows src [planes, batch, rows,
+        heads, dim] as bfloat16 or float32 numbers in rows 0 .. n_rows[b] - 1 of out, which
+        is allocated as zeros of src's shape when None."""
+        if not isinstance(src, QuantRows):
+            raise TypeError("src must be QuantRows")
+        if out is None:
+            out = torch.zeros(src.shape, dtype=dtype, device=src.device)
+        m = self._move(src, out, n_rows, start, None, False)
+        _check(lib().graft_cache_read(self._h, C.byref(m), _stream()), "graft_cache_read")
+        return out
 
     def profile_begin(self, max_calls: int):
         _check(lib().graft_profile_begin(self._h, int(max_calls)), "graft_profile_begin")

@@ -170,6 +170,109 @@ int build_tree_with(graft_ctx *ctx, const graft_round_in *in, const graft_tree_o
   return GRAFT_OK;
 }
 
+// The device of a context's workspace has to be the current one: launches and the
+// tensors' memory go there.
+int check_device(const graft_ctx *ctx, const char *who) {
+  int dev = -1;
+  const hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return hip_fail(e, who);
+  if (dev != ctx->device)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: device %d is current; the context is of device %d", who,
+                dev, ctx->device);
+  return GRAFT_OK;
+}
+
+int type_bytes(int dtype) { return dtype == GRAFT_F32 ? 4 : dtype == GRAFT_E4M3 ? 1 : 2; }
+
+// Strides and, with pointers, alignment of a graft_rows of this type.
+int check_rows(const graft_rows &r, int dtype, bool pointers, const char *who, const char *name) {
+  const int64_t per = 16 / type_bytes(dtype);
+  const int64_t v[4] = {r.plane_stride, r.batch_stride, r.row_stride, r.head_stride};
+  for (int64_t x : v)
+    if (x < 0 || x % per != 0)
+      return fail(GRAFT_ERR_INVALID_ARG, "%s: %s's strides must be non-negative multiples of %d elements",
+                  who, name, static_cast<int>(per));
+  if (!pointers) return GRAFT_OK;
+  if (!r.data || (reinterpret_cast<uintptr_t>(r.data) & 15u) != 0)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: %s must be given and 16-byte aligned", who, name);
+  if (dtype == GRAFT_E4M3) {
+    const int64_t w[4] = {r.scale_plane_stride, r.scale_batch_stride, r.scale_row_stride,
+                          r.scale_head_stride};
+    for (int64_t x : w)
+      if (x < 0) return fail(GRAFT_ERR_INVALID_ARG, "%s: %s's scale strides must not be negative", who, name);
+    if (!r.scale) return fail(GRAFT_ERR_INVALID_ARG, "%s: %s needs scales", who, name);
+  }
+  return GRAFT_OK;
+}
+
+// Sizes of an attention call; pointers too when they are to be used.
+int check_attention(const graft_ctx *ctx, const graft_attention *a, bool pointers, const char *who) {
+  if (!ctx || !a) return fail(GRAFT_ERR_INVALID_ARG, "%s: NULL argument", who);
+  const graft_dims &d = ctx->dims;
+  if (a->batch < 1 || a->batch > d.max_batch)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: batch %d outside 1..%d", who, a->batch, d.max_batch);
+  const int most = d.max_nodes + (a->with_root ? 1 : 0);
+  if (a->slots < 1 || a->slots > most)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: slots %d outside 1..%d", who, a->slots, most);
+  if (a->kv_heads < 1 || a->q_heads < 1 || a->q_heads % a->kv_heads != 0)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: q_heads %d must be a positive multiple of kv_heads %d",
+                who, a->q_heads, a->kv_heads);
+  if (a->q_heads > 1024) return fail(GRAFT_ERR_UNSUPPORTED, "%s: q_heads %d > 1024", who, a->q_heads);
+  if (a->head_dim < 16 || a->head_dim % 16 != 0)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: head_dim %d must be a multiple of 16", who, a->head_dim);
+  if (a->head_dim > 128) return fail(GRAFT_ERR_UNSUPPORTED, "%s: head_dim %d > 128", who, a->head_dim);
+  if (a->dtype != GRAFT_BF16 && a->dtype != GRAFT_F16)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: dtype %d is neither bf16 (1) nor fp16 (2)", who, a->dtype);
+  if (a->cache_dtype != a->dtype && !(a->cache_dtype == GRAFT_E4M3 && a->dtype == GRAFT_BF16))
+    return fail(GRAFT_ERR_UNSUPPORTED, "%s: a cache of type %d with queries of type %d", who,
+                a->cache_dtype, a->dtype);
+  if (!std::isfinite(a->scale) || !(a->scale > 0.0f))
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: scale must be positive and finite", who);
+  if (a->cache_rows < 0 || a->shared_len < 0)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: cache_rows and shared_len must not be negative", who);
+  if (a->cache_rows > (1 << 30) || a->shared_len > (1 << 30))
+    return fail(GRAFT_ERR_UNSUPPORTED, "%s: more than 2^30 keys", who);
+  if (static_cast<int64_t>(a->batch) * a->slots * a->q_heads > (int64_t{1} << 30))
+    return fail(GRAFT_ERR_UNSUPPORTED, "%s: more than 2^30 query rows", who);
+  if (!pointers) return GRAFT_OK;
+  if (!a->n_nodes) return fail(GRAFT_ERR_INVALID_ARG, "%s: n_nodes is required", who);
+  int rc = check_rows(a->q, a->dtype, true, who, "q");
+  if (rc == GRAFT_OK) rc = check_rows(a->k, a->dtype, true, who, "k");
+  if (rc == GRAFT_OK) rc = check_rows(a->v, a->dtype, true, who, "v");
+  if (rc == GRAFT_OK) rc = check_rows(a->out, a->dtype, true, who, "out");
+  if (rc == GRAFT_OK && a->cache_rows > 0) {
+    if (!a->cache_len) return fail(GRAFT_ERR_INVALID_ARG, "%s: a cache needs cache_len", who);
+    rc = check_rows(a->cache_k, a->cache_dtype, true, who, "cache_k");
+    if (rc == GRAFT_OK) rc = check_rows(a->cache_v, a->cache_dtype, true, who, "cache_v");
+  }
+  if (rc == GRAFT_OK && a->shared_len > 0) {
+    rc = check_rows(a->shared_k, a->cache_dtype, true, who, "shared_k");
+    if (rc == GRAFT_OK) rc = check_rows(a->shared_v, a->cache_dtype, true, who, "shared_v");
+  }
+  return rc;
+}
+
+int check_move(const graft_ctx *ctx, const graft_cache_move *m, const char *who) {
+  if (!ctx || !m || !m->n_rows) return fail(GRAFT_ERR_INVALID_ARG, "%s: NULL argument", who);
+  if (m->batch < 1 || m->batch > ctx->dims.max_batch)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: batch %d outside 1..%d", who, m->batch,
+                ctx->dims.max_batch);
+  if (m->n_planes < 1 || m->heads < 1 || m->src_rows < 1 || m->dst_rows < 1)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: n_planes, heads, src_rows and dst_rows must be positive", who);
+  if (m->head_dim < 16 || m->head_dim % 16 != 0)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: head_dim %d must be a multiple of 16", who, m->head_dim);
+  if (m->head_dim > 128) return fail(GRAFT_ERR_UNSUPPORTED, "%s: head_dim %d > 128", who, m->head_dim);
+  int rc = check_rows(m->src, m->src_dtype, true, who, "src");
+  if (rc == GRAFT_OK) rc = check_rows(m->dst, m->dst_dtype, true, who, "dst");
+  if (rc != GRAFT_OK) return rc;
+  // workgroups of 256 columns of 16 numbers and of at least 16 rows
+  const int64_t cols = static_cast<int64_t>(m->n_planes) * m->heads * 8;
+  const int64_t rows = std::max(m->src_rows, std::max(m->dst_rows, m->list_len + 1));
+  if (cols > (1 << 28) || (cols / 256 + 1) * (rows / 16 + 1) > (int64_t{1} << 31) / m->batch - 1)
+    return fail(GRAFT_ERR_UNSUPPORTED, "%s: too many rows to move in one call", who);
+  return check_device(ctx, who);
+}
+
 }  // namespace
 
 extern "C" {
@@ -471,6 +574,112 @@ int graft_commit_accepted(graft_ctx *ctx, int32_t batch, const int32_t *acc_len,
                                       src_row_stride, dst_plane_stride, dst_batch_stride,
                                       dst_row_stride, reinterpret_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "graft_commit_accepted");
+  return GRAFT_OK;
+}
+
+int graft_tree_attention_workspace(graft_ctx *ctx, const graft_attention *a, int64_t *bytes) {
+  if (!bytes) return fail(GRAFT_ERR_INVALID_ARG, "graft_tree_attention_workspace: NULL argument");
+  const int rc = check_attention(ctx, a, false, "graft_tree_attention_workspace");
+  if (rc != GRAFT_OK) return rc;
+  *bytes = graft::attend_plan(*a).bytes;
+  return GRAFT_OK;
+}
+
+int graft_tree_attention(graft_ctx *ctx, const graft_attention *a, graft_stream_t stream) {
+  const char *who = "graft_tree_attention";
+  int rc = check_attention(ctx, a, true, who);
+  if (rc == GRAFT_OK) rc = check_device(ctx, who);
+  if (rc != GRAFT_OK) return rc;
+  const graft::AttendPlan p = graft::attend_plan(*a);
+  if (p.bytes > 0 && (!a->workspace || (reinterpret_cast<uintptr_t>(a->workspace) & 15u) != 0 ||
+                      a->workspace_bytes < p.bytes))
+    return fail(GRAFT_ERR_INVALID_ARG,
+                "graft_tree_attention: needs a 16-byte aligned workspace of %lld bytes",
+                static_cast<long long>(p.bytes));
+  const hipError_t e = graft::launch_attend(ctx, *a, p, reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, who);
+  return GRAFT_OK;
+}
+
+int graft_accept_sampled_workspace(graft_ctx *ctx, int32_t batch, int64_t *bytes) {
+  if (!ctx || !bytes) return fail(GRAFT_ERR_INVALID_ARG, "graft_accept_sampled_workspace: NULL argument");
+  if (batch < 1 || batch > ctx->dims.max_batch)
+    return fail(GRAFT_ERR_INVALID_ARG, "graft_accept_sampled_workspace: batch %d outside 1..%d",
+                batch, ctx->dims.max_batch);
+  *bytes = graft::sample_bytes(ctx->dims, batch);
+  return GRAFT_OK;
+}
+
+int graft_accept_sampled(graft_ctx *ctx, int32_t batch, const int32_t *n_nodes,
+                         const int32_t *tokens, const int32_t *parents,
+                         const graft_target_logits *t, int32_t *acc_len, int32_t *acc_nodes,
+                         int32_t *bonus, float *logp, int32_t update_history, void *workspace,
+                         int64_t workspace_bytes, graft_stream_t stream) {
+  const char *who = "graft_accept_sampled";
+  if (!ctx || !n_nodes || !tokens || !parents || !t || !acc_len || !acc_nodes || !bonus)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: NULL argument", who);
+  if (batch < 1 || batch > ctx->dims.max_batch)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: batch %d outside 1..%d", who, batch, ctx->dims.max_batch);
+  if (t->dtype != GRAFT_F32 && t->dtype != GRAFT_BF16 && t->dtype != GRAFT_F16)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: dtype %d is none of fp32 (0), bf16 (1), fp16 (2)", who,
+                t->dtype);
+  if (!t->root || !t->uniform || (t->node_rows > 0 && !t->node))
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: root, uniform and, with node_rows, node are required", who);
+  if (t->node_rows < 0 || t->node_rows > ctx->dims.max_nodes)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: node_rows %d outside 0..%d", who, t->node_rows,
+                ctx->dims.max_nodes);
+  const int64_t V = ctx->dims.vocab;
+  if ((batch > 1 && t->root_stride < 0) || t->node_batch_stride < 0 || t->node_row_stride < 0 ||
+      (t->node_rows > 1 && t->node_row_stride < V))
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: strides must not be negative, node rows not overlap", who);
+  const uintptr_t at = reinterpret_cast<uintptr_t>(t->root) | reinterpret_cast<uintptr_t>(t->node);
+  if (at % type_bytes(t->dtype) != 0 || reinterpret_cast<uintptr_t>(t->uniform) % 8 != 0)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: misaligned logits or uniform", who);
+  if (V > (1 << 30)) return fail(GRAFT_ERR_UNSUPPORTED, "%s: vocab over 2^30", who);
+  if (update_history && !ctx->has_history)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: no history ring (graft_set_history)", who);
+  const int64_t need = graft::sample_bytes(ctx->dims, batch);
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15u) != 0 || workspace_bytes < need)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: needs a 16-byte aligned workspace of %lld bytes", who,
+                static_cast<long long>(need));
+  const int rc = check_device(ctx, who);
+  if (rc != GRAFT_OK) return rc;
+  const hipError_t e = graft::launch_accept_sampled(
+      ctx, batch, n_nodes, tokens, parents, t, acc_len, acc_nodes, bonus, logp, update_history,
+      workspace, reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, who);
+  return GRAFT_OK;
+}
+
+int graft_cache_write(graft_ctx *ctx, const graft_cache_move *m, graft_stream_t stream) {
+  const char *who = "graft_cache_write";
+  if (m && !((m->src_dtype == GRAFT_BF16 && m->dst_dtype == GRAFT_E4M3) ||
+             (m->src_dtype == m->dst_dtype &&
+              (m->src_dtype == GRAFT_BF16 || m->src_dtype == GRAFT_F16))))
+    return fail(GRAFT_ERR_UNSUPPORTED, "%s: rows of type %d into a cache of type %d", who,
+                m->src_dtype, m->dst_dtype);
+  if (m && (m->list ? m->list_len < 1 : m->list_len < 0))
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: list_len %d", who, m->list_len);
+  if (m && m->with_root && !m->list)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: with_root needs a list", who);
+  const int rc = check_move(ctx, m, who);
+  if (rc != GRAFT_OK) return rc;
+  const hipError_t e = graft::launch_cache_write(ctx, *m, reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, who);
+  return GRAFT_OK;
+}
+
+int graft_cache_read(graft_ctx *ctx, const graft_cache_move *m, graft_stream_t stream) {
+  const char *who = "graft_cache_read";
+  if (m && (m->src_dtype != GRAFT_E4M3 || (m->dst_dtype != GRAFT_BF16 && m->dst_dtype != GRAFT_F32)))
+    return fail(GRAFT_ERR_UNSUPPORTED, "%s: a cache of type %d read as type %d", who, m->src_dtype,
+                m->dst_dtype);
+  if (m && (m->list || m->with_root || m->list_len != 0))
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: takes no list and no root", who);
+  const int rc = check_move(ctx, m, who);
+  if (rc != GRAFT_OK) return rc;
+  const hipError_t e = graft::launch_cache_read(ctx, *m, reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, who);
   return GRAFT_OK;
 }
 

@@ -276,6 +276,31 @@ hipError_t launch_commit(graft_ctx *ctx, int batch, const int32_t *acc_len,
                          const int32_t *acc_nodes, const void *src, void *dst, int64_t row_bytes,
                          int n_planes, int64_t sp, int64_t sb, int64_t sr, int64_t dp,
                          int64_t db, int64_t dr, hipStream_t stream);
+// The draft block's attention: how a call is cut into workgroups, and its launches.
+struct AttendPlan {
+  int row_tiles;      // tiles of 128 (slot, head of the group) rows of one sequence
+  int splits;         // parts of a sequence's keys at most
+  int min_tiles;      // 64-key tiles of a part at least
+  int shared_tiles;   // row tiles over the whole batch for the shared prefix, 0: no own pass
+  int shared_splits;  // parts of the shared prefix then
+  int parts;          // splits + shared_splits
+  int64_t bytes;      // workspace
+};
+AttendPlan attend_plan(const graft_attention &a);
+hipError_t launch_attend(graft_ctx *ctx, const graft_attention &a, const AttendPlan &p,
+                         hipStream_t stream);
+// The sampled walk: the workgroups of a row, the workspace, and the launches (one a level).
+int sample_splits(const graft_dims &d, int batch);
+int64_t sample_bytes(const graft_dims &d, int batch);
+hipError_t launch_accept_sampled(graft_ctx *ctx, int batch, const int32_t *n_nodes,
+                                 const int32_t *tokens, const int32_t *parents,
+                                 const graft_target_logits *t, int32_t *acc_len,
+                                 int32_t *acc_nodes, int32_t *bonus, float *logp,
+                                 int update_history, void *workspace, hipStream_t stream);
+hipError_t launch_cache_write(graft_ctx *ctx, const graft_cache_move &m, hipStream_t stream);
+hipError_t launch_cache_read(graft_ctx *ctx, const graft_cache_move &m, hipStream_t stream);
+// Bits of a context's error flag set by these (1, 2 and 4 are the round's).
+constexpr uint32_t kErrBlockSizes = 8u, kErrTargetRow = 16u, kErrCacheRow = 32u;
 hipError_t launch_synth_targets(graft_ctx *ctx, int batch, uint64_t seed,
                                 const int32_t *root_token, const int32_t *n_nodes,
                                 const int32_t *tokens, const int32_t *parents,

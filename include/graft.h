@@ -345,6 +345,8 @@ typedef struct {
  * A slot that sees nothing gets zeros and an lse of -inf.  Keys and values of
  * slots it does not see never reach it, whatever they hold.  Rows of out and
  * lse from slot S_b on are left as they were.
+ * Rows of k, v, the cache and the shared prefix are at least head_dim and at most
+ * 2^22 elements apart (scales at most 2^22 bytes).
  * Sums and softmax statistics are fp32; the probabilities are rounded to dtype
  * for the product with v.  The result is the same bits for the same arguments.
  * Plane strides are ignored. */

@@ -205,6 +205,18 @@ int check_rows(const graft_rows &r, int dtype, bool pointers, const char *who, c
   return GRAFT_OK;
 }
 
+// Rows of keys or values that the attention walks: side by side, a tile of 64 of them
+// within 31-bit offsets.
+int check_walked(const graft_rows &r, int dtype, int rows, int dim, const char *who, const char *name) {
+  const int rc = check_rows(r, dtype, true, who, name);
+  if (rc != GRAFT_OK || rows <= 1) return rc;
+  if (r.row_stride < dim)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: %s's rows overlap", who, name);
+  if (r.row_stride > (1 << 22) || r.scale_row_stride > (1 << 22))
+    return fail(GRAFT_ERR_UNSUPPORTED, "%s: %s's rows are more than 2^22 elements apart", who, name);
+  return GRAFT_OK;
+}
+
 // Sizes of an attention call; pointers too when they are to be used.
 int check_attention(const graft_ctx *ctx, const graft_attention *a, bool pointers, const char *who) {
   if (!ctx || !a) return fail(GRAFT_ERR_INVALID_ARG, "%s: NULL argument", who);
@@ -237,17 +249,17 @@ int check_attention(const graft_ctx *ctx, const graft_attention *a, bool pointer
   if (!pointers) return GRAFT_OK;
   if (!a->n_nodes) return fail(GRAFT_ERR_INVALID_ARG, "%s: n_nodes is required", who);
   int rc = check_rows(a->q, a->dtype, true, who, "q");
-  if (rc == GRAFT_OK) rc = check_rows(a->k, a->dtype, true, who, "k");
-  if (rc == GRAFT_OK) rc = check_rows(a->v, a->dtype, true, who, "v");
+  if (rc == GRAFT_OK) rc = check_walked(a->k, a->dtype, a->slots, a->head_dim, who, "k");
+  if (rc == GRAFT_OK) rc = check_walked(a->v, a->dtype, a->slots, a->head_dim, who, "v");
   if (rc == GRAFT_OK) rc = check_rows(a->out, a->dtype, true, who, "out");
   if (rc == GRAFT_OK && a->cache_rows > 0) {
     if (!a->cache_len) return fail(GRAFT_ERR_INVALID_ARG, "%s: a cache needs cache_len", who);
-    rc = check_rows(a->cache_k, a->cache_dtype, true, who, "cache_k");
-    if (rc == GRAFT_OK) rc = check_rows(a->cache_v, a->cache_dtype, true, who, "cache_v");
+    rc = check_walked(a->cache_k, a->cache_dtype, a->cache_rows, a->head_dim, who, "cache_k");
+    if (rc == GRAFT_OK) rc = check_walked(a->cache_v, a->cache_dtype, a->cache_rows, a->head_dim, who, "cache_v");
   }
   if (rc == GRAFT_OK && a->shared_len > 0) {
-    rc = check_rows(a->shared_k, a->cache_dtype, true, who, "shared_k");
-    if (rc == GRAFT_OK) rc = check_rows(a->shared_v, a->cache_dtype, true, who, "shared_v");
+    rc = check_walked(a->shared_k, a->cache_dtype, a->shared_len, a->head_dim, who, "shared_k");
+    if (rc == GRAFT_OK) rc = check_walked(a->shared_v, a->cache_dtype, a->shared_len, a->head_dim, who, "shared_v");
   }
   return rc;
 }

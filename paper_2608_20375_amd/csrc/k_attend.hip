@@ -9,9 +9,7 @@
 //
 // Layout.  The query heads of a key head are rows beside each other: row = slot *
 // group + head of the group, so a single token of eight query heads is eight rows of
-// one tile and a key is loaded once for all of them.  A workgroup takes 128 rows, 32
-// a wave, and walks 64-key tiles staged in LDS, the next tile's loads in flight in
-// registers meanwhile, two LDS buffers, one barrier a tile.
+// one tile and a key is loaded once for all of them.
 //
 // Products.  v_mfma_f32_32x32x16: lane l gives row (or column) l % 32 and 8 of the 16
 // contracted entries from 8 (l / 32) on; of the 32 x 32 result it holds column l % 32,
@@ -20,18 +18,33 @@
 // the wave.  O^T = V^T P^T then wants P^T as its right operand: any order of the
 // contracted keys will do as long as V^T's is the same, so a lane's own 8 numbers of a
 // 16-key group are used where they are, keys 4 h + {0..3, 8..11} of the group in lane
-// half h, and V is stored transposed in LDS with the keys of each group in that order.
+// half h; V^T's fragments come out of row-major LDS by the transposing read
+// ds_read_b64_tr_b16 (of 16 lanes, each giving the address of 4 numbers of row s / 4,
+// columns 4 (s % 4).., lane i gets column i of the 4 rows).
 //
-// LDS.  K: 16-byte chunk c of key r at chunk c ^ (r % 8 or 16), V^T: row d, 8-byte slot
-// p at p ^ 2 ((d ^ d / 8) % 8): a wave's 16-byte reads of 8 rows and its stores of a
-// column of chunks then touch different banks.
+// wide_part: 128 rows a workgroup, 32 a wave; 64-key tiles in LDS for all four waves, the
+// next tile's loads in flight in registers meanwhile, two LDS buffers, one barrier a
+// tile.  For blocks with many rows: bound by the matrix and vector units.
+// narrow_part: up to 32 rows a workgroup; every wave walks 32-key tiles of its own (four
+// waves, four times the keys in flight), keys from memory straight into fragments, the
+// values through a stretch of LDS of the wave's own, no barriers; the four waves' sums
+// are joined at the end.  For single tokens and small blocks: bound by the cache's bytes.
 //
-// The keys of a sequence (the shared prefix, its cache, its block: 64-key tiles of each)
-// are split into parts where rows alone do not fill the chip; every part leaves its
-// sums, maximum and unnormalised row in the workspace and merge_kernel joins them.
-// When a sequence has fewer rows than a tile, the shared prefix is walked by
+// LDS.  16-byte chunk c of a row goes to c ^ f(row), f = row % 16 for keys (a fragment read
+// takes one chunk of 32 rows) and 2 (row % 8) for values (a transposing read takes 2
+// chunks of 8 rows), so that the lanes of a read touch different banks.
+//
+// The keys of a sequence (tiles of the shared prefix, of its cache, of its block) are
+// split into parts where rows alone do not fill the chip; every part leaves its sums,
+// maximum and unnormalised rows in the workspace and merge_parts_kernel joins them.
+// When a sequence has fewer rows than a tile, the shared prefix is walked by wide
 // workgroups of their own whose rows come from all sequences: it is read once for 128
 // rows instead of once for every sequence.
+//
+// The running maximum is only moved when some row's new maximum is more than 2^8 above it
+// (in exp2's argument): the sums and rows are fp32 and the probabilities, then up to
+// 2^8, keep their relative precision in 16 bits, while rescaling a row's numbers every
+// time would cost a fifth of the vector work.
 #include <algorithm>
 
 #include "graft_internal.h"
@@ -41,12 +54,16 @@ namespace {
 
 constexpr int kAttThreads = 256;
 constexpr int kAttWaves = kAttThreads / kWave;
-constexpr int kRowTile = 128;
-constexpr int kKeyTile = 64;
-constexpr int kMaxParts = 64;          // one a lane of the merge
+constexpr int kRowTile = 128, kKeyTile = 64;      // wide_part
+constexpr int kFewRows = 32, kFewKeys = 32;       // narrow_part; keys of one wave's tile
+constexpr int kMaxParts = 64;                     // one a lane of the merge
+constexpr float kSlack = 8.0f;                    // log2 by which a maximum may be passed
+constexpr int kOutside = 0x40000000;              // an offset past every buffer's end
+static_assert(kFewKeys * kAttWaves == 2 * kKeyTile, "tiles of both kinds are counted in the plan");
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -82,16 +99,19 @@ struct F16 {
   }
 };
 
-// A side (keys or values) of one source of rows; strides in bytes.
+// A side (keys or values) of a source of rows; strides in bytes.
 struct Side {
   const char *p;
-  int64_t batch, row, head;
   const uint8_t *s;
-  int64_t s_batch, s_row, s_head;
+  int64_t batch, head, s_batch, s_head;
+  int32_t row, s_row;
+};
+struct Source {
+  Side k, v;
 };
 
 struct AttendArgs {
-  Side block_k, block_v, cache_k, cache_v, shared_k, shared_v;
+  Source src[3];          // shared prefix, cache, block
   const char *q;
   char *out;
   int64_t q_batch, q_slot, q_head, o_batch, o_slot, o_head;   // bytes
@@ -104,7 +124,7 @@ struct AttendArgs {
   int64_t rows_all;       // batch * slots * q_heads
   int32_t batch, slots, root, q_heads, kv_heads, group, dim;
   int32_t n_max, words, cache_rows, shared_len;
-  int32_t row_tiles, splits, min_tiles, shared_tiles, shared_splits, parts;
+  int32_t few, row_tiles, splits, min_tiles, shared_tiles, shared_splits, parts;
   int32_t shared_items;   // workgroups of the shared prefix's own pass
   float c;
 };
@@ -116,76 +136,233 @@ __device__ __forceinline__ int slots_of(const AttendArgs &a, int b, bool *bad) {
   return (n < 0 ? 0 : (n > most ? most : n)) + a.root;
 }
 
-// One 64-key tile of a source.
-struct Tile {
-  Side k, v;              // p, s moved to the sequence and key head
-  int key0, count;
-  bool quant, block;
+__device__ __forceinline__ float half_max(float v) {   // with the other half's lane
+  const u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(
+      __float_as_uint(v), __float_as_uint(v), false, false));
+  return fmaxf(__uint_as_float(r.x), __uint_as_float(r.y));
+}
+__device__ __forceinline__ float half_sum(float v) {
+  const u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(
+      __float_as_uint(v), __float_as_uint(v), false, false));
+  return __uint_as_float(r.x) + __uint_as_float(r.y);
+}
+
+// Buffers with the hardware's bounds check: a load past `bytes` gives zeros.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void *p, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, bytes, 0x00020000);
+}
+__device__ __forceinline__ u32x4 load16(__amdgpu_buffer_rsrc_t r, int at) {
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0));
+}
+
+// 4 codes and their scale's byte -> two pairs of bf16, exact.
+__device__ __forceinline__ u32x2 widen(uint32_t w, float unit) {
+  u32x2 r;
+  r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, unit, false));
+  r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, unit, true));
+  return r;
+}
+__device__ __forceinline__ float unit_of(uint32_t s) { return __uint_as_float(s << 23); }
+
+// Infinite and NaN numbers of w to 0; true if there were any.
+template <typename T>
+__device__ __forceinline__ bool tame(u32x4 &w) {
+  bool odd = false;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const bool lo = (w[j] & T::kExp) == T::kExp;
+    const bool hi = (w[j] & (T::kExp << 16)) == T::kExp << 16;
+    odd |= lo | hi;
+    w[j] &= ~((lo ? 0xFFFFu : 0u) | (hi ? 0xFFFF0000u : 0u));
+  }
+  return odd;
+}
+
+// The walk over the keys of one (sequence, key head): tiles of KEYS keys of each
+// source in turn.  All of it is the same for every lane of a wave.
+struct Walk {
+  const char *k, *v;            // first row of the tile
+  const uint8_t *ks, *vs;
+  int k_row, v_row, ks_row, vs_row;
+  int source, left, tile;       // keys from the tile's first on; tile's number in the source
 };
 
-// e4m3 pair -> two numbers of 16 bits with the scale applied; exact in bf16.
-__device__ __forceinline__ uint32_t widen(uint32_t w, bool high, float unit) {
-  const f32x2 x = high ? __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(w), true)
-                       : __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(w), false);
-  return (__float_as_uint(x.x * unit) >> 16) | (__float_as_uint(x.y * unit) & 0xFFFF0000u);
-}
-__device__ __forceinline__ float unit_of(uint32_t s) {
-  return __uint_as_float(s ? s << 23 : 0x00400000u);
+__device__ __forceinline__ void enter(const AttendArgs &a, Walk &w, int source, int tile, int keys,
+                                      int count, int b, int kvh) {
+  const Source &s = source == 0 ? a.src[0] : source == 1 ? a.src[1] : a.src[2];
+  const int64_t base = source == 0 ? 0 : b, first = static_cast<int64_t>(tile) * keys;
+  w.source = source;
+  w.tile = tile;
+  w.left = count - tile * keys;
+  w.k_row = s.k.row;
+  w.v_row = s.v.row;
+  w.ks_row = s.k.s_row;
+  w.vs_row = s.v.s_row;
+  w.k = s.k.p + base * s.k.batch + kvh * s.k.head + first * s.k.row;
+  w.v = s.v.p + base * s.v.batch + kvh * s.v.head + first * s.v.row;
+  w.ks = s.k.s + base * s.k.s_batch + kvh * s.k.s_head + first * s.k.s_row;
+  w.vs = s.v.s + base * s.v.s_batch + kvh * s.v.s_head + first * s.v.s_row;
 }
 
-__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
+// Tile t of the walk whose sources have n0, n1, ... tiles of `keys` keys, c0, c1, c2 keys.
+__device__ __forceinline__ void seek(const AttendArgs &a, Walk &w, int t, int keys, int n0, int n1, int c0,
+                                     int c1, int c2, int b, int kvh) {
+  if (t < n0) enter(a, w, 0, t, keys, c0, b, kvh);
+  else if (t < n0 + n1) enter(a, w, 1, t - n0, keys, c1, b, kvh);
+  else enter(a, w, 2, t - n0 - n1, keys, c2, b, kvh);
+}
+// n tiles on in the same source.
+__device__ __forceinline__ void advance(Walk &w, int n, int keys) {
+  const int64_t rows = static_cast<int64_t>(n) * keys;
+  w.k += rows * w.k_row;
+  w.v += rows * w.v_row;
+  w.ks += rows * w.ks_row;
+  w.vs += rows * w.vs_row;
+  w.left -= n * keys;
+  w.tile += n;
+}
+
+// The slots 64 * word .. + 63 of the block that row (rb, slot) sees.
+__device__ __forceinline__ uint64_t seen_word(const AttendArgs &a, int rb, int slot, int word, int live) {
+  uint64_t w;
+  if (a.mask) {
+    const int node = slot - a.root;
+    if (node < 0) {
+      w = word == 0 ? 1 : 0;
+    } else {
+      const uint64_t *m = a.mask + (static_cast<int64_t>(rb) * a.n_max + node) * a.words;
+      w = word < a.words ? m[word] : 0;
+      if (a.root) w = (w << 1) | (word > 0 ? m[word - 1] >> 63 : 1);
+    }
+  } else {
+    const int n = slot - word * 64 + 1;
+    w = n <= 0 ? 0 : (n >= 64 ? ~0ull : (1ull << n) - 1);
+  }
+  const int have = live - word * 64;
+  return have < 64 ? w & ((1ull << (have < 0 ? 0 : have)) - 1) : w;
+}
+
+// Running state of 32 rows in a wave.
+template <int DP>
+struct Sums {
+  f32x16 o[DP / 32];
+  float m, l;                   // m: what the probabilities are relative to
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+    m = -INFINITY;
+    l = 0.0f;
+  }
+};
+
+// One step of the softmax over KT 32-key score tiles: probabilities, packed as right
+// operands of the second product (two 16-key groups a tile).
+template <typename T, int KT, int DP>
+__device__ __forceinline__ void softmax_step(Sums<DP> &st, f32x16 (&s)[KT], u32x4 (&p)[2 * KT], float c) {
+  float mx = s[0][0];
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[kt][i]);
+  mx = half_max(mx);
+  if (__ballot((mx - st.m) * c > kSlack) != 0) {     // -inf on both sides is not above
+    const float to = fmaxf(mx, st.m);
+    const float alpha = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((st.m - to) * c);
+    st.l *= alpha;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) st.o[d][i] *= alpha;
+    st.m = to;
+  }
+  const float off = st.m == -INFINITY ? 0.0f : -st.m * c;
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt) {
+    float e[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][i], c, off));
+    float l0 = 0.0f, l1 = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      l0 += e[i];
+      l1 += e[i + 1];
+      p[2 * kt + i / 8][(i / 2) % 4] = T::pack(e[i], e[i + 1]);
+    }
+    st.l += l0 + l1;
+  }
+}
+
+// Infinite and NaN values of the `count` slots of a block tile that a row sees (bits of
+// seen): they were stored as 0.  Not reached but for such values.
+template <typename T, int DP>
+__device__ __forceinline__ void add_odd(const char *v, int v_row, int count, uint64_t seen, int h, int dim,
+                                        Sums<DP> &st) {
+  for (int j = 0; j < count; ++j) {
+    if (!((seen >> j) & 1)) continue;
+    const uint16_t *row = reinterpret_cast<const uint16_t *>(v + static_cast<int64_t>(j) * v_row);
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int at = d * 32 + 8 * (i / 4) + 4 * h + i % 4;
+        if (at < dim && (row[at] & T::kExp) == T::kExp) st.o[d][i] += T::number(row[at]);
+      }
+  }
+}
+
+// LDS place of 16-byte chunk c of a row of C chunks.
+template <int C> __device__ __forceinline__ int k_at(int r, int c) { return r * C + (c ^ (r & (C - 1))); }
+template <int C> __device__ __forceinline__ int v_at(int r, int c) { return r * C + (c ^ (2 * (r & (C / 2 - 1)))); }
+
+// V^T's fragment: columns 32 d .. + 31 of keys 16 g + 4 h + {0..3, 8..11}; base is the
+// lane's row and column of the transposing read, for g = 0.
+template <int C>
+__device__ __forceinline__ u32x4 v_fragment(const u32x4 *s_v, int d, int g, int lane) {
+  typedef __attribute__((address_space(3))) s16x4 *at;
+  const int h = lane >> 5, s = lane & 15;
+  const int r = 4 * h + (s >> 2), c = 4 * d + 2 * ((lane >> 4) & 1) + ((s & 3) >> 1);
+  const char *p = reinterpret_cast<const char *>(s_v + v_at<C>(r, c)) + (s & 1) * 8 + g * 16 * C * 16;
+  const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)(p)));
+  const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)(p + 8 * C * 16)));
+  return u32x4{lo.x, lo.y, hi.x, hi.y};
+}
+
+// What a workgroup works on, whichever way it walks.
+struct Item {
+  int b, kvh, tile_row, part;
+  bool packed;
+};
 
 template <typename T, bool Q8, int DP>
-__global__ void __launch_bounds__(kAttThreads, 2)
-attend_kernel(AttendArgs a) {
-  constexpr int kChunks = DP / 8;                       // 16-byte chunks of a key row in LDS
+__device__ __forceinline__ void wide_part(const AttendArgs &a, const Item &it, u32x4 *lds) {
+  constexpr int C = DP / 8;                             // 16-byte chunks of a row in LDS
   constexpr int kSteps = DP / 16, kDTiles = DP / 32;
-  constexpr int kKUnits = kKeyTile * kChunks / kAttThreads;
-  constexpr int kVThreads = kKeyTile / 4 * kChunks;     // 4 keys x 8 numbers each
-  __shared__ __align__(16) u32x4 s_k[2][kKeyTile * kChunks];
-  __shared__ __align__(16) u32x2 s_v[2][DP * (kKeyTile / 4)];
+  constexpr int kBuf = kKeyTile * C;                    // a buffer of keys, or of values
+  constexpr int kUnits = kBuf / kAttThreads, kStep = kAttThreads / C;
+  u32x4 *s_k = lds, *s_v = lds + 2 * kBuf;
 
   const int tid = threadIdx.x, lane = lane_id(), wave = tid / kWave;
   const int h = lane >> 5, col = lane & 31;
+  const int b = it.b, kvh = it.kvh;
+  const bool packed = it.packed;
 
-  // which rows and which keys
-  const bool packed = static_cast<int>(blockIdx.x) < a.shared_items;
-  int b = 0, kvh, tile_row, part;
-  if (packed) {
-    int i = blockIdx.x;
-    part = i % a.shared_splits;
-    i /= a.shared_splits;
-    tile_row = i % a.shared_tiles;
-    kvh = i / a.shared_tiles;
-  } else {
-    // the row tiles of one (sequence, key head, part) read the same keys: they
-    // follow each other on one XCD (workgroups go round the 8 XCDs)
-    const int i = blockIdx.x - a.shared_items;
-    const int j = i >> 3;
-    const int g = (j / a.row_tiles) * 8 + (i & 7);
-    tile_row = j % a.row_tiles;
-    part = g % a.splits;
-    const int bh = g / a.splits;
-    b = bh / a.kv_heads;
-    kvh = bh - b * a.kv_heads;
-    if (b >= a.batch) return;
-  }
-
-  bool bad = false;
+  bool bad = false, unused;
   const int per_seq = a.slots * a.group;
-  const int live = packed ? 0 : slots_of(a, b, &bad);
-  if (!packed && tile_row * kRowTile >= live * a.group) {
-    if (bad && tile_row == 0 && part == 0 && kvh == 0 && tid == 0) atomicOr(a.error_flag, kErrBlockSizes);
+  const int live = packed ? 0 : __builtin_amdgcn_readfirstlane(slots_of(a, b, &bad));
+  const bool speaks = it.tile_row == 0 && it.part == 0 && kvh == 0 && tid == 0;
+  if (!packed && it.tile_row * kRowTile >= live * a.group) {
+    if (bad && speaks) atomicOr(a.error_flag, kErrBlockSizes);
     return;
   }
-  int row = tile_row * kRowTile + wave * 32 + col;
+  int row = it.tile_row * kRowTile + wave * 32 + col;
   int rb = b;
   if (packed) {
-    const int total = a.batch * per_seq;
-    rb = row < total ? row / per_seq : a.batch - 1;
+    rb = row < a.batch * per_seq ? row / per_seq : a.batch - 1;
     row -= rb * per_seq;
   }
-  bool unused;
   const int rlive = packed ? slots_of(a, rb, &unused) : live;
   const bool valid = row < rlive * a.group;
   row = row < per_seq ? row : per_seq - 1;
@@ -195,188 +372,82 @@ attend_kernel(AttendArgs a) {
 
   int len = 0;
   if (!packed && a.cache_rows > 0) {
-    len = a.cache_len[b];
+    len = __builtin_amdgcn_readfirstlane(a.cache_len[b]);
     bad |= len < 0 || len > a.cache_rows;
     len = len < 0 ? 0 : (len > a.cache_rows ? a.cache_rows : len);
   }
-  if (bad && tile_row == 0 && part == 0 && kvh == 0 && tid == 0) atomicOr(a.error_flag, kErrBlockSizes);
-  const int n_shared = packed || a.shared_items == 0 ? (a.shared_len + kKeyTile - 1) / kKeyTile : 0;
-  const int n_cache = packed ? 0 : (len + kKeyTile - 1) / kKeyTile;
-  const int n_block = packed ? 0 : (live + kKeyTile - 1) / kKeyTile;
-  const int n_tiles = n_shared + n_cache + n_block;
+  if (bad && speaks) atomicOr(a.error_flag, kErrBlockSizes);
+  const int n0 = packed || a.shared_items == 0 ? (a.shared_len + kKeyTile - 1) / kKeyTile : 0;
+  const int n1 = (len + kKeyTile - 1) / kKeyTile, n2 = (live + kKeyTile - 1) / kKeyTile;
+  const int n_tiles = n0 + n1 + n2;
   const int splits = packed ? a.shared_splits : a.splits;
   int per = (n_tiles + splits - 1) / splits;
   per = per < a.min_tiles ? a.min_tiles : per;
-  const int t0 = part * per < n_tiles ? part * per : n_tiles;
+  const int t0 = it.part * per < n_tiles ? it.part * per : n_tiles;
   const int t1 = t0 + per < n_tiles ? t0 + per : n_tiles;
 
-  auto tile_at = [&](int t) {
-    Tile x;
-    int64_t base;
-    if (t < n_shared) {
-      x.k = a.shared_k;
-      x.v = a.shared_v;
-      x.key0 = t * kKeyTile;
-      x.count = a.shared_len - x.key0;
-      x.quant = Q8;
-      x.block = false;
-      base = 0;
-    } else if (t < n_shared + n_cache) {
-      x.k = a.cache_k;
-      x.v = a.cache_v;
-      x.key0 = (t - n_shared) * kKeyTile;
-      x.count = len - x.key0;
-      x.quant = Q8;
-      x.block = false;
-      base = b;
-    } else {
-      x.k = a.block_k;
-      x.v = a.block_v;
-      x.key0 = (t - n_shared - n_cache) * kKeyTile;
-      x.count = live - x.key0;
-      x.quant = false;
-      x.block = true;
-      base = b;
-    }
-    x.count = x.count < kKeyTile ? x.count : kKeyTile;
-    x.k.p += base * x.k.batch + kvh * x.k.head;
-    x.v.p += base * x.v.batch + kvh * x.v.head;
-    if (Q8 && x.quant) {
-      x.k.s += base * x.k.s_batch + kvh * x.k.s_head;
-      x.v.s += base * x.v.s_batch + kvh * x.v.s_head;
-    }
-    return x;
-  };
-
-  // a thread's share of a tile: kKUnits 16-byte chunks of keys (or half as many of
-  // codes), and 4 keys x 8 numbers of the values
-  u32x4 rk[kKUnits], rv[4];
-  uint32_t sk[kKUnits], sv[4];
-  const int vc = tid % kChunks, vg = tid / kChunks;
-  const bool v_mine = tid < kVThreads && vc * 8 < a.dim;
-  auto load = [&](const Tile &x) {
-    if (Q8 && x.quant) {
-      constexpr int kQ = kChunks / 2;
+  // a thread's share of a tile: chunk ch of rows r0, r0 + kStep, ...; of codes, 16 of rows
+  // q0, q0 + 2 kStep, ...
+  const int r0 = tid / C, ch = tid % C, q0 = tid / (C / 2), qc = tid % (C / 2);
+  const int at16 = ch * 8 < a.dim ? ch * 16 : kOutside, at8 = qc * 16 < a.dim ? qc * 16 : kOutside;
+  u32x4 rk[kUnits], rv[kUnits];
+  uint32_t sk[kUnits / 2], sv[kUnits / 2];
+  auto load = [&](const Walk &w) {
+    const int n = w.left < kKeyTile ? w.left : kKeyTile;
+    if (Q8 && w.source != 2) {
+      const auto bk = buffer(w.k, (n - 1) * w.k_row + a.dim), bv = buffer(w.v, (n - 1) * w.v_row + a.dim);
+      const auto bks = buffer(w.ks, (n - 1) * w.ks_row + 1), bvs = buffer(w.vs, (n - 1) * w.vs_row + 1);
 #pragma unroll
-      for (int i = 0; i < kKUnits / 2; ++i) {
-        const int u = tid + i * kAttThreads, r = u / kQ, c = u % kQ;
-        rk[i] = u32x4{0, 0, 0, 0};
-        sk[i] = 127;
-        if (r < x.count && c * 16 < a.dim) {
-          const int64_t key = x.key0 + r;
-          rk[i] = *reinterpret_cast<const u32x4 *>(x.k.p + key * x.k.row + c * 16);
-          sk[i] = x.k.s[key * x.k.s_row];
-        }
+      for (int i = 0; i < kUnits / 2; ++i) {
+        const int r = q0 + i * 2 * kStep;
+        rk[i] = load16(bk, r * w.k_row + at8);
+        sk[i] = __builtin_amdgcn_raw_buffer_load_b8(bks, r * w.ks_row, 0, 0);
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = vg * 4 + i;
-        rv[i] = u32x4{0, 0, 0, 0};
-        sv[i] = 127;
-        if (v_mine && r < x.count) {
-          const int64_t key = x.key0 + r;
-          const u32x2 w = *reinterpret_cast<const u32x2 *>(x.v.p + key * x.v.row + vc * 8);
-          rv[i] = u32x4{w.x, w.y, 0, 0};
-          sv[i] = x.v.s[key * x.v.s_row];
-        }
+      for (int i = 0; i < kUnits / 2; ++i) {
+        const int r = q0 + i * 2 * kStep;
+        rv[i] = load16(bv, r * w.v_row + at8);
+        sv[i] = __builtin_amdgcn_raw_buffer_load_b8(bvs, r * w.vs_row, 0, 0);
       }
     } else {
+      const auto bk = buffer(w.k, (n - 1) * w.k_row + 2 * a.dim), bv = buffer(w.v, (n - 1) * w.v_row + 2 * a.dim);
 #pragma unroll
-      for (int i = 0; i < kKUnits; ++i) {
-        const int u = tid + i * kAttThreads, r = u / kChunks, c = u % kChunks;
-        rk[i] = u32x4{0, 0, 0, 0};
-        if (r < x.count && c * 8 < a.dim)
-          rk[i] = *reinterpret_cast<const u32x4 *>(x.k.p + static_cast<int64_t>(x.key0 + r) * x.k.row + c * 16);
-      }
+      for (int i = 0; i < kUnits; ++i) rk[i] = load16(bk, (r0 + i * kStep) * w.k_row + at16);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = vg * 4 + i;
-        rv[i] = u32x4{0, 0, 0, 0};
-        if (v_mine && r < x.count)
-          rv[i] = *reinterpret_cast<const u32x4 *>(x.v.p + static_cast<int64_t>(x.key0 + r) * x.v.row + vc * 16);
-      }
+      for (int i = 0; i < kUnits; ++i) rv[i] = load16(bv, (r0 + i * kStep) * w.v_row + at16);
     }
   };
-  // Stores the share; true if a block's value is infinite or NaN (stored as 0 then:
-  // a zero probability of a hidden slot must not meet it).
-  auto store = [&](const Tile &x, int buf) {
+  auto store = [&](int source, int buf) {
     bool odd = false;
-    if (Q8 && x.quant) {
-      constexpr int kQ = kChunks / 2;
+    u32x4 *k = s_k + buf * kBuf, *v = s_v + buf * kBuf;
+    if (Q8 && source != 2) {
 #pragma unroll
-      for (int i = 0; i < kKUnits / 2; ++i) {
-        const int u = tid + i * kAttThreads, r = u / kQ, c = u % kQ;
-        const float unit = unit_of(sk[i]);
-        u32x4 w0, w1;
+      for (int i = 0; i < kUnits / 2; ++i) {
+        const int r = q0 + i * 2 * kStep;
+        const float uk = unit_of(sk[i]), uv = unit_of(sv[i]);
+        u32x2 x[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t lo = widen(rk[i][j], false, unit), hi = widen(rk[i][j], true, unit);
-          if (j < 2) { w0[2 * j] = lo; w0[2 * j + 1] = hi; }
-          else { w1[2 * j - 4] = lo; w1[2 * j - 3] = hi; }
-        }
-        const int sw = r & (kChunks - 1);
-        s_k[buf][r * kChunks + ((2 * c) ^ sw)] = w0;
-        s_k[buf][r * kChunks + ((2 * c + 1) ^ sw)] = w1;
-      }
+        for (int j = 0; j < 4; ++j) x[j] = widen(rk[i][j], uk);
+        k[k_at<C>(r, 2 * qc)] = u32x4{x[0].x, x[0].y, x[1].x, x[1].y};
+        k[k_at<C>(r, 2 * qc + 1)] = u32x4{x[2].x, x[2].y, x[3].x, x[3].y};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float unit = unit_of(sv[i]);
-        const uint32_t x0 = rv[i].x, x1 = rv[i].y;
-        rv[i] = u32x4{widen(x0, false, unit), widen(x0, true, unit), widen(x1, false, unit),
-                      widen(x1, true, unit)};
+        for (int j = 0; j < 4; ++j) x[j] = widen(rv[i][j], uv);
+        v[v_at<C>(r, 2 * qc)] = u32x4{x[0].x, x[0].y, x[1].x, x[1].y};
+        v[v_at<C>(r, 2 * qc + 1)] = u32x4{x[2].x, x[2].y, x[3].x, x[3].y};
       }
     } else {
+      if (source == 2) {
 #pragma unroll
-      for (int i = 0; i < kKUnits; ++i) {
-        const int u = tid + i * kAttThreads, r = u / kChunks, c = u % kChunks;
-        s_k[buf][r * kChunks + (c ^ (r & (kChunks - 1)))] = rk[i];
+        for (int i = 0; i < kUnits; ++i) odd |= tame<T>(rv[i]);
       }
-      if (x.block) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t w = rv[i][j];
-            const uint32_t e = T::kExp;
-            const bool lo = (w & e) == e, hi = (w & (e << 16)) == e << 16;
-            odd |= lo | hi;
-            rv[i][j] = w & ~((lo ? 0xFFFFu : 0u) | (hi ? 0xFFFF0000u : 0u));
-          }
-      }
-    }
-    if (tid < kVThreads) {
-      // keys 4 vg .. + 3 are the low or the high four of half (vg & 1) of group vg / 4
-      const int p = (vg >> 2) * 4 + (vg & 1) * 2 + ((vg >> 1) & 1);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int d = vc * 8 + j;
-        const uint32_t sel = j & 1 ? 0x07060302u : 0x05040100u;
-        u32x2 w;
-        w.x = __builtin_amdgcn_perm(rv[1][j / 2], rv[0][j / 2], sel);
-        w.y = __builtin_amdgcn_perm(rv[3][j / 2], rv[2][j / 2], sel);
-        s_v[buf][d * (kKeyTile / 4) + (p ^ (2 * ((d ^ (d >> 3)) & 7)))] = w;
+      for (int i = 0; i < kUnits; ++i) {
+        const int r = r0 + i * kStep;
+        k[k_at<C>(r, ch)] = rk[i];
+        v[v_at<C>(r, ch)] = rv[i];
       }
     }
     return odd;
-  };
-  // The slots of block tile x that this lane's row sees.
-  auto sees = [&](const Tile &x) -> uint64_t {
-    const int tb = x.key0 / kKeyTile;
-    uint64_t w;
-    if (a.mask) {
-      const int node = slot - a.root;
-      if (node < 0) {
-        w = tb == 0 ? 1 : 0;
-      } else {
-        const uint64_t *m = a.mask + (static_cast<int64_t>(rb) * a.n_max + node) * a.words;
-        w = tb < a.words ? m[tb] : 0;
-        if (a.root) w = (w << 1) | (tb > 0 ? m[tb - 1] >> 63 : 1);
-      }
-    } else {
-      const int n = slot - x.key0 + 1;
-      w = n <= 0 ? 0 : (n >= 64 ? ~0ull : (1ull << n) - 1);
-    }
-    return x.count < 64 ? w & ((1ull << x.count) - 1) : w;
   };
 
   // the queries: the right operand of S^T = K Q^T
@@ -386,120 +457,71 @@ attend_kernel(AttendArgs a) {
   for (int s = 0; s < kSteps; ++s)
     rq[s] = s * 16 < a.dim ? *reinterpret_cast<const u32x4 *>(qp + s * 32 + h * 16) : u32x4{0, 0, 0, 0};
 
-  f32x16 o[kDTiles];
-#pragma unroll
-  for (int d = 0; d < kDTiles; ++d)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
-  float m = -INFINITY, l = 0.0f;
-
-  Tile cur{}, next{};
-  uint64_t seen = 0, seen_next = 0;
+  Sums<DP> st;
+  st.clear();
+  Walk w{};
+  uint64_t seen_next = 0;
   if (t0 < t1) {
-    cur = tile_at(t0);
-    load(cur);
-    if (cur.block) seen = sees(cur);
+    seek(a, w, t0, kKeyTile, n0, n1, a.shared_len, len, live, b, kvh);
+    load(w);
+    if (w.source == 2) seen_next = seen_word(a, rb, slot, w.tile, live);
   }
   for (int t = t0; t < t1; ++t) {
     const int buf = (t - t0) & 1;
-    const bool odd = store(cur, buf);
+    const int source = w.source, left = w.left;
+    const char *v_rows = w.v;
+    const int v_row = w.v_row;
+    const uint64_t seen = seen_next;
+    const bool odd = store(source, buf);
     if (t + 1 < t1) {
-      next = tile_at(t + 1);
-      load(next);
-      if (next.block) seen_next = sees(next);
+      if (w.left > kKeyTile) advance(w, 1, kKeyTile);
+      else seek(a, w, t + 1, kKeyTile, n0, n1, a.shared_len, len, live, b, kvh);
+      load(w);
+      if (w.source == 2) seen_next = seen_word(a, rb, slot, w.tile, live);
     }
     bool any_odd = false;
-    if (cur.block) any_odd = __syncthreads_or(odd);
+    if (source == 2) any_odd = __syncthreads_or(odd);
     else __syncthreads();
-    if (busy) {
-      f32x16 s[2];
+    if (!busy) continue;
+    const u32x4 *k = s_k + buf * kBuf, *v = s_v + buf * kBuf;
+    f32x16 s[2];
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[kt][i] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i)
+        if (i * 16 < a.dim) s[kt] = T::mfma(k[k_at<C>(kt * 32 + col, 2 * i + h)], rq[i], s[kt]);
+    }
+    if (source == 2 || left < kKeyTile) {
+      const uint64_t bits = (source == 2 ? seen : (1ull << left) - 1) >> (4 * h);
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt) {
+        const uint32_t x = static_cast<uint32_t>(bits >> (32 * kt));
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[kt][i] = 0.0f;
-        const int r = kt * 32 + col;
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i)
-          if (i * 16 < a.dim)
-            s[kt] = T::mfma(s_k[buf][r * kChunks + ((2 * i + h) ^ (r & (kChunks - 1)))], rq[i], s[kt]);
-      }
-      if (cur.block || cur.count < kKeyTile) {
-        const uint64_t w = cur.block ? seen : (1ull << cur.count) - 1;
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
-          const uint32_t bits = static_cast<uint32_t>(w >> (32 * kt)) >> (4 * h);
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            s[kt][i] = (bits >> (8 * (i / 4) + i % 4)) & 1u ? s[kt][i] : -INFINITY;
-        }
-      }
-      float mx = m;
-#pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[kt][i]);
-      mx = fmaxf(mx, other_half(mx));
-      const float off = mx == -INFINITY ? 0.0f : mx * a.c;
-      if (__ballot(mx != m) != 0) {
-        const float alpha = __builtin_amdgcn_exp2f(m * a.c - off);
-        l *= alpha;
-#pragma unroll
-        for (int d = 0; d < kDTiles; ++d)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
-        m = mx;
-      }
-      u32x4 p[4];
-#pragma unroll
-      for (int kt = 0; kt < 2; ++kt) {
-        float e[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][i], a.c, -off));
-          l += e[i];
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) p[2 * kt + i / 4][i % 4] = T::pack(e[2 * i], e[2 * i + 1]);
-      }
-#pragma unroll
-      for (int d = 0; d < kDTiles; ++d) {
-        if (d * 32 >= a.dim) continue;
-        const int r = d * 32 + col;
-        const int sw = 2 * ((r ^ (r >> 3)) & 7);
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const u32x4 v = *reinterpret_cast<const u32x4 *>(
-              &s_v[buf][r * (kKeyTile / 4) + ((4 * g + 2 * h) ^ sw)]);
-          o[d] = T::mfma(v, p[g], o[d]);
-        }
-      }
-      if (any_odd) {
-        // infinite and NaN values of the slots that the row does see
-        for (int j = 0; j < cur.count; ++j) {
-          const uint16_t *v = reinterpret_cast<const uint16_t *>(
-              cur.v.p + static_cast<int64_t>(cur.key0 + j) * cur.v.row);
-          if (!((seen >> j) & 1)) continue;
-#pragma unroll
-          for (int d = 0; d < kDTiles; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int at = d * 32 + 8 * (i / 4) + 4 * h + i % 4;
-              if (at < a.dim && (v[at] & T::kExp) == T::kExp) o[d][i] += T::number(v[at]);
-            }
-        }
+        for (int i = 0; i < 16; ++i) s[kt][i] = (x >> (8 * (i / 4) + i % 4)) & 1u ? s[kt][i] : -INFINITY;
       }
     }
-    cur = next;
-    seen = seen_next;
+    u32x4 p[4];
+    softmax_step<T, 2>(st, s, p, a.c);
+#pragma unroll
+    for (int d = 0; d < kDTiles; ++d) {
+      if (d * 32 >= a.dim) continue;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) st.o[d] = T::mfma(v_fragment<C>(v, d, g, lane), p[g], st.o[d]);
+    }
+    if (any_odd) {
+      add_odd<T, DP>(v_rows, v_row, left < kKeyTile ? left : kKeyTile, seen, h, a.dim, st);
+    }
   }
 
-  l += other_half(l);
+  st.l = half_sum(st.l);
   if (!valid) return;
   if (a.parts > 1) {
-    const int at_part = packed ? a.splits + part : part;
+    const int at_part = packed ? a.splits + it.part : it.part;
     const int64_t r = (static_cast<int64_t>(rb) * a.slots + slot) * a.q_heads + head;
     const int64_t at = at_part * a.rows_all + r;
-    if (h == 0) a.part_ml[at] = f32x2{t0 < t1 ? m * a.c : -INFINITY, l};
+    if (h == 0) a.part_ml[at] = f32x2{t0 < t1 ? st.m * a.c : -INFINITY, st.l};
     if (t0 >= t1) return;
     float *po = a.part_o + at * a.dim;
 #pragma unroll
@@ -509,11 +531,11 @@ attend_kernel(AttendArgs a) {
         const int x = d * 32 + 8 * i + 4 * h;
         if (x < a.dim)
           *reinterpret_cast<f32x4 *>(po + x) =
-              f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+              f32x4{st.o[d][4 * i], st.o[d][4 * i + 1], st.o[d][4 * i + 2], st.o[d][4 * i + 3]};
       }
     return;
   }
-  const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+  const float inv = st.l > 0.0f || st.l != st.l ? 1.0f / st.l : 0.0f;
   char *op = a.out + rb * a.o_batch + slot * a.o_slot + head * a.o_head;
 #pragma unroll
   for (int d = 0; d < kDTiles; ++d)
@@ -522,12 +544,260 @@ attend_kernel(AttendArgs a) {
       const int x = d * 32 + 8 * i + 4 * h;
       if (x < a.dim)
         *reinterpret_cast<u32x2 *>(op + 2 * x) =
-            u32x2{T::pack(o[d][4 * i] * inv, o[d][4 * i + 1] * inv),
-                  T::pack(o[d][4 * i + 2] * inv, o[d][4 * i + 3] * inv)};
+            u32x2{T::pack(st.o[d][4 * i] * inv, st.o[d][4 * i + 1] * inv),
+                  T::pack(st.o[d][4 * i + 2] * inv, st.o[d][4 * i + 3] * inv)};
     }
   if (a.lse && h == 0)
     a.lse[(static_cast<int64_t>(rb) * a.slots + slot) * a.q_heads + head] =
-        l == 0.0f ? -INFINITY : (m * a.c + __log2f(l)) * 0.69314718055994531f;
+        st.l == 0.0f ? -INFINITY : (st.m * a.c + __log2f(st.l)) * 0.69314718055994531f;
+}
+
+template <typename T, bool Q8, int DP>
+__device__ __forceinline__ void narrow_part(const AttendArgs &a, const Item &it, u32x4 *lds) {
+  constexpr int C = DP / 8;
+  constexpr int kSteps = DP / 16, kDTiles = DP / 32;
+  constexpr int kPad = DP + 4;                          // floats of a row when the waves are joined
+  const int tid = threadIdx.x, lane = lane_id(), wave = tid / kWave;
+  const int h = lane >> 5, col = lane & 31;
+  const int b = it.b, kvh = it.kvh;
+  u32x4 *s_v = lds + wave * kFewKeys * C;
+
+  bool bad = false;
+  const int live = __builtin_amdgcn_readfirstlane(slots_of(a, b, &bad));
+  const bool speaks = it.tile_row == 0 && it.part == 0 && kvh == 0 && tid == 0;
+  if (it.tile_row * kFewRows >= live * a.group) {
+    if (bad && speaks) atomicOr(a.error_flag, kErrBlockSizes);
+    return;
+  }
+  const int per_seq = a.slots * a.group;
+  int row = it.tile_row * kFewRows + col;
+  row = row < per_seq ? row : per_seq - 1;
+  const int slot = row / a.group, head = kvh * a.group + row - slot * a.group;
+  int len = 0;
+  if (a.cache_rows > 0) {
+    len = __builtin_amdgcn_readfirstlane(a.cache_len[b]);
+    bad |= len < 0 || len > a.cache_rows;
+    len = len < 0 ? 0 : (len > a.cache_rows ? a.cache_rows : len);
+  }
+  if (bad && speaks) atomicOr(a.error_flag, kErrBlockSizes);
+  const int n0 = a.shared_items == 0 ? (a.shared_len + kFewKeys - 1) / kFewKeys : 0;
+  const int n1 = (len + kFewKeys - 1) / kFewKeys, n2 = (live + kFewKeys - 1) / kFewKeys;
+  const int n_tiles = n0 + n1 + n2;
+  // a part's tiles, in rounds of one tile a wave
+  const int rounds = (n_tiles + kAttWaves - 1) / kAttWaves;
+  int per = (rounds + a.splits - 1) / a.splits;
+  per = (per < a.min_tiles ? a.min_tiles : per) * kAttWaves;
+  const int t0 = it.part * per < n_tiles ? it.part * per : n_tiles;
+  const int t1 = t0 + per < n_tiles ? t0 + per : n_tiles;
+
+  // Contracted entries 8 of a step from chunk k_chunk(step) of a row on: 16 codes that one
+  // load brings are two steps' 8.
+  auto k_chunk = [&](int s) { return Q8 ? 2 * (2 * (s / 2) + h) + s % 2 : 2 * s + h; };
+  u32x4 rq[kSteps];
+  const char *qp = a.q + b * a.q_batch + slot * a.q_slot + head * a.q_head;
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s)
+    rq[s] = k_chunk(s) * 8 < a.dim ? *reinterpret_cast<const u32x4 *>(qp + k_chunk(s) * 16) : u32x4{0, 0, 0, 0};
+
+  const int r0 = lane / C, ch = lane % C, q0 = lane / (C / 2), qc = lane % (C / 2);
+  const int at16 = ch * 8 < a.dim ? ch * 16 : kOutside, at8 = qc * 16 < a.dim ? qc * 16 : kOutside;
+  u32x4 rk[kSteps], rv[C / 2];
+  uint32_t sk = 0, sv[C / 4];
+  auto load = [&](const Walk &w) {
+    const int n = w.left < kFewKeys ? w.left : kFewKeys;
+    if (Q8 && w.source != 2) {
+      const auto bk = buffer(w.k, (n - 1) * w.k_row + a.dim), bv = buffer(w.v, (n - 1) * w.v_row + a.dim);
+      const auto bks = buffer(w.ks, (n - 1) * w.ks_row + 1), bvs = buffer(w.vs, (n - 1) * w.vs_row + 1);
+#pragma unroll
+      for (int i = 0; i < kSteps / 2; ++i)
+        rk[i] = load16(bk, col * w.k_row + ((2 * i + h) * 16 < a.dim ? (2 * i + h) * 16 : kOutside));
+      sk = __builtin_amdgcn_raw_buffer_load_b8(bks, col * w.ks_row, 0, 0);
+#pragma unroll
+      for (int i = 0; i < C / 4; ++i) {
+        const int r = q0 + i * (2 * kWave / C);
+        rv[i] = load16(bv, r * w.v_row + at8);
+        sv[i] = __builtin_amdgcn_raw_buffer_load_b8(bvs, r * w.vs_row, 0, 0);
+      }
+    } else {
+      const auto bk = buffer(w.k, (n - 1) * w.k_row + 2 * a.dim), bv = buffer(w.v, (n - 1) * w.v_row + 2 * a.dim);
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s)
+        rk[s] = load16(bk, col * w.k_row + (k_chunk(s) * 8 < a.dim ? k_chunk(s) * 16 : kOutside));
+#pragma unroll
+      for (int i = 0; i < C / 2; ++i) rv[i] = load16(bv, (r0 + i * (kWave / C)) * w.v_row + at16);
+    }
+  };
+
+  Sums<DP> st;
+  st.clear();
+  Walk w{};
+  int t = t0 + wave;
+  uint64_t seen_next = 0;
+  if (t < t1) {
+    seek(a, w, t, kFewKeys, n0, n1, a.shared_len, len, live, b, kvh);
+    load(w);
+    if (w.source == 2) seen_next = seen_word(a, b, slot, w.tile / 2, live) >> (32 * (w.tile & 1));
+  }
+  for (; t < t1; t += kAttWaves) {
+    const int source = w.source, left = w.left;
+    const char *v_rows = w.v;
+    const int v_row = w.v_row;
+    const uint32_t seen = static_cast<uint32_t>(seen_next);
+    // the tile out of the loaded registers: scores, and the values to LDS
+    f32x16 s[1];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[0][i] = 0.0f;
+    bool odd = false;
+    if (Q8 && source != 2) {
+      const float uk = unit_of(sk);
+#pragma unroll
+      for (int i = 0; i < kSteps / 2; ++i) {
+        u32x2 x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = widen(rk[i][j], uk);
+        s[0] = T::mfma(u32x4{x[0].x, x[0].y, x[1].x, x[1].y}, rq[2 * i], s[0]);
+        s[0] = T::mfma(u32x4{x[2].x, x[2].y, x[3].x, x[3].y}, rq[2 * i + 1], s[0]);
+      }
+#pragma unroll
+      for (int i = 0; i < C / 4; ++i) {
+        const int r = q0 + i * (2 * kWave / C);
+        const float uv = unit_of(sv[i]);
+        u32x2 x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = widen(rv[i][j], uv);
+        s_v[v_at<C>(r, 2 * qc)] = u32x4{x[0].x, x[0].y, x[1].x, x[1].y};
+        s_v[v_at<C>(r, 2 * qc + 1)] = u32x4{x[2].x, x[2].y, x[3].x, x[3].y};
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) s[0] = T::mfma(rk[i], rq[i], s[0]);
+      if (source == 2) {
+#pragma unroll
+        for (int i = 0; i < C / 2; ++i) odd |= tame<T>(rv[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < C / 2; ++i) s_v[v_at<C>(r0 + i * (kWave / C), ch)] = rv[i];
+    }
+    if (t + kAttWaves < t1) {
+      if (w.left > kAttWaves * kFewKeys) advance(w, kAttWaves, kFewKeys);
+      else seek(a, w, t + kAttWaves, kFewKeys, n0, n1, a.shared_len, len, live, b, kvh);
+      load(w);
+      if (w.source == 2) seen_next = seen_word(a, b, slot, w.tile / 2, live) >> (32 * (w.tile & 1));
+    }
+    if (source == 2 || left < kFewKeys) {
+      const uint32_t bits = (source == 2 ? seen : (1u << left) - 1) >> (4 * h);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[0][i] = (bits >> (8 * (i / 4) + i % 4)) & 1u ? s[0][i] : -INFINITY;
+    }
+    u32x4 p[2];
+    softmax_step<T, 1>(st, s, p, a.c);
+    // the wave's LDS operations are done in order
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int d = 0; d < kDTiles; ++d) {
+      if (d * 32 >= a.dim) continue;
+#pragma unroll
+      for (int g = 0; g < 2; ++g) st.o[d] = T::mfma(v_fragment<C>(s_v, d, g, lane), p[g], st.o[d]);
+    }
+    __builtin_amdgcn_wave_barrier();
+    if (source == 2 && __ballot(odd) != 0) {
+      add_odd<T, DP>(v_rows, v_row, left < kFewKeys ? left : kFewKeys, seen, h, a.dim, st);
+    }
+  }
+
+  // the four waves' rows, one wave after the other so that the sums have one order
+  float *s_o = reinterpret_cast<float *>(lds);
+  float *s_m = s_o + kFewRows * kPad, *s_l = s_m + kAttWaves * kFewRows;
+  st.l = half_sum(st.l);
+  __syncthreads();
+  if (h == 0) {
+    s_m[wave * kFewRows + col] = st.m;
+    s_l[wave * kFewRows + col] = st.l;
+  }
+  __syncthreads();
+  float top = s_m[col];
+#pragma unroll
+  for (int i = 1; i < kAttWaves; ++i) top = fmaxf(top, s_m[i * kFewRows + col]);
+  const float alpha = st.m == top ? 1.0f : __builtin_amdgcn_exp2f((st.m - top) * a.c);
+  float total = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kAttWaves; ++i) {
+    const float x = s_m[i * kFewRows + col];
+    total += s_l[i * kFewRows + col] * (x == top ? 1.0f : __builtin_amdgcn_exp2f((x - top) * a.c));
+  }
+  for (int i = 0; i < kAttWaves; ++i) {
+    if (wave == i) {
+#pragma unroll
+      for (int d = 0; d < kDTiles; ++d)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          f32x4 *at = reinterpret_cast<f32x4 *>(s_o + col * kPad + d * 32 + 8 * j + 4 * h);
+          f32x4 x = f32x4{st.o[d][4 * j], st.o[d][4 * j + 1], st.o[d][4 * j + 2], st.o[d][4 * j + 3]} * alpha;
+          if (i > 0) x += *at;
+          *at = x;
+        }
+    }
+    __syncthreads();
+  }
+  // statistics of the row by its first lanes, then the rows by all threads
+  if (wave == 0 && h == 0) {
+    s_m[col] = top;
+    s_l[col] = total;
+  }
+  __syncthreads();
+  const int rows = min(kFewRows, live * a.group - it.tile_row * kFewRows);
+  for (int u = tid; u < rows * (DP / 4); u += kAttThreads) {
+    const int r = u / (DP / 4), x = (u % (DP / 4)) * 4;
+    if (x >= a.dim) continue;
+    const int i = it.tile_row * kFewRows + r;
+    const int sl = i / a.group, hd = kvh * a.group + i - sl * a.group;
+    const int64_t all = (static_cast<int64_t>(b) * a.slots + sl) * a.q_heads + hd;
+    const float m = s_m[r], l = s_l[r];
+    const f32x4 o = *reinterpret_cast<const f32x4 *>(s_o + r * kPad + x);
+    if (a.parts > 1) {
+      const int64_t at = it.part * a.rows_all + all;
+      if (x == 0) a.part_ml[at] = f32x2{t0 < t1 ? m * a.c : -INFINITY, l};
+      if (t0 < t1) *reinterpret_cast<f32x4 *>(a.part_o + at * a.dim + x) = o;
+    } else {
+      const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+      *reinterpret_cast<u32x2 *>(a.out + b * a.o_batch + sl * a.o_slot + hd * a.o_head + 2 * x) =
+          u32x2{T::pack(o.x * inv, o.y * inv), T::pack(o.z * inv, o.w * inv)};
+      if (a.lse && x == 0)
+        a.lse[all] = l == 0.0f ? -INFINITY : (m * a.c + __log2f(l)) * 0.69314718055994531f;
+    }
+  }
+}
+
+template <typename T, bool Q8, int DP>
+__global__ void __launch_bounds__(kAttThreads, 2)
+attend_kernel(AttendArgs a) {
+  __shared__ __align__(16) u32x4 lds[4 * kKeyTile * (DP / 8)];
+  static_assert(sizeof lds >= (kFewRows * (DP + 4) + 2 * kAttWaves * kFewRows) * 4, "joining the waves");
+  Item it;
+  it.packed = static_cast<int>(blockIdx.x) < a.shared_items;
+  if (it.packed) {
+    int i = blockIdx.x;
+    it.part = i % a.shared_splits;
+    i /= a.shared_splits;
+    it.tile_row = i % a.shared_tiles;
+    it.kvh = i / a.shared_tiles;
+    it.b = 0;
+    wide_part<T, Q8, DP>(a, it, lds);
+    return;
+  }
+  // the row tiles of one (sequence, key head, part) read the same keys: they follow
+  // each other on one XCD (workgroups go round the 8 XCDs)
+  const int i = blockIdx.x - a.shared_items;
+  const int j = i >> 3;
+  const int g = (j / a.row_tiles) * 8 + (i & 7);
+  it.tile_row = j % a.row_tiles;
+  it.part = g % a.splits;
+  const int bh = g / a.splits;
+  it.b = bh / a.kv_heads;
+  it.kvh = bh - it.b * a.kv_heads;
+  if (it.b >= a.batch) return;
+  if (a.few) narrow_part<T, Q8, DP>(a, it, lds);
+  else wide_part<T, Q8, DP>(a, it, lds);
 }
 
 // Joins the parts of a row: a wave each, one part a lane for the statistics, two
@@ -569,15 +839,17 @@ merge_parts_kernel(AttendArgs a) {
   if (a.lse && lane == 0) a.lse[r] = l == 0.0f ? -INFINITY : (off + __log2f(l)) * 0.69314718055994531f;
 }
 
-Side side(const graft_rows &r, int bytes) {
+// rows: extent along the row stride; a stride that one row does not need is the row's own
+// length, since the bounds of a tile's buffer are counted with it.
+Side side(const graft_rows &r, int bytes, int dim, int rows) {
   Side s;
   s.p = static_cast<const char *>(r.data);
   s.batch = r.batch_stride * bytes;
-  s.row = r.row_stride * bytes;
+  s.row = static_cast<int32_t>((rows > 1 ? r.row_stride : dim) * bytes);
   s.head = r.head_stride * bytes;
   s.s = r.scale;
   s.s_batch = r.scale_batch_stride;
-  s.s_row = r.scale_row_stride;
+  s.s_row = static_cast<int32_t>(rows > 1 ? r.scale_row_stride : 1);
   s.s_head = r.scale_head_stride;
   return s;
 }
@@ -588,24 +860,25 @@ AttendPlan attend_plan(const graft_attention &a) {
   AttendPlan p{};
   const int group = a.q_heads / a.kv_heads;
   const int64_t rows = static_cast<int64_t>(a.slots) * group;
-  const int root = a.with_root ? 1 : 0;
-  p.row_tiles = static_cast<int>((rows + kRowTile - 1) / kRowTile);
+  p.few = rows <= kFewRows;
+  const int tile = p.few ? kFewRows : kRowTile;
+  p.row_tiles = static_cast<int>((rows + tile - 1) / tile);
   const int64_t units = static_cast<int64_t>(a.batch) * a.kv_heads * p.row_tiles;
-  auto tiles = [](int64_t n) { return (n + kKeyTile - 1) / kKeyTile; };
-  const int64_t shared = tiles(a.shared_len);
+  // keys of a tile of the wide walk, or of a round of the narrow one's four waves
+  const int keys = p.few ? kFewKeys * kAttWaves : kKeyTile;
+  auto tiles = [](int64_t n, int k) { return (n + k - 1) / k; };
   // a pass of its own where sequences share a row tile
   const bool own_pass = a.shared_len > 0 && a.batch > 1 && rows * 2 <= kRowTile;
-  const int64_t most = (own_pass ? 0 : shared) + tiles(a.cache_rows) + tiles(a.slots);
-  p.min_tiles = 4;
+  const int64_t most = (own_pass ? 0 : tiles(a.shared_len, keys)) + tiles(a.cache_rows, keys) + tiles(a.slots, keys);
+  p.min_tiles = p.few ? 2 : 4;
   auto cut = [&](int64_t n_units, int64_t n_tiles, int64_t want, int64_t cap) {
     int64_t s = (want + n_units - 1) / n_units;
     s = std::min(s, (n_tiles + p.min_tiles - 1) / p.min_tiles);
     return static_cast<int>(std::max<int64_t>(1, std::min(s, cap)));
   };
-  (void)root;
   if (own_pass) {
     p.shared_tiles = static_cast<int>((a.batch * rows + kRowTile - 1) / kRowTile);
-    p.shared_splits = cut(static_cast<int64_t>(a.kv_heads) * p.shared_tiles, shared, 512, 32);
+    p.shared_splits = cut(static_cast<int64_t>(a.kv_heads) * p.shared_tiles, tiles(a.shared_len, kKeyTile), 512, 32);
   }
   p.splits = cut(units, most, 2048, own_pass ? 32 : kMaxParts);
   p.parts = p.splits + p.shared_splits;
@@ -618,12 +891,10 @@ hipError_t launch_attend(graft_ctx *ctx, const graft_attention &d, const AttendP
                          hipStream_t stream) {
   const bool q8 = d.cache_dtype == GRAFT_E4M3;
   AttendArgs a{};
-  a.block_k = side(d.k, 2);
-  a.block_v = side(d.v, 2);
-  a.cache_k = side(d.cache_k, q8 ? 1 : 2);
-  a.cache_v = side(d.cache_v, q8 ? 1 : 2);
-  a.shared_k = side(d.shared_k, q8 ? 1 : 2);
-  a.shared_v = side(d.shared_v, q8 ? 1 : 2);
+  const int w = q8 ? 1 : 2;
+  a.src[0] = Source{side(d.shared_k, w, d.head_dim, d.shared_len), side(d.shared_v, w, d.head_dim, d.shared_len)};
+  a.src[1] = Source{side(d.cache_k, w, d.head_dim, d.cache_rows), side(d.cache_v, w, d.head_dim, d.cache_rows)};
+  a.src[2] = Source{side(d.k, 2, d.head_dim, d.slots), side(d.v, 2, d.head_dim, d.slots)};
   a.q = static_cast<const char *>(d.q.data);
   a.q_batch = d.q.batch_stride * 2;
   a.q_slot = d.q.row_stride * 2;
@@ -651,6 +922,7 @@ hipError_t launch_attend(graft_ctx *ctx, const graft_attention &d, const AttendP
   a.words = (ctx->dims.max_nodes + 63) / 64;
   a.cache_rows = d.cache_rows;
   a.shared_len = d.shared_len;
+  a.few = p.few;
   a.row_tiles = p.row_tiles;
   a.splits = p.splits;
   a.min_tiles = p.min_tiles;

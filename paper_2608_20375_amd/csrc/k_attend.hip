@@ -46,6 +46,8 @@
 // 2^8, keep their relative precision in 16 bits, while rescaling a row's numbers every
 // time would cost a fifth of the vector work.
 #include <algorithm>
+#include <cstddef>
+#include <type_traits>
 
 #include "graft_internal.h"
 
@@ -124,7 +126,7 @@ struct AttendArgs {
   int64_t rows_all;       // batch * slots * q_heads
   int32_t batch, slots, root, q_heads, kv_heads, group, dim;
   int32_t n_max, words, cache_rows, shared_len;
-  int32_t few, row_tiles, splits, min_tiles, shared_tiles, shared_splits, parts;
+  int32_t row_tiles, splits, min_tiles, shared_tiles, shared_splits, parts;
   int32_t shared_items;   // workgroups of the shared prefix's own pass
   float c;
 };
@@ -187,29 +189,34 @@ struct Walk {
   int source, left, tile;       // keys from the tile's first on; tile's number in the source
 };
 
-__device__ __forceinline__ void enter(const AttendArgs &a, Walk &w, int source, int tile, int keys,
+__device__ __forceinline__ void enter(Walk &w, int source, int tile, int keys,
                                       int count, int b, int kvh) {
-  const Source &s = source == 0 ? a.src[0] : source == 1 ? a.src[1] : a.src[2];
+  // Read from the kernel's argument memory where it is needed (sources come first there):
+  // kept in registers over the walk's loop, the three would push out what the loop uses.
+  typedef const __attribute__((address_space(4))) Source *Arguments;
+  static_assert(offsetof(AttendArgs, src) == 0, "the sources are the first argument");
+  Arguments s = (Arguments)__builtin_amdgcn_kernarg_segment_ptr() + source;
+  asm volatile("" : "+s"(s));
   const int64_t base = source == 0 ? 0 : b, first = static_cast<int64_t>(tile) * keys;
   w.source = source;
   w.tile = tile;
   w.left = count - tile * keys;
-  w.k_row = s.k.row;
-  w.v_row = s.v.row;
-  w.ks_row = s.k.s_row;
-  w.vs_row = s.v.s_row;
-  w.k = s.k.p + base * s.k.batch + kvh * s.k.head + first * s.k.row;
-  w.v = s.v.p + base * s.v.batch + kvh * s.v.head + first * s.v.row;
-  w.ks = s.k.s + base * s.k.s_batch + kvh * s.k.s_head + first * s.k.s_row;
-  w.vs = s.v.s + base * s.v.s_batch + kvh * s.v.s_head + first * s.v.s_row;
+  w.k_row = s->k.row;
+  w.v_row = s->v.row;
+  w.ks_row = s->k.s_row;
+  w.vs_row = s->v.s_row;
+  w.k = s->k.p + base * s->k.batch + kvh * s->k.head + first * s->k.row;
+  w.v = s->v.p + base * s->v.batch + kvh * s->v.head + first * s->v.row;
+  w.ks = s->k.s + base * s->k.s_batch + kvh * s->k.s_head + first * s->k.s_row;
+  w.vs = s->v.s + base * s->v.s_batch + kvh * s->v.s_head + first * s->v.s_row;
 }
 
 // Tile t of the walk whose sources have n0, n1, ... tiles of `keys` keys, c0, c1, c2 keys.
-__device__ __forceinline__ void seek(const AttendArgs &a, Walk &w, int t, int keys, int n0, int n1, int c0,
+__device__ __forceinline__ void seek(Walk &w, int t, int keys, int n0, int n1, int c0,
                                      int c1, int c2, int b, int kvh) {
-  if (t < n0) enter(a, w, 0, t, keys, c0, b, kvh);
-  else if (t < n0 + n1) enter(a, w, 1, t - n0, keys, c1, b, kvh);
-  else enter(a, w, 2, t - n0 - n1, keys, c2, b, kvh);
+  if (t < n0) enter(w, 0, t, keys, c0, b, kvh);
+  else if (t < n0 + n1) enter(w, 1, t - n0, keys, c1, b, kvh);
+  else enter(w, 2, t - n0 - n1, keys, c2, b, kvh);
 }
 // n tiles on in the same source.
 __device__ __forceinline__ void advance(Walk &w, int n, int keys) {
@@ -300,15 +307,21 @@ __device__ __forceinline__ void softmax_step(Sums<DP> &st, f32x16 (&s)[KT], u32x
 template <typename T, int DP>
 __device__ __forceinline__ void add_odd(const char *v, int v_row, int count, uint64_t seen, int h, int dim,
                                         Sums<DP> &st) {
+#pragma unroll 1
   for (int j = 0; j < count; ++j) {
-    if (!((seen >> j) & 1)) continue;
-    const uint16_t *row = reinterpret_cast<const uint16_t *>(v + static_cast<int64_t>(j) * v_row);
+    const bool on = (seen >> j) & 1;
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int at = d * 32 + 8 * (i / 4) + 4 * h + i % 4;
-        if (at < dim && (row[at] & T::kExp) == T::kExp) st.o[d][i] += T::number(row[at]);
+      for (int i = 0; i < 4; ++i) {
+        const int at = d * 32 + 8 * i + 4 * h;
+        u32x2 w{0, 0};
+        if (on && at < dim) w = *reinterpret_cast<const u32x2 *>(v + static_cast<int64_t>(j) * v_row + 2 * at);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const uint16_t n = static_cast<uint16_t>(w[x / 2] >> (16 * (x & 1)));
+          st.o[d][4 * i + x] += (n & T::kExp) == T::kExp ? T::number(n) : 0.0f;
+        }
       }
   }
 }
@@ -462,7 +475,7 @@ __device__ __forceinline__ void wide_part(const AttendArgs &a, const Item &it, u
   Walk w{};
   uint64_t seen_next = 0;
   if (t0 < t1) {
-    seek(a, w, t0, kKeyTile, n0, n1, a.shared_len, len, live, b, kvh);
+    seek(w, t0, kKeyTile, n0, n1, a.shared_len, len, live, b, kvh);
     load(w);
     if (w.source == 2) seen_next = seen_word(a, rb, slot, w.tile, live);
   }
@@ -475,7 +488,7 @@ __device__ __forceinline__ void wide_part(const AttendArgs &a, const Item &it, u
     const bool odd = store(source, buf);
     if (t + 1 < t1) {
       if (w.left > kKeyTile) advance(w, 1, kKeyTile);
-      else seek(a, w, t + 1, kKeyTile, n0, n1, a.shared_len, len, live, b, kvh);
+      else seek(w, t + 1, kKeyTile, n0, n1, a.shared_len, len, live, b, kvh);
       load(w);
       if (w.source == 2) seen_next = seen_word(a, rb, slot, w.tile, live);
     }
@@ -491,7 +504,7 @@ __device__ __forceinline__ void wide_part(const AttendArgs &a, const Item &it, u
       for (int i = 0; i < 16; ++i) s[kt][i] = 0.0f;
 #pragma unroll
       for (int i = 0; i < kSteps; ++i)
-        if (i * 16 < a.dim) s[kt] = T::mfma(k[k_at<C>(kt * 32 + col, 2 * i + h)], rq[i], s[kt]);
+        s[kt] = T::mfma(k[k_at<C>(kt * 32 + col, 2 * i + h)], rq[i], s[kt]);
     }
     if (source == 2 || left < kKeyTile) {
       const uint64_t bits = (source == 2 ? seen : (1ull << left) - 1) >> (4 * h);
@@ -506,7 +519,6 @@ __device__ __forceinline__ void wide_part(const AttendArgs &a, const Item &it, u
     softmax_step<T, 2>(st, s, p, a.c);
 #pragma unroll
     for (int d = 0; d < kDTiles; ++d) {
-      if (d * 32 >= a.dim) continue;
 #pragma unroll
       for (int g = 0; g < 4; ++g) st.o[d] = T::mfma(v_fragment<C>(v, d, g, lane), p[g], st.o[d]);
     }
@@ -634,7 +646,7 @@ __device__ __forceinline__ void narrow_part(const AttendArgs &a, const Item &it,
   int t = t0 + wave;
   uint64_t seen_next = 0;
   if (t < t1) {
-    seek(a, w, t, kFewKeys, n0, n1, a.shared_len, len, live, b, kvh);
+    seek(w, t, kFewKeys, n0, n1, a.shared_len, len, live, b, kvh);
     load(w);
     if (w.source == 2) seen_next = seen_word(a, b, slot, w.tile / 2, live) >> (32 * (w.tile & 1));
   }
@@ -680,7 +692,7 @@ __device__ __forceinline__ void narrow_part(const AttendArgs &a, const Item &it,
     }
     if (t + kAttWaves < t1) {
       if (w.left > kAttWaves * kFewKeys) advance(w, kAttWaves, kFewKeys);
-      else seek(a, w, t + kAttWaves, kFewKeys, n0, n1, a.shared_len, len, live, b, kvh);
+      else seek(w, t + kAttWaves, kFewKeys, n0, n1, a.shared_len, len, live, b, kvh);
       load(w);
       if (w.source == 2) seen_next = seen_word(a, b, slot, w.tile / 2, live) >> (32 * (w.tile & 1));
     }
@@ -695,7 +707,6 @@ __device__ __forceinline__ void narrow_part(const AttendArgs &a, const Item &it,
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int d = 0; d < kDTiles; ++d) {
-      if (d * 32 >= a.dim) continue;
 #pragma unroll
       for (int g = 0; g < 2; ++g) st.o[d] = T::mfma(v_fragment<C>(s_v, d, g, lane), p[g], st.o[d]);
     }
@@ -768,7 +779,9 @@ __device__ __forceinline__ void narrow_part(const AttendArgs &a, const Item &it,
   }
 }
 
-template <typename T, bool Q8, int DP>
+// FEW: sequences of at most kFewRows rows; the shared prefix's own pass is a wide walk all
+// the same.
+template <typename T, bool Q8, int DP, bool FEW>
 __global__ void __launch_bounds__(kAttThreads, 2)
 attend_kernel(AttendArgs a) {
   __shared__ __align__(16) u32x4 lds[4 * kKeyTile * (DP / 8)];
@@ -796,7 +809,7 @@ attend_kernel(AttendArgs a) {
   it.b = bh / a.kv_heads;
   it.kvh = bh - it.b * a.kv_heads;
   if (it.b >= a.batch) return;
-  if (a.few) narrow_part<T, Q8, DP>(a, it, lds);
+  if (FEW) narrow_part<T, Q8, DP>(a, it, lds);
   else wide_part<T, Q8, DP>(a, it, lds);
 }
 
@@ -922,7 +935,6 @@ hipError_t launch_attend(graft_ctx *ctx, const graft_attention &d, const AttendP
   a.words = (ctx->dims.max_nodes + 63) / 64;
   a.cache_rows = d.cache_rows;
   a.shared_len = d.shared_len;
-  a.few = p.few;
   a.row_tiles = p.row_tiles;
   a.splits = p.splits;
   a.min_tiles = p.min_tiles;
@@ -933,17 +945,20 @@ hipError_t launch_attend(graft_ctx *ctx, const graft_attention &d, const AttendP
   a.c = d.scale * 1.4426950408889634f;
   const int64_t groups = (static_cast<int64_t>(d.batch) * d.kv_heads * p.splits + 7) / 8 * 8;
   const dim3 grid(static_cast<unsigned>(a.shared_items + groups * p.row_tiles)), block(kAttThreads);
-  const bool wide = d.head_dim > 64;
-  if (d.dtype == GRAFT_F16) {
-    if (wide) hipLaunchKernelGGL((attend_kernel<F16, false, 128>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((attend_kernel<F16, false, 64>), grid, block, 0, stream, a);
-  } else if (q8) {
-    if (wide) hipLaunchKernelGGL((attend_kernel<Bf16, true, 128>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((attend_kernel<Bf16, true, 64>), grid, block, 0, stream, a);
-  } else {
-    if (wide) hipLaunchKernelGGL((attend_kernel<Bf16, false, 128>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((attend_kernel<Bf16, false, 64>), grid, block, 0, stream, a);
-  }
+  auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };
+  auto pick = [&](auto few, auto dp) {
+    constexpr bool F = decltype(few)::value;
+    constexpr int D = decltype(dp)::value;
+    if (d.dtype == GRAFT_F16) run(attend_kernel<F16, false, D, F>);
+    else if (q8) run(attend_kernel<Bf16, true, D, F>);
+    else run(attend_kernel<Bf16, false, D, F>);
+  };
+  auto width = [&](auto few) {
+    if (d.head_dim > 64) pick(few, std::integral_constant<int, 128>{});
+    else pick(few, std::integral_constant<int, 64>{});
+  };
+  if (p.few) width(std::true_type{});
+  else width(std::false_type{});
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.parts <= 1) return e;
   const dim3 mgrid(static_cast<unsigned>((a.rows_all + kAttWaves - 1) / kAttWaves));

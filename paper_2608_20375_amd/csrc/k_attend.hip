@@ -25,7 +25,7 @@
 // wide_part: 128 rows a workgroup, 32 a wave; 64-key tiles in LDS for all four waves, the
 // next tile's loads in flight in registers meanwhile, two LDS buffers, one barrier a
 // tile.  For blocks with many rows: bound by the matrix and vector units.
-// narrow_part: up to 32 rows a workgroup; every wave walks 32-key tiles of its own (four
+// narrow_part: 16 or 32 rows a workgroup; every wave walks 32-key tiles of its own (four
 // waves, four times the keys in flight), keys from memory straight into fragments, the
 // values through a stretch of LDS of the wave's own, no barriers; the four waves' sums
 // are joined at the end.  For single tokens and small blocks: bound by the cache's bytes.
@@ -37,9 +37,9 @@
 // The keys of a sequence (tiles of the shared prefix, of its cache, of its block) are
 // split into parts where rows alone do not fill the chip; every part leaves its sums,
 // maximum and unnormalised rows in the workspace and merge_parts_kernel joins them.
-// When a sequence has fewer rows than a tile, the shared prefix is walked by wide
-// workgroups of their own whose rows come from all sequences: it is read once for 128
-// rows instead of once for every sequence.
+// When a sequence has fewer rows than a tile, the shared prefix is walked by workgroups
+// of their own whose rows come from all sequences: it is read once for a tile of rows
+// instead of once for every sequence.
 //
 // The running maximum is only moved when some row's new maximum is more than 2^8 above it
 // (in exp2's argument): the sums and rows are fp32 and the probabilities, then up to
@@ -80,6 +80,10 @@ struct Bf16 {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
                                                    __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
   }
+  static __device__ __forceinline__ f32x4 mfma(const u32x4 &a, const u32x4 &b, const f32x4 &c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
+                                                   __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  }
   static __device__ __forceinline__ uint32_t pack(float x, float y) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, bf16x2));
   }
@@ -91,6 +95,10 @@ struct F16 {
   static constexpr uint32_t kExp = 0x7C00u;
   static __device__ __forceinline__ f32x16 mfma(const u32x4 &a, const u32x4 &b, const f32x16 &c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a),
+                                                  __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ f32x4 mfma(const u32x4 &a, const u32x4 &b, const f32x4 &c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a),
                                                   __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
   }
   static __device__ __forceinline__ uint32_t pack(float x, float y) {
@@ -145,6 +153,20 @@ __device__ __forceinline__ float half_max(float v) {   // with the other half's 
 }
 __device__ __forceinline__ float half_sum(float v) {
   const u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(
+      __float_as_uint(v), __float_as_uint(v), false, false));
+  return __uint_as_float(r.x) + __uint_as_float(r.y);
+}
+
+// Over the wave's four quarters (lanes l, l ^ 16, l ^ 32, l ^ 48).
+__device__ __forceinline__ float quarter_max(float v) {
+  v = half_max(v);
+  const u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(
+      __float_as_uint(v), __float_as_uint(v), false, false));
+  return fmaxf(__uint_as_float(r.x), __uint_as_float(r.y));
+}
+__device__ __forceinline__ float quarter_sum(float v) {
+  v = half_sum(v);
+  const u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(
       __float_as_uint(v), __float_as_uint(v), false, false));
   return __uint_as_float(r.x) + __uint_as_float(r.y);
 }
@@ -357,7 +379,8 @@ __device__ __forceinline__ void wide_part(const AttendArgs &a, const Item &it, u
   constexpr int kUnits = kBuf / kAttThreads, kStep = kAttThreads / C;
   u32x4 *s_k = lds, *s_v = lds + 2 * kBuf;
 
-  const int tid = threadIdx.x, lane = lane_id(), wave = tid / kWave;
+  const int tid = threadIdx.x, lane = lane_id();
+  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);   // uniform: the walk's tables stay scalar
   const int h = lane >> 5, col = lane & 31;
   const int b = it.b, kvh = it.kvh;
   const bool packed = it.packed;
@@ -564,228 +587,333 @@ __device__ __forceinline__ void wide_part(const AttendArgs &a, const Item &it, u
         st.l == 0.0f ? -INFINITY : (st.m * a.c + __log2f(st.l)) * 0.69314718055994531f;
 }
 
-template <typename T, bool Q8, int DP>
+// Infinite and NaN values as in add_odd, for the narrow walk's rows.
+template <typename T, int DP>
+__device__ __forceinline__ void add_odd(const char *v, int v_row, int count, uint32_t seen, int quarter, int dim,
+                                        f32x4 (&o)[DP / 16]) {
+#pragma unroll 1
+  for (int j = 0; j < count; ++j) {
+    const bool on = (seen >> j) & 1;
+#pragma unroll
+    for (int d = 0; d < DP / 16; ++d) {
+      const int at = d * 16 + 4 * quarter;
+      u32x2 w{0, 0};
+      if (on && at < dim) w = *reinterpret_cast<const u32x2 *>(v + static_cast<int64_t>(j) * v_row + 2 * at);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const uint16_t n = static_cast<uint16_t>(w[x / 2] >> (16 * (x & 1)));
+        o[d][x] += (n & T::kExp) == T::kExp ? T::number(n) : 0.0f;
+      }
+    }
+  }
+}
+
+// Rows of the narrow walk, 16 QT of them, on v_mfma_f32_16x16x32: lane l gives row (or
+// column) l % 16 and 8 of the 32 contracted entries from 8 (l / 16) on; of the 16 x 16
+// result it holds column l % 16, rows 4 (l / 16) + i.  The same forms as the wide walk's:
+// scores transposed, a lane's 8 of a 32-key tile (keys 4 c + i and 16 + 4 c + i in
+// quarter c) used as they are.
+template <typename T, bool Q8, int DP, int QT>
 __device__ __forceinline__ void narrow_part(const AttendArgs &a, const Item &it, u32x4 *lds) {
-  constexpr int C = DP / 8;
-  constexpr int kSteps = DP / 16, kDTiles = DP / 32;
+  constexpr int C = DP / 8, kSteps = DP / 32, kDTiles = DP / 16, kRows = 16 * QT;
+  constexpr int kLoads = Q8 ? DP / 64 : kSteps;         // 16-byte loads of a lane and 16 keys
   constexpr int kPad = DP + 4;                          // floats of a row when the waves are joined
-  const int tid = threadIdx.x, lane = lane_id(), wave = tid / kWave;
-  const int h = lane >> 5, col = lane & 31;
+  const int tid = threadIdx.x, lane = lane_id();
+  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);   // uniform: the walk's tables stay scalar
+  const int quarter = lane >> 4, col = lane & 15;
   const int b = it.b, kvh = it.kvh;
+  const bool packed = it.packed;
   u32x4 *s_v = lds + wave * kFewKeys * C;
 
-  bool bad = false;
-  const int live = __builtin_amdgcn_readfirstlane(slots_of(a, b, &bad));
-  const bool speaks = it.tile_row == 0 && it.part == 0 && kvh == 0 && tid == 0;
-  if (it.tile_row * kFewRows >= live * a.group) {
-    if (bad && speaks) atomicOr(a.error_flag, kErrBlockSizes);
-    return;
-  }
+  bool bad = false, unused;
   const int per_seq = a.slots * a.group;
-  int row = it.tile_row * kFewRows + col;
-  row = row < per_seq ? row : per_seq - 1;
-  const int slot = row / a.group, head = kvh * a.group + row - slot * a.group;
+  const int live = packed ? 0 : __builtin_amdgcn_readfirstlane(slots_of(a, b, &bad));
   int len = 0;
-  if (a.cache_rows > 0) {
+  if (!packed && a.cache_rows > 0) {
     len = __builtin_amdgcn_readfirstlane(a.cache_len[b]);
     bad |= len < 0 || len > a.cache_rows;
     len = len < 0 ? 0 : (len > a.cache_rows ? a.cache_rows : len);
   }
-  if (bad && speaks) atomicOr(a.error_flag, kErrBlockSizes);
-  const int n0 = a.shared_items == 0 ? (a.shared_len + kFewKeys - 1) / kFewKeys : 0;
+  if (bad && it.tile_row == 0 && it.part == 0 && kvh == 0 && tid == 0) atomicOr(a.error_flag, kErrBlockSizes);
+  if (!packed && it.tile_row * kRows >= live * a.group) return;
+
+  // sequence, slot and query head of row i of the workgroup's tile
+  auto place = [&](int i, int *rb, int *slot, int *head) {
+    int row = it.tile_row * kRows + i;
+    *rb = b;
+    if (packed) {
+      *rb = row < a.batch * per_seq ? row / per_seq : a.batch - 1;
+      row -= *rb * per_seq;
+    }
+    const int rlive = packed ? slots_of(a, *rb, &unused) : live;
+    const bool valid = row < rlive * a.group;
+    row = row < per_seq ? row : per_seq - 1;
+    *slot = row / a.group;
+    *head = kvh * a.group + row - *slot * a.group;
+    return valid;
+  };
+
+  const int n0 = packed || a.shared_items == 0 ? (a.shared_len + kFewKeys - 1) / kFewKeys : 0;
   const int n1 = (len + kFewKeys - 1) / kFewKeys, n2 = (live + kFewKeys - 1) / kFewKeys;
   const int n_tiles = n0 + n1 + n2;
   // a part's tiles, in rounds of one tile a wave
   const int rounds = (n_tiles + kAttWaves - 1) / kAttWaves;
-  int per = (rounds + a.splits - 1) / a.splits;
+  const int splits = packed ? a.shared_splits : a.splits;
+  int per = (rounds + splits - 1) / splits;
   per = (per < a.min_tiles ? a.min_tiles : per) * kAttWaves;
   const int t0 = it.part * per < n_tiles ? it.part * per : n_tiles;
   const int t1 = t0 + per < n_tiles ? t0 + per : n_tiles;
 
-  // Contracted entries 8 of a step from chunk k_chunk(step) of a row on: 16 codes that one
+  // Contracted entries 8 of a step are chunk k_chunk(step) of a row: the 16 codes that one
   // load brings are two steps' 8.
-  auto k_chunk = [&](int s) { return Q8 ? 2 * (2 * (s / 2) + h) + s % 2 : 2 * s + h; };
-  u32x4 rq[kSteps];
-  const char *qp = a.q + b * a.q_batch + slot * a.q_slot + head * a.q_head;
+  auto k_chunk = [&](int s) { return Q8 ? 2 * (4 * (s / 2) + quarter) + s % 2 : 4 * s + quarter; };
+  u32x4 rq[QT][kSteps];
+  int slots[QT];
 #pragma unroll
-  for (int s = 0; s < kSteps; ++s)
-    rq[s] = k_chunk(s) * 8 < a.dim ? *reinterpret_cast<const u32x4 *>(qp + k_chunk(s) * 16) : u32x4{0, 0, 0, 0};
+  for (int q = 0; q < QT; ++q) {
+    int rb, head;
+    place(q * 16 + col, &rb, &slots[q], &head);
+    const char *qp = a.q + rb * a.q_batch + slots[q] * a.q_slot + head * a.q_head;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+      rq[q][s] = k_chunk(s) * 8 < a.dim ? *reinterpret_cast<const u32x4 *>(qp + k_chunk(s) * 16) : u32x4{0, 0, 0, 0};
+  }
 
   const int r0 = lane / C, ch = lane % C, q0 = lane / (C / 2), qc = lane % (C / 2);
   const int at16 = ch * 8 < a.dim ? ch * 16 : kOutside, at8 = qc * 16 < a.dim ? qc * 16 : kOutside;
-  u32x4 rk[kSteps], rv[C / 2];
-  uint32_t sk = 0, sv[C / 4];
+  constexpr int kVLoads = Q8 ? C / 4 : C / 2, kVStep = Q8 ? 2 * kWave / C : kWave / C;
+  u32x4 rk[2][kLoads], rv[kVLoads];
+  uint32_t sk[2] = {0, 0}, sv[kVLoads];
   auto load = [&](const Walk &w) {
     const int n = w.left < kFewKeys ? w.left : kFewKeys;
-    if (Q8 && w.source != 2) {
-      const auto bk = buffer(w.k, (n - 1) * w.k_row + a.dim), bv = buffer(w.v, (n - 1) * w.v_row + a.dim);
+    constexpr int kBytes = Q8 ? 1 : 2;
+    const auto bk = buffer(w.k, (n - 1) * w.k_row + kBytes * a.dim), bv = buffer(w.v, (n - 1) * w.v_row + kBytes * a.dim);
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int at = (4 * i + quarter) * 16;
+        rk[kt][i] = load16(bk, (16 * kt + col) * w.k_row + (at < kBytes * a.dim ? at : kOutside));
+      }
+#pragma unroll
+    for (int i = 0; i < kVLoads; ++i) {
+      const int r = (Q8 ? q0 : r0) + i * kVStep;
+      rv[i] = load16(bv, r * w.v_row + (Q8 ? at8 : at16));
+    }
+    if (Q8) {
       const auto bks = buffer(w.ks, (n - 1) * w.ks_row + 1), bvs = buffer(w.vs, (n - 1) * w.vs_row + 1);
 #pragma unroll
-      for (int i = 0; i < kSteps / 2; ++i)
-        rk[i] = load16(bk, col * w.k_row + ((2 * i + h) * 16 < a.dim ? (2 * i + h) * 16 : kOutside));
-      sk = __builtin_amdgcn_raw_buffer_load_b8(bks, col * w.ks_row, 0, 0);
+      for (int kt = 0; kt < 2; ++kt) sk[kt] = __builtin_amdgcn_raw_buffer_load_b8(bks, (16 * kt + col) * w.ks_row, 0, 0);
 #pragma unroll
-      for (int i = 0; i < C / 4; ++i) {
-        const int r = q0 + i * (2 * kWave / C);
-        rv[i] = load16(bv, r * w.v_row + at8);
-        sv[i] = __builtin_amdgcn_raw_buffer_load_b8(bvs, r * w.vs_row, 0, 0);
-      }
-    } else {
-      const auto bk = buffer(w.k, (n - 1) * w.k_row + 2 * a.dim), bv = buffer(w.v, (n - 1) * w.v_row + 2 * a.dim);
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s)
-        rk[s] = load16(bk, col * w.k_row + (k_chunk(s) * 8 < a.dim ? k_chunk(s) * 16 : kOutside));
-#pragma unroll
-      for (int i = 0; i < C / 2; ++i) rv[i] = load16(bv, (r0 + i * (kWave / C)) * w.v_row + at16);
+      for (int i = 0; i < kVLoads; ++i) sv[i] = __builtin_amdgcn_raw_buffer_load_b8(bvs, (q0 + i * kVStep) * w.vs_row, 0, 0);
     }
   };
 
-  Sums<DP> st;
-  st.clear();
+  f32x4 o[QT][kDTiles];
+  float m[QT], l[QT];
+#pragma unroll
+  for (int q = 0; q < QT; ++q) {
+    m[q] = -INFINITY;
+    l[q] = 0.0f;
+#pragma unroll
+    for (int d = 0; d < kDTiles; ++d) o[q][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  // A tile's scores into the running sums, its values being in LDS.  The wave's LDS
+  // operations are done in order.
+  auto take = [&](f32x4 (&s)[QT][2]) {
+    u32x4 p[QT];
+#pragma unroll
+    for (int q = 0; q < QT; ++q) {
+      float mx = s[q][0][0];
+#pragma unroll
+      for (int i = 1; i < 8; ++i) mx = fmaxf(mx, s[q][i / 4][i % 4]);
+      mx = quarter_max(mx);
+      if (__ballot((mx - m[q]) * a.c > kSlack) != 0) {     // -inf on both sides is not above
+        const float to = fmaxf(mx, m[q]);
+        const float alpha = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m[q] - to) * a.c);
+        l[q] *= alpha;
+#pragma unroll
+        for (int d = 0; d < kDTiles; ++d) o[q][d] *= alpha;
+        m[q] = to;
+      }
+      const float off = m[q] == -INFINITY ? 0.0f : -m[q] * a.c;
+      float e[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[q][i / 4][i % 4], a.c, off));
+      l[q] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+      p[q] = u32x4{T::pack(e[0], e[1]), T::pack(e[2], e[3]), T::pack(e[4], e[5]), T::pack(e[6], e[7])};
+    }
+    __builtin_amdgcn_wave_barrier();
+    const int vr = 4 * quarter + (col >> 2);
+#pragma unroll
+    for (int d = 0; d < kDTiles; ++d) {
+      typedef __attribute__((address_space(3))) s16x4 *at;
+      const char *vp = reinterpret_cast<const char *>(s_v + v_at<C>(vr, 2 * d + ((col & 3) >> 1))) + (col & 1) * 8;
+      const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)(vp)));
+      const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)(vp + 16 * C * 16)));
+#pragma unroll
+      for (int q = 0; q < QT; ++q) o[q][d] = T::mfma(u32x4{lo.x, lo.y, hi.x, hi.y}, p[q], o[q][d]);
+    }
+    __builtin_amdgcn_wave_barrier();
+  };
+  auto hide = [&](f32x4 (&s)[2], uint32_t seen) {
+    const uint32_t bits = seen >> (4 * quarter);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[i / 4][i % 4] = (bits >> (16 * (i / 4) + i % 4)) & 1u ? s[i / 4][i % 4] : -INFINITY;
+  };
+
+  // the prefix's tiles
   Walk w{};
   int t = t0 + wave;
-  uint64_t seen_next = 0;
-  if (t < t1) {
+  const int t_end = t1 < n0 + n1 ? t1 : n0 + n1;
+  if (t < t_end) {
     seek(w, t, kFewKeys, n0, n1, a.shared_len, len, live, b, kvh);
     load(w);
-    if (w.source == 2) seen_next = seen_word(a, b, slot, w.tile / 2, live) >> (32 * (w.tile & 1));
   }
-  for (; t < t1; t += kAttWaves) {
-    const int source = w.source, left = w.left;
-    const char *v_rows = w.v;
-    const int v_row = w.v_row;
-    const uint32_t seen = static_cast<uint32_t>(seen_next);
-    // the tile out of the loaded registers: scores, and the values to LDS
-    f32x16 s[1];
+  for (; t < t_end; t += kAttWaves) {
+    const int left = w.left;
+    f32x4 s[QT][2];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[0][i] = 0.0f;
-    bool odd = false;
-    if (Q8 && source != 2) {
-      const float uk = unit_of(sk);
+    for (int q = 0; q < QT; ++q) s[q][0] = s[q][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int i = 0; i < kSteps / 2; ++i) {
-        u32x2 x[4];
+    for (int kt = 0; kt < 2; ++kt) {
+      const float uk = unit_of(sk[kt]);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = widen(rk[i][j], uk);
-        s[0] = T::mfma(u32x4{x[0].x, x[0].y, x[1].x, x[1].y}, rq[2 * i], s[0]);
-        s[0] = T::mfma(u32x4{x[2].x, x[2].y, x[3].x, x[3].y}, rq[2 * i + 1], s[0]);
+      for (int i = 0; i < kLoads; ++i) {
+        u32x4 f[2];
+        if (Q8) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const u32x2 x = widen(rk[kt][i][j], uk);
+            f[j / 2][2 * (j % 2)] = x.x;
+            f[j / 2][2 * (j % 2) + 1] = x.y;
+          }
+        } else {
+          f[0] = rk[kt][i];
+        }
+#pragma unroll
+        for (int j = 0; j < (Q8 ? 2 : 1); ++j)
+#pragma unroll
+          for (int q = 0; q < QT; ++q) s[q][kt] = T::mfma(f[j], rq[q][Q8 ? 2 * i + j : i], s[q][kt]);
       }
+    }
 #pragma unroll
-      for (int i = 0; i < C / 4; ++i) {
-        const int r = q0 + i * (2 * kWave / C);
+    for (int i = 0; i < kVLoads; ++i) {
+      const int r = (Q8 ? q0 : r0) + i * kVStep;
+      if (Q8) {
         const float uv = unit_of(sv[i]);
         u32x2 x[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) x[j] = widen(rv[i][j], uv);
         s_v[v_at<C>(r, 2 * qc)] = u32x4{x[0].x, x[0].y, x[1].x, x[1].y};
         s_v[v_at<C>(r, 2 * qc + 1)] = u32x4{x[2].x, x[2].y, x[3].x, x[3].y};
+      } else {
+        s_v[v_at<C>(r, ch)] = rv[i];
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < kSteps; ++i) s[0] = T::mfma(rk[i], rq[i], s[0]);
-      if (source == 2) {
-#pragma unroll
-        for (int i = 0; i < C / 2; ++i) odd |= tame<T>(rv[i]);
-      }
-#pragma unroll
-      for (int i = 0; i < C / 2; ++i) s_v[v_at<C>(r0 + i * (kWave / C), ch)] = rv[i];
     }
-    if (t + kAttWaves < t1) {
+    if (t + kAttWaves < t_end) {
       if (w.left > kAttWaves * kFewKeys) advance(w, kAttWaves, kFewKeys);
       else seek(w, t + kAttWaves, kFewKeys, n0, n1, a.shared_len, len, live, b, kvh);
       load(w);
-      if (w.source == 2) seen_next = seen_word(a, b, slot, w.tile / 2, live) >> (32 * (w.tile & 1));
     }
-    if (source == 2 || left < kFewKeys) {
-      const uint32_t bits = (source == 2 ? seen : (1u << left) - 1) >> (4 * h);
+    if (left < kFewKeys) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[0][i] = (bits >> (8 * (i / 4) + i % 4)) & 1u ? s[0][i] : -INFINITY;
+      for (int q = 0; q < QT; ++q) hide(s[q], (1u << left) - 1);
     }
-    u32x4 p[2];
-    softmax_step<T, 1>(st, s, p, a.c);
-    // the wave's LDS operations are done in order
-    __builtin_amdgcn_wave_barrier();
+    take(s);
+  }
+  // the block: at most 32 slots, one tile, by the wave whose turn it is
+  if (t == n0 + n1 && t < t1) {
+    seek(w, t, kFewKeys, n0, n1, a.shared_len, len, live, b, kvh);
+    const auto bk = buffer(w.k, (live - 1) * w.k_row + 2 * a.dim), bv = buffer(w.v, (live - 1) * w.v_row + 2 * a.dim);
+    f32x4 s[QT][2];
 #pragma unroll
-    for (int d = 0; d < kDTiles; ++d) {
+    for (int q = 0; q < QT; ++q) s[q][0] = s[q][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int g = 0; g < 2; ++g) st.o[d] = T::mfma(v_fragment<C>(s_v, d, g, lane), p[g], st.o[d]);
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+        const u32x4 f = load16(bk, (16 * kt + col) * w.k_row + (k_chunk(i) * 8 < a.dim ? k_chunk(i) * 16 : kOutside));
+#pragma unroll
+        for (int q = 0; q < QT; ++q) s[q][kt] = T::mfma(f, rq[q][i], s[q][kt]);
+      }
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < C / 2; ++i) {
+      const int r = r0 + i * (kWave / C);
+      u32x4 x = load16(bv, r * w.v_row + at16);
+      odd |= tame<T>(x);
+      s_v[v_at<C>(r, ch)] = x;
     }
-    __builtin_amdgcn_wave_barrier();
-    if (source == 2 && __ballot(odd) != 0) {
-      add_odd<T, DP>(v_rows, v_row, left < kFewKeys ? left : kFewKeys, seen, h, a.dim, st);
+    uint32_t seen[QT];
+#pragma unroll
+    for (int q = 0; q < QT; ++q) {
+      seen[q] = static_cast<uint32_t>(seen_word(a, b, slots[q], 0, live));
+      hide(s[q], seen[q]);
+    }
+    take(s);
+    if (__ballot(odd) != 0) {
+#pragma unroll
+      for (int q = 0; q < QT; ++q) add_odd<T, DP>(w.v, w.v_row, live, seen[q], quarter, a.dim, o[q]);
     }
   }
 
-  // the four waves' rows, one wave after the other so that the sums have one order
+  // The four waves' rows: each leaves its own with its maximum and sum, then every thread
+  // joins 4 numbers of a row, the waves in order.
   float *s_o = reinterpret_cast<float *>(lds);
-  float *s_m = s_o + kFewRows * kPad, *s_l = s_m + kAttWaves * kFewRows;
-  st.l = half_sum(st.l);
-  __syncthreads();
-  if (h == 0) {
-    s_m[wave * kFewRows + col] = st.m;
-    s_l[wave * kFewRows + col] = st.l;
-  }
-  __syncthreads();
-  float top = s_m[col];
+  float *s_m = s_o + kAttWaves * 16 * kPad, *s_l = s_m + kAttWaves * 16;
 #pragma unroll
-  for (int i = 1; i < kAttWaves; ++i) top = fmaxf(top, s_m[i * kFewRows + col]);
-  const float alpha = st.m == top ? 1.0f : __builtin_amdgcn_exp2f((st.m - top) * a.c);
-  float total = 0.0f;
-#pragma unroll
-  for (int i = 0; i < kAttWaves; ++i) {
-    const float x = s_m[i * kFewRows + col];
-    total += s_l[i * kFewRows + col] * (x == top ? 1.0f : __builtin_amdgcn_exp2f((x - top) * a.c));
-  }
-  for (int i = 0; i < kAttWaves; ++i) {
-    if (wave == i) {
-#pragma unroll
-      for (int d = 0; d < kDTiles; ++d)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          f32x4 *at = reinterpret_cast<f32x4 *>(s_o + col * kPad + d * 32 + 8 * j + 4 * h);
-          f32x4 x = f32x4{st.o[d][4 * j], st.o[d][4 * j + 1], st.o[d][4 * j + 2], st.o[d][4 * j + 3]} * alpha;
-          if (i > 0) x += *at;
-          *at = x;
-        }
-    }
+  for (int q = 0; q < QT; ++q) {
     __syncthreads();
-  }
-  // statistics of the row by its first lanes, then the rows by all threads
-  if (wave == 0 && h == 0) {
-    s_m[col] = top;
-    s_l[col] = total;
-  }
-  __syncthreads();
-  const int rows = min(kFewRows, live * a.group - it.tile_row * kFewRows);
-  for (int u = tid; u < rows * (DP / 4); u += kAttThreads) {
-    const int r = u / (DP / 4), x = (u % (DP / 4)) * 4;
-    if (x >= a.dim) continue;
-    const int i = it.tile_row * kFewRows + r;
-    const int sl = i / a.group, hd = kvh * a.group + i - sl * a.group;
-    const int64_t all = (static_cast<int64_t>(b) * a.slots + sl) * a.q_heads + hd;
-    const float m = s_m[r], l = s_l[r];
-    const f32x4 o = *reinterpret_cast<const f32x4 *>(s_o + r * kPad + x);
-    if (a.parts > 1) {
-      const int64_t at = it.part * a.rows_all + all;
-      if (x == 0) a.part_ml[at] = f32x2{t0 < t1 ? m * a.c : -INFINITY, l};
-      if (t0 < t1) *reinterpret_cast<f32x4 *>(a.part_o + at * a.dim + x) = o;
-    } else {
-      const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-      *reinterpret_cast<u32x2 *>(a.out + b * a.o_batch + sl * a.o_slot + hd * a.o_head + 2 * x) =
-          u32x2{T::pack(o.x * inv, o.y * inv), T::pack(o.z * inv, o.w * inv)};
-      if (a.lse && x == 0)
-        a.lse[all] = l == 0.0f ? -INFINITY : (m * a.c + __log2f(l)) * 0.69314718055994531f;
+    l[q] = quarter_sum(l[q]);
+    if (quarter == 0) {
+      s_m[wave * 16 + col] = m[q];
+      s_l[wave * 16 + col] = l[q];
+    }
+#pragma unroll
+    for (int d = 0; d < kDTiles; ++d)
+      *reinterpret_cast<f32x4 *>(s_o + (wave * 16 + col) * kPad + d * 16 + 4 * quarter) = o[q][d];
+    __syncthreads();
+    for (int u = tid; u < 16 * (DP / 4); u += kAttThreads) {
+      const int r = u / (DP / 4), x = (u % (DP / 4)) * 4;
+      int rb, slot, head;
+      if (!place(q * 16 + r, &rb, &slot, &head) || x >= a.dim) continue;
+      float top = s_m[r];
+#pragma unroll
+      for (int i = 1; i < kAttWaves; ++i) top = fmaxf(top, s_m[i * 16 + r]);
+      f32x4 sum{0.0f, 0.0f, 0.0f, 0.0f};
+      float total = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kAttWaves; ++i) {
+        const float mi = s_m[i * 16 + r];
+        const float f = mi == top ? 1.0f : __builtin_amdgcn_exp2f((mi - top) * a.c);
+        total += s_l[i * 16 + r] * f;
+        sum += *reinterpret_cast<const f32x4 *>(s_o + (i * 16 + r) * kPad + x) * f;
+      }
+      const int64_t all = (static_cast<int64_t>(rb) * a.slots + slot) * a.q_heads + head;
+      if (a.parts > 1) {
+        const int64_t at = (packed ? a.splits + it.part : it.part) * a.rows_all + all;
+        if (x == 0) a.part_ml[at] = f32x2{t0 < t1 ? top * a.c : -INFINITY, total};
+        if (t0 < t1) *reinterpret_cast<f32x4 *>(a.part_o + at * a.dim + x) = sum;
+      } else {
+        const float inv = total > 0.0f || total != total ? 1.0f / total : 0.0f;
+        *reinterpret_cast<u32x2 *>(a.out + rb * a.o_batch + slot * a.o_slot + head * a.o_head + 2 * x) =
+            u32x2{T::pack(sum.x * inv, sum.y * inv), T::pack(sum.z * inv, sum.w * inv)};
+        if (a.lse && x == 0)
+          a.lse[all] = total == 0.0f ? -INFINITY : (top * a.c + __log2f(total)) * 0.69314718055994531f;
+      }
     }
   }
 }
 
-// FEW: sequences of at most kFewRows rows; the shared prefix's own pass is a wide walk all
-// the same.
-template <typename T, bool Q8, int DP, bool FEW>
-__global__ void __launch_bounds__(kAttThreads, 2)
+// QT = 0: the wide walk; else the narrow one, 16 QT rows.  The narrow one's registers
+// leave room for a third or fourth wave on a SIMD.
+template <typename T, bool Q8, int DP, int QT>
+__global__ void __launch_bounds__(kAttThreads, QT == 0 ? 2 : (QT == 1 ? (Q8 || DP == 64 ? 4 : 3) : (DP == 64 ? 3 : 2)))
 attend_kernel(AttendArgs a) {
-  __shared__ __align__(16) u32x4 lds[4 * kKeyTile * (DP / 8)];
-  static_assert(sizeof lds >= (kFewRows * (DP + 4) + 2 * kAttWaves * kFewRows) * 4, "joining the waves");
+  constexpr int kNarrow = (kAttWaves * 16 * (DP + 4) + 2 * kAttWaves * 16 + 3) / 4;   // joining the waves
+  constexpr int kValues = kAttWaves * kFewKeys * (DP / 8);
+  __shared__ __align__(16) u32x4 lds[QT == 0 ? 4 * kKeyTile * (DP / 8) : (kNarrow > kValues ? kNarrow : kValues)];
   Item it;
   it.packed = static_cast<int>(blockIdx.x) < a.shared_items;
   if (it.packed) {
@@ -795,22 +923,21 @@ attend_kernel(AttendArgs a) {
     it.tile_row = i % a.shared_tiles;
     it.kvh = i / a.shared_tiles;
     it.b = 0;
-    wide_part<T, Q8, DP>(a, it, lds);
-    return;
+  } else {
+    // the row tiles of one (sequence, key head, part) read the same keys: they follow
+    // each other on one XCD (workgroups go round the 8 XCDs)
+    const int i = blockIdx.x - a.shared_items;
+    const int j = i >> 3;
+    const int g = (j / a.row_tiles) * 8 + (i & 7);
+    it.tile_row = j % a.row_tiles;
+    it.part = g % a.splits;
+    const int bh = g / a.splits;
+    it.b = bh / a.kv_heads;
+    it.kvh = bh - it.b * a.kv_heads;
+    if (it.b >= a.batch) return;
   }
-  // the row tiles of one (sequence, key head, part) read the same keys: they follow
-  // each other on one XCD (workgroups go round the 8 XCDs)
-  const int i = blockIdx.x - a.shared_items;
-  const int j = i >> 3;
-  const int g = (j / a.row_tiles) * 8 + (i & 7);
-  it.tile_row = j % a.row_tiles;
-  it.part = g % a.splits;
-  const int bh = g / a.splits;
-  it.b = bh / a.kv_heads;
-  it.kvh = bh - it.b * a.kv_heads;
-  if (it.b >= a.batch) return;
-  if (FEW) narrow_part<T, Q8, DP>(a, it, lds);
-  else wide_part<T, Q8, DP>(a, it, lds);
+  if (QT == 0) wide_part<T, Q8, DP>(a, it, lds);
+  else narrow_part<T, Q8, DP, QT == 0 ? 1 : QT>(a, it, lds);
 }
 
 // Joins the parts of a row: a wave each, one part a lane for the statistics, two
@@ -873,8 +1000,8 @@ AttendPlan attend_plan(const graft_attention &a) {
   AttendPlan p{};
   const int group = a.q_heads / a.kv_heads;
   const int64_t rows = static_cast<int64_t>(a.slots) * group;
-  p.few = rows <= kFewRows;
-  const int tile = p.few ? kFewRows : kRowTile;
+  p.few = rows <= 16 ? 1 : rows <= kFewRows ? 2 : 0;
+  const int tile = p.few ? 16 * p.few : kRowTile;
   p.row_tiles = static_cast<int>((rows + tile - 1) / tile);
   const int64_t units = static_cast<int64_t>(a.batch) * a.kv_heads * p.row_tiles;
   // keys of a tile of the wide walk, or of a round of the narrow one's four waves
@@ -890,8 +1017,8 @@ AttendPlan attend_plan(const graft_attention &a) {
     return static_cast<int>(std::max<int64_t>(1, std::min(s, cap)));
   };
   if (own_pass) {
-    p.shared_tiles = static_cast<int>((a.batch * rows + kRowTile - 1) / kRowTile);
-    p.shared_splits = cut(static_cast<int64_t>(a.kv_heads) * p.shared_tiles, tiles(a.shared_len, kKeyTile), 512, 32);
+    p.shared_tiles = static_cast<int>((a.batch * rows + tile - 1) / tile);
+    p.shared_splits = cut(static_cast<int64_t>(a.kv_heads) * p.shared_tiles, tiles(a.shared_len, keys), 512, 32);
   }
   p.splits = cut(units, most, 2048, own_pass ? 32 : kMaxParts);
   p.parts = p.splits + p.shared_splits;
@@ -947,7 +1074,7 @@ hipError_t launch_attend(graft_ctx *ctx, const graft_attention &d, const AttendP
   const dim3 grid(static_cast<unsigned>(a.shared_items + groups * p.row_tiles)), block(kAttThreads);
   auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };
   auto pick = [&](auto few, auto dp) {
-    constexpr bool F = decltype(few)::value;
+    constexpr int F = decltype(few)::value;
     constexpr int D = decltype(dp)::value;
     if (d.dtype == GRAFT_F16) run(attend_kernel<F16, false, D, F>);
     else if (q8) run(attend_kernel<Bf16, true, D, F>);
@@ -957,8 +1084,9 @@ hipError_t launch_attend(graft_ctx *ctx, const graft_attention &d, const AttendP
     if (d.head_dim > 64) pick(few, std::integral_constant<int, 128>{});
     else pick(few, std::integral_constant<int, 64>{});
   };
-  if (p.few) width(std::true_type{});
-  else width(std::false_type{});
+  if (p.few == 1) width(std::integral_constant<int, 1>{});
+  else if (p.few == 2) width(std::integral_constant<int, 2>{});
+  else width(std::integral_constant<int, 0>{});
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.parts <= 1) return e;
   const dim3 mgrid(static_cast<unsigned>((a.rows_all + kAttWaves - 1) / kAttWaves));

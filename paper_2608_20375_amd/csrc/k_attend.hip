@@ -682,9 +682,13 @@ __device__ __forceinline__ void narrow_part(const AttendArgs &a, const Item &it,
   const int r0 = lane / C, ch = lane % C, q0 = lane / (C / 2), qc = lane % (C / 2);
   const int at16 = ch * 8 < a.dim ? ch * 16 : kOutside, at8 = qc * 16 < a.dim ? qc * 16 : kOutside;
   constexpr int kVLoads = Q8 ? C / 4 : C / 2, kVStep = Q8 ? 2 * kWave / C : kWave / C;
-  u32x4 rk[2][kLoads], rv[kVLoads];
-  uint32_t sk[2] = {0, 0}, sv[kVLoads];
-  auto load = [&](const Walk &w) {
+  struct Held {                                         // a tile on its way
+    u32x4 rk[2][kLoads], rv[kVLoads];
+    uint32_t sk, sv;                                    // scales of row lane % 32
+    int left;
+  };
+  auto load = [&](Held &x, const Walk &w) {
+    x.left = w.left;
     const int n = w.left < kFewKeys ? w.left : kFewKeys;
     constexpr int kBytes = Q8 ? 1 : 2;
     const auto bk = buffer(w.k, (n - 1) * w.k_row + kBytes * a.dim), bv = buffer(w.v, (n - 1) * w.v_row + kBytes * a.dim);
@@ -693,19 +697,17 @@ __device__ __forceinline__ void narrow_part(const AttendArgs &a, const Item &it,
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
         const int at = (4 * i + quarter) * 16;
-        rk[kt][i] = load16(bk, (16 * kt + col) * w.k_row + (at < kBytes * a.dim ? at : kOutside));
+        x.rk[kt][i] = load16(bk, (16 * kt + col) * w.k_row + (at < kBytes * a.dim ? at : kOutside));
       }
 #pragma unroll
     for (int i = 0; i < kVLoads; ++i) {
       const int r = (Q8 ? q0 : r0) + i * kVStep;
-      rv[i] = load16(bv, r * w.v_row + (Q8 ? at8 : at16));
+      x.rv[i] = load16(bv, r * w.v_row + (Q8 ? at8 : at16));
     }
     if (Q8) {
       const auto bks = buffer(w.ks, (n - 1) * w.ks_row + 1), bvs = buffer(w.vs, (n - 1) * w.vs_row + 1);
-#pragma unroll
-      for (int kt = 0; kt < 2; ++kt) sk[kt] = __builtin_amdgcn_raw_buffer_load_b8(bks, (16 * kt + col) * w.ks_row, 0, 0);
-#pragma unroll
-      for (int i = 0; i < kVLoads; ++i) sv[i] = __builtin_amdgcn_raw_buffer_load_b8(bvs, (q0 + i * kVStep) * w.vs_row, 0, 0);
+      x.sk = __builtin_amdgcn_raw_buffer_load_b8(bks, (lane & 31) * w.ks_row, 0, 0);
+      x.sv = __builtin_amdgcn_raw_buffer_load_b8(bvs, (lane & 31) * w.vs_row, 0, 0);
     }
   };
 
@@ -762,34 +764,42 @@ __device__ __forceinline__ void narrow_part(const AttendArgs &a, const Item &it,
     for (int i = 0; i < 8; ++i) s[i / 4][i % 4] = (bits >> (16 * (i / 4) + i % 4)) & 1u ? s[i / 4][i % 4] : -INFINITY;
   };
 
-  // the prefix's tiles
+  // the prefix's tiles, the next one on its way (two: no faster, and 60 to 90 registers more)
   Walk w{};
   int t = t0 + wave;
   const int t_end = t1 < n0 + n1 ? t1 : n0 + n1;
-  if (t < t_end) {
-    seek(w, t, kFewKeys, n0, n1, a.shared_len, len, live, b, kvh);
-    load(w);
-  }
-  for (; t < t_end; t += kAttWaves) {
-    const int left = w.left;
+  int ahead = t;                                        // the walk's tile
+  auto fetch = [&](Held &x) {
+    if (ahead >= t_end) return;
+    if (ahead == t0 + wave || w.left <= kAttWaves * kFewKeys)
+      seek(w, ahead, kFewKeys, n0, n1, a.shared_len, len, live, b, kvh);
+    else
+      advance(w, kAttWaves, kFewKeys);
+    load(x, w);
+    ahead += kAttWaves;
+  };
+  auto step = [&](Held &x) {
+    const int left = x.left;
+    // row 16 kt + col's scale: lanes col and col + 16 of each half hold both
+    const u32x2 pair = Q8 ? __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(x.sk, x.sk, false, false)) : u32x2{0, 0};
     f32x4 s[QT][2];
 #pragma unroll
     for (int q = 0; q < QT; ++q) s[q][0] = s[q][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
-      const float uk = unit_of(sk[kt]);
+      const float uk = unit_of(kt == 0 ? pair.x : pair.y);
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
         u32x4 f[2];
         if (Q8) {
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const u32x2 x = widen(rk[kt][i][j], uk);
-            f[j / 2][2 * (j % 2)] = x.x;
-            f[j / 2][2 * (j % 2) + 1] = x.y;
+            const u32x2 y = widen(x.rk[kt][i][j], uk);
+            f[j / 2][2 * (j % 2)] = y.x;
+            f[j / 2][2 * (j % 2) + 1] = y.y;
           }
         } else {
-          f[0] = rk[kt][i];
+          f[0] = x.rk[kt][i];
         }
 #pragma unroll
         for (int j = 0; j < (Q8 ? 2 : 1); ++j)
@@ -801,27 +811,27 @@ __device__ __forceinline__ void narrow_part(const AttendArgs &a, const Item &it,
     for (int i = 0; i < kVLoads; ++i) {
       const int r = (Q8 ? q0 : r0) + i * kVStep;
       if (Q8) {
-        const float uv = unit_of(sv[i]);
-        u32x2 x[4];
+        const float uv = unit_of(__builtin_amdgcn_ds_bpermute(4 * r, static_cast<int>(x.sv)));
+        u32x2 y[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = widen(rv[i][j], uv);
-        s_v[v_at<C>(r, 2 * qc)] = u32x4{x[0].x, x[0].y, x[1].x, x[1].y};
-        s_v[v_at<C>(r, 2 * qc + 1)] = u32x4{x[2].x, x[2].y, x[3].x, x[3].y};
+        for (int j = 0; j < 4; ++j) y[j] = widen(x.rv[i][j], uv);
+        s_v[v_at<C>(r, 2 * qc)] = u32x4{y[0].x, y[0].y, y[1].x, y[1].y};
+        s_v[v_at<C>(r, 2 * qc + 1)] = u32x4{y[2].x, y[2].y, y[3].x, y[3].y};
       } else {
-        s_v[v_at<C>(r, ch)] = rv[i];
+        s_v[v_at<C>(r, ch)] = x.rv[i];
       }
     }
-    if (t + kAttWaves < t_end) {
-      if (w.left > kAttWaves * kFewKeys) advance(w, kAttWaves, kFewKeys);
-      else seek(w, t + kAttWaves, kFewKeys, n0, n1, a.shared_len, len, live, b, kvh);
-      load(w);
-    }
+    fetch(x);
     if (left < kFewKeys) {
 #pragma unroll
       for (int q = 0; q < QT; ++q) hide(s[q], (1u << left) - 1);
     }
     take(s);
-  }
+    t += kAttWaves;
+  };
+  Held held;
+  fetch(held);
+  while (t < t_end) step(held);
   // the block: at most 32 slots, one tile, by the wave whose turn it is
   if (t == n0 + n1 && t < t1) {
     seek(w, t, kFewKeys, n0, n1, a.shared_len, len, live, b, kvh);
@@ -906,10 +916,9 @@ __device__ __forceinline__ void narrow_part(const AttendArgs &a, const Item &it,
   }
 }
 
-// QT = 0: the wide walk; else the narrow one, 16 QT rows.  The narrow one's registers
-// leave room for a third or fourth wave on a SIMD.
+// QT = 0: the wide walk; else the narrow one, 16 QT rows.
 template <typename T, bool Q8, int DP, int QT>
-__global__ void __launch_bounds__(kAttThreads, QT == 0 ? 2 : (QT == 1 ? (Q8 || DP == 64 ? 4 : 3) : (DP == 64 ? 3 : 2)))
+__global__ void __launch_bounds__(kAttThreads, QT == 1 || (QT == 2 && DP == 64) ? 3 : 2)
 attend_kernel(AttendArgs a) {
   constexpr int kNarrow = (kAttWaves * 16 * (DP + 4) + 2 * kAttWaves * 16 + 3) / 4;   // joining the waves
   constexpr int kValues = kAttWaves * kFewKeys * (DP / 8);
@@ -924,17 +933,19 @@ attend_kernel(AttendArgs a) {
     it.kvh = i / a.shared_tiles;
     it.b = 0;
   } else {
-    // the row tiles of one (sequence, key head, part) read the same keys: they follow
-    // each other on one XCD (workgroups go round the 8 XCDs)
+    // Workgroups go round the 8 XCDs.  The row tiles of one (sequence, part, key head)
+    // read the same keys, and the heads' rows of it lie side by side: they follow each
+    // other on one XCD.  Sequences go by an odd number (one of them may be empty), so that a
+    // sequence's parts fall on all XCDs; parts that short sequences leave empty come last.
     const int i = blockIdx.x - a.shared_items;
-    const int j = i >> 3;
-    const int g = (j / a.row_tiles) * 8 + (i & 7);
-    it.tile_row = j % a.row_tiles;
-    it.part = g % a.splits;
-    const int bh = g / a.splits;
-    it.b = bh / a.kv_heads;
-    it.kvh = bh - it.b * a.kv_heads;
-    if (it.b >= a.batch) return;
+    const int j = i >> 3, inner = a.kv_heads * a.row_tiles;
+    const int g = (j / inner) * 8 + (i & 7), r = j % inner;
+    it.kvh = r / a.row_tiles;
+    it.tile_row = r - it.kvh * a.row_tiles;
+    const int odd = a.batch | 1;
+    it.part = g / odd;
+    it.b = g - it.part * odd;
+    if (it.part >= a.splits || it.b >= a.batch) return;
   }
   if (QT == 0) wide_part<T, Q8, DP>(a, it, lds);
   else narrow_part<T, Q8, DP, QT == 0 ? 1 : QT>(a, it, lds);
@@ -1010,7 +1021,7 @@ AttendPlan attend_plan(const graft_attention &a) {
   // a pass of its own where sequences share a row tile
   const bool own_pass = a.shared_len > 0 && a.batch > 1 && rows * 2 <= kRowTile;
   const int64_t most = (own_pass ? 0 : tiles(a.shared_len, keys)) + tiles(a.cache_rows, keys) + tiles(a.slots, keys);
-  p.min_tiles = p.few ? 2 : 4;
+  p.min_tiles = 4;
   auto cut = [&](int64_t n_units, int64_t n_tiles, int64_t want, int64_t cap) {
     int64_t s = (want + n_units - 1) / n_units;
     s = std::min(s, (n_tiles + p.min_tiles - 1) / p.min_tiles);
@@ -1018,9 +1029,9 @@ AttendPlan attend_plan(const graft_attention &a) {
   };
   if (own_pass) {
     p.shared_tiles = static_cast<int>((a.batch * rows + tile - 1) / tile);
-    p.shared_splits = cut(static_cast<int64_t>(a.kv_heads) * p.shared_tiles, tiles(a.shared_len, keys), 512, 32);
+    p.shared_splits = cut(static_cast<int64_t>(a.kv_heads) * p.shared_tiles, tiles(a.shared_len, keys), 256, 32);
   }
-  p.splits = cut(units, most, 2048, own_pass ? 32 : kMaxParts);
+  p.splits = cut(units, most, p.few ? 4096 : 2048, own_pass ? 32 : kMaxParts);
   p.parts = p.splits + p.shared_splits;
   const int64_t all = static_cast<int64_t>(a.batch) * a.slots * a.q_heads;
   p.bytes = p.parts > 1 ? p.parts * all * (a.head_dim * int64_t{4} + 8) : 0;
@@ -1070,7 +1081,7 @@ hipError_t launch_attend(graft_ctx *ctx, const graft_attention &d, const AttendP
   a.parts = p.parts;
   a.shared_items = p.shared_tiles * p.shared_splits * d.kv_heads;
   a.c = d.scale * 1.4426950408889634f;
-  const int64_t groups = (static_cast<int64_t>(d.batch) * d.kv_heads * p.splits + 7) / 8 * 8;
+  const int64_t groups = (static_cast<int64_t>(d.batch | 1) * p.splits + 7) / 8 * 8 * d.kv_heads;
   const dim3 grid(static_cast<unsigned>(a.shared_items + groups * p.row_tiles)), block(kAttThreads);
   auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };
   auto pick = [&](auto few, auto dp) {

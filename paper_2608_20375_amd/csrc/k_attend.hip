@@ -30,10 +30,6 @@
 // values through a stretch of LDS of the wave's own, no barriers; the four waves' sums
 // are joined at the end.  For single tokens and small blocks: bound by the cache's bytes.
 //
-// LDS.  16-byte chunk c of a row goes to c ^ f(row), f = row % 16 for keys (a fragment read
-// takes one chunk of 32 rows) and 2 (row % 8) for values (a transposing read takes 2
-// chunks of 8 rows), so that the lanes of a read touch different banks.
-//
 // The keys of a sequence (tiles of the shared prefix, of its cache, of its block) are
 // split into parts where rows alone do not fill the chip; every part leaves its sums,
 // maximum and unnormalised rows in the workspace and merge_parts_kernel joins them.
@@ -134,6 +130,7 @@ struct AttendArgs {
   int64_t rows_all;       // batch * slots * q_heads
   int32_t batch, slots, root, q_heads, kv_heads, group, dim;
   int32_t n_max, words, cache_rows, shared_len;
+  int32_t tile_keys, turns;   // keys of a tile, tiles that a workgroup's waves take at a time
   int32_t row_tiles, splits, min_tiles, shared_tiles, shared_splits, parts;
   int32_t shared_items;   // workgroups of the shared prefix's own pass
   float c;
@@ -144,6 +141,31 @@ __device__ __forceinline__ int slots_of(const AttendArgs &a, int b, bool *bad) {
   const int n = a.n_nodes[b], most = a.slots - a.root;
   *bad = n < 0 || n > most;
   return (n < 0 ? 0 : (n > most ? most : n)) + a.root;
+}
+
+// Tiles of a sequence's keys: the shared prefix's (where it has no pass of its own), the
+// cache's, the block's; and how many a part takes.  The walks and the merge agree on it.
+struct Tiles {
+  int n0, n1, n2, per;
+  __device__ __forceinline__ int all() const { return n0 + n1 + n2; }
+};
+__device__ __forceinline__ Tiles tiles_of(const AttendArgs &a, bool packed, int len, int live) {
+  const int k = a.tile_keys;
+  Tiles t;
+  t.n0 = packed || a.shared_items == 0 ? (a.shared_len + k - 1) / k : 0;
+  t.n1 = (len + k - 1) / k;
+  t.n2 = (live + k - 1) / k;
+  const int splits = packed ? a.shared_splits : a.splits;
+  const int rounds = (t.all() + a.turns - 1) / a.turns;
+  const int per = (rounds + splits - 1) / splits;
+  t.per = (per < a.min_tiles ? a.min_tiles : per) * a.turns;
+  return t;
+}
+__device__ __forceinline__ int len_of(const AttendArgs &a, int b, bool *bad) {
+  if (a.cache_rows == 0) return 0;
+  const int n = a.cache_len[b];
+  *bad |= n < 0 || n > a.cache_rows;
+  return n < 0 ? 0 : (n > a.cache_rows ? a.cache_rows : n);
 }
 
 __device__ __forceinline__ float half_max(float v) {   // with the other half's lane
@@ -348,9 +370,18 @@ __device__ __forceinline__ void add_odd(const char *v, int v_row, int count, uin
   }
 }
 
-// LDS place of 16-byte chunk c of a row of C chunks.
-template <int C> __device__ __forceinline__ int k_at(int r, int c) { return r * C + (c ^ (r & (C - 1))); }
-template <int C> __device__ __forceinline__ int v_at(int r, int c) { return r * C + (c ^ (2 * (r & (C / 2 - 1)))); }
+// LDS place of 16-byte chunk c of row r of C chunks (256 or 128 bytes), so that what a read or
+// a write touches at a time, 16 lanes of 16 bytes or 32 of 8, falls on all 64 banks: a
+// fragment of the keys is one chunk of 16 rows, the writes are 8 lanes a row in pairs of chunks
+// (codes), and the transposing reads take 4 chunks of 4 rows (wide) or 2 of 8 (narrow).
+template <int C> __device__ __forceinline__ int k_at(int r, int c) {
+  return r * C + (c ^ (C == 16 ? r & 15 : (r >> 1) & 7));
+}
+template <int C> __device__ __forceinline__ int v_at(int r, int c) {
+  const int f = C == 16 ? ((r & 3) << 2) | ((r >> 2) & 1) << 1 | (r & 1)
+                        : ((r >> 1) & 1) * 5 | ((r >> 2) & 1) << 1;
+  return r * C + (c ^ f);
+}
 
 // V^T's fragment: columns 32 d .. + 31 of keys 16 g + 4 h + {0..3, 8..11}; base is the
 // lane's row and column of the transposing read, for g = 0.
@@ -364,6 +395,10 @@ __device__ __forceinline__ u32x4 v_fragment(const u32x4 *s_v, int d, int g, int 
   const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)(p + 8 * C * 16)));
   return u32x4{lo.x, lo.y, hi.x, hi.y};
 }
+
+// Waits for a loaded value here.  Left to its first use inside the walk's loop, the wait would
+// be for all loads in every round, the next tile's among them.
+__device__ __forceinline__ void settle(u32x4 &x) { asm volatile("" : "+v"(x)); }
 
 // What a workgroup works on, whichever way it walks.
 struct Item {
@@ -406,21 +441,14 @@ __device__ __forceinline__ void wide_part(const AttendArgs &a, const Item &it, u
   if (packed && !__syncthreads_or(valid)) return;
   const bool busy = __ballot(valid) != 0;
 
-  int len = 0;
-  if (!packed && a.cache_rows > 0) {
-    len = __builtin_amdgcn_readfirstlane(a.cache_len[b]);
-    bad |= len < 0 || len > a.cache_rows;
-    len = len < 0 ? 0 : (len > a.cache_rows ? a.cache_rows : len);
-  }
+  const int len = packed ? 0 : __builtin_amdgcn_readfirstlane(len_of(a, b, &bad));
   if (bad && speaks) atomicOr(a.error_flag, kErrBlockSizes);
-  const int n0 = packed || a.shared_items == 0 ? (a.shared_len + kKeyTile - 1) / kKeyTile : 0;
-  const int n1 = (len + kKeyTile - 1) / kKeyTile, n2 = (live + kKeyTile - 1) / kKeyTile;
-  const int n_tiles = n0 + n1 + n2;
-  const int splits = packed ? a.shared_splits : a.splits;
-  int per = (n_tiles + splits - 1) / splits;
-  per = per < a.min_tiles ? a.min_tiles : per;
+  const Tiles n = tiles_of(a, packed, len, live);
+  const int n0 = n.n0, n1 = n.n1, n_tiles = n.all(), per = n.per;
   const int t0 = it.part * per < n_tiles ? it.part * per : n_tiles;
   const int t1 = t0 + per < n_tiles ? t0 + per : n_tiles;
+  const bool alone = a.shared_items == 0 && per >= n_tiles;   // the only part: no merge
+  if (alone && it.part > 0) return;
 
   // a thread's share of a tile: chunk ch of rows r0, r0 + kStep, ...; of codes, 16 of rows
   // q0, q0 + 2 kStep, ...
@@ -453,6 +481,8 @@ __device__ __forceinline__ void wide_part(const AttendArgs &a, const Item &it, u
       for (int i = 0; i < kUnits; ++i) rv[i] = load16(bv, (r0 + i * kStep) * w.v_row + at16);
     }
   };
+  // Stores the share; true if a block's value is infinite or NaN (stored as 0 then: a zero
+  // probability of a hidden slot must not meet it).
   auto store = [&](int source, int buf) {
     bool odd = false;
     u32x4 *k = s_k + buf * kBuf, *v = s_v + buf * kBuf;
@@ -492,6 +522,8 @@ __device__ __forceinline__ void wide_part(const AttendArgs &a, const Item &it, u
 #pragma unroll
   for (int s = 0; s < kSteps; ++s)
     rq[s] = s * 16 < a.dim ? *reinterpret_cast<const u32x4 *>(qp + s * 32 + h * 16) : u32x4{0, 0, 0, 0};
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s) settle(rq[s]);
 
   Sums<DP> st;
   st.clear();
@@ -522,13 +554,14 @@ __device__ __forceinline__ void wide_part(const AttendArgs &a, const Item &it, u
     const u32x4 *k = s_k + buf * kBuf, *v = s_v + buf * kBuf;
     f32x16 s[2];
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
+    for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[kt][i] = 0.0f;
 #pragma unroll
-      for (int i = 0; i < kSteps; ++i)
+    for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
         s[kt] = T::mfma(k[k_at<C>(kt * 32 + col, 2 * i + h)], rq[i], s[kt]);
-    }
     if (source == 2 || left < kKeyTile) {
       const uint64_t bits = (source == 2 ? seen : (1ull << left) - 1) >> (4 * h);
 #pragma unroll
@@ -552,7 +585,7 @@ __device__ __forceinline__ void wide_part(const AttendArgs &a, const Item &it, u
 
   st.l = half_sum(st.l);
   if (!valid) return;
-  if (a.parts > 1) {
+  if (!alone) {
     const int at_part = packed ? a.splits + it.part : it.part;
     const int64_t r = (static_cast<int64_t>(rb) * a.slots + slot) * a.q_heads + head;
     const int64_t at = at_part * a.rows_all + r;
@@ -628,12 +661,7 @@ __device__ __forceinline__ void narrow_part(const AttendArgs &a, const Item &it,
   bool bad = false, unused;
   const int per_seq = a.slots * a.group;
   const int live = packed ? 0 : __builtin_amdgcn_readfirstlane(slots_of(a, b, &bad));
-  int len = 0;
-  if (!packed && a.cache_rows > 0) {
-    len = __builtin_amdgcn_readfirstlane(a.cache_len[b]);
-    bad |= len < 0 || len > a.cache_rows;
-    len = len < 0 ? 0 : (len > a.cache_rows ? a.cache_rows : len);
-  }
+  const int len = packed ? 0 : __builtin_amdgcn_readfirstlane(len_of(a, b, &bad));
   if (bad && it.tile_row == 0 && it.part == 0 && kvh == 0 && tid == 0) atomicOr(a.error_flag, kErrBlockSizes);
   if (!packed && it.tile_row * kRows >= live * a.group) return;
 
@@ -653,16 +681,13 @@ __device__ __forceinline__ void narrow_part(const AttendArgs &a, const Item &it,
     return valid;
   };
 
-  const int n0 = packed || a.shared_items == 0 ? (a.shared_len + kFewKeys - 1) / kFewKeys : 0;
-  const int n1 = (len + kFewKeys - 1) / kFewKeys, n2 = (live + kFewKeys - 1) / kFewKeys;
-  const int n_tiles = n0 + n1 + n2;
   // a part's tiles, in rounds of one tile a wave
-  const int rounds = (n_tiles + kAttWaves - 1) / kAttWaves;
-  const int splits = packed ? a.shared_splits : a.splits;
-  int per = (rounds + splits - 1) / splits;
-  per = (per < a.min_tiles ? a.min_tiles : per) * kAttWaves;
+  const Tiles n = tiles_of(a, packed, len, live);
+  const int n0 = n.n0, n1 = n.n1, n_tiles = n.all(), per = n.per;
   const int t0 = it.part * per < n_tiles ? it.part * per : n_tiles;
   const int t1 = t0 + per < n_tiles ? t0 + per : n_tiles;
+  const bool alone = a.shared_items == 0 && per >= n_tiles;   // the only part: no merge
+  if (alone && it.part > 0) return;
 
   // Contracted entries 8 of a step are chunk k_chunk(step) of a row: the 16 codes that one
   // load brings are two steps' 8.
@@ -678,6 +703,10 @@ __device__ __forceinline__ void narrow_part(const AttendArgs &a, const Item &it,
     for (int s = 0; s < kSteps; ++s)
       rq[q][s] = k_chunk(s) * 8 < a.dim ? *reinterpret_cast<const u32x4 *>(qp + k_chunk(s) * 16) : u32x4{0, 0, 0, 0};
   }
+#pragma unroll
+  for (int q = 0; q < QT; ++q)
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) settle(rq[q][s]);
 
   const int r0 = lane / C, ch = lane % C, q0 = lane / (C / 2), qc = lane % (C / 2);
   const int at16 = ch * 8 < a.dim ? ch * 16 : kOutside, at8 = qc * 16 < a.dim ? qc * 16 : kOutside;
@@ -901,7 +930,7 @@ __device__ __forceinline__ void narrow_part(const AttendArgs &a, const Item &it,
         sum += *reinterpret_cast<const f32x4 *>(s_o + (i * 16 + r) * kPad + x) * f;
       }
       const int64_t all = (static_cast<int64_t>(rb) * a.slots + slot) * a.q_heads + head;
-      if (a.parts > 1) {
+      if (!alone) {
         const int64_t at = (packed ? a.splits + it.part : it.part) * a.rows_all + all;
         if (x == 0) a.part_ml[at] = f32x2{t0 < t1 ? top * a.c : -INFINITY, total};
         if (t0 < t1) *reinterpret_cast<f32x4 *>(a.part_o + at * a.dim + x) = sum;
@@ -966,7 +995,10 @@ merge_parts_kernel(AttendArgs a) {
   const int head = static_cast<int>(r - bs * a.q_heads);
   const int b = static_cast<int>(bs / a.slots), slot = static_cast<int>(bs - static_cast<int64_t>(b) * a.slots);
   bool unused;
-  if (slot >= slots_of(a, b, &unused)) return;
+  const int live = slots_of(a, b, &unused);
+  if (slot >= live) return;
+  const Tiles n = tiles_of(a, false, len_of(a, b, &unused), live);
+  if (a.shared_items == 0 && n.per >= n.all()) return;     // its only part wrote the row
   const f32x2 ml = lane < a.parts ? a.part_ml[lane * a.rows_all + r] : f32x2{-INFINITY, 0.0f};
   float top = ml.x;
 #pragma unroll
@@ -1024,7 +1056,7 @@ AttendPlan attend_plan(const graft_attention &a) {
   // a pass of its own where sequences share a row tile
   const bool own_pass = a.shared_len > 0 && a.batch > 1 && rows * 2 <= kRowTile;
   const int64_t most = (own_pass ? 0 : tiles(a.shared_len, keys)) + tiles(a.cache_rows, keys) + tiles(a.slots, keys);
-  p.min_tiles = 4;
+  p.min_tiles = p.few ? 4 : 8;
   auto cut = [&](int64_t n_units, int64_t n_tiles, int64_t want, int64_t cap) {
     int64_t s = (want + n_units - 1) / n_units;
     s = std::min(s, (n_tiles + p.min_tiles - 1) / p.min_tiles);
@@ -1034,7 +1066,9 @@ AttendPlan attend_plan(const graft_attention &a) {
     p.shared_tiles = static_cast<int>((a.batch * rows + tile - 1) / tile);
     p.shared_splits = cut(static_cast<int64_t>(a.kv_heads) * p.shared_tiles, tiles(a.shared_len, keys), 256, 32);
   }
-  p.splits = cut(units, most, p.few ? 4096 : 2048, own_pass ? 32 : kMaxParts);
+  // a wide part leaves 512 bytes for each of its rows, which the merge reads: splitting pays
+  // only where the chip is not filled (16 trees of up to 256 nodes: 200 us whole, 240 in 4 parts)
+  p.splits = cut(units, most, p.few ? 4096 : 1024, own_pass ? 32 : kMaxParts);
   p.parts = p.splits + p.shared_splits;
   const int64_t all = static_cast<int64_t>(a.batch) * a.slots * a.q_heads;
   p.bytes = p.parts > 1 ? p.parts * all * (a.head_dim * int64_t{4} + 8) : 0;
@@ -1076,6 +1110,8 @@ hipError_t launch_attend(graft_ctx *ctx, const graft_attention &d, const AttendP
   a.words = (ctx->dims.max_nodes + 63) / 64;
   a.cache_rows = d.cache_rows;
   a.shared_len = d.shared_len;
+  a.tile_keys = p.few ? kFewKeys : kKeyTile;
+  a.turns = p.few ? kAttWaves : 1;
   a.row_tiles = p.row_tiles;
   a.splits = p.splits;
   a.min_tiles = p.min_tiles;

@@ -290,9 +290,16 @@ struct AttendPlan {
 AttendPlan attend_plan(const graft_attention &a);
 hipError_t launch_attend(graft_ctx *ctx, const graft_attention &a, const AttendPlan &p,
                          hipStream_t stream);
-// The sampled walk: the workgroups of a row, the workspace, and the launches (one a level).
-int sample_splits(const graft_dims &d, int batch);
-int64_t sample_bytes(const graft_dims &d, int batch);
+// The sampled walk: how a row is cut, where the workspace's arrays are, and the launches
+// (one a level).
+struct SamplePlan {
+  int flights;        // pieces of a row
+  int rep;            // 16-byte vectors of a lane and run of a piece
+  int splits;         // workgroups of a row
+  int64_t tops_at, sums_at, bytes;
+};
+SamplePlan sample_plan(const graft_dims &d, int batch, int dtype);
+int64_t sample_bytes(const graft_dims &d, int batch);   // enough for any type
 hipError_t launch_accept_sampled(graft_ctx *ctx, int batch, const int32_t *n_nodes,
                                  const int32_t *tokens, const int32_t *parents,
                                  const graft_target_logits *t, int32_t *acc_len,

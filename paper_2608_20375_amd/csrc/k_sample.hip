@@ -8,15 +8,16 @@
 // x = min{v : sum_{w <= v} e_w > u S}.  T = 0: the largest logit, lowest index.
 //
 // Only the rows on the walk's path are read, but the next row is known only when
-// this one's token is.  So a launch takes one level: a row's words are dealt to
-// `splits` workgroups and their waves, each of which leaves the maximum of its run
-// of words and the sum of their exponentials over it.  The next launch's workgroups
-// each combine the level's partials (at most 256, one a thread), find the run that
-// holds u S by a scan, read that run again for the token, look for the child, and go
-// on with the child's row; every workgroup of a sequence does this by itself and
-// arrives at the same bits, so no flag, counter or wait between workgroups is
-// needed.  Sequences whose walk has ended leave at once.  Row pairs of partials
-// alternate by level.
+// this one's token is.  So a launch takes one level.  A row's 16-byte vectors are cut
+// into runs of 64 `rep` (one vector a lane; rep is 1 up to 2^19 words), four runs make a
+// flight, and the flights are dealt to the waves of the sequence's workgroups.  A wave
+// leaves its flight's maximum and the four runs' sums of exponentials over it.  The
+// next launch's waves each combine the level's flights (at most 256, one to four a
+// lane), find the run that holds u S by a scan, read that run again for the token,
+// look for the child, and go on with the child's row.  Every wave of a sequence does
+// this by itself and arrives at the same bits, so there is no flag, counter or wait
+// between workgroups, nor a barrier inside one.  Sequences whose walk has ended leave
+// at once.  The flights' arrays alternate by level.
 //
 // Exponentials and sums are fp64: with V borders between tokens on [0, 1), an error
 // of 1e-7 in the sums would change one draw in a hundred at V = 150000.
@@ -27,15 +28,17 @@ namespace {
 
 constexpr int kSampThreads = 256;
 constexpr int kSampWaves = kSampThreads / kWave;
-constexpr int kSampParts = 256;          // partials of a row at most: one a thread
-constexpr int kSampFlight = 4;           // 16-byte vectors of a lane in flight
+constexpr int kRuns = 4;                 // runs of a flight: vectors of a lane in flight
+constexpr int kGroups = 4;               // flights of a row at most: kGroups a lane
+constexpr int64_t kSampTarget = 8192;    // waves of a launch, about
+constexpr int kSampTree = 4;             // tree slots a lane loads ahead
 constexpr int kStopped = -2;             // a walk that has ended; -1 is the root
-static_assert(kMaxNodes % kSampThreads == 0, "tree slots a thread");
+constexpr double kLog2e = 1.4426950408889634;
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
-struct Part {
-  double max, sum;                       // T = 0: the sum is the index of the maximum
+struct Sums {
+  double run[kRuns];                     // T = 0: run[0] is the index of the maximum
 };
 
 struct SampleArgs {
@@ -48,31 +51,29 @@ struct SampleArgs {
   float *logp;
   int32_t *ring, *ring_pos;
   int32_t *state;                        // [L + 1][batch] node of each level
-  Part *parts;                           // [2][batch][splits * kSampWaves]
+  float *tops;                           // [2][batch][flights] maxima
+  Sums *sums;                            // [2][batch][flights]
   uint32_t *error_flag;
   int32_t batch, L, V, n_max, node_rows, window, update;
-  int32_t splits;
+  int32_t splits, flights, rep;          // workgroups and flights of a row; vectors of a lane and run
 };
-
-__device__ __forceinline__ float value(const float *p) { return *p; }
-__device__ __forceinline__ float value(const uint16_t *p) {
-  return __uint_as_float(static_cast<uint32_t>(*p) << 16);
-}
-__device__ __forceinline__ float value(const _Float16 *p) { return static_cast<float>(*p); }
 
 template <typename E> struct Vec;
 template <> struct Vec<float> {
   static constexpr int kPer = 4;
+  static constexpr uint32_t kNone = 0xFF800000u;          // -inf
   static __device__ __forceinline__ float get(const u32x4 &v, int i) { return __uint_as_float(v[i]); }
 };
 template <> struct Vec<uint16_t> {
   static constexpr int kPer = 8;
+  static constexpr uint32_t kNone = 0xFF80u;
   static __device__ __forceinline__ float get(const u32x4 &v, int i) {
     return __uint_as_float(i & 1 ? v[i / 2] & 0xFFFF0000u : v[i / 2] << 16);
   }
 };
 template <> struct Vec<_Float16> {
   static constexpr int kPer = 8;
+  static constexpr uint32_t kNone = 0xFC00u;
   static __device__ __forceinline__ float get(const u32x4 &v, int i) {
     union { uint32_t u; _Float16 h[2]; } c{v[i / 2]};
     return static_cast<float>(c.h[i & 1]);
@@ -82,46 +83,112 @@ template <> struct Vec<_Float16> {
 // A row cut at 16-byte borders: vector j holds tokens j * kPer - off .. + kPer - 1.
 template <typename E>
 struct Row {
+  static constexpr int kPer = Vec<E>::kPer;
   const E *row;
   int off, n_vec, V;
   __device__ __forceinline__ Row(const E *r, int v) : row(r), V(v) {
     off = static_cast<int>((reinterpret_cast<uintptr_t>(r) & 15u) / sizeof(E));
-    n_vec = (off + v + Vec<E>::kPer - 1) / Vec<E>::kPer;
+    n_vec = (off + v + kPer - 1) / kPer;
   }
-  __device__ __forceinline__ int first(int j) const { return j * Vec<E>::kPer - off; }
-  // Vector j as fp32; -inf where it has no token, and for NaN.  Only whole vectors
-  // are loaded as such: nothing outside the row is read.
-  __device__ __forceinline__ void load(int j, bool on, u32x4 *raw) const {
-    const int t = first(j);
-    if (on && t >= 0 && t + Vec<E>::kPer <= V)
-      *raw = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(row + t));
+  __device__ __forceinline__ int first(int j) const { return j * kPer - off; }
+  // vectors j .. j + n - 1 hold tokens only
+  __device__ __forceinline__ bool inside(int j, int n) const {
+    return first(j) >= 0 && static_cast<int64_t>(first(j)) + static_cast<int64_t>(n) * kPer <= V;
   }
-  __device__ __forceinline__ void take(int j, bool on, const u32x4 &raw,
-                                       float (&x)[Vec<E>::kPer]) const {
-    const int t = first(j);
-    const bool whole = on && t >= 0 && t + Vec<E>::kPer <= V;
+  __device__ __forceinline__ u32x4 whole(int j) const {
+    return *reinterpret_cast<const u32x4 *>(row + first(j));
+  }
+  // Any vector, -inf where it has no token.  Nothing outside the row is read.
+  __device__ __forceinline__ u32x4 any(int j) const {
+    constexpr int kBits = 8 * sizeof(E), kIn = 32 / kBits;
+    u32x4 raw;
 #pragma unroll
-    for (int i = 0; i < Vec<E>::kPer; ++i) {
-      float z = -INFINITY;
-      if (whole) z = Vec<E>::get(raw, i);
-      else if (on && t + i >= 0 && t + i < V) z = value(row + t + i);
-      x[i] = z != z ? -INFINITY : z;
+    for (int i = 0; i < 4; ++i) raw[i] = Vec<E>::kNone | (kIn == 2 ? Vec<E>::kNone << 16 : 0u);
+    if (j >= n_vec) return raw;
+    if (inside(j, 1)) return whole(j);
+    const int t = first(j);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int at = t + i < 0 ? 0 : (t + i < V ? t + i : V - 1);
+      uint32_t w;
+      if constexpr (sizeof(E) == 4) w = reinterpret_cast<const uint32_t *>(row)[at];
+      else w = reinterpret_cast<const uint16_t *>(row)[at];
+      w = at == t + i ? w : Vec<E>::kNone;
+      raw[i / kIn] = i % kIn ? (raw[i / kIn] & 0xFFFFu) | w << 16 : w | (kIn == 2 ? raw[i / kIn] & 0xFFFF0000u : 0u);
     }
+    return raw;
   }
 };
 
-// e_v: 1 at the maximum (an infinite one too), 0 for masked tokens.
-__device__ __forceinline__ double weight(float z, double max, double inv_t) {
-  const double d = static_cast<double>(z);
-  if (d == max) return 1.0;
-  if (z == -INFINITY || max == INFINITY) return 0.0;
-  return exp((d - max) * inv_t);
+// Exponentials under a maximum: e_v = 2^(c (z_v - M)), c = log2(e) / T.  y = c (z - M) is split
+// by adding 1.5 * 2^52, which leaves the nearest whole number in the low word; 2^f of the rest f
+// in [-1/2, 1/2] is the polynomial that equals it at the 11 Chebyshev nodes, off by 3e-16 of
+// the value at most and 1 at f = 0; the whole number goes to the exponent.  Differences below
+// 1100 / c, masked tokens' and NaN among them, give 0.  17 instructions in all.
+struct Exp2 {
+  static constexpr int kDeg = 10;
+  double c, low, round, coef[kDeg];
+  __device__ __forceinline__ explicit Exp2(double T) {
+    c = kLog2e / T;
+    c = c > 1e-300 ? c : 1e-300;
+    low = -1100.0 / c;
+    round = 6755399441055744.0;
+    asm("" : "+s"(round));
+    constexpr double k[kDeg] = {0.69314718055995, 0.24022650695910097, 0.05550410866444772,
+                                0.009618129107606888, 0.0013333558230164974, 0.0001540353044173605,
+                                1.5252657260200837e-05, 1.321544258792169e-06,
+                                1.0208690299958306e-07, 7.072585949269223e-09};
+#pragma unroll
+    for (int i = 0; i < kDeg; ++i) {
+      coef[i] = k[i];
+      // one scalar operand of a multiply-add, not a move before it
+      asm("" : "+s"(coef[i]));
+    }
+  }
+  // N at a time, step by step: a multiply-add's successor waits for it.
+  template <int N>
+  __device__ __forceinline__ void run(const float (&z)[N], double top, double (&w)[N]) const {
+    double f[N];
+    int n[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const double d = fmax(static_cast<double>(z[i]) - top, low), t = fma(d, c, round);
+      f[i] = fma(d, c, round - t);
+      n[i] = static_cast<int>(static_cast<uint32_t>(__double_as_longlong(t)));
+      w[i] = coef[kDeg - 1];
+    }
+#pragma unroll
+    for (int k = kDeg - 2; k >= -1; --k)
+#pragma unroll
+      for (int i = 0; i < N; ++i) w[i] = fma(w[i], f[i], k < 0 ? 1.0 : coef[k < 0 ? 0 : k]);
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = ldexp(w[i], n[i]);
+  }
+};
+// e of a vector's tokens: 1 at the maximum, which may be infinite (a case of its own).
+template <typename E>
+__device__ __forceinline__ void weights(const u32x4 &raw, float top, const Exp2 &ex,
+                                        double (&w)[Vec<E>::kPer]) {
+  float z[Vec<E>::kPer];
+  if (top == INFINITY) {
+#pragma unroll
+    for (int i = 0; i < Vec<E>::kPer; ++i) w[i] = Vec<E>::get(raw, i) == INFINITY ? 1.0 : 0.0;
+  } else {
+#pragma unroll
+    for (int i = 0; i < Vec<E>::kPer; ++i) z[i] = Vec<E>::get(raw, i);
+    ex.run(z, top, w);
+  }
 }
-// A part's sum over another maximum.
-__device__ __forceinline__ double rescale(double sum, double from, double to, double inv_t) {
-  if (from == to) return sum;
-  if (from == -INFINITY || to == INFINITY) return 0.0;
-  return sum * exp((from - to) * inv_t);
+// Factor of a sum over the maximum `from` under the maximum `to`.
+__device__ __forceinline__ double factor(float from, float to, const Exp2 &ex) {
+  if (to == INFINITY) return from == INFINITY ? 1.0 : 0.0;
+  const float z[1] = {from};
+  double w[1];
+  ex.run(z, to, w);
+  return w[0];
+}
+__device__ __forceinline__ float uniform(float v) {
+  return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v)));
 }
 
 __device__ __forceinline__ float wave_max(float v) {
@@ -130,48 +197,41 @@ __device__ __forceinline__ float wave_max(float v) {
     v = fmaxf(v, __uint_as_float(xor_lane(__float_as_uint(v), m)));
   return v;
 }
-__device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-  for (int m = 1; m < kWave; m <<= 1) v += xor_lane_f64(v, m);
-  return v;
-}
-__device__ __forceinline__ double shfl_up_f64(double v, int d) {
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp_f64(double v) {   // lanes without a source: 0
   const uint64_t u = static_cast<uint64_t>(__double_as_longlong(v));
-  const uint32_t lo = __shfl_up(static_cast<uint32_t>(u), d);
-  const uint32_t hi = __shfl_up(static_cast<uint32_t>(u >> 32), d);
+  const uint32_t lo = static_cast<uint32_t>(
+      __builtin_amdgcn_update_dpp(0, static_cast<int>(u), CTRL, ROWS, 0xF, false));
+  const uint32_t hi = static_cast<uint32_t>(
+      __builtin_amdgcn_update_dpp(0, static_cast<int>(u >> 32), CTRL, ROWS, 0xF, false));
   return __longlong_as_double(static_cast<long long>((static_cast<uint64_t>(hi) << 32) | lo));
 }
-
-// Inclusive prefix sums over the workgroup's threads in thread order.
-__device__ __forceinline__ double block_scan(double v, double *s_wave) {
-  const int lane = lane_id(), wave = threadIdx.x / kWave;
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) {
-    const double o = shfl_up_f64(v, d);
-    if (lane >= d) v += o;
-  }
-  __syncthreads();
-  if (lane == kWave - 1) s_wave[wave] = v;
-  __syncthreads();
-  double before = 0.0;
-  for (int w = 0; w < wave; ++w) before += s_wave[w];
-  return before + v;
+// Inclusive prefix sums over the lanes, by the steps of wave_incl_scan.
+__device__ __forceinline__ double wave_scan(double v) {
+  v += dpp_f64<0x111, 0xF>(v);
+  v += dpp_f64<0x112, 0xF>(v);
+  v += dpp_f64<0x114, 0xF>(v);
+  v += dpp_f64<0x118, 0xF>(v);
+  v += dpp_f64<0x142, 0xA>(v);
+  v += dpp_f64<0x143, 0xC>(v);
+  return v;
 }
-// Smallest and largest of one int a thread.
-__device__ __forceinline__ int block_min(int v, int *s_int) {
+__device__ __forceinline__ double lane_f64(double v, int lane) {   // of a uniform lane
+  const uint64_t u = static_cast<uint64_t>(__double_as_longlong(v));
+  const uint32_t lo = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(u), lane));
+  const uint32_t hi = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(u >> 32), lane));
+  return __longlong_as_double(static_cast<long long>((static_cast<uint64_t>(hi) << 32) | lo));
+}
+__device__ __forceinline__ int wave_min(int v) {
 #pragma unroll
   for (int m = 1; m < kWave; m <<= 1) {
     const int o = static_cast<int>(xor_lane(static_cast<uint32_t>(v), m));
     v = o < v ? o : v;
   }
-  __syncthreads();
-  if (lane_id() == 0) s_int[threadIdx.x / kWave] = v;
-  __syncthreads();
-  int r = s_int[0];
-#pragma unroll
-  for (int w = 1; w < kSampWaves; ++w) r = s_int[w] < r ? s_int[w] : r;
-  return r;
+  return __builtin_amdgcn_readfirstlane(v);
 }
+__device__ __forceinline__ int first_lane(uint64_t lanes) { return __builtin_ctzll(lanes); }
+__device__ __forceinline__ int last_lane(uint64_t lanes) { return 63 - __builtin_clzll(lanes); }
 
 template <typename E>
 __device__ __forceinline__ const E *row_of(const SampleArgs &a, int b, int node) {
@@ -185,154 +245,221 @@ __device__ __forceinline__ double temperature(const SampleArgs &a, int b, bool *
   return *bad ? 0.0 : static_cast<double>(t);
 }
 
-// The token of a level from its partials, -1 if no token has a positive
-// probability; *lp its log-probability.  Every thread gets both.
+// A level's flights, one to kGroups a lane.
+struct Level {
+  float top[kGroups];
+  Sums sums[kGroups];
+};
+
+// The token of a level from its flights, -1 if no token has a positive probability;
+// *lp its log-probability.  All lanes return the same.
 template <typename E>
-__device__ int draw_token(const SampleArgs &a, const Part &mine, int n_parts, const Row<E> &row,
-                          double T, double u, double *s_wave, float *s_max, int *s_int, double *lp) {
-  const int tid = threadIdx.x, lane = lane_id(), wave = tid / kWave;
-  const double inv_t = 1.0 / T;
-  const bool have = tid < n_parts;
-  // maxima are fp32 numbers
-  const float m = have ? static_cast<float>(mine.max) : -INFINITY;
-  const float wm = wave_max(m);
-  __syncthreads();
-  if (lane == 0) s_max[wave] = wm;
-  __syncthreads();
-  float top = s_max[0];
+__device__ __forceinline__ int draw_token(const SampleArgs &a, Level &at, const Row<E> &row,
+                                          const Exp2 &ex, double T, double u, double *lp) {
+  const int lane = lane_id();
+  const int per = kWave * a.rep;                         // vectors of a run
+  const int flights = (row.n_vec + kRuns * per - 1) / (kRuns * per);
+  float m = -INFINITY;
 #pragma unroll
-  for (int w = 1; w < kSampWaves; ++w) top = fmaxf(top, s_max[w]);
+  for (int g = 0; g < kGroups; ++g) {
+    if (g * kWave + lane >= flights) {
+      at.top[g] = -INFINITY;
+      at.sums[g] = Sums{};
+    }
+    m = fmaxf(m, at.top[g]);
+  }
+  const float top = uniform(wave_max(m));
   *lp = 0.0;
   if (top == -INFINITY) {
     *lp = -INFINITY;
     return -1;
   }
-  if (T == 0.0) return block_min(have && m == top ? static_cast<int>(mine.sum) : INT32_MAX, s_int);
-  const double M = static_cast<double>(top);
-  const double part = have ? rescale(mine.sum, mine.max, M, inv_t) : 0.0;
-  const double upto = block_scan(part, s_wave);
-  __syncthreads();
-  if (tid == kSampThreads - 1) s_wave[0] = upto;
-  __syncthreads();
-  const double total = s_wave[0], goal = u * total;
-  // the run that holds the goal: the first whose sum passes it; rounding or u >= 1
-  // may leave none, then the last with a token
-  int run = block_min(have && upto > goal && part > 0.0 ? tid : kSampThreads, s_int);
-  const bool past = run == kSampThreads;
-  if (past) run = -block_min(have && part > 0.0 ? -tid : 1, s_int);
-  __syncthreads();
-  if (tid == run) s_wave[0] = upto - part;
-  __syncthreads();
-  const double before = s_wave[0];
-  const int per = (row.n_vec + n_parts - 1) / n_parts;
-  const int v0 = run * per, v1 = v0 + per < row.n_vec ? v0 + per : row.n_vec;
-  const int each = (per + kSampThreads - 1) / kSampThreads;
-  const int a0 = v0 + tid * each < v1 ? v0 + tid * each : v1;
-  const int a1 = a0 + each < v1 ? a0 + each : v1;
-  double sum = 0.0;
-  float x[Vec<E>::kPer];
-  for (int j = a0; j < a1; ++j) {
-    u32x4 raw{};
-    row.load(j, true, &raw);
-    row.take(j, true, raw, x);
+  if (T == 0.0) {
+    int best = INT32_MAX;
 #pragma unroll
-    for (int i = 0; i < Vec<E>::kPer; ++i) sum += weight(x[i], M, inv_t);
+    for (int g = 0; g < kGroups; ++g) {
+      const int i = static_cast<int>(at.sums[g].run[0]);
+      if (at.top[g] == top && i < best) best = i;
+    }
+    return wave_min(best);
   }
-  const double end = before + block_scan(sum, s_wave);
-  double at = end - sum;
-  int hit = INT32_MAX, last = -1;                 // -1: none (and block_min gives 1)
-  // this thread's tokens: the first past the goal, and the last with a probability
-  for (int j = a0; j < a1; ++j) {
-    u32x4 raw{};
-    row.load(j, true, &raw);
-    row.take(j, true, raw, x);
+  double all[kGroups], upto[kGroups], total = 0.0;
 #pragma unroll
-    for (int i = 0; i < Vec<E>::kPer; ++i) {
-      const double w = weight(x[i], M, inv_t);
-      at += w;
-      const int t = row.first(j) + i;
-      if (w > 0.0) {
-        last = t;
-        if (at > goal && hit == INT32_MAX) hit = t;
+  for (int g = 0; g < kGroups; ++g) {
+    all[g] = 0.0;
+    upto[g] = total;
+    if (g * kWave >= flights) continue;
+    const double f = factor(at.top[g], top, ex);
+#pragma unroll
+    for (int r = 0; r < kRuns; ++r) {
+      at.sums[g].run[r] *= f;
+      all[g] += at.sums[g].run[r];
+    }
+    upto[g] = total + wave_scan(all[g]);
+    total = lane_f64(upto[g], kWave - 1);
+  }
+  const double goal = u * total;
+  // the first flight whose sum passes the goal; rounding or u >= 1 may leave none, then the
+  // last with a token, and its last token
+  uint64_t lanes = 0;
+  int group = 0;
+#pragma unroll
+  for (int g = 0; g < kGroups; ++g)
+    if (lanes == 0 && (lanes = __ballot(all[g] > 0.0 && upto[g] > goal)) != 0) group = g;
+  bool past = lanes == 0;
+  int who = past ? 0 : first_lane(lanes);
+  if (past) {
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      const uint64_t some = __ballot(all[g] > 0.0);
+      if (some != 0) {
+        group = g;
+        who = last_lane(some);
       }
     }
   }
-  int x_tok = past ? INT32_MAX : block_min(hit, s_int);
-  if (x_tok == INT32_MAX) x_tok = -block_min(-last, s_int);
-  if (x_tok < 0) {   // only if the row changed under the call
+  double sum[kRuns] = {}, before = 0.0;
+#pragma unroll
+  for (int g = 0; g < kGroups; ++g)
+    if (g == group) {
+      before = lane_f64(upto[g] - all[g], who);
+#pragma unroll
+      for (int r = 0; r < kRuns; ++r) sum[r] = lane_f64(at.sums[g].run[r], who);
+    }
+  // likewise the run
+  int run = -1, last = 0;
+  double base = before, last_base = before;
+#pragma unroll
+  for (int r = 0; r < kRuns; ++r) {
+    if (sum[r] > 0.0) {
+      last = r;
+      last_base = before;
+      if (run < 0 && !past && before + sum[r] > goal) {
+        run = r;
+        base = before;
+      }
+    }
+    before += sum[r];
+  }
+  if (run < 0) {
+    run = last;
+    base = last_base;
+    past = true;
+  }
+  // and the token
+  const int v0 = ((group * kWave + who) * kRuns + run) * per;
+  int tok = -1;
+  float z = 0.0f;
+  for (int r = 0; r < a.rep; ++r) {
+    const int j = v0 + r * kWave + lane;
+    const u32x4 raw = row.any(j);
+    double w[Vec<E>::kPer], mine = 0.0;
+    weights<E>(raw, top, ex, w);
+#pragma unroll
+    for (int i = 0; i < Vec<E>::kPer; ++i) mine += w[i];
+    const double end = base + wave_scan(mine);
+    const uint64_t hits = past ? 0 : __ballot(mine > 0.0 && end > goal), some = __ballot(mine > 0.0);
+    base = lane_f64(end, kWave - 1);
+    if (some == 0) continue;
+    // the lane's first token past the goal, its last with a probability where rounding leaves none
+    double upto_i = end - mine;
+    int hit = -1;
+    float hit_z = 0.0f;
+    bool found = false;
+#pragma unroll
+    for (int i = 0; i < Vec<E>::kPer; ++i) {
+      upto_i += w[i];
+      if (w[i] > 0.0 && !found) {
+        hit = row.first(j) + i;
+        hit_z = Vec<E>::get(raw, i);
+        found = hits != 0 && upto_i > goal;
+      }
+    }
+    const int from = hits != 0 ? first_lane(hits) : last_lane(some);
+    tok = __builtin_amdgcn_readlane(hit, from);
+    z = __uint_as_float(static_cast<uint32_t>(
+        __builtin_amdgcn_readlane(static_cast<int>(__float_as_uint(hit_z)), from)));
+    if (hits != 0) break;
+  }
+  if (tok < 0) {   // only if the row changed under the call
     *lp = -INFINITY;
     return -1;
   }
-  const float z = value(row.row + x_tok);
-  *lp = (static_cast<double>(z) == M ? 0.0 : (static_cast<double>(z) - M) * inv_t) - log(total);
-  return x_tok;
+  *lp = (z == top ? 0.0 : (static_cast<double>(z) - static_cast<double>(top)) / T) - log(total);
+  return tok;
 }
 
 // Level `level` of every walk: its node from the level before, then this
-// workgroup's share of the node's row.  level L + 1 ends the walks.
+// wave's flights of the node's row.  level L + 1 ends the walks.
 template <typename E>
 __global__ void __launch_bounds__(kSampThreads)
 sample_kernel(SampleArgs a, int level) {
-  __shared__ double s_wave[kSampWaves];
-  __shared__ float s_max[kSampWaves];
-  __shared__ int s_int[kSampWaves];
   const int splits = level <= a.L ? a.splits : 1;
-  const int b = blockIdx.x / splits, split = blockIdx.x - b * splits;
-  const int tid = threadIdx.x, lane = lane_id(), wave = tid / kWave;
-  const int n_parts = a.splits * kSampWaves;
+  const int b = blockIdx.x / splits;
+  const int lane = lane_id();
+  const int wave = __builtin_amdgcn_readfirstlane((blockIdx.x - b * splits) * kSampWaves + threadIdx.x / kWave);
+  if (level > a.L && wave > 0) return;
   bool bad_t;
   const double T = temperature(a, b, &bad_t);
+  const Exp2 ex(T);
   int node = -1;
   if (level > 0) {
     const int before = a.state[(level - 1) * a.batch + b];
     if (before == kStopped) {
-      if (split == 0 && tid == 0 && level <= a.L) a.state[level * a.batch + b] = kStopped;
+      if (wave == 0 && lane == 0 && level <= a.L) a.state[level * a.batch + b] = kStopped;
       return;
     }
-    // the tree's arrays with the partials: one round trip
-    constexpr int kPer = kMaxNodes / kSampThreads;
-    int32_t par[kPer], tok[kPer];
+    // the tree's arrays with the flights: one round trip
+    int32_t par[kSampTree], tok[kSampTree];
+    const int64_t tree = static_cast<int64_t>(b) * a.n_max;
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-      const int i = tid + k * kSampThreads;
-      const int64_t at = static_cast<int64_t>(b) * a.n_max + (i < a.n_max ? i : a.n_max - 1);
-      par[k] = a.parents[at];
-      tok[k] = a.tokens[at];
+    for (int k = 0; k < kSampTree; ++k) {
+      const int i = lane + k * kWave;
+      par[k] = a.parents[tree + (i < a.n_max ? i : a.n_max - 1)];
+      tok[k] = a.tokens[tree + (i < a.n_max ? i : a.n_max - 1)];
     }
-    Part mine{-INFINITY, 0.0};
-    if (tid < n_parts)
-      mine = a.parts[(static_cast<int64_t>((level - 1) & 1) * a.batch + b) * n_parts + tid];
+    Level left;
+    const int64_t at = (static_cast<int64_t>((level - 1) & 1) * a.batch + b) * a.flights;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      const int f = g * kWave + lane;
+      if (f < a.flights) {
+        left.top[g] = a.tops[at + f];
+        left.sums[g] = a.sums[at + f];
+      }
+    }
     const double u = a.uniform[static_cast<int64_t>(b) * (a.L + 1) + level - 1];
     int n = a.n_nodes[b];
     n = n < 0 ? 0 : (n > a.n_max ? a.n_max : n);
     n = n > a.node_rows ? a.node_rows : n;
     double lp;
-    const Row<E> row(row_of<E>(a, b, before), a.V);
-    const int x = draw_token<E>(a, mine, n_parts, row, T, u, s_wave, s_max, s_int, &lp);
+    const int x = draw_token<E>(a, left, Row<E>(row_of<E>(a, b, before), a.V), ex, T, u, &lp);
     int child = INT32_MAX;
+    for (int i = kSampTree * kWave + lane; i < n; i += kWave)
+      if (i > before && i < child && a.parents[tree + i] == before && a.tokens[tree + i] == x) child = i;
 #pragma unroll
-    for (int k = kPer - 1; k >= 0; --k) {
-      const int i = tid + k * kSampThreads;
+    for (int k = kSampTree - 1; k >= 0; --k) {
+      const int i = lane + k * kWave;
       if (i < n && i > before && par[k] == before && tok[k] == x) child = i;
     }
-    child = block_min(child, s_int);
+    child = wave_min(child);
     const bool go = child != INT32_MAX && level <= a.L && x >= 0;
     node = go ? child : kStopped;
-    if (split == 0) {
+    if (wave == 0) {
       const int d = level - 1;                  // nodes accepted before this token
-      if (tid == 0) {
+      if (lane == 0) {
         if (level <= a.L) a.state[level * a.batch + b] = node;
         if (a.logp) a.logp[static_cast<int64_t>(b) * (a.L + 1) + d] = static_cast<float>(lp);
         if (go) a.acc_nodes[static_cast<int64_t>(b) * a.L + d] = child;
         if (x < 0) atomicOr(a.error_flag, kErrTargetRow);
       }
       if (!go) {
-        for (int i = d + tid; i < a.L; i += kSampThreads)
+        for (int i = d + lane; i < a.L; i += kWave)
           a.acc_nodes[static_cast<int64_t>(b) * a.L + i] = -1;
         if (a.logp)
-          for (int i = d + 1 + tid; i <= a.L; i += kSampThreads)
+          for (int i = d + 1 + lane; i <= a.L; i += kWave)
             a.logp[static_cast<int64_t>(b) * (a.L + 1) + i] = 0.0f;
-        if (tid == 0) {
+        if (lane == 0) {
           a.acc_len[b] = d;
           a.bonus[b] = x;
           if (a.update) {
@@ -344,92 +471,112 @@ sample_kernel(SampleArgs a, int level) {
       }
     }
     if (!go) return;
-  } else if (split == 0 && tid == 0) {
+  } else if (wave == 0 && lane == 0) {
     a.state[b] = -1;
     if (bad_t) atomicOr(a.error_flag, kErrTargetRow);
   }
 
-  // this wave's run of the row's vectors
+  // this wave's flights of the row
   const Row<E> row(row_of<E>(a, b, node), a.V);
-  const int per = (row.n_vec + n_parts - 1) / n_parts;
-  const int run = split * kSampWaves + wave;
-  const int v0 = run * per, v1 = v0 + per < row.n_vec ? v0 + per : row.n_vec;
-  const double inv_t = 1.0 / T;
-  float m = -INFINITY;
-  double sum = 0.0;                               // T = 0: the index of m
-  for (int j0 = v0; j0 < v1; j0 += kSampFlight * kWave) {
-    u32x4 raw[kSampFlight] = {};
+  const int per = kWave * a.rep;
+  const int flights = (row.n_vec + kRuns * per - 1) / (kRuns * per);
+  const int64_t at = (static_cast<int64_t>(level & 1) * a.batch + b) * a.flights;
+  for (int f = wave; f < flights; f += splits * kSampWaves) {
+    float m = -INFINITY;
+    int best = INT32_MAX;                         // T = 0: index of this lane's maximum
+    double sum[kRuns] = {};
+    for (int r = 0; r < a.rep; ++r) {
+      const int j0 = f * kRuns * per + r * kWave;
+      u32x4 raw[kRuns];
+      if (row.inside(j0, 3 * per + kWave)) {
 #pragma unroll
-    for (int k = 0; k < kSampFlight; ++k) {
-      const int j = j0 + k * kWave + lane;
-      row.load(j, j < v1, &raw[k]);
-    }
-    float x[kSampFlight][Vec<E>::kPer];
-    float g = m;
+        for (int k = 0; k < kRuns; ++k) raw[k] = row.whole(j0 + k * per + lane);
+      } else {
 #pragma unroll
-    for (int k = 0; k < kSampFlight; ++k) {
-      const int j = j0 + k * kWave + lane;
-      row.take(j, j < v1, raw[k], x[k]);
+        for (int k = 0; k < kRuns; ++k) raw[k] = row.any(j0 + k * per + lane);
+      }
+      float g = m;
 #pragma unroll
-      for (int i = 0; i < Vec<E>::kPer; ++i) g = fmaxf(g, x[k][i]);
-    }
-    if (T == 0.0) {
-      // a later equal value never replaces an earlier one of this lane
+      for (int k = 0; k < kRuns; ++k)
 #pragma unroll
-      for (int k = 0; k < kSampFlight; ++k)
+        for (int i = 0; i < Vec<E>::kPer; ++i) g = fmaxf(g, Vec<E>::get(raw[k], i));
+      if (T == 0.0) {
 #pragma unroll
-        for (int i = 0; i < Vec<E>::kPer; ++i)
-          if (x[k][i] > m) {
-            m = x[k][i];
-            sum = static_cast<double>(row.first(j0 + k * kWave + lane) + i);
+        for (int k = 0; k < kRuns; ++k)
+#pragma unroll
+          for (int i = 0; i < Vec<E>::kPer; ++i) {
+            const float z = Vec<E>::get(raw[k], i);
+            const int t = row.first(j0 + k * per + lane) + i;
+            if (z > m || (z == m && m != -INFINITY && t < best)) {
+              m = z;
+              best = t;
+            }
           }
-    } else {
-      const float all = wave_max(g);
+        continue;
+      }
+      const float all = uniform(wave_max(g));
       if (all == -INFINITY) continue;
-      const double M = static_cast<double>(all);
-      sum = rescale(sum, static_cast<double>(m), M, inv_t);
+      if (r > 0) {
+        const double scale = factor(m, all, ex);
+#pragma unroll
+        for (int k = 0; k < kRuns; ++k) sum[k] *= scale;
+      }
       m = all;
 #pragma unroll
-      for (int k = 0; k < kSampFlight; ++k)
+      for (int k = 0; k < kRuns; ++k) {
+        double w[Vec<E>::kPer];
+        weights<E>(raw[k], all, ex, w);
 #pragma unroll
-        for (int i = 0; i < Vec<E>::kPer; ++i) sum += weight(x[k][i], M, inv_t);
+        for (int i = 0; i < Vec<E>::kPer; ++i) sum[k] += w[i];
+      }
     }
+    if (T == 0.0) {
+      const float all = wave_max(m);
+      best = wave_min(m == all ? best : INT32_MAX);
+      if (lane == 0) {
+        a.tops[at + f] = all;
+        a.sums[at + f].run[0] = static_cast<double>(best);
+      }
+      continue;
+    }
+    // the four sums together: halves of the wave keep two each, then rows of 16 one each
+    const bool up = lane & 32, odd = lane & 16;
+    const double s0 = (up ? sum[2] : sum[0]) + xor_lane_f64(up ? sum[0] : sum[2], 32);
+    const double s1 = (up ? sum[3] : sum[1]) + xor_lane_f64(up ? sum[1] : sum[3], 32);
+    double s = (odd ? s1 : s0) + xor_lane_f64(odd ? s0 : s1, 16);
+    s += xor_lane_f64(s, 8);
+    s += xor_lane_f64(s, 4);
+    s += xor_lane_f64(s, 2);
+    s += xor_lane_f64(s, 1);
+    if ((lane & 15) == 0) a.sums[at + f].run[lane / 16] = s;
+    if (lane == 0) a.tops[at + f] = m;
   }
-  if (T == 0.0) {
-    const float all = wave_max(m);
-    double best = m == all ? sum : 4294967296.0;
-#pragma unroll
-    for (int k = 1; k < kWave; k <<= 1) best = fmin(best, xor_lane_f64(best, k));
-    m = all;
-    sum = best;
-  } else {
-    sum = wave_sum(sum);
-  }
-  if (lane == 0)
-    a.parts[(static_cast<int64_t>(level & 1) * a.batch + b) * n_parts + run] =
-        Part{static_cast<double>(m), sum};
-}
-
-int64_t state_bytes(const graft_dims &d, int batch) {
-  return (static_cast<int64_t>(d.num_pos + 1) * batch * 4 + 255) & ~int64_t{255};
 }
 
 }  // namespace
 
-// Workgroups of a row: enough to give every CU a few, each wave at least 512
-// words, at most kSampParts partials.
-int sample_splits(const graft_dims &d, int batch) {
-  int s = (1024 + batch - 1) / batch;
-  const int most = (d.vocab + 512 * kSampWaves - 1) / (512 * kSampWaves);
-  s = s < most ? s : most;
-  const int cap = kSampParts / kSampWaves;
-  s = s < cap ? s : cap;
-  return s < 1 ? 1 : s;
+SamplePlan sample_plan(const graft_dims &d, int batch, int dtype) {
+  SamplePlan p;
+  const int64_t once = kRuns * kWave, most = kGroups * kWave;
+  // 16-byte vectors of a row, whatever its alignment
+  const int words = dtype == GRAFT_F32 ? 4 : 8;
+  const int64_t vectors = (static_cast<int64_t>(d.vocab) + 2 * words - 2) / words;
+  p.rep = static_cast<int>((vectors + once * most - 1) / (once * most));
+  p.flights = static_cast<int>((vectors + once * p.rep - 1) / (once * p.rep));
+  const int64_t want = kSampTarget / batch > 1 ? kSampTarget / batch : 1;   // waves a row
+  const int64_t each = (p.flights + want - 1) / want;
+  p.splits = static_cast<int>((p.flights + each * kSampWaves - 1) / (each * kSampWaves));
+  const int64_t n = int64_t{2} * batch * p.flights;
+  p.tops_at = (static_cast<int64_t>(d.num_pos + 1) * batch * 4 + 255) & ~int64_t{255};
+  p.sums_at = (p.tops_at + n * 4 + 255) & ~int64_t{255};
+  p.bytes = p.sums_at + n * static_cast<int64_t>(sizeof(Sums));
+  return p;
 }
 
 int64_t sample_bytes(const graft_dims &d, int batch) {
-  return state_bytes(d, batch) +
-         int64_t{2} * batch * sample_splits(d, batch) * kSampWaves * sizeof(Part);
+  const int64_t wide = sample_plan(d, batch, GRAFT_F32).bytes;
+  const int64_t half = sample_plan(d, batch, GRAFT_BF16).bytes;
+  return wide > half ? wide : half;
 }
 
 hipError_t launch_accept_sampled(graft_ctx *ctx, int batch, const int32_t *n_nodes,
@@ -438,6 +585,7 @@ hipError_t launch_accept_sampled(graft_ctx *ctx, int batch, const int32_t *n_nod
                                  int32_t *acc_nodes, int32_t *bonus, float *logp,
                                  int update_history, void *workspace, hipStream_t stream) {
   const graft_dims &d = ctx->dims;
+  const SamplePlan p = sample_plan(d, batch, t->dtype);
   SampleArgs a{};
   a.n_nodes = n_nodes;
   a.tokens = tokens;
@@ -456,7 +604,8 @@ hipError_t launch_accept_sampled(graft_ctx *ctx, int batch, const int32_t *n_nod
   a.ring = ctx->hist_ring;
   a.ring_pos = ctx->hist_pos;
   a.state = static_cast<int32_t *>(workspace);
-  a.parts = reinterpret_cast<Part *>(static_cast<char *>(workspace) + state_bytes(d, batch));
+  a.tops = reinterpret_cast<float *>(static_cast<char *>(workspace) + p.tops_at);
+  a.sums = reinterpret_cast<Sums *>(static_cast<char *>(workspace) + p.sums_at);
   a.error_flag = ctx->error_flag;
   a.batch = batch;
   a.L = d.num_pos;
@@ -465,7 +614,9 @@ hipError_t launch_accept_sampled(graft_ctx *ctx, int batch, const int32_t *n_nod
   a.node_rows = t->node_rows;
   a.window = d.hist_window;
   a.update = update_history;
-  a.splits = sample_splits(d, batch);
+  a.splits = p.splits;
+  a.flights = p.flights;
+  a.rep = p.rep;
   hipError_t e = hipSuccess;
   for (int level = 0; e == hipSuccess && level <= d.num_pos + 1; ++level) {
     const dim3 grid(static_cast<unsigned>(batch) * (level <= d.num_pos ? a.splits : 1));

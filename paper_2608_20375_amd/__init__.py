@@ -320,23 +320,26 @@ class QuantRows:
         return QuantRows(self.codes[index], self.scales[index])
 
 
-def _strides(t, names):
-    """Element strides of t's leading extents by name; 0 where there is one entry."""
-    return {n: (t.stride(i) if t.shape[i] > 1 else 0) for i, n in enumerate(names)}
+def _strides(t, n):
+    """Element strides of the last n of (plane, batch, row, head), t's leading extents;
+    0 for the others and where there is one entry."""
+    shape, stride = t.shape, t.stride()
+    if n == 3:
+        return (0, stride[0] if shape[0] > 1 else 0, stride[1] if shape[1] > 1 else 0,
+                stride[2] if shape[2] > 1 else 0)
+    return (0,) * (4 - n) + tuple([stride[i] if shape[i] > 1 else 0 for i in range(n)])
 
 
-def _rows(t, names, name):
-    """graft_rows of a tensor or QuantRows whose extents are names + head_dim."""
-    data = t.codes if isinstance(t, QuantRows) else t
+def _rows(t, n, name):
+    """graft_rows of a tensor or QuantRows: n extents, the last of (plane, batch, row, head),
+    and head_dim."""
+    quant = isinstance(t, QuantRows)
+    data = t.codes if quant else t
     if data.stride(-1) != 1 and data.shape[-1] > 1:
         raise ValueError("%s must have unit stride along its last dimension" % name)
-    r = Rows(data=data.data_ptr(),
-             **{n + "_stride": s for n, s in _strides(data, names).items()})
-    if isinstance(t, QuantRows):
-        r.scale = t.scales.data_ptr()
-        for n, s in _strides(t.scales, names).items():
-            setattr(r, "scale_%s_stride" % n, s)
-    return r
+    if quant:
+        return Rows(data.data_ptr(), *_strides(data, n), t.scales.data_ptr(), *_strides(t.scales, n))
+    return Rows(data.data_ptr(), *_strides(data, n))
 
 
 class TreeBuffers:
@@ -681,11 +684,45 @@ class Context:
         if torch.cuda.current_device() != self._device:
             raise ValueError("the context's device %d is not the current one" % self._device)
 
+    def _args(self, others, *args):
+        """Device pointers of contiguous tensors, after all extents, devices and types have
+        been checked: args are (name, tensor, type, extents as _need's, shape), a tensor of
+        that very shape being right without a second look; others: (name, tensor or
+        QuantRows) for which only the device is checked.  None stays None."""
+        dev = self._device
+        out = []
+        for name, t, dtype, dims, shape in args:
+            if t is None:
+                out.append(None)
+            elif (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape
+                  and t.get_device() == dev and t.is_contiguous()):
+                out.append(t.data_ptr())
+            else:
+                break
+        else:
+            for _, t in others:
+                if t is not None and (t.codes if isinstance(t, QuantRows) else t).get_device() != dev:
+                    break
+            else:
+                self._here()
+                return out
+        for name, t, dtype, dims, shape in args:
+            _need(t, name, *dims)
+        self._here(**dict(others), **{a[0]: a[1] for a in args})
+        return [_ptr(t, dtype, name) for name, t, dtype, dims, shape in args]
+
     def _kv_pair(self, pair, name, lead, heads, dim, dtype):
         """(rows, type) of a key and a value tensor or QuantRows; lead: the extents in
         front of heads, None for any."""
         if not isinstance(pair, (tuple, list)) or len(pair) != 2:
             raise ValueError("%s must be a pair of keys and values" % name)
+        x, y = pair
+        n = len(lead)
+        if type(x) is type(y) and isinstance(x, (torch.Tensor, QuantRows)) and x.shape == y.shape:
+            quant, s = isinstance(x, QuantRows), x.shape
+            if (len(s) == n + 2 and s[-1] == dim and s[-2] == heads and (n == 1 or s[0] >= lead[0])
+                    and (quant or (x.dtype is dtype and y.dtype is dtype))):
+                return s[n - 1], quant
         kinds = set()
         for t in pair:
             if not isinstance(t, (torch.Tensor, QuantRows)):
@@ -715,7 +752,7 @@ class Context:
         Writes out (allocated as zeros when None) up to each sequence's slots and, when
         given, lse [batch, slots, q_heads] float32; returns out.  workspace: uint8, at
         least tree_attention_workspace bytes; allocated when None."""
-        a, out, keep = self._attention(q, k, v, n_nodes, mask, cache, cache_len, shared, scale,
+        a, out = self._attention(q, k, v, n_nodes, mask, cache, cache_len, shared, scale,
                                        with_root, out, lse)
         L = lib()
         need = C.c_int64()
@@ -730,7 +767,7 @@ class Context:
     def tree_attention_workspace(self, q, k, v, n_nodes, mask=None, cache=None, cache_len=None,
                                  shared=None, scale=None, with_root=False, out=None, lse=None):
         """Bytes of workspace that tree_attention needs for these arguments."""
-        a, _, _ = self._attention(q, k, v, n_nodes, mask, cache, cache_len, shared, scale,
+        a, _ = self._attention(q, k, v, n_nodes, mask, cache, cache_len, shared, scale,
                                   with_root, out, lse)
         need = C.c_int64()
         _check(lib().graft_tree_attention_workspace(self._h, C.byref(a), C.byref(need)),
@@ -751,15 +788,15 @@ class Context:
         for name, t in (("q", q), ("k", k), ("v", v)):
             if not isinstance(t, torch.Tensor) or t.dim() != 4 or min(t.shape) < 1:
                 raise ValueError("%s must be [batch, slots, heads, dim]" % name)
-        B, S, Hq, D = q.shape
+        shape = q.shape
+        B, S, Hq, D = shape
         H, N = k.shape[2], self.dims.max_nodes
-        _need(k, "k", B, S, H, D)
-        _need(v, "v", B, S, H, D)
-        _need(n_nodes, "n_nodes", B)
-        _need(mask, "mask", (B,), N, (N + 63) // 64)
-        _need(cache_len, "cache_len", B)
-        _need(out, "out", B, S, Hq, D)
-        _need(lse, "lse", B, S, Hq)
+        W = (N + 63) // 64
+        if k.shape != (B, S, H, D) or v.shape != (B, S, H, D):
+            _need(k, "k", B, S, H, D)
+            _need(v, "v", B, S, H, D)
+        if out is not None and not (isinstance(out, torch.Tensor) and out.shape == shape):
+            _need(out, "out", B, S, Hq, D)
         if n_nodes is None:
             raise ValueError("n_nodes is required")
         if q.dtype not in (torch.bfloat16, torch.float16):
@@ -767,39 +804,39 @@ class Context:
         for name, t in (("k", k), ("v", v), ("out", out)):
             if t is not None and t.dtype != q.dtype:
                 raise TypeError("%s must be %s" % (name, q.dtype))
-        a = Attention(batch=B, slots=S, with_root=1 if with_root else 0, q_heads=Hq, kv_heads=H,
-                      head_dim=D, dtype=_DTYPES[q.dtype], cache_dtype=_DTYPES[q.dtype],
-                      scale=float(D ** -0.5 if scale is None else scale))
-        kinds = set()
+        dtype = _DTYPES[q.dtype]
+        a = Attention(B, S, 1 if with_root else 0, Hq, H, D, dtype, dtype,
+                      float(D ** -0.5 if scale is None else scale))
+        quant = None
         if cache is not None:
             if cache_len is None:
                 raise ValueError("a cache needs cache_len")
             a.cache_rows, quant = self._kv_pair(cache, "cache", (B, None), H, D, q.dtype)
-            kinds.add(quant)
         if shared is not None:
-            a.shared_len, quant = self._kv_pair(shared, "shared", (None,), H, D, q.dtype)
-            kinds.add(quant)
-        if len(kinds) > 1:
-            raise ValueError("cache and shared must be of one type")
-        if True in kinds:
+            a.shared_len, other = self._kv_pair(shared, "shared", (None,), H, D, q.dtype)
+            if quant is not None and other != quant:
+                raise ValueError("cache and shared must be of one type")
+            quant = other
+        if quant:
             a.cache_dtype = 3
-        self._here(q=q, k=k, v=v, n_nodes=n_nodes, mask=mask, cache_len=cache_len, out=out, lse=lse,
-                   **({"cache keys": cache[0], "cache values": cache[1]} if cache is not None else {}),
-                   **({"shared keys": shared[0], "shared values": shared[1]}
-                      if shared is not None else {}))
+        ck, cv = cache or (None, None)
+        sk, sv = shared or (None, None)
+        one, i32 = (B,), torch.int32
+        a.n_nodes, a.mask, a.cache_len, a.lse = self._args(
+            (("q", q), ("k", k), ("v", v), ("out", out), ("cache keys", ck), ("cache values", cv),
+             ("shared keys", sk), ("shared values", sv)),
+            ("n_nodes", n_nodes, i32, one, one),
+            ("mask", mask, torch.int64, (one, N, W), (B, N, W)),
+            ("cache_len", cache_len, i32, one, one),
+            ("lse", lse, torch.float32, (B, S, Hq), (B, S, Hq)))
         if out is None:
             out = torch.zeros_like(q, memory_format=torch.contiguous_format)
-        a.q, a.k, a.v, a.out = (_rows(t, ("batch", "row", "head"), n)
-                                for t, n in ((q, "q"), (k, "k"), (v, "v"), (out, "out")))
+        a.q, a.k, a.v, a.out = _rows(q, 3, "q"), _rows(k, 3, "k"), _rows(v, 3, "v"), _rows(out, 3, "out")
         if a.cache_rows:
-            a.cache_k, a.cache_v = (_rows(t, ("batch", "row", "head"), "cache") for t in cache)
+            a.cache_k, a.cache_v = _rows(ck, 3, "cache"), _rows(cv, 3, "cache")
         if a.shared_len:
-            a.shared_k, a.shared_v = (_rows(t, ("row", "head"), "shared") for t in shared)
-        a.n_nodes = _ptr(n_nodes, torch.int32, "n_nodes")
-        a.mask = _ptr(mask, torch.int64, "mask")
-        a.cache_len = _ptr(cache_len, torch.int32, "cache_len")
-        a.lse = _ptr(lse, torch.float32, "lse")
-        return a, out, None
+            a.shared_k, a.shared_v = _rows(sk, 2, "shared"), _rows(sv, 2, "shared")
+        return a, out
 
     def accept_sampled(self, n_nodes, tokens, parents, root_logits, node_logits, uniform,
                        temperature=None, update_history=False, acc_len=None, acc_nodes=None,
@@ -813,50 +850,56 @@ class Context:
         dm = self.dims
         batch = _batch_of(n_nodes, "n_nodes")
         L, N, V = dm.num_pos, dm.max_nodes, dm.vocab
-        _need(n_nodes, "n_nodes", batch)
-        _need(tokens, "tokens", (batch,), N)
-        _need(parents, "parents", (batch,), N)
-        _need(root_logits, "root_logits", (batch,), V)
-        _need(node_logits, "node_logits", (batch,), (0,), V)
-        _need(uniform, "uniform", (batch,), L + 1)
-        _need(temperature, "temperature", (batch,))
-        _need(acc_len, "acc_len", (batch,))
-        _need(acc_nodes, "acc_nodes", (batch,), L)
-        _need(bonus, "bonus", (batch,))
-        _need(logp, "logp", (batch,), L + 1)
         if root_logits is None or node_logits is None or uniform is None:
             raise ValueError("root_logits, node_logits and uniform are required")
+        _need(root_logits, "root_logits", (batch,), V)
+        _need(node_logits, "node_logits", (batch,), (0,), V)
         if root_logits.dtype not in _DTYPES or node_logits.dtype != root_logits.dtype:
             raise TypeError("logits must both be float32, bfloat16 or float16")
-        for name, t in (("root_logits", root_logits), ("node_logits", node_logits)):
-            if V > 1 and t.stride(-1) != 1:
-                raise ValueError("%s must have unit stride along V" % name)
-        self._here(n_nodes=n_nodes, tokens=tokens, parents=parents, root_logits=root_logits,
-                   node_logits=node_logits, uniform=uniform, temperature=temperature,
-                   acc_len=acc_len, acc_nodes=acc_nodes, bonus=bonus, logp=logp)
+        root, node = root_logits.stride(), node_logits.stride()
+        if V > 1 and (root[1] != 1 or node[2] != 1):
+            raise ValueError("%s must have unit stride along V"
+                             % ("root_logits" if root[1] != 1 else "node_logits"))
+        i32, f32, one = torch.int32, torch.float32, (batch,)
+        if tokens is None or parents is None:
+            raise ValueError("tokens and parents are required")
+        p_n, p_tok, p_par, p_u, p_t, p_acc, p_path, p_bonus, p_lp = self._args(
+            (("root_logits", root_logits), ("node_logits", node_logits)),
+            ("n_nodes", n_nodes, i32, one, one),
+            ("tokens", tokens, i32, (one, N), (batch, N)),
+            ("parents", parents, i32, (one, N), (batch, N)),
+            ("uniform", uniform, torch.float64, (one, L + 1), (batch, L + 1)),
+            ("temperature", temperature, f32, (one,), one),
+            ("acc_len", acc_len, i32, (one,), one),
+            ("acc_nodes", acc_nodes, i32, (one, L), (batch, L)),
+            ("bonus", bonus, i32, (one,), one),
+            ("logp", logp, f32, (one, L + 1), (batch, L + 1)))
         dev = n_nodes.device
-        i32 = dict(dtype=torch.int32, device=dev)
-        acc_len = torch.empty(batch, **i32) if acc_len is None else acc_len
-        acc_nodes = torch.empty(batch, L, **i32) if acc_nodes is None else acc_nodes
-        bonus = torch.empty(batch, **i32) if bonus is None else bonus
-        logp = torch.empty(batch, L + 1, dtype=torch.float32, device=dev) if logp is None else logp
+        if acc_len is None:
+            acc_len = torch.empty(batch, dtype=i32, device=dev)
+            p_acc = acc_len.data_ptr()
+        if acc_nodes is None:
+            acc_nodes = torch.empty(batch, L, dtype=i32, device=dev)
+            p_path = acc_nodes.data_ptr()
+        if bonus is None:
+            bonus = torch.empty(batch, dtype=i32, device=dev)
+            p_bonus = bonus.data_ptr()
+        if logp is None:
+            logp = torch.empty(batch, L + 1, dtype=f32, device=dev)
+            p_lp = logp.data_ptr()
         rows = min(node_logits.shape[1], N)
-        t = TargetLogits(_DTYPES[root_logits.dtype], root_logits.data_ptr(), root_logits.stride(0),
-                         node_logits.data_ptr() if rows else None, node_logits.stride(0),
-                         node_logits.stride(1) if rows > 1 else 0, rows,
-                         _ptr(temperature, torch.float32, "temperature"),
-                         _ptr(uniform, torch.float64, "uniform"))
+        t = TargetLogits(_DTYPES[root_logits.dtype], root_logits.data_ptr(), root[0],
+                         node_logits.data_ptr() if rows else None, node[0],
+                         node[1] if rows > 1 else 0, rows, p_t, p_u)
         lib_ = lib()
         need = C.c_int64()
         _check(lib_.graft_accept_sampled_workspace(self._h, batch, C.byref(need)),
                "graft_accept_sampled_workspace")
         workspace = self._workspace(workspace, need.value, dev)
         _check(lib_.graft_accept_sampled(
-            self._h, batch, _ptr(n_nodes, torch.int32, "n_nodes"), _ptr(tokens, torch.int32, "tokens"),
-            _ptr(parents, torch.int32, "parents"), C.byref(t), _ptr(acc_len, torch.int32, "acc_len"),
-            _ptr(acc_nodes, torch.int32, "acc_nodes"), _ptr(bonus, torch.int32, "bonus"),
-            _ptr(logp, torch.float32, "logp"), 1 if update_history else 0, workspace.data_ptr(),
-            workspace.numel(), _stream()), "graft_accept_sampled")
+            self._h, batch, p_n, p_tok, p_par, C.byref(t), p_acc, p_path, p_bonus, p_lp,
+            1 if update_history else 0, workspace.data_ptr(), workspace.numel(), _stream()),
+            "graft_accept_sampled")
         return acc_len, acc_nodes, bonus, logp
 
     def _move(self, src, dst, n_rows, start, rows, with_root):
@@ -867,22 +910,23 @@ class Context:
                 raise ValueError("%s must be [planes, batch, rows, heads, dim], got %s"
                                  % (name, list(t.shape)))
         batch = _batch_of(n_rows, "n_rows")
-        _need(n_rows, "n_rows", batch)
-        _need(start, "start", (batch,))
-        _need(rows, "rows", (batch,), (1,))
         P, _, _, H, D = src.shape
         for name, t in (("src", src), ("dst", dst)):
-            if t.shape[0] != P or t.shape[1] < batch or tuple(t.shape[3:]) != (H, D):
+            s = t.shape
+            if s[0] != P or s[1] < batch or s[3] != H or s[4] != D:
                 raise ValueError("%s must be [%d, >=%d, rows, %d, %d], got %s"
-                                 % (name, P, batch, H, D, list(t.shape)))
-        self._here(src=src, dst=dst, n_rows=n_rows, start=start, rows=rows)
+                                 % (name, P, batch, H, D, list(s)))
+        i32, one = torch.int32, (batch,)
+        entries = rows.shape[1] if isinstance(rows, torch.Tensor) and rows.dim() == 2 else 0
+        p_n, p_start, p_list = self._args(
+            (("src", src), ("dst", dst)),
+            ("n_rows", n_rows, i32, one, one),
+            ("start", start, i32, (one,), one),
+            ("rows", rows, i32, (one, (1,)), (batch, entries) if entries else None))
         kind = lambda t: 3 if isinstance(t, QuantRows) else _DTYPES.get(t.dtype, -1)
-        names = ("plane", "batch", "row", "head")
-        return CacheMove(batch, P, H, D, kind(src), kind(dst), _rows(src, names, "src"),
-                         _rows(dst, names, "dst"), src.shape[2], dst.shape[2],
-                         _ptr(n_rows, torch.int32, "n_rows"), _ptr(start, torch.int32, "start"),
-                         _ptr(rows, torch.int32, "rows"), 0 if rows is None else rows.shape[1],
-                         1 if with_root else 0)
+        return CacheMove(batch, P, H, D, kind(src), kind(dst), _rows(src, 4, "src"),
+                         _rows(dst, 4, "dst"), src.shape[2], dst.shape[2], p_n, p_start, p_list,
+                         entries, 1 if with_root else 0)
 
     def cache_write(self, dst, src, n_rows, rows=None, start=None, with_root=False):
         """Appends rows of src [planes, batch, rows, heads, dim] to the cache dst of the same

@@ -24,6 +24,7 @@ constexpr int kMoveGroups = 4;   // such groups of rows a workgroup
 constexpr uint32_t kBf16Inf = 0x7F80u;
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 enum class Move { kCopy, kQuantise, kRead16, kRead32 };
@@ -33,7 +34,7 @@ struct MoveArgs {
   const int32_t *n_rows, *start, *list;
   int32_t list_len, root;
   int32_t src_rows, dst_rows, most;    // most: rows of a sequence at most
-  int32_t heads, chunks, lanes;        // chunks of 16 numbers a head; lanes a head
+  int32_t heads, chunks, lanes;        // threads that a head needs, and has
   int32_t cols;                        // n_planes * heads * lanes
   int32_t at_once;                     // rows side by side in a workgroup
   int32_t col_blocks, row_blocks;
@@ -43,32 +44,31 @@ struct MoveArgs {
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
-// Largest finite magnitude of the 16 numbers, as bf16 bits.
-__device__ __forceinline__ uint32_t largest(const u32x4 &a, const u32x4 &b) {
+// Largest finite magnitude of the 8 numbers, as bf16 bits.
+__device__ __forceinline__ uint32_t largest(const u32x4 &a) {
   uint32_t m = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t w = i < 4 ? a[i & 3] : b[i & 3];
-    const uint32_t lo = w & 0x7FFFu, hi = (w >> 16) & 0x7FFFu;
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t lo = a[i] & 0x7FFFu, hi = (a[i] >> 16) & 0x7FFFu;
     m = lo > m && lo < kBf16Inf ? lo : m;
     m = hi > m && hi < kBf16Inf ? hi : m;
   }
   return m;
 }
 
-// Codes of the 16 numbers over 2^e.
-__device__ __forceinline__ u32x4 encode(const u32x4 &a, const u32x4 &b, int e) {
+// Codes of the 8 numbers over 2^e.
+__device__ __forceinline__ u32x2 encode(const u32x4 &a, int e) {
   const float inv = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
   // 256 * 2^120 is past fp32
   const float top = e == 120 ? 240.0f : 448.0f;
-  u32x4 out;
+  u32x2 out;
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
+  for (int q = 0; q < 2; ++q) {
     uint32_t code = 0, nan = 0;
     float v[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint32_t w = q < 2 ? a[(2 * q + i / 2) & 3] : b[(2 * q + i / 2) & 3];
+      const uint32_t w = a[2 * q + i / 2];
       const float x = i & 1 ? bf16_hi(w) : bf16_lo(w);
       nan |= x != x ? 0x7Fu << (8 * i) : 0u;
       v[i] = fminf(fmaxf(x * inv, -top), top);   // only infinities and e = 120 are cut
@@ -80,9 +80,13 @@ __device__ __forceinline__ u32x4 encode(const u32x4 &a, const u32x4 &b, int e) {
   return out;
 }
 
+// Numbers of a thread: 16 bytes of the wider side.
+constexpr int numbers(Move m) { return m == Move::kRead32 ? 4 : 8; }
+
 template <Move MODE>
 __global__ void __launch_bounds__(kMoveThreads)
 move_kernel(MoveArgs a) {
+  constexpr int kNum = numbers(MODE);
   constexpr bool kWrite = MODE == Move::kCopy || MODE == Move::kQuantise;
   int blk = blockIdx.x;
   const int cb = blk % a.col_blocks;
@@ -100,7 +104,7 @@ move_kernel(MoveArgs a) {
   const int chunk = col & (a.lanes - 1), ph = col / a.lanes;
   const int plane = ph / a.heads, head = ph - plane * a.heads;
   const bool mine = sub < a.at_once && col < a.cols && chunk < a.chunks;
-  const int64_t p = mine ? plane : 0, h = mine ? head : 0, c = mine ? chunk * 16 : 0;
+  const int64_t p = mine ? plane : 0, h = mine ? head : 0, c = mine ? chunk * kNum : 0;
   const int64_t s_at = p * a.src.plane_stride + b * a.src.batch_stride + h * a.src.head_stride + c;
   const int64_t d_at = p * a.dst.plane_stride + b * a.dst.batch_stride + h * a.dst.head_stride + c;
   const graft_rows &q = kWrite ? a.dst : a.src;    // the cache
@@ -114,7 +118,7 @@ move_kernel(MoveArgs a) {
   for (int g = 0; g < kMoveGroups; ++g) {
     const int base = row0 + g * (a.at_once * kMoveRows) + sub;
     if (row0 + g * (a.at_once * kMoveRows) >= n) break;
-    u32x4 v0[kMoveRows], v1[kMoveRows];
+    u32x4 v[kMoveRows];
     int64_t to[kMoveRows];
     uint32_t sc[kMoveRows];
     bool ok[kMoveRows];
@@ -141,16 +145,21 @@ move_kernel(MoveArgs a) {
         }
         if (!ok[k]) atomicOr(a.error_flag, kErrCacheRow);
       }
-      v0[k] = v1[k] = u32x4{0, 0, 0, 0};
+      v[k] = u32x4{0, 0, 0, 0};
       sc[k] = 0;
       if (ok[k]) {
         if (kWrite) {
-          const u32x4 *at = reinterpret_cast<const u32x4 *>(src + 2 * (s_at + from * a.src.row_stride));
-          v0[k] = __builtin_nontemporal_load(at);
-          v1[k] = __builtin_nontemporal_load(at + 1);
+          v[k] = __builtin_nontemporal_load(
+              reinterpret_cast<const u32x4 *>(src + 2 * (s_at + from * a.src.row_stride)));
         } else {
-          v0[k] = __builtin_nontemporal_load(
-              reinterpret_cast<const u32x4 *>(src + s_at + from * a.src.row_stride));
+          const char *at = src + s_at + from * a.src.row_stride;
+          if constexpr (kNum == 8) {
+            const u32x2 w = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(at));
+            v[k].x = w.x;
+            v[k].y = w.y;
+          } else {
+            v[k].x = __builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(at));
+          }
           sc[k] = scale[from * a.src.scale_row_stride];
         }
       }
@@ -158,13 +167,9 @@ move_kernel(MoveArgs a) {
 #pragma unroll
     for (int k = 0; k < kMoveRows; ++k) {
       if (MODE == Move::kCopy) {
-        if (ok[k]) {
-          u32x4 *at = reinterpret_cast<u32x4 *>(dst + 2 * (d_at + to[k] * a.dst.row_stride));
-          at[0] = v0[k];
-          at[1] = v1[k];
-        }
+        if (ok[k]) *reinterpret_cast<u32x4 *>(dst + 2 * (d_at + to[k] * a.dst.row_stride)) = v[k];
       } else if (MODE == Move::kQuantise) {
-        uint32_t m = largest(v0[k], v1[k]);
+        uint32_t m = largest(v[k]);
         // the head's lanes hold the same row; the others' zeros change nothing
         for (int x = 1; x < a.lanes; x <<= 1) {
           const uint32_t o = xor_lane(m, x);
@@ -173,43 +178,33 @@ move_kernel(MoveArgs a) {
         int e = static_cast<int>(m >> 7) - 135 + ((m & 0x7Fu) > 0x60u ? 1 : 0);
         e = e < -118 ? -118 : e;
         if (ok[k]) {
-          *reinterpret_cast<u32x4 *>(dst + d_at + to[k] * a.dst.row_stride) = encode(v0[k], v1[k], e);
+          *reinterpret_cast<u32x2 *>(dst + d_at + to[k] * a.dst.row_stride) = encode(v[k], e);
           if (chunk == 0) scale[to[k] * a.dst.scale_row_stride] = static_cast<uint8_t>(e + 127);
         }
       } else if (ok[k]) {
         const float unit = __uint_as_float(sc[k] ? sc[k] << 23 : 0x00400000u);
-        float x[16];
+        float x[kNum];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(v0[k][i]), false);
-          const f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(v0[k][i]), true);
+        for (int i = 0; i < kNum / 4; ++i) {
+          const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(v[k][i]), false);
+          const f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(v[k][i]), true);
           x[4 * i] = lo.x * unit;
           x[4 * i + 1] = lo.y * unit;
           x[4 * i + 2] = hi.x * unit;
           x[4 * i + 3] = hi.y * unit;
         }
-        if (MODE == Move::kRead16) {
+        u32x4 w;
+        if constexpr (kNum == 8) {
           // at most 4 significant bits: the upper half of the fp32 number is the bf16 number
-          u32x4 *at = reinterpret_cast<u32x4 *>(dst + 2 * (d_at + to[k] * a.dst.row_stride));
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            u32x4 w;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              w[i] = (__float_as_uint(x[8 * j + 2 * i]) >> 16) |
-                     (__float_as_uint(x[8 * j + 2 * i + 1]) & 0xFFFF0000u);
-            __builtin_nontemporal_store(w, at + j);
-          }
+          for (int i = 0; i < 4; ++i)
+            w[i] = (__float_as_uint(x[2 * i]) >> 16) | (__float_as_uint(x[2 * i + 1]) & 0xFFFF0000u);
         } else {
-          u32x4 *at = reinterpret_cast<u32x4 *>(dst + 4 * (d_at + to[k] * a.dst.row_stride));
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            u32x4 w;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(x[4 * j + i]);
-            __builtin_nontemporal_store(w, at + j);
-          }
+          for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(x[i]);
         }
+        __builtin_nontemporal_store(
+            w, reinterpret_cast<u32x4 *>(dst + (kNum == 8 ? 2 : 4) * (d_at + to[k] * a.dst.row_stride)));
       }
     }
   }
@@ -231,7 +226,7 @@ hipError_t launch_move(graft_ctx *ctx, const graft_cache_move &m, Move mode, int
   a.dst_rows = m.dst_rows;
   a.most = most;
   a.heads = m.heads;
-  a.chunks = m.head_dim / 16;
+  a.chunks = m.head_dim / numbers(mode);
   a.lanes = 1;
   while (a.lanes < a.chunks) a.lanes *= 2;
   a.cols = m.n_planes * m.heads * a.lanes;

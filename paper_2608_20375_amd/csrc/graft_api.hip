@@ -277,10 +277,10 @@ int check_move(const graft_ctx *ctx, const graft_cache_move *m, const char *who)
   int rc = check_rows(m->src, m->src_dtype, true, who, "src");
   if (rc == GRAFT_OK) rc = check_rows(m->dst, m->dst_dtype, true, who, "dst");
   if (rc != GRAFT_OK) return rc;
-  // workgroups of 256 columns, at most 32 a head, and of at least 16 rows
+  // workgroups of 256 columns, at most 32 a head, and of at least 4 rows
   const int64_t cols = static_cast<int64_t>(m->n_planes) * m->heads * 32;
   const int64_t rows = std::max(m->src_rows, std::max(m->dst_rows, m->list_len + 1));
-  if (cols > (1 << 28) || (cols / 256 + 1) * (rows / 16 + 1) > (int64_t{1} << 31) / m->batch - 1)
+  if (cols > (1 << 28) || (cols / 256 + 1) * (rows / 4 + 1) > (int64_t{1} << 31) / m->batch - 1)
     return fail(GRAFT_ERR_UNSUPPORTED, "%s: too many rows to move in one call", who);
   return check_device(ctx, who);
 }

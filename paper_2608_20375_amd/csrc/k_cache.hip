@@ -20,7 +20,6 @@ namespace {
 
 constexpr int kMoveThreads = 256;
 constexpr int kMoveRows = 4;     // rows a thread loads before it stores any
-constexpr int kMoveGroups = 4;   // such groups of rows a workgroup
 constexpr uint32_t kBf16Inf = 0x7F80u;
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
@@ -96,7 +95,7 @@ move_kernel(MoveArgs a) {
   const int first = a.start ? a.start[b] : 0;
   const int cap = kWrite && a.list ? a.list_len : a.most;
   n = (n < 0 ? 0 : (n > cap ? cap : n)) + a.root;
-  const int row0 = rb * (a.at_once * kMoveRows * kMoveGroups);
+  const int row0 = rb * (a.at_once * kMoveRows);
   if (row0 >= n) return;
 
   const int sub = a.at_once > 1 ? threadIdx.x / a.cols : 0;
@@ -115,97 +114,94 @@ move_kernel(MoveArgs a) {
   const char *src = static_cast<const char *>(a.src.data);
   char *dst = static_cast<char *>(a.dst.data);
 
-  for (int g = 0; g < kMoveGroups; ++g) {
-    const int base = row0 + g * (a.at_once * kMoveRows) + sub;
-    if (row0 + g * (a.at_once * kMoveRows) >= n) break;
-    u32x4 v[kMoveRows];
-    int64_t to[kMoveRows];
-    uint32_t sc[kMoveRows];
-    bool ok[kMoveRows];
+  const int base = row0 + sub;
+  u32x4 v[kMoveRows];
+  int64_t to[kMoveRows];
+  uint32_t sc[kMoveRows];
+  bool ok[kMoveRows];
 #pragma unroll
-    for (int k = 0; k < kMoveRows; ++k) {
-      const int i = base + k * a.at_once;
-      ok[k] = mine && i < n;
-      int64_t from = 0;
-      to[k] = 0;
-      if (ok[k]) {
-        if (kWrite) {
-          from = i;
-          if (a.list)
-            from = i < a.root ? 0 : a.list[static_cast<int64_t>(b) * a.list_len + i - a.root] +
-                                        static_cast<int64_t>(a.root);
-          // a node's entry is at least 0: with a root, row 0 is the root's alone
-          const bool good = from >= (a.list && i >= a.root ? a.root : 0) && from < a.src_rows;
-          to[k] = static_cast<int64_t>(first) + i;
-          ok[k] = good && to[k] >= 0 && to[k] < a.dst_rows;
-        } else {
-          to[k] = i;
-          from = static_cast<int64_t>(first) + i;
-          ok[k] = from >= 0 && from < a.src_rows;
-        }
-        if (!ok[k]) atomicOr(a.error_flag, kErrCacheRow);
+  for (int k = 0; k < kMoveRows; ++k) {
+    const int i = base + k * a.at_once;
+    ok[k] = mine && i < n;
+    int64_t from = 0;
+    to[k] = 0;
+    if (ok[k]) {
+      if (kWrite) {
+        from = i;
+        if (a.list)
+          from = i < a.root ? 0 : a.list[static_cast<int64_t>(b) * a.list_len + i - a.root] +
+                                      static_cast<int64_t>(a.root);
+        // a node's entry is at least 0: with a root, row 0 is the root's alone
+        const bool good = from >= (a.list && i >= a.root ? a.root : 0) && from < a.src_rows;
+        to[k] = static_cast<int64_t>(first) + i;
+        ok[k] = good && to[k] >= 0 && to[k] < a.dst_rows;
+      } else {
+        to[k] = i;
+        from = static_cast<int64_t>(first) + i;
+        ok[k] = from >= 0 && from < a.src_rows;
       }
-      v[k] = u32x4{0, 0, 0, 0};
-      sc[k] = 0;
-      if (ok[k]) {
-        if (kWrite) {
-          v[k] = __builtin_nontemporal_load(
-              reinterpret_cast<const u32x4 *>(src + 2 * (s_at + from * a.src.row_stride)));
+      if (!ok[k]) atomicOr(a.error_flag, kErrCacheRow);
+    }
+    v[k] = u32x4{0, 0, 0, 0};
+    sc[k] = 0;
+    if (ok[k]) {
+      if (kWrite) {
+        v[k] = __builtin_nontemporal_load(
+            reinterpret_cast<const u32x4 *>(src + 2 * (s_at + from * a.src.row_stride)));
+      } else {
+        const char *at = src + s_at + from * a.src.row_stride;
+        if constexpr (kNum == 8) {
+          const u32x2 w = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(at));
+          v[k].x = w.x;
+          v[k].y = w.y;
         } else {
-          const char *at = src + s_at + from * a.src.row_stride;
-          if constexpr (kNum == 8) {
-            const u32x2 w = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(at));
-            v[k].x = w.x;
-            v[k].y = w.y;
-          } else {
-            v[k].x = __builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(at));
-          }
-          sc[k] = scale[from * a.src.scale_row_stride];
+          v[k].x = __builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(at));
         }
+        sc[k] = scale[from * a.src.scale_row_stride];
       }
     }
+  }
 #pragma unroll
-    for (int k = 0; k < kMoveRows; ++k) {
-      if (MODE == Move::kCopy) {
-        if (ok[k]) *reinterpret_cast<u32x4 *>(dst + 2 * (d_at + to[k] * a.dst.row_stride)) = v[k];
-      } else if (MODE == Move::kQuantise) {
-        uint32_t m = largest(v[k]);
-        // the head's lanes hold the same row; the others' zeros change nothing
-        for (int x = 1; x < a.lanes; x <<= 1) {
-          const uint32_t o = xor_lane(m, x);
-          m = o > m ? o : m;
-        }
-        int e = static_cast<int>(m >> 7) - 135 + ((m & 0x7Fu) > 0x60u ? 1 : 0);
-        e = e < -118 ? -118 : e;
-        if (ok[k]) {
-          *reinterpret_cast<u32x2 *>(dst + d_at + to[k] * a.dst.row_stride) = encode(v[k], e);
-          if (chunk == 0) scale[to[k] * a.dst.scale_row_stride] = static_cast<uint8_t>(e + 127);
-        }
-      } else if (ok[k]) {
-        const float unit = __uint_as_float(sc[k] ? sc[k] << 23 : 0x00400000u);
-        float x[kNum];
-#pragma unroll
-        for (int i = 0; i < kNum / 4; ++i) {
-          const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(v[k][i]), false);
-          const f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(v[k][i]), true);
-          x[4 * i] = lo.x * unit;
-          x[4 * i + 1] = lo.y * unit;
-          x[4 * i + 2] = hi.x * unit;
-          x[4 * i + 3] = hi.y * unit;
-        }
-        u32x4 w;
-        if constexpr (kNum == 8) {
-          // at most 4 significant bits: the upper half of the fp32 number is the bf16 number
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            w[i] = (__float_as_uint(x[2 * i]) >> 16) | (__float_as_uint(x[2 * i + 1]) & 0xFFFF0000u);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(x[i]);
-        }
-        __builtin_nontemporal_store(
-            w, reinterpret_cast<u32x4 *>(dst + (kNum == 8 ? 2 : 4) * (d_at + to[k] * a.dst.row_stride)));
+  for (int k = 0; k < kMoveRows; ++k) {
+    if (MODE == Move::kCopy) {
+      if (ok[k]) *reinterpret_cast<u32x4 *>(dst + 2 * (d_at + to[k] * a.dst.row_stride)) = v[k];
+    } else if (MODE == Move::kQuantise) {
+      uint32_t m = largest(v[k]);
+      // the head's lanes hold the same row; the others' zeros change nothing
+      for (int x = 1; x < a.lanes; x <<= 1) {
+        const uint32_t o = xor_lane(m, x);
+        m = o > m ? o : m;
       }
+      int e = static_cast<int>(m >> 7) - 135 + ((m & 0x7Fu) > 0x60u ? 1 : 0);
+      e = e < -118 ? -118 : e;
+      if (ok[k]) {
+        *reinterpret_cast<u32x2 *>(dst + d_at + to[k] * a.dst.row_stride) = encode(v[k], e);
+        if (chunk == 0) scale[to[k] * a.dst.scale_row_stride] = static_cast<uint8_t>(e + 127);
+      }
+    } else if (ok[k]) {
+      const float unit = __uint_as_float(sc[k] ? sc[k] << 23 : 0x00400000u);
+      float x[kNum];
+#pragma unroll
+      for (int i = 0; i < kNum / 4; ++i) {
+        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(v[k][i]), false);
+        const f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(v[k][i]), true);
+        x[4 * i] = lo.x * unit;
+        x[4 * i + 1] = lo.y * unit;
+        x[4 * i + 2] = hi.x * unit;
+        x[4 * i + 3] = hi.y * unit;
+      }
+      u32x4 w;
+      if constexpr (kNum == 8) {
+        // at most 4 significant bits: the upper half of the fp32 number is the bf16 number
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          w[i] = (__float_as_uint(x[2 * i]) >> 16) | (__float_as_uint(x[2 * i + 1]) & 0xFFFF0000u);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(x[i]);
+      }
+      __builtin_nontemporal_store(
+          w, reinterpret_cast<u32x4 *>(dst + (kNum == 8 ? 2 : 4) * (d_at + to[k] * a.dst.row_stride)));
     }
   }
 }
@@ -232,7 +228,7 @@ hipError_t launch_move(graft_ctx *ctx, const graft_cache_move &m, Move mode, int
   a.cols = m.n_planes * m.heads * a.lanes;
   a.at_once = a.cols < kMoveThreads ? kMoveThreads / a.cols : 1;
   a.col_blocks = (a.cols + kMoveThreads - 1) / kMoveThreads;
-  const int per = a.at_once * kMoveRows * kMoveGroups;
+  const int per = a.at_once * kMoveRows;
   a.row_blocks = (most + per - 1) / per;
   a.error_flag = ctx->error_flag;
   const dim3 grid(static_cast<unsigned>(a.col_blocks) * a.row_blocks * m.batch), block(kMoveThreads);

@@ -187,15 +187,22 @@ __device__ __forceinline__ double factor(float from, float to, const Exp2 &ex) {
   ex.run(z, to, w);
   return w[0];
 }
-__device__ __forceinline__ float uniform(float v) {
-  return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v)));
+// Largest over the lanes, in scalar registers: the steps of wave_incl_scan, lanes without a
+// source keeping their own.
+template <int CTRL, int ROWS> __device__ __forceinline__ float dpp_max(float v) {
+  const int x = static_cast<int>(__float_as_uint(v));
+  return fmaxf(v, __uint_as_float(static_cast<uint32_t>(
+                      __builtin_amdgcn_update_dpp(x, x, CTRL, ROWS, 0xF, false))));
 }
-
 __device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int m = 1; m < kWave; m <<= 1)
-    v = fmaxf(v, __uint_as_float(xor_lane(__float_as_uint(v), m)));
-  return v;
+  v = dpp_max<0x111, 0xF>(v);
+  v = dpp_max<0x112, 0xF>(v);
+  v = dpp_max<0x114, 0xF>(v);
+  v = dpp_max<0x118, 0xF>(v);
+  v = dpp_max<0x142, 0xA>(v);
+  v = dpp_max<0x143, 0xC>(v);
+  return __uint_as_float(static_cast<uint32_t>(
+      __builtin_amdgcn_readlane(static_cast<int>(__float_as_uint(v)), kWave - 1)));
 }
 template <int CTRL, int ROWS>
 __device__ __forceinline__ double dpp_f64(double v) {   // lanes without a source: 0
@@ -215,6 +222,23 @@ __device__ __forceinline__ double wave_scan(double v) {
   v += dpp_f64<0x142, 0xA>(v);
   v += dpp_f64<0x143, 0xC>(v);
   return v;
+}
+// x over the lanes' pairs (lane, lane ^ M) in the lanes without bit M, y in those with it.
+template <int M> __device__ __forceinline__ double swap_add(double x, double y) {
+  const uint64_t u = static_cast<uint64_t>(__double_as_longlong(x)), v = static_cast<uint64_t>(__double_as_longlong(y));
+  uint32_t w[2][2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t p = static_cast<uint32_t>(u >> (32 * i)), q = static_cast<uint32_t>(v >> (32 * i));
+    const auto r = M == 32 ? __builtin_amdgcn_permlane32_swap(p, q, false, false)
+                           : __builtin_amdgcn_permlane16_swap(p, q, false, false);
+    w[0][i] = r[0];
+    w[1][i] = r[1];
+  }
+  const auto f64 = [](const uint32_t (&z)[2]) {
+    return __longlong_as_double(static_cast<long long>((static_cast<uint64_t>(z[1]) << 32) | z[0]));
+  };
+  return f64(w[0]) + f64(w[1]);
 }
 __device__ __forceinline__ double lane_f64(double v, int lane) {   // of a uniform lane
   const uint64_t u = static_cast<uint64_t>(__double_as_longlong(v));
@@ -251,11 +275,23 @@ struct Level {
   Sums sums[kGroups];
 };
 
-// The token of a level from its flights, -1 if no token has a positive probability;
-// *lp its log-probability.  All lanes return the same.
+// A drawn token: -1 if none has a positive probability.  Its logit, the maximum and the
+// sum give the log-probability.
+struct Draw {
+  int token;
+  float z, top;
+  double total;
+  __device__ __forceinline__ float logp(double T) const {
+    if (token < 0) return -INFINITY;
+    if (T == 0.0) return 0.0f;
+    const double d = z == top ? 0.0 : (static_cast<double>(z) - static_cast<double>(top)) / T;
+    return static_cast<float>(d - log(total));
+  }
+};
+// The token of a level from its flights, the same in all lanes.
 template <typename E>
-__device__ __forceinline__ int draw_token(const SampleArgs &a, Level &at, const Row<E> &row,
-                                          const Exp2 &ex, double T, double u, double *lp) {
+__device__ __forceinline__ Draw draw_token(const SampleArgs &a, Level &at, const Row<E> &row,
+                                          const Exp2 &ex, double T, double u) {
   const int lane = lane_id();
   const int per = kWave * a.rep;                         // vectors of a run
   const int flights = (row.n_vec + kRuns * per - 1) / (kRuns * per);
@@ -268,12 +304,8 @@ __device__ __forceinline__ int draw_token(const SampleArgs &a, Level &at, const 
     }
     m = fmaxf(m, at.top[g]);
   }
-  const float top = uniform(wave_max(m));
-  *lp = 0.0;
-  if (top == -INFINITY) {
-    *lp = -INFINITY;
-    return -1;
-  }
+  const float top = wave_max(m);
+  if (top == -INFINITY) return Draw{-1, top, top, 0.0};
   if (T == 0.0) {
     int best = INT32_MAX;
 #pragma unroll
@@ -281,7 +313,7 @@ __device__ __forceinline__ int draw_token(const SampleArgs &a, Level &at, const 
       const int i = static_cast<int>(at.sums[g].run[0]);
       if (at.top[g] == top && i < best) best = i;
     }
-    return wave_min(best);
+    return Draw{wave_min(best), top, top, 1.0};
   }
   double all[kGroups], upto[kGroups], total = 0.0;
 #pragma unroll
@@ -381,12 +413,7 @@ __device__ __forceinline__ int draw_token(const SampleArgs &a, Level &at, const 
         __builtin_amdgcn_readlane(static_cast<int>(__float_as_uint(hit_z)), from)));
     if (hits != 0) break;
   }
-  if (tok < 0) {   // only if the row changed under the call
-    *lp = -INFINITY;
-    return -1;
-  }
-  *lp = (z == top ? 0.0 : (static_cast<double>(z) - static_cast<double>(top)) / T) - log(total);
-  return tok;
+  return Draw{tok, z, top, total};   // tok < 0 only if the row changed under the call
 }
 
 // Level `level` of every walk: its node from the level before, then this
@@ -402,6 +429,7 @@ sample_kernel(SampleArgs a, int level) {
   bool bad_t;
   const double T = temperature(a, b, &bad_t);
   const Exp2 ex(T);
+  Draw drawn{};
   int node = -1;
   if (level > 0) {
     const int before = a.state[(level - 1) * a.batch + b];
@@ -432,24 +460,27 @@ sample_kernel(SampleArgs a, int level) {
     int n = a.n_nodes[b];
     n = n < 0 ? 0 : (n > a.n_max ? a.n_max : n);
     n = n > a.node_rows ? a.node_rows : n;
-    double lp;
-    const int x = draw_token<E>(a, left, Row<E>(row_of<E>(a, b, before), a.V), ex, T, u, &lp);
+    drawn = draw_token<E>(a, left, Row<E>(row_of<E>(a, b, before), a.V), ex, T, u);
+    const int x = drawn.token;
     int child = INT32_MAX;
-    for (int i = kSampTree * kWave + lane; i < n; i += kWave)
-      if (i > before && i < child && a.parents[tree + i] == before && a.tokens[tree + i] == x) child = i;
 #pragma unroll
     for (int k = kSampTree - 1; k >= 0; --k) {
       const int i = lane + k * kWave;
-      if (i < n && i > before && par[k] == before && tok[k] == x) child = i;
+      const uint64_t hits = __ballot(i < n && i > before && par[k] == before && tok[k] == x);
+      if (hits != 0) child = k * kWave + first_lane(hits);
     }
-    child = wave_min(child);
+    for (int k = kSampTree * kWave; k < n && child == INT32_MAX; k += kWave) {
+      const int i = k + lane;
+      const uint64_t hits = __ballot(i < n && i > before && a.parents[tree + i] == before && a.tokens[tree + i] == x);
+      if (hits != 0) child = k + first_lane(hits);
+    }
     const bool go = child != INT32_MAX && level <= a.L && x >= 0;
     node = go ? child : kStopped;
     if (wave == 0) {
       const int d = level - 1;                  // nodes accepted before this token
       if (lane == 0) {
         if (level <= a.L) a.state[level * a.batch + b] = node;
-        if (a.logp) a.logp[static_cast<int64_t>(b) * (a.L + 1) + d] = static_cast<float>(lp);
+        if (!go && a.logp) a.logp[static_cast<int64_t>(b) * (a.L + 1) + d] = drawn.logp(T);
         if (go) a.acc_nodes[static_cast<int64_t>(b) * a.L + d] = child;
         if (x < 0) atomicOr(a.error_flag, kErrTargetRow);
       }
@@ -514,7 +545,7 @@ sample_kernel(SampleArgs a, int level) {
           }
         continue;
       }
-      const float all = uniform(wave_max(g));
+      const float all = wave_max(g);
       if (all == -INFINITY) continue;
       if (r > 0) {
         const double scale = factor(m, all, ex);
@@ -540,17 +571,17 @@ sample_kernel(SampleArgs a, int level) {
       continue;
     }
     // the four sums together: halves of the wave keep two each, then rows of 16 one each
-    const bool up = lane & 32, odd = lane & 16;
-    const double s0 = (up ? sum[2] : sum[0]) + xor_lane_f64(up ? sum[0] : sum[2], 32);
-    const double s1 = (up ? sum[3] : sum[1]) + xor_lane_f64(up ? sum[1] : sum[3], 32);
-    double s = (odd ? s1 : s0) + xor_lane_f64(odd ? s0 : s1, 16);
-    s += xor_lane_f64(s, 8);
-    s += xor_lane_f64(s, 4);
-    s += xor_lane_f64(s, 2);
-    s += xor_lane_f64(s, 1);
-    if ((lane & 15) == 0) a.sums[at + f].run[lane / 16] = s;
+    double t = swap_add<16>(swap_add<32>(sum[0], sum[2]), swap_add<32>(sum[1], sum[3]));
+    t += xor_lane_f64(t, 8);
+    t += xor_lane_f64(t, 4);
+    t += xor_lane_f64(t, 2);
+    t += xor_lane_f64(t, 1);
+    if ((lane & 15) == 0) a.sums[at + f].run[lane / 16] = t;
     if (lane == 0) a.tops[at + f] = m;
   }
+  // the token's log-probability, which nothing waits for
+  if (level > 0 && wave == splits * kSampWaves - 1 && lane == 0 && a.logp)
+    a.logp[static_cast<int64_t>(b) * (a.L + 1) + level - 1] = drawn.logp(T);
 }
 
 }  // namespace

@@ -426,17 +426,17 @@ sample_kernel(SampleArgs a, int level) {
   const int lane = lane_id();
   const int wave = __builtin_amdgcn_readfirstlane((blockIdx.x - b * splits) * kSampWaves + threadIdx.x / kWave);
   if (level > a.L && wave > 0) return;
+  const int before = level > 0 ? a.state[(level - 1) * a.batch + b] : -1;
+  if (before == kStopped) {
+    if (wave == 0 && lane == 0 && level <= a.L) a.state[level * a.batch + b] = kStopped;
+    return;
+  }
   bool bad_t;
   const double T = temperature(a, b, &bad_t);
   const Exp2 ex(T);
   Draw drawn{};
   int node = -1;
   if (level > 0) {
-    const int before = a.state[(level - 1) * a.batch + b];
-    if (before == kStopped) {
-      if (wave == 0 && lane == 0 && level <= a.L) a.state[level * a.batch + b] = kStopped;
-      return;
-    }
     // the tree's arrays with the flights: one round trip
     int32_t par[kSampTree], tok[kSampTree];
     const int64_t tree = static_cast<int64_t>(b) * a.n_max;

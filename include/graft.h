@@ -322,7 +322,9 @@ GRAFT_API int graft_commit_accepted(graft_ctx *ctx, int32_t batch, const int32_t
  * is 16-byte aligned and every stride is non-negative and a multiple of 16
  * bytes.  E4M3 rows have one scale a (plane, b, row, head), a byte s at the
  * scale strides (in bytes) that stands for 2^(s - 127): the numbers are code *
- * 2^(s - 127).  scale and its strides are ignored for other types. */
+ * 2^(s - 127).  graft_cache_write makes s from 9 to 247, for which every number is
+ * exact in bf16 and fp32 (codes end at 240 for 247); with other bytes they may be
+ * rounded, or infinite or NaN.  scale and its strides are ignored for other types. */
 typedef struct {
     void *data;
     int64_t plane_stride, batch_stride, row_stride, head_stride;
@@ -465,14 +467,15 @@ typedef struct {
  * value is finite in fp32 and exact in bf16.
  * Rows whose source row is outside 0 .. src_rows - 1 or whose cache row is
  * outside 0 .. dst_rows - 1 are skipped and reported by graft_get_device_status.
- * src and dst must not overlap. */
+ * src and dst must not overlap.  At most 2^30 rows and 2^28 planes or heads. */
 GRAFT_API int graft_cache_write(graft_ctx *ctx, const graft_cache_move *m /* host */,
                                 graft_stream_t stream);
 
 /* Reads rows start[b] .. start[b] + n_rows[b] - 1 of a GRAFT_E4M3 cache (src)
  * back as GRAFT_BF16 or GRAFT_F32 numbers, to rows 0 .. n_rows[b] - 1 of dst.
  * Exact in both types.  n_rows is clamped to 0 .. dst_rows; rows outside the cache are
- * skipped and reported.  list and with_root are not used (NULL and 0). */
+ * skipped and reported.  list and with_root are not used (NULL and 0); limits and overlap
+ * as above. */
 GRAFT_API int graft_cache_read(graft_ctx *ctx, const graft_cache_move *m /* host */,
                                graft_stream_t stream);
 

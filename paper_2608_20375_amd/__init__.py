@@ -283,7 +283,8 @@ _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 class QuantRows:
     """Quantised key/value rows: codes [..., rows, heads, head_dim] (e4m3: uint8 or
     float8_e4m3fn) and scales [..., rows, heads] (uint8, s stands for 2^(s - 127)),
-    the numbers being code * 2^(s - 127).  Indexing takes views of both."""
+    the numbers being code * 2^(s - 127); s from 9 to 247 as cache_write makes it.
+    Indexing takes views of both."""
 
     __slots__ = ("codes", "scales")
 

@@ -277,6 +277,10 @@ int check_move(const graft_ctx *ctx, const graft_cache_move *m, const char *who)
   int rc = check_rows(m->src, m->src_dtype, true, who, "src");
   if (rc == GRAFT_OK) rc = check_rows(m->dst, m->dst_dtype, true, who, "dst");
   if (rc != GRAFT_OK) return rc;
+  // row numbers of a workgroup's last rows stay below 2^31, the products below 2^63
+  if (m->src_rows > (1 << 30) || m->dst_rows > (1 << 30) || m->list_len > (1 << 30) ||
+      m->n_planes > (1 << 28) || m->heads > (1 << 28))
+    return fail(GRAFT_ERR_UNSUPPORTED, "%s: more than 2^30 rows or 2^28 planes or heads", who);
   // workgroups of 256 columns, at most 32 a head, and of at least 4 rows
   const int64_t cols = static_cast<int64_t>(m->n_planes) * m->heads * 32;
   const int64_t rows = std::max(m->src_rows, std::max(m->dst_rows, m->list_len + 1));

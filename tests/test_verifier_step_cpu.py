@@ -145,6 +145,22 @@ def test_cache_entry_points():
     assert L.graft_cache_read(f.h, None, None) == 1
 
 
+def test_cache_sizes_past_32_bits_are_refused():
+    """Row numbers of a workgroup's last rows, and products of the sizes, would wrap."""
+    L, f = G.lib(), Fake()
+    write = lambda m: L.graft_cache_write(f.h, C.byref(m), None)
+    read = lambda m: L.graft_cache_read(f.h, C.byref(m), None)
+    small = dict(batch=1, n_planes=1, heads=1, head_dim=16)
+    back = dict(small, src_dtype=3, dst_dtype=1, src=rows(True), dst=rows(), list=0, list_len=0, with_root=0)
+    top = 2 ** 31 - 1
+    for kw in (dict(src_rows=top, list=0, list_len=0, with_root=0), dict(dst_rows=top), dict(list_len=top),
+               dict(n_planes=top, heads=top), dict(n_planes=1 << 29), dict(heads=1 << 29)):
+        assert write(move(**dict(small, **kw))) == 2, kw
+    for kw in (dict(src_rows=top), dict(dst_rows=top), dict(n_planes=top, heads=top)):
+        assert read(move(**dict(back, **kw))) == 2, kw
+    assert read(move(**dict(back, src_rows=1 << 30, dst_rows=1 << 30))) == NO_GPU
+
+
 def test_binding_refuses_shapes_and_types_before_any_call():
     ctx = context()
     bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)

@@ -113,3 +113,26 @@ def test_slots_past_the_block_are_not_read():
     out, lse, _ = call(ctx, c, **wide)
     check(c, out, lse)
     ctx.close()
+
+
+@pytest.mark.parametrize("nodes", [1, 40])
+@pytest.mark.parametrize("quant", [False, True])
+def test_one_sequence_past_32_bit_offsets(nodes, quant):
+    """Rows 4 MB apart, so that a sequence's later tiles start more than 2^31 bytes after its
+    first."""
+    rows = 600
+    c = make(1, nodes, [rows], 0, 2, 1, 64, "bfloat16", quant, 1, seed=nodes, extra=0)
+    import paper_2608_20375_amd as G
+    space = torch.empty(rows * (1 << 22), dtype=torch.uint8, device="cuda")
+    pair = []
+    for i, x in enumerate(c["cache"]):
+        codes = x[0] if quant else x
+        at = space.view(codes.dtype)
+        per = at.numel() // rows
+        far = at.as_strided((1, rows, 1, 64), (0, per, 64, 1), 128 * i)
+        far.copy_(codes.cuda())
+        pair.append(G.QuantRows(far, x[1].cuda()) if quant else far)
+    ctx = context(c)
+    out, lse, _ = call(ctx, c, cache=tuple(pair))
+    check(c, out, lse)
+    ctx.close()

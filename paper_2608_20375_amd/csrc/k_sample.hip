@@ -11,13 +11,15 @@
 // this one's token is.  So a launch takes one level.  A row's 16-byte vectors are cut
 // into runs of 64 `rep` (one vector a lane; rep is 1 up to 2^19 words), four runs make a
 // flight, and the flights are dealt to the waves of the sequence's workgroups.  A wave
-// leaves its flight's maximum and the four runs' sums of exponentials over it.  The
-// next launch's waves each combine the level's flights (at most 256, one to four a
-// lane), find the run that holds u S by a scan, read that run again for the token,
-// look for the child, and go on with the child's row.  Every wave of a sequence does
-// this by itself and arrives at the same bits, so there is no flag, counter or wait
-// between workgroups, nor a barrier inside one.  Sequences whose walk has ended leave
-// at once.  The flights' arrays alternate by level.
+// leaves its flight's maximum and the four runs' sums of exponentials over it.  In the
+// next launch one wave of each workgroup combines the level's flights (at most 256, one
+// to four a lane), finds the run that holds u S by a scan, reads that run again for the
+// token, looks for the child, and all go on with the child's row.  Every workgroup of a
+// sequence does this by itself and arrives at the same bits, so there is no flag, counter
+// or wait between workgroups.  (Every wave by itself, without a barrier: 64 walks of
+// 128256 words 211 us instead of 198, the vector units being busy with it.  Workgroups of
+// 512 threads: 209.)  Sequences whose walk has ended leave at once.  The flights' arrays
+// alternate by level.
 //
 // Exponentials and sums are fp64: with V borders between tokens on [0, 1), an error
 // of 1e-7 in the sums would change one draw in a hundred at V = 150000.
@@ -27,9 +29,9 @@
 // without walks is 2.8 us.  A level of many walks is bound by the fp64 multiply-adds: 128
 // rows of 151936 words 23 us before any walk has ended, of which the instructions alone
 // are 11.  The vector registers (190 for 16-bit logits) leave two waves a SIMD; held to
-// 168 or 128 they spill, and the 128 walks take 382 and 518 us instead of 332.
-// Whole calls: 40 us for one walk of 32000 words and up to 8 levels, 72 for 5 of 70001
-// fp32 words, 206 for 64 of 128256, 332 for 128 of 151936 words and up to 32 levels.
+// 168 or 128 they spill: a sixth and a half more time for the 128 walks.
+// Whole calls: 40 to 67 us for one walk of 32000 words and up to 8 levels, 63 for 5 of
+// 70001 fp32 words, 198 for 64 of 128256, 316 for 128 of 151936 words and up to 32 levels.
 #include "graft_internal.h"
 
 namespace graft {
@@ -39,8 +41,8 @@ constexpr int kSampThreads = 256;
 constexpr int kSampWaves = kSampThreads / kWave;
 constexpr int kRuns = 4;                 // runs of a flight: vectors of a lane in flight
 constexpr int kGroups = 4;               // flights of a row at most: kGroups a lane
-// Waves of a launch, about: 128 walks of 151936 words take 351, 332 and 373 us for 4096, 8192
-// and 16384, each of which resolves the level before.
+// Waves of a launch, about: 128 walks of 151936 words take 341, 316 and 340 us for 4096, 8192
+// and 16384.
 constexpr int64_t kSampTarget = 8192;
 constexpr int kSampTree = 4;             // tree slots a lane loads ahead
 constexpr int kStopped = -2;             // a walk that has ended; -1 is the root
@@ -432,11 +434,12 @@ __device__ __forceinline__ Draw draw_token(const SampleArgs &a, Level &at, const
 template <typename E>
 __global__ void __launch_bounds__(kSampThreads)
 sample_kernel(SampleArgs a, int level) {
+  __shared__ int s_node;
+  __shared__ Draw s_drawn;
   const int splits = level <= a.L ? a.splits : 1;
   const int b = blockIdx.x / splits;
   const int lane = lane_id();
   const int wave = __builtin_amdgcn_readfirstlane((blockIdx.x - b * splits) * kSampWaves + threadIdx.x / kWave);
-  if (level > a.L && wave > 0) return;
   const int before = level > 0 ? a.state[(level - 1) * a.batch + b] : -1;
   if (before == kStopped) {
     if (wave == 0 && lane == 0 && level <= a.L) a.state[level * a.batch + b] = kStopped;
@@ -445,74 +448,81 @@ sample_kernel(SampleArgs a, int level) {
   bool bad_t;
   const double T = temperature(a, b, &bad_t);
   const Exp2 ex(T);
-  Draw drawn{};
   int node = -1;
   if (level > 0) {
-    // the tree's arrays with the flights: one round trip
-    int32_t par[kSampTree], tok[kSampTree];
-    const int64_t tree = static_cast<int64_t>(b) * a.n_max;
+    if (wave % kSampWaves == 0) {
+      // the tree's arrays with the flights: one round trip
+      int32_t par[kSampTree], tok[kSampTree];
+      const int64_t tree = static_cast<int64_t>(b) * a.n_max;
 #pragma unroll
-    for (int k = 0; k < kSampTree; ++k) {
-      const int i = lane + k * kWave;
-      par[k] = a.parents[tree + (i < a.n_max ? i : a.n_max - 1)];
-      tok[k] = a.tokens[tree + (i < a.n_max ? i : a.n_max - 1)];
-    }
-    Level left;
-    const int64_t at = (static_cast<int64_t>((level - 1) & 1) * a.batch + b) * a.flights;
-#pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
-      const int f = g * kWave + lane;
-      if (f < a.flights) {
-        left.top[g] = a.tops[at + f];
-        left.sums[g] = a.sums[at + f];
+      for (int k = 0; k < kSampTree; ++k) {
+        const int i = lane + k * kWave;
+        par[k] = a.parents[tree + (i < a.n_max ? i : a.n_max - 1)];
+        tok[k] = a.tokens[tree + (i < a.n_max ? i : a.n_max - 1)];
       }
-    }
-    const double u = a.uniform[static_cast<int64_t>(b) * (a.L + 1) + level - 1];
-    int n = a.n_nodes[b];
-    n = n < 0 ? 0 : (n > a.n_max ? a.n_max : n);
-    n = n > a.node_rows ? a.node_rows : n;
-    drawn = draw_token<E>(a, left, Row<E>(row_of<E>(a, b, before), a.V), ex, T, u);
-    const int x = drawn.token;
-    int child = INT32_MAX;
+      Level left;
+      const int64_t at = (static_cast<int64_t>((level - 1) & 1) * a.batch + b) * a.flights;
 #pragma unroll
-    for (int k = kSampTree - 1; k >= 0; --k) {
-      const int i = lane + k * kWave;
-      const uint64_t hits = __ballot(i < n && i > before && par[k] == before && tok[k] == x);
-      if (hits != 0) child = k * kWave + first_lane(hits);
-    }
-    for (int k = kSampTree * kWave; k < n && child == INT32_MAX; k += kWave) {
-      const int i = k + lane;
-      const uint64_t hits = __ballot(i < n && i > before && a.parents[tree + i] == before && a.tokens[tree + i] == x);
-      if (hits != 0) child = k + first_lane(hits);
-    }
-    const bool go = child != INT32_MAX && level <= a.L && x >= 0;
-    node = go ? child : kStopped;
-    if (wave == 0) {
-      const int d = level - 1;                  // nodes accepted before this token
-      if (lane == 0) {
-        if (level <= a.L) a.state[level * a.batch + b] = node;
-        if (!go && a.logp) a.logp[static_cast<int64_t>(b) * (a.L + 1) + d] = drawn.logp(T);
-        if (go) a.acc_nodes[static_cast<int64_t>(b) * a.L + d] = child;
-        if (x < 0) atomicOr(a.error_flag, kErrTargetRow);
+      for (int g = 0; g < kGroups; ++g) {
+        const int f = g * kWave + lane;
+        if (f < a.flights) {
+          left.top[g] = a.tops[at + f];
+          left.sums[g] = a.sums[at + f];
+        }
       }
-      if (!go) {
-        for (int i = d + lane; i < a.L; i += kWave)
-          a.acc_nodes[static_cast<int64_t>(b) * a.L + i] = -1;
-        if (a.logp)
-          for (int i = d + 1 + lane; i <= a.L; i += kWave)
-            a.logp[static_cast<int64_t>(b) * (a.L + 1) + i] = 0.0f;
+      const double u = a.uniform[static_cast<int64_t>(b) * (a.L + 1) + level - 1];
+      int n = a.n_nodes[b];
+      n = n < 0 ? 0 : (n > a.n_max ? a.n_max : n);
+      n = n > a.node_rows ? a.node_rows : n;
+      const Draw drawn = draw_token<E>(a, left, Row<E>(row_of<E>(a, b, before), a.V), ex, T, u);
+      const int x = drawn.token;
+      int child = INT32_MAX;
+#pragma unroll
+      for (int k = kSampTree - 1; k >= 0; --k) {
+        const int i = lane + k * kWave;
+        const uint64_t hits = __ballot(i < n && i > before && par[k] == before && tok[k] == x);
+        if (hits != 0) child = k * kWave + first_lane(hits);
+      }
+      for (int k = kSampTree * kWave; k < n && child == INT32_MAX; k += kWave) {
+        const int i = k + lane;
+        const uint64_t hits = __ballot(i < n && i > before && a.parents[tree + i] == before && a.tokens[tree + i] == x);
+        if (hits != 0) child = k + first_lane(hits);
+      }
+      const bool go = child != INT32_MAX && level <= a.L && x >= 0;
+      node = go ? child : kStopped;
+      if (wave == 0) {
+        const int d = level - 1;                  // nodes accepted before this token
         if (lane == 0) {
-          a.acc_len[b] = d;
-          a.bonus[b] = x;
-          if (a.update) {
-            const int p = a.ring_pos[b];
-            a.ring[static_cast<int64_t>(b) * a.window + p] = d;
-            a.ring_pos[b] = (p + 1) % a.window;
+          if (level <= a.L) a.state[level * a.batch + b] = node;
+          if (!go && a.logp) a.logp[static_cast<int64_t>(b) * (a.L + 1) + d] = drawn.logp(T);
+          if (go) a.acc_nodes[static_cast<int64_t>(b) * a.L + d] = child;
+          if (x < 0) atomicOr(a.error_flag, kErrTargetRow);
+        }
+        if (!go) {
+          for (int i = d + lane; i < a.L; i += kWave)
+            a.acc_nodes[static_cast<int64_t>(b) * a.L + i] = -1;
+          if (a.logp)
+            for (int i = d + 1 + lane; i <= a.L; i += kWave)
+              a.logp[static_cast<int64_t>(b) * (a.L + 1) + i] = 0.0f;
+          if (lane == 0) {
+            a.acc_len[b] = d;
+            a.bonus[b] = x;
+            if (a.update) {
+              const int p = a.ring_pos[b];
+              a.ring[static_cast<int64_t>(b) * a.window + p] = d;
+              a.ring_pos[b] = (p + 1) % a.window;
+            }
           }
         }
       }
+      if (lane == 0) {
+        s_node = node;
+        s_drawn = drawn;
+      }
     }
-    if (!go) return;
+    __syncthreads();
+    node = __builtin_amdgcn_readfirstlane(s_node);
+    if (node == kStopped) return;
   } else if (wave == 0 && lane == 0) {
     a.state[b] = -1;
     if (bad_t) atomicOr(a.error_flag, kErrTargetRow);
@@ -592,7 +602,7 @@ sample_kernel(SampleArgs a, int level) {
   }
   // the token's log-probability, which nothing waits for
   if (level > 0 && wave == splits * kSampWaves - 1 && lane == 0 && a.logp)
-    a.logp[static_cast<int64_t>(b) * (a.L + 1) + level - 1] = drawn.logp(T);
+    a.logp[static_cast<int64_t>(b) * (a.L + 1) + level - 1] = s_drawn.logp(T);
 }
 
 }  // namespace

@@ -321,26 +321,23 @@ class QuantRows:
         return QuantRows(self.codes[index], self.scales[index])
 
 
-def _strides(t, n):
-    """Element strides of the last n of (plane, batch, row, head), t's leading extents;
-    0 for the others and where there is one entry."""
-    shape, stride = t.shape, t.stride()
-    if n == 3:
-        return (0, stride[0] if shape[0] > 1 else 0, stride[1] if shape[1] > 1 else 0,
-                stride[2] if shape[2] > 1 else 0)
-    return (0,) * (4 - n) + tuple([stride[i] if shape[i] > 1 else 0 for i in range(n)])
-
-
 def _rows(t, n, name):
     """graft_rows of a tensor or QuantRows: n extents, the last of (plane, batch, row, head),
-    and head_dim."""
+    and head_dim.  Strides of extents with one entry are 0."""
     quant = isinstance(t, QuantRows)
     data = t.codes if quant else t
-    if data.stride(-1) != 1 and data.shape[-1] > 1:
+    e, s = data.shape, data.stride()
+    if s[n] != 1 and e[n] > 1:
         raise ValueError("%s must have unit stride along its last dimension" % name)
-    if quant:
-        return Rows(data.data_ptr(), *_strides(data, n), t.scales.data_ptr(), *_strides(t.scales, n))
-    return Rows(data.data_ptr(), *_strides(data, n))
+    if n == 3 and not quant:
+        return Rows(data.data_ptr(), 0, s[0] if e[0] > 1 else 0, s[1] if e[1] > 1 else 0,
+                    s[2] if e[2] > 1 else 0)
+    lead = (0,) * (4 - n)
+    at = (data.data_ptr(), *lead, *[s[i] if e[i] > 1 else 0 for i in range(n)])
+    if not quant:
+        return Rows(*at)
+    s = t.scales.stride()
+    return Rows(*at, t.scales.data_ptr(), *lead, *[s[i] if e[i] > 1 else 0 for i in range(n)])
 
 
 class TreeBuffers:

@@ -17,8 +17,9 @@
 // token, looks for the child, and all go on with the child's row.  Every workgroup of a
 // sequence does this by itself and arrives at the same bits, so there is no flag, counter
 // or wait between workgroups.  (Every wave by itself, without a barrier: 64 walks of
-// 128256 words 211 us instead of 198, the vector units being busy with it.  Workgroups of
-// 512 threads: 209.)  Sequences whose walk has ended leave at once.  The flights' arrays
+// 128256 words 211 us instead of 198, the vector units being busy with it; workgroups of
+// 512 threads: 209; all levels of a walk in one workgroup: 85 instead of 71 us at 32000
+// words.)  Sequences whose walk has ended leave at once.  The flights' arrays
 // alternate by level.
 //
 // Exponentials and sums are fp64: with V borders between tokens on [0, 1), an error
@@ -30,8 +31,9 @@
 // rows of 151936 words 23 us before any walk has ended, of which the instructions alone
 // are 11.  The vector registers (190 for 16-bit logits) leave two waves a SIMD; held to
 // 168 or 128 they spill: a sixth and a half more time for the 128 walks.
-// Whole calls: 40 to 67 us for one walk of 32000 words and up to 8 levels, 63 for 5 of
-// 70001 fp32 words, 198 for 64 of 128256, 316 for 128 of 151936 words and up to 32 levels.
+// Whole calls: 43 to 67 us for one walk of 32000 words and up to 8 levels, 63 to 83 for 5 of
+// 70001 fp32 words, 200 for 64 of 128256, 316 to 365 for 128 of 151936 words and up to 32
+// levels, as far as the walks go.
 #include "graft_internal.h"
 
 namespace graft {

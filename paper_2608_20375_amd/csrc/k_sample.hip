@@ -9,7 +9,7 @@
 //
 // Only the rows on the walk's path are read, but the next row is known only when
 // this one's token is.  So a launch takes one level.  A row's 16-byte vectors are cut
-// into runs of 64 `rep` (one vector a lane; rep is 1 up to 2^19 words), four runs make a
+// into runs of 64 `rep` (one vector a lane; rep is 1 up to 2^19 words of 16 bits, 2^18 of fp32), four runs make a
 // flight, and the flights are dealt to the waves of the sequence's workgroups.  A wave
 // leaves its flight's maximum and the four runs' sums of exponentials over it.  In the
 // next launch one wave of each workgroup combines the level's flights (at most 256, one

@@ -9,18 +9,18 @@
 //
 // Only the rows on the walk's path are read, but the next row is known only when
 // this one's token is.  So a launch takes one level.  A row's 16-byte vectors are cut
-// into runs of 64 `rep` (one vector a lane; rep is 1 up to 2^19 words of 16 bits, 2^18 of fp32), four runs make a
-// flight, and the flights are dealt to the waves of the sequence's workgroups.  A wave
-// leaves its flight's maximum and the four runs' sums of exponentials over it.  In the
-// next launch one wave of each workgroup combines the level's flights (at most 256, one
-// to four a lane), finds the run that holds u S by a scan, reads that run again for the
-// token, looks for the child, and all go on with the child's row.  Every workgroup of a
-// sequence does this by itself and arrives at the same bits, so there is no flag, counter
-// or wait between workgroups.  (Every wave by itself, without a barrier: 64 walks of
-// 128256 words 211 us instead of 198, the vector units being busy with it; workgroups of
-// 512 threads: 209; all levels of a walk in one workgroup: 85 instead of 71 us at 32000
-// words.)  Sequences whose walk has ended leave at once.  The flights' arrays
-// alternate by level.
+// into runs of 64 `rep` (one vector a lane; rep is 1 up to 2^19 words of 16 bits, 2^18 of
+// fp32), four runs make a flight, and the flights are dealt to the waves of the
+// sequence's workgroups.  A wave leaves its flight's maximum and the four runs' sums of
+// exponentials over it.  In the next launch one wave of each workgroup combines the
+// level's flights (at most 256, one to four a lane), finds the run that holds u S by a
+// scan, reads that run again for the token, looks for the child, and all go on with the
+// child's row.  Every workgroup of a sequence does this by itself and arrives at the same
+// bits, so there is no flag, counter or wait between workgroups.  (Every wave by itself,
+// without a barrier: 64 walks of 128256 words 211 us instead of 198, the vector units
+// being busy with it; workgroups of 512 threads: 209; all levels of a walk in one
+// workgroup: 85 instead of 71 us at 32000 words.)  Sequences whose walk has ended leave
+// at once.  The flights' arrays alternate by level.
 //
 // Exponentials and sums are fp64: with V borders between tokens on [0, 1), an error
 // of 1e-7 in the sums would change one draw in a hundred at V = 150000.

@@ -47,10 +47,11 @@
 // of their own whose rows come from all sequences: it is read once for a tile of rows
 // instead of once for every sequence.
 //
-// The running maximum is only moved when some row's new maximum is more than 2^8 above it
+// A row's running maximum is only moved when its new maximum is more than 2^8 above it
 // (in exp2's argument): the sums and rows are fp32 and the probabilities, then up to
 // 2^8, keep their relative precision in 16 bits, while rescaling a row's numbers every
-// time would cost a fifth of the vector work.
+// time would cost a fifth of the vector work.  Each row decides by itself: were a wave's rows
+// to move together, a row's roundings would depend on keys that only its neighbours see.
 #include <algorithm>
 #include <cstddef>
 #include <type_traits>
@@ -329,15 +330,16 @@ __device__ __forceinline__ void softmax_step(Sums<DP> &st, f32x16 (&s)[KT], u32x
 #pragma unroll
     for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[kt][i]);
   mx = half_max(mx);
-  if (__ballot((mx - st.m) * c > kSlack) != 0) {     // -inf on both sides is not above
-    const float to = fmaxf(mx, st.m);
-    const float alpha = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((st.m - to) * c);
+  const bool up = (mx - st.m) * c > kSlack;          // -inf on both sides is not above
+  if (__ballot(up) != 0) {
+    // a row moves by its own maximum alone: the others' factor is 1
+    const float alpha = up ? __builtin_amdgcn_exp2f((st.m - mx) * c) : 1.0f;
     st.l *= alpha;
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
       for (int i = 0; i < 16; ++i) st.o[d][i] *= alpha;
-    st.m = to;
+    st.m = up ? mx : st.m;
   }
   const float off = st.m == -INFINITY ? 0.0f : -st.m * c;
 #pragma unroll
@@ -770,13 +772,13 @@ __device__ __forceinline__ void narrow_part(const AttendArgs &a, const Item &it,
 #pragma unroll
       for (int i = 1; i < 8; ++i) mx = fmaxf(mx, s[q][i / 4][i % 4]);
       mx = quarter_max(mx);
-      if (__ballot((mx - m[q]) * a.c > kSlack) != 0) {     // -inf on both sides is not above
-        const float to = fmaxf(mx, m[q]);
-        const float alpha = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m[q] - to) * a.c);
+      const bool up = (mx - m[q]) * a.c > kSlack;          // as in softmax_step
+      if (__ballot(up) != 0) {
+        const float alpha = up ? __builtin_amdgcn_exp2f((m[q] - mx) * a.c) : 1.0f;
         l[q] *= alpha;
 #pragma unroll
         for (int d = 0; d < kDTiles; ++d) o[q][d] *= alpha;
-        m[q] = to;
+        m[q] = up ? mx : m[q];
       }
       const float off = m[q] == -INFINITY ? 0.0f : -m[q] * a.c;
       float e[8];

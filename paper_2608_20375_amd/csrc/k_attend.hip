@@ -66,7 +66,7 @@ constexpr int kAttWaves = kAttThreads / kWave;
 constexpr int kRowTile = 128, kKeyTile = 64;      // wide_part
 constexpr int kFewRows = 32, kFewKeys = 32;       // narrow_part; keys of one wave's tile
 constexpr int kMaxParts = 64;                     // one a lane of the merge
-constexpr float kSlack = 8.0f;                    // log2 by which a maximum may be passed
+constexpr float kFar = 268435456.0f;              // exp2's argument whose last bit is 16
 constexpr int kOutside = 0x40000000;              // an offset past every buffer's end
 static_assert(kFewKeys * kAttWaves == 2 * kKeyTile, "tiles of both kinds are counted in the plan");
 
@@ -81,8 +81,11 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
+// kSlack: log2 by which a maximum may be passed.  kLift: log2 of a factor on all
+// probabilities and their sums, taken off the lse again.
 struct Bf16 {
   static constexpr uint32_t kExp = 0x7F80u;      // exponent of infinities and NaN
+  static constexpr float kSlack = 8.0f, kLift = 0.0f;
   static __device__ __forceinline__ f32x16 mfma(const u32x4 &a, const u32x4 &b, const f32x16 &c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
                                                    __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -100,6 +103,7 @@ struct Bf16 {
 };
 struct F16 {
   static constexpr uint32_t kExp = 0x7C00u;
+  static constexpr float kSlack = 8.0f, kLift = 0.0f;
   static __device__ __forceinline__ f32x16 mfma(const u32x4 &a, const u32x4 &b, const f32x16 &c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a),
                                                   __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
@@ -136,7 +140,7 @@ struct AttendArgs {
   const uint64_t *mask;
   float *lse;
   float *part_o;          // [parts][batch * slots * q_heads][head_dim], unnormalised
-  f32x2 *part_ml;         // [parts][batch * slots * q_heads] c * maximum, sum
+  f32x2 *part_ml;         // [parts][batch * slots * q_heads] reference, sum
   uint32_t *error_flag;
   int64_t rows_all;       // batch * slots * q_heads
   int32_t batch, slots, root, q_heads, kv_heads, group, dim;
@@ -304,19 +308,54 @@ __device__ __forceinline__ uint64_t seen_word(const AttendArgs &a, int rb, int s
   return have < 64 ? w & ((1ull << (have < 0 ? 0 : have)) - 1) : w;
 }
 
+// What a row's probabilities are relative to: the score m stands for 2^at, a score s for
+// 2^(c s + off), in one multiply-add.  off is rounded, so `at` is not exactly kLift; it is kept
+// with the sums wherever two references meet.  A score too far out for that (its last bit is 16
+// in exp2's argument) gets a power of two as c: then c m is exact, and whatever is below m
+// is nothing beside it, as it is under the true c.
+struct Ref {
+  float c, off, at;
+};
+constexpr float kNoRef = 3.0e38f;    // off without a reference: any score is above it, -inf gives 0
+template <typename T>
+__device__ __forceinline__ Ref ref_of(float m, float c) {
+  const float size = fabsf(m * c);
+  const uint32_t next = (__float_as_uint(c) + 0x7FFFFFu) & 0xFF800000u;         // c's next power
+  const uint32_t e = (__float_as_uint(m) >> 23) & 0xFFu;
+  const uint32_t most = (e < 90u ? 254u : 344u - e) << 23;                      // c |m| < 2^91
+  Ref r;
+  r.c = size >= kFar ? __uint_as_float(next < most ? next : most) : c;
+  r.off = __builtin_fmaf(-m, r.c, T::kLift);
+  // a large off's last bit counts, and fp16 could overflow: at from below
+  const uint32_t below = __float_as_uint(r.off) + (r.off < 0.0f ? 1u : ~0u);
+  r.off = __builtin_fmaf(m, r.c, r.off) > T::kLift + 0.25f ? __uint_as_float(below) : r.off;
+  r.at = __builtin_fmaf(m, r.c, r.off);
+  const bool none = m == -INFINITY;
+  r.off = none ? kNoRef : r.off;
+  r.at = none ? T::kLift : r.at;
+  return r;
+}
+// Factor that takes sums under the reference `from`, whose `at` is given, to `to`, which is `now`.
+__device__ __forceinline__ float factor(float from, float at, float to, const Ref &now, float c) {
+  return from == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((from - to) * c + (now.at - at));
+}
+
 // Running state of 32 rows in a wave.
 template <int DP>
 struct Sums {
   f32x16 o[DP / 32];
   float m, l;                   // m: what the probabilities are relative to
+  float c, off;                 // its ref_of
 
-  __device__ __forceinline__ void clear() {
+  __device__ __forceinline__ void clear(float scale) {
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
     m = -INFINITY;
     l = 0.0f;
+    off = kNoRef;
+    c = scale;
   }
 };
 
@@ -330,23 +369,25 @@ __device__ __forceinline__ void softmax_step(Sums<DP> &st, f32x16 (&s)[KT], u32x
 #pragma unroll
     for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[kt][i]);
   mx = half_max(mx);
-  const bool up = (mx - st.m) * c > kSlack;          // -inf on both sides is not above
+  const bool up = __builtin_fmaf(mx, st.c, st.off) > T::kLift + T::kSlack;
   if (__ballot(up) != 0) {
     // a row moves by its own maximum alone: the others' factor is 1
-    const float alpha = up ? __builtin_amdgcn_exp2f((st.m - mx) * c) : 1.0f;
+    const Ref now = ref_of<T>(up ? mx : st.m, c);
+    const float alpha = up ? factor(st.m, __builtin_fmaf(st.m, st.c, st.off), mx, now, c) : 1.0f;
     st.l *= alpha;
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
       for (int i = 0; i < 16; ++i) st.o[d][i] *= alpha;
     st.m = up ? mx : st.m;
+    st.c = now.c;
+    st.off = now.off;
   }
-  const float off = st.m == -INFINITY ? 0.0f : -st.m * c;
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt) {
     float e[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][i], c, off));
+    for (int i = 0; i < 16; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][i], st.c, st.off));
     float l0 = 0.0f, l1 = 0.0f;
 #pragma unroll
     for (int i = 0; i < 16; i += 2) {
@@ -539,7 +580,7 @@ __device__ __forceinline__ void wide_part(const AttendArgs &a, const Item &it, u
   for (int s = 0; s < kSteps; ++s) settle(rq[s]);
 
   Sums<DP> st;
-  st.clear();
+  st.clear(a.c);
   Walk w{};
   uint64_t seen_next = 0;
   if (t0 < t1) {
@@ -602,7 +643,7 @@ __device__ __forceinline__ void wide_part(const AttendArgs &a, const Item &it, u
     const int at_part = packed ? a.splits + it.part : it.part;
     const int64_t r = (static_cast<int64_t>(rb) * a.slots + slot) * a.q_heads + head;
     const int64_t at = at_part * a.rows_all + r;
-    if (h == 0) a.part_ml[at] = f32x2{t0 < t1 ? st.m * a.c : -INFINITY, st.l};
+    if (h == 0) a.part_ml[at] = f32x2{t0 < t1 ? st.m : -INFINITY, st.l};
     if (t0 >= t1) return;
     float *po = a.part_o + at * a.dim;
 #pragma unroll
@@ -630,7 +671,7 @@ __device__ __forceinline__ void wide_part(const AttendArgs &a, const Item &it, u
     }
   if (a.lse && h == 0)
     a.lse[(static_cast<int64_t>(rb) * a.slots + slot) * a.q_heads + head] =
-        st.l == 0.0f ? -INFINITY : (st.m * a.c + __log2f(st.l)) * 0.69314718055994531f;
+        st.l == 0.0f ? -INFINITY : (st.m * a.c + (__log2f(st.l) - ref_of<T>(st.m, a.c).at)) * 0.69314718055994531f;
 }
 
 // Infinite and NaN values as in add_odd, for the narrow walk's rows.
@@ -755,10 +796,12 @@ __device__ __forceinline__ void narrow_part(const AttendArgs &a, const Item &it,
 
   f32x4 o[QT][kDTiles];
   float m[QT], l[QT];
+  Ref ref[QT];                  // of m
 #pragma unroll
   for (int q = 0; q < QT; ++q) {
     m[q] = -INFINITY;
     l[q] = 0.0f;
+    ref[q] = ref_of<T>(m[q], a.c);
 #pragma unroll
     for (int d = 0; d < kDTiles; ++d) o[q][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
@@ -772,18 +815,19 @@ __device__ __forceinline__ void narrow_part(const AttendArgs &a, const Item &it,
 #pragma unroll
       for (int i = 1; i < 8; ++i) mx = fmaxf(mx, s[q][i / 4][i % 4]);
       mx = quarter_max(mx);
-      const bool up = (mx - m[q]) * a.c > kSlack;          // as in softmax_step
+      const bool up = __builtin_fmaf(mx, ref[q].c, ref[q].off) > T::kLift + T::kSlack;   // as in softmax_step
       if (__ballot(up) != 0) {
-        const float alpha = up ? __builtin_amdgcn_exp2f((m[q] - mx) * a.c) : 1.0f;
+        const Ref now = ref_of<T>(up ? mx : m[q], a.c);
+        const float alpha = up ? factor(m[q], ref[q].at, mx, now, a.c) : 1.0f;
         l[q] *= alpha;
 #pragma unroll
         for (int d = 0; d < kDTiles; ++d) o[q][d] *= alpha;
         m[q] = up ? mx : m[q];
+        ref[q] = now;
       }
-      const float off = m[q] == -INFINITY ? 0.0f : -m[q] * a.c;
       float e[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[q][i / 4][i % 4], a.c, off));
+      for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[q][i / 4][i % 4], ref[q].c, ref[q].off));
       l[q] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
       p[q] = u32x4{T::pack(e[0], e[1]), T::pack(e[2], e[3]), T::pack(e[4], e[5]), T::pack(e[6], e[7])};
     }
@@ -933,26 +977,28 @@ __device__ __forceinline__ void narrow_part(const AttendArgs &a, const Item &it,
       float top = s_m[r];
 #pragma unroll
       for (int i = 1; i < kAttWaves; ++i) top = fmaxf(top, s_m[i * 16 + r]);
+      const Ref now = ref_of<T>(top, a.c);
       f32x4 sum{0.0f, 0.0f, 0.0f, 0.0f};
       float total = 0.0f;
 #pragma unroll
       for (int i = 0; i < kAttWaves; ++i) {
         const float mi = s_m[i * 16 + r];
-        const float f = mi == top ? 1.0f : __builtin_amdgcn_exp2f((mi - top) * a.c);
+        const float f = mi == top ? 1.0f : factor(mi, ref_of<T>(mi, a.c).at, top, now, a.c);
         total += s_l[i * 16 + r] * f;
         sum += *reinterpret_cast<const f32x4 *>(s_o + (i * 16 + r) * kPad + x) * f;
       }
       const int64_t all = (static_cast<int64_t>(rb) * a.slots + slot) * a.q_heads + head;
       if (!alone) {
         const int64_t at = (packed ? a.splits + it.part : it.part) * a.rows_all + all;
-        if (x == 0) a.part_ml[at] = f32x2{t0 < t1 ? top * a.c : -INFINITY, total};
+        if (x == 0) a.part_ml[at] = f32x2{t0 < t1 ? top : -INFINITY, total};
         if (t0 < t1) *reinterpret_cast<f32x4 *>(a.part_o + at * a.dim + x) = sum;
       } else {
         const float inv = total > 0.0f || total != total ? 1.0f / total : 0.0f;
         *reinterpret_cast<u32x2 *>(a.out + rb * a.o_batch + slot * a.o_slot + head * a.o_head + 2 * x) =
             u32x2{T::pack(sum.x * inv, sum.y * inv), T::pack(sum.z * inv, sum.w * inv)};
         if (a.lse && x == 0)
-          a.lse[all] = total == 0.0f ? -INFINITY : (top * a.c + __log2f(total)) * 0.69314718055994531f;
+          a.lse[all] =
+              total == 0.0f ? -INFINITY : (top * a.c + (__log2f(total) - now.at)) * 0.69314718055994531f;
       }
     }
   }
@@ -1016,8 +1062,9 @@ merge_parts_kernel(AttendArgs a) {
   float top = ml.x;
 #pragma unroll
   for (int k = 1; k < kWave; k <<= 1) top = fmaxf(top, __uint_as_float(xor_lane(__float_as_uint(top), k)));
-  const float off = top == -INFINITY ? 0.0f : top;
-  const float w = __builtin_amdgcn_exp2f(ml.x - off);      // 0 for a part without keys
+  // 0 for a part without keys
+  const Ref now = ref_of<T>(top, a.c);
+  const float w = ml.x == top && top != -INFINITY ? 1.0f : factor(ml.x, ref_of<T>(ml.x, a.c).at, top, now, a.c);
   float l = w * ml.y;
 #pragma unroll
   for (int k = 1; k < kWave; k <<= 1) l += __uint_as_float(xor_lane(__float_as_uint(l), k));
@@ -1035,7 +1082,8 @@ merge_parts_kernel(AttendArgs a) {
     *reinterpret_cast<uint32_t *>(a.out + b * a.o_batch + slot * a.o_slot + head * a.o_head + lane * 4) =
         T::pack(x * inv, y * inv);
   }
-  if (a.lse && lane == 0) a.lse[r] = l == 0.0f ? -INFINITY : (off + __log2f(l)) * 0.69314718055994531f;
+  if (a.lse && lane == 0)
+    a.lse[r] = l == 0.0f ? -INFINITY : (top * a.c + (__log2f(l) - now.at)) * 0.69314718055994531f;
 }
 
 // rows: extent along the row stride; a stride that one row does not need is the row's own

@@ -350,7 +350,8 @@ typedef struct {
  * Rows of k, v, the cache and the shared prefix are at least head_dim and at most
  * 2^22 elements apart (scales at most 2^22 bytes).
  * Sums and softmax statistics are fp32; the probabilities are rounded to dtype
- * for the product with v.  The result is the same bits for the same arguments.
+ * for the product with v (fp16: to 11 bits down to 2^-26 of the row's largest so far,
+ * below that to a multiple of 2^-36 of it).  The result is the same bits for the same arguments.
  * Plane strides are ignored. */
 typedef struct {
     int32_t batch;               /* 1..max_batch */

@@ -1,5 +1,6 @@
-"""Context.tree_attention at the ends of its numbers' range: scores far past what a 32-bit
-exponent's argument holds."""
+"""Context.tree_attention at the ends of its numbers' range: many small probabilities beside a
+dominant one, and scores far past what a 32-bit exponent's argument holds."""
+import math
 import os
 import sys
 
@@ -9,9 +10,33 @@ torch = pytest.importorskip("torch")
 
 sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
 import verifier_ref as R  # noqa: E402
-from test_tree_attention_gpu import call, context, make  # noqa: E402
+from test_tree_attention_gpu import call, check, context, make  # noqa: E402
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("below", [20.0, 24.4, 25.4, 25.9])
+@pytest.mark.parametrize("nodes", [0, 40])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+def test_many_small_probabilities(below, nodes, dtype):
+    """Ten keys that take nearly all of the probability, with values of 0, among 24000 whose
+    probabilities are 2^-below of theirs: the result is those keys' sum, and each of them has to
+    keep the relative precision that verifier_ref.attention counts."""
+    print("small probabilities", below, nodes, dtype, flush=True)
+    c = make(1, nodes, [24000], 0, 1, 1, 64, dtype, False, 1, chain=True, n=[nodes])
+    g = torch.Generator().manual_seed(7)
+    c["q"].fill_(1.0)
+    c["k"].zero_()
+    c["v"].zero_()
+    keys, values = c["cache"]
+    keys.copy_(torch.randn(keys.shape, generator=g) * 0.02)
+    values.copy_(torch.randn(values.shape, generator=g) + 8.0)
+    keys[:, ::2400] = below * math.log(2.0) / (64 * 0.125)
+    values[:, ::2400] = 0.0
+    ctx = context(c)
+    out, lse, _ = call(ctx, c)
+    check(c, out, lse)
+    ctx.close()
 
 
 @pytest.mark.parametrize("kind,power", [(k, p) for k in ("bfloat16", "e4m3") for p in (4, 20, 26, 30, 40, 100)]

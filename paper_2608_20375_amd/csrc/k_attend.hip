@@ -61,6 +61,8 @@
 
 #include "graft_internal.h"
 
+#include "attend_tiles.h"
+
 namespace graft {
 namespace {
 
@@ -162,23 +164,9 @@ __device__ __forceinline__ int slots_of(const AttendArgs &a, int b, bool *bad) {
   return (n < 0 ? 0 : (n > most ? most : n)) + a.root;
 }
 
-// Tiles of a sequence's keys: the shared prefix's (where it has no pass of its own), the
-// cache's, the block's; and how many a part takes.  The walks and the merge agree on it.
-struct Tiles {
-  int n0, n1, n2, per;
-  __device__ __forceinline__ int all() const { return n0 + n1 + n2; }
-};
 __device__ __forceinline__ Tiles tiles_of(const AttendArgs &a, bool packed, int len, int live) {
-  const int k = a.tile_keys;
-  Tiles t;
-  t.n0 = packed || a.shared_items == 0 ? (a.shared_len + k - 1) / k : 0;
-  t.n1 = (len + k - 1) / k;
-  t.n2 = (live + k - 1) / k;
-  const int splits = packed ? a.shared_splits : a.splits;
-  const int rounds = (t.all() + a.turns - 1) / a.turns;
-  const int per = (rounds + splits - 1) / splits;
-  t.per = (per < a.min_tiles ? a.min_tiles : per) * a.turns;
-  return t;
+  const int shared = packed || a.shared_items == 0 ? a.shared_len : 0;
+  return cut_tiles(shared, len, live, a.tile_keys, a.turns, packed ? a.shared_splits : a.splits, a.min_tiles);
 }
 __device__ __forceinline__ int len_of(const AttendArgs &a, int b, bool *bad) {
   if (a.cache_rows == 0) return 0;
@@ -252,18 +240,20 @@ struct Walk {
   int source, left, tile;       // keys from the tile's first on; tile's number in the source
 };
 
-__device__ __forceinline__ void enter(Walk &w, int source, int tile, int keys,
-                                      int count, int b, int kvh) {
+// To tile t of the walk; b's cache has c1 rows, its block c2 slots.
+__device__ __forceinline__ void seek(Walk &w, const Tiles &n, int t, int keys, int c0, int c1, int c2, int b,
+                                     int kvh) {
+  const Spot at = spot_of(n, t, keys, c0, c1, c2);
   // Read from the kernel's argument memory where it is needed (sources come first there):
   // kept in registers over the walk's loop, the three would push out what the loop uses.
   typedef const __attribute__((address_space(4))) Source *Arguments;
   static_assert(offsetof(AttendArgs, src) == 0, "the sources are the first argument");
-  Arguments s = (Arguments)__builtin_amdgcn_kernarg_segment_ptr() + source;
+  Arguments s = (Arguments)__builtin_amdgcn_kernarg_segment_ptr() + at.source;
   asm volatile("" : "+s"(s));
-  const int64_t base = source == 0 ? 0 : b, first = static_cast<int64_t>(tile) * keys;
-  w.source = source;
-  w.tile = tile;
-  w.left = count - tile * keys;
+  const int64_t base = at.source == 0 ? 0 : b, first = static_cast<int64_t>(at.tile) * keys;
+  w.source = at.source;
+  w.tile = at.tile;
+  w.left = at.left;
   w.k_row = s->k.row;
   w.v_row = s->v.row;
   w.ks_row = s->k.s_row;
@@ -272,14 +262,6 @@ __device__ __forceinline__ void enter(Walk &w, int source, int tile, int keys,
   w.v = s->v.p + base * s->v.batch + kvh * s->v.head + first * s->v.row;
   w.ks = s->k.s + base * s->k.s_batch + kvh * s->k.s_head + first * s->k.s_row;
   w.vs = s->v.s + base * s->v.s_batch + kvh * s->v.s_head + first * s->v.s_row;
-}
-
-// Tile t of the walk whose sources have n0, n1, ... tiles of `keys` keys, c0, c1, c2 keys.
-__device__ __forceinline__ void seek(Walk &w, int t, int keys, int n0, int n1, int c0,
-                                     int c1, int c2, int b, int kvh) {
-  if (t < n0) enter(w, 0, t, keys, c0, b, kvh);
-  else if (t < n0 + n1) enter(w, 1, t - n0, keys, c1, b, kvh);
-  else enter(w, 2, t - n0 - n1, keys, c2, b, kvh);
 }
 // n tiles on in the same source.
 __device__ __forceinline__ void advance(Walk &w, int n, int keys) {
@@ -502,10 +484,9 @@ __device__ __forceinline__ void wide_part(const AttendArgs &a, const Item &it, u
   const int len = packed ? 0 : __builtin_amdgcn_readfirstlane(len_of(a, b, &bad));
   if (bad && speaks) atomicOr(a.error_flag, kErrBlockSizes);
   const Tiles n = tiles_of(a, packed, len, live);
-  const int n0 = n.n0, n1 = n.n1, n_tiles = n.all(), per = n.per;
-  const int t0 = it.part * per < n_tiles ? it.part * per : n_tiles;
-  const int t1 = t0 + per < n_tiles ? t0 + per : n_tiles;
-  const bool alone = a.shared_items == 0 && per >= n_tiles;   // the only part: no merge
+  const Part part = part_of(n, it.part);
+  const int t0 = part.first, t1 = part.last;
+  const bool alone = a.shared_items == 0 && n.per >= n.all();   // the only part: no merge
   if (alone && it.part > 0) return;
 
   // a thread's share of a tile: chunk ch of rows r0, r0 + kStep, ...; of codes, 16 of rows
@@ -515,10 +496,11 @@ __device__ __forceinline__ void wide_part(const AttendArgs &a, const Item &it, u
   u32x4 rk[kUnits], rv[kUnits];
   uint32_t sk[kUnits / 2], sv[kUnits / 2];
   auto load = [&](const Walk &w) {
-    const int n = w.left < kKeyTile ? w.left : kKeyTile;
     if (Q8 && w.source != 2) {
-      const auto bk = buffer(w.k, (n - 1) * w.k_row + a.dim), bv = buffer(w.v, (n - 1) * w.v_row + a.dim);
-      const auto bks = buffer(w.ks, (n - 1) * w.ks_row + 1), bvs = buffer(w.vs, (n - 1) * w.vs_row + 1);
+      const auto bk = buffer(w.k, extent(w.left, kKeyTile, w.k_row, a.dim));
+      const auto bv = buffer(w.v, extent(w.left, kKeyTile, w.v_row, a.dim));
+      const auto bks = buffer(w.ks, extent(w.left, kKeyTile, w.ks_row, 1));
+      const auto bvs = buffer(w.vs, extent(w.left, kKeyTile, w.vs_row, 1));
 #pragma unroll
       for (int i = 0; i < kUnits / 2; ++i) {
         const int r = q0 + i * 2 * kStep;
@@ -532,7 +514,8 @@ __device__ __forceinline__ void wide_part(const AttendArgs &a, const Item &it, u
         sv[i] = __builtin_amdgcn_raw_buffer_load_b8(bvs, r * w.vs_row, 0, 0);
       }
     } else {
-      const auto bk = buffer(w.k, (n - 1) * w.k_row + 2 * a.dim), bv = buffer(w.v, (n - 1) * w.v_row + 2 * a.dim);
+      const auto bk = buffer(w.k, extent(w.left, kKeyTile, w.k_row, 2 * a.dim));
+      const auto bv = buffer(w.v, extent(w.left, kKeyTile, w.v_row, 2 * a.dim));
 #pragma unroll
       for (int i = 0; i < kUnits; ++i) rk[i] = load16(bk, (r0 + i * kStep) * w.k_row + at16);
 #pragma unroll
@@ -588,7 +571,7 @@ __device__ __forceinline__ void wide_part(const AttendArgs &a, const Item &it, u
   Walk w{};
   uint64_t seen_next = 0;
   if (t0 < t1) {
-    seek(w, t0, kKeyTile, n0, n1, a.shared_len, len, live, b, kvh);
+    seek(w, n, t0, kKeyTile, a.shared_len, len, live, b, kvh);
     load(w);
     if (w.source == 2) seen_next = seen_word(a, rb, slot, w.tile, live);
   }
@@ -601,7 +584,7 @@ __device__ __forceinline__ void wide_part(const AttendArgs &a, const Item &it, u
     const bool odd = store(source, buf);
     if (t + 1 < t1) {
       if (w.left > kKeyTile) advance(w, 1, kKeyTile);
-      else seek(w, t + 1, kKeyTile, n0, n1, a.shared_len, len, live, b, kvh);
+      else seek(w, n, t + 1, kKeyTile, a.shared_len, len, live, b, kvh);
       load(w);
       if (w.source == 2) seen_next = seen_word(a, rb, slot, w.tile, live);
     }
@@ -741,10 +724,9 @@ __device__ __forceinline__ void narrow_part(const AttendArgs &a, const Item &it,
 
   // a part's tiles, in rounds of one tile a wave
   const Tiles n = tiles_of(a, packed, len, live);
-  const int n0 = n.n0, n1 = n.n1, n_tiles = n.all(), per = n.per;
-  const int t0 = it.part * per < n_tiles ? it.part * per : n_tiles;
-  const int t1 = t0 + per < n_tiles ? t0 + per : n_tiles;
-  const bool alone = a.shared_items == 0 && per >= n_tiles;   // the only part: no merge
+  const Part part = part_of(n, it.part);
+  const int t0 = part.first, t1 = part.last;
+  const bool alone = a.shared_items == 0 && n.per >= n.all();   // the only part: no merge
   if (alone && it.part > 0) return;
 
   // Contracted entries 8 of a step are chunk k_chunk(step) of a row: the 16 codes that one
@@ -776,9 +758,9 @@ __device__ __forceinline__ void narrow_part(const AttendArgs &a, const Item &it,
   };
   auto load = [&](Held &x, const Walk &w) {
     x.left = w.left;
-    const int n = w.left < kFewKeys ? w.left : kFewKeys;
     constexpr int kBytes = Q8 ? 1 : 2;
-    const auto bk = buffer(w.k, (n - 1) * w.k_row + kBytes * a.dim), bv = buffer(w.v, (n - 1) * w.v_row + kBytes * a.dim);
+    const auto bk = buffer(w.k, extent(w.left, kFewKeys, w.k_row, kBytes * a.dim));
+    const auto bv = buffer(w.v, extent(w.left, kFewKeys, w.v_row, kBytes * a.dim));
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -792,7 +774,8 @@ __device__ __forceinline__ void narrow_part(const AttendArgs &a, const Item &it,
       x.rv[i] = load16(bv, r * w.v_row + (Q8 ? at8 : at16));
     }
     if (Q8) {
-      const auto bks = buffer(w.ks, (n - 1) * w.ks_row + 1), bvs = buffer(w.vs, (n - 1) * w.vs_row + 1);
+      const auto bks = buffer(w.ks, extent(w.left, kFewKeys, w.ks_row, 1));
+      const auto bvs = buffer(w.vs, extent(w.left, kFewKeys, w.vs_row, 1));
       x.sk = __builtin_amdgcn_raw_buffer_load_b8(bks, (lane & 31) * w.ks_row, 0, 0);
       x.sv = __builtin_amdgcn_raw_buffer_load_b8(bvs, (lane & 31) * w.vs_row, 0, 0);
     }
@@ -857,12 +840,12 @@ __device__ __forceinline__ void narrow_part(const AttendArgs &a, const Item &it,
   // the prefix's tiles, the next one on its way (two: no faster, and 60 to 90 registers more)
   Walk w{};
   int t = t0 + wave;
-  const int t_end = t1 < n0 + n1 ? t1 : n0 + n1;
+  const int prefix = n.n0 + n.n1, t_end = t1 < prefix ? t1 : prefix;
   int ahead = t;                                        // the walk's tile
   auto fetch = [&](Held &x) {
     if (ahead >= t_end) return;
     if (ahead == t0 + wave || w.left <= kAttWaves * kFewKeys)
-      seek(w, ahead, kFewKeys, n0, n1, a.shared_len, len, live, b, kvh);
+      seek(w, n, ahead, kFewKeys, a.shared_len, len, live, b, kvh);
     else
       advance(w, kAttWaves, kFewKeys);
     load(x, w);
@@ -923,9 +906,10 @@ __device__ __forceinline__ void narrow_part(const AttendArgs &a, const Item &it,
   fetch(held);
   while (t < t_end) step(held);
   // the block: at most 32 slots, one tile, by the wave whose turn it is
-  if (t == n0 + n1 && t < t1) {
-    seek(w, t, kFewKeys, n0, n1, a.shared_len, len, live, b, kvh);
-    const auto bk = buffer(w.k, (live - 1) * w.k_row + 2 * a.dim), bv = buffer(w.v, (live - 1) * w.v_row + 2 * a.dim);
+  if (t == prefix && t < t1) {
+    seek(w, n, t, kFewKeys, a.shared_len, len, live, b, kvh);
+    const auto bk = buffer(w.k, extent(live, kFewKeys, w.k_row, 2 * a.dim));
+    const auto bv = buffer(w.v, extent(live, kFewKeys, w.v_row, 2 * a.dim));
     f32x4 s[QT][2];
 #pragma unroll
     for (int q = 0; q < QT; ++q) s[q][0] = s[q][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};

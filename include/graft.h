@@ -371,7 +371,8 @@ typedef struct {
     const int32_t *cache_len;    /* [batch] (ignored when cache_rows is 0) */
     graft_rows shared_k, shared_v; /* [shared_len, kv_heads, head_dim]; shared_len 0: none */
     int32_t shared_len;
-    graft_rows out;              /* [batch, slots, q_heads, head_dim]; no overlap with inputs */
+    graft_rows out;              /* [batch, slots, q_heads, head_dim]; no overlap with inputs or
+                                    of its rows */
     float *lse;                  /* [batch, slots, q_heads] or NULL */
     void *workspace;             /* 16-byte aligned, graft_tree_attention_workspace bytes */
     int64_t workspace_bytes;
@@ -468,7 +469,8 @@ typedef struct {
  * value is finite in fp32 and exact in bf16.
  * Rows whose source row is outside 0 .. src_rows - 1 or whose cache row is
  * outside 0 .. dst_rows - 1 are skipped and reported by graft_get_device_status.
- * src and dst must not overlap.  At most 2^30 rows and 2^28 planes or heads. */
+ * src and dst must not overlap, nor dst's rows (or scales) each other: a stride of dst below
+ * head_dim is refused.  At most 2^30 rows and 2^28 planes or heads. */
 GRAFT_API int graft_cache_write(graft_ctx *ctx, const graft_cache_move *m /* host */,
                                 graft_stream_t stream);
 

@@ -340,6 +340,20 @@ def _rows(t, n, name):
     return Rows(*at, t.scales.data_ptr(), *lead, *[s[i] if e[i] > 1 else 0 for i in range(n)])
 
 
+def _apart(t, name):
+    """Raises unless every number of a tensor or QuantRows that is written has a place of its own:
+    in the order of their size, each stride passes what the smaller ones span."""
+    for x in (t.codes, t.scales) if isinstance(t, QuantRows) else (t,):
+        if x.is_contiguous():
+            continue
+        span = 1
+        for stride, n in sorted((a, b) for a, b in zip(x.stride(), x.shape) if b > 1):
+            if stride < span:
+                raise ValueError("%s is written and must not overlap itself (strides %s of %s)"
+                                 % (name, list(x.stride()), list(x.shape)))
+            span += stride * (n - 1)
+
+
 class TreeBuffers:
     """Preallocated outputs of one build_tree call (torch tensors on the device)."""
 
@@ -795,6 +809,8 @@ class Context:
             _need(v, "v", B, S, H, D)
         if out is not None and not (isinstance(out, torch.Tensor) and out.shape == shape):
             _need(out, "out", B, S, Hq, D)
+        if out is not None:
+            _apart(out, "out")
         if n_nodes is None:
             raise ValueError("n_nodes is required")
         if q.dtype not in (torch.bfloat16, torch.float16):
@@ -914,6 +930,7 @@ class Context:
             if s[0] != P or s[1] < batch or s[3] != H or s[4] != D:
                 raise ValueError("%s must be [%d, >=%d, rows, %d, %d], got %s"
                                  % (name, P, batch, H, D, list(s)))
+        _apart(dst, "dst")
         i32, one = torch.int32, (batch,)
         entries = rows.shape[1] if isinstance(rows, torch.Tensor) and rows.dim() == 2 else 0
         p_n, p_start, p_list = self._args(

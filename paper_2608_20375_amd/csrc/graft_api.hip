@@ -205,6 +205,19 @@ int check_rows(const graft_rows &r, int dtype, bool pointers, const char *who, c
   return GRAFT_OK;
 }
 
+// Rows that are written: no two at one place by a stride that repeats them (an expanded
+// tensor's) or that is shorter than a row.  entries: of plane, batch, row and head.
+int check_written(const graft_rows &r, int dtype, const int64_t (&entries)[4], int dim, const char *who,
+                  const char *name) {
+  const int rc = check_rows(r, dtype, true, who, name);
+  if (rc != GRAFT_OK) return rc;
+  const int64_t v[4] = {r.plane_stride, r.batch_stride, r.row_stride, r.head_stride};
+  for (int i = 0; i < 4; ++i)
+    if (entries[i] > 1 && v[i] < dim)
+      return fail(GRAFT_ERR_INVALID_ARG, "%s: %s's rows overlap", who, name);
+  return GRAFT_OK;
+}
+
 // Rows of keys or values that the attention walks: side by side, a tile of 64 of them
 // within 31-bit offsets.
 int check_walked(const graft_rows &r, int dtype, int rows, int dim, const char *who, const char *name) {
@@ -251,7 +264,8 @@ int check_attention(const graft_ctx *ctx, const graft_attention *a, bool pointer
   int rc = check_rows(a->q, a->dtype, true, who, "q");
   if (rc == GRAFT_OK) rc = check_walked(a->k, a->dtype, a->slots, a->head_dim, who, "k");
   if (rc == GRAFT_OK) rc = check_walked(a->v, a->dtype, a->slots, a->head_dim, who, "v");
-  if (rc == GRAFT_OK) rc = check_rows(a->out, a->dtype, true, who, "out");
+  if (rc == GRAFT_OK)
+    rc = check_written(a->out, a->dtype, {1, a->batch, a->slots, a->q_heads}, a->head_dim, who, "out");
   if (rc == GRAFT_OK && a->cache_rows > 0) {
     if (!a->cache_len) return fail(GRAFT_ERR_INVALID_ARG, "%s: a cache needs cache_len", who);
     rc = check_walked(a->cache_k, a->cache_dtype, a->cache_rows, a->head_dim, who, "cache_k");
@@ -275,7 +289,8 @@ int check_move(const graft_ctx *ctx, const graft_cache_move *m, const char *who)
     return fail(GRAFT_ERR_INVALID_ARG, "%s: head_dim %d must be a multiple of 16", who, m->head_dim);
   if (m->head_dim > 128) return fail(GRAFT_ERR_UNSUPPORTED, "%s: head_dim %d > 128", who, m->head_dim);
   int rc = check_rows(m->src, m->src_dtype, true, who, "src");
-  if (rc == GRAFT_OK) rc = check_rows(m->dst, m->dst_dtype, true, who, "dst");
+  if (rc == GRAFT_OK)
+    rc = check_written(m->dst, m->dst_dtype, {m->n_planes, m->batch, m->dst_rows, m->heads}, m->head_dim, who, "dst");
   if (rc != GRAFT_OK) return rc;
   // row numbers of a workgroup's last rows stay below 2^31, the products below 2^63
   if (m->src_rows > (1 << 30) || m->dst_rows > (1 << 30) || m->list_len > (1 << 30) ||

@@ -1,0 +1,83 @@
+"""More refusals of the verifier-side operators, on the CPU, by test_verifier_step_cpu's stand-ins for
+a context."""
+import ctypes as C
+import os
+import sys
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+import paper_2608_20375_amd as G  # noqa: E402
+from test_verifier_step_cpu import NO_GPU, Fake, attention, context, move, rows  # noqa: E402
+
+pytestmark = pytest.mark.skipif(torch.cuda.is_available(), reason="stands in for a context")
+
+
+def bf(*s):
+    return torch.zeros(*s, dtype=torch.bfloat16)
+
+
+def i32(*s):
+    return torch.zeros(*s, dtype=torch.int32)
+
+
+def quant(*s):
+    return G.QuantRows(torch.zeros(s, dtype=torch.uint8), torch.zeros(s[:-1], dtype=torch.uint8))
+
+
+def block(**kw):
+    a = dict(q=bf(2, 8, 4, 64), k=bf(2, 8, 2, 64), v=bf(2, 8, 2, 64), n_nodes=i32(2),
+             mask=torch.zeros(2, 32, 1, dtype=torch.int64), cache=(bf(2, 9, 2, 64), bf(2, 9, 2, 64)),
+             cache_len=i32(2), shared=(bf(5, 2, 64), bf(5, 2, 64)), with_root=True)
+    a.update(kw)
+    return a
+
+
+def test_entry_points_refuse_rows_written_twice():
+    L, f = G.lib(), Fake()
+    attend = lambda **kw: L.graft_tree_attention(f.h, C.byref(attention(**kw)), None)
+    write = lambda **kw: L.graft_cache_write(f.h, C.byref(move(**kw)), None)
+    back = dict(src_dtype=3, dst_dtype=1, src=rows(True), dst=rows(), list=0, list_len=0, with_root=0)
+    read = lambda **kw: L.graft_cache_read(f.h, C.byref(move(**dict(back, **kw))), None)
+    for name in ("batch_stride", "row_stride", "head_stride"):
+        for stride in (0, 16, 48):
+            assert attend(out=rows(**{name: stride})) == 1, (name, stride)
+    assert attend(out=rows(plane_stride=0)) == NO_GPU            # not used
+    assert attend(out=rows(batch_stride=0), batch=1) == NO_GPU   # one entry
+    for name in ("plane_stride", "batch_stride", "row_stride", "head_stride"):
+        for stride in (0, 16, 48):
+            assert write(dst=rows(True, **{name: stride})) == 1, (name, stride)
+            assert write(dst_dtype=1, dst=rows(**{name: stride})) == 1, (name, stride)
+            assert read(dst=rows(**{name: stride})) == 1, (name, stride)
+            # what is read may repeat
+            assert write(src=rows(**{name: stride})) == NO_GPU, (name, stride)
+    assert write(dst=rows(True, plane_stride=0), n_planes=1) == NO_GPU
+
+
+def test_binding_refuses_tensors_written_twice():
+    ctx = context()
+    for out in (bf(1, 8, 4, 64).expand(2, 8, 4, 64), bf(2, 1, 4, 64).expand(2, 8, 4, 64),
+                bf(2, 8, 1, 64).expand(2, 8, 4, 64), bf(2, 8, 4, 1).expand(2, 8, 4, 64),
+                bf(4096).as_strided((2, 8, 4, 64), (1024, 128, 64, 1))):
+        with pytest.raises(ValueError, match="overlap"):
+            ctx.tree_attention(**block(out=out))
+    w = dict(dst=quant(3, 2, 20, 2, 64), src=bf(3, 2, 9, 2, 64), n_rows=i32(2), rows=i32(2, 4), start=i32(2))
+    codes, scales = w["dst"].codes, w["dst"].scales
+    for dst in (G.QuantRows(codes[:1].expand(3, -1, -1, -1, -1), scales),
+                G.QuantRows(codes, scales[:, :1].expand(-1, 2, -1, -1)),
+                G.QuantRows(codes, scales.flatten().as_strided((3, 2, 20, 2), (80, 40, 1, 1))),
+                bf(3, 1, 20, 2, 64).expand(3, 2, 20, 2, 64), bf(3, 2, 1, 2, 64).expand(3, 2, 20, 2, 64)):
+        with pytest.raises(ValueError, match="overlap"):
+            ctx.cache_write(**{**w, "dst": dst})
+    with pytest.raises(ValueError, match="overlap"):
+        ctx.cache_read(quant(3, 2, 20, 2, 64), i32(2), out=bf(1, 2, 20, 2, 64).expand(3, 2, 20, 2, 64))
+    # views without overlap, and tensors that are read, pass on to the device's check
+    with pytest.raises(TypeError, match="CUDA"):
+        ctx.tree_attention(**block(out=bf(2, 8, 4, 80)[..., :64]))
+    with pytest.raises(TypeError, match="CUDA"):
+        ctx.tree_attention(**block(out=bf(2, 4, 8, 64).transpose(1, 2), q=bf(1, 8, 4, 64).expand(2, 8, 4, 64)))
+    with pytest.raises(TypeError, match="CUDA"):
+        ctx.cache_write(**{**w, "dst": G.QuantRows(quant(3, 2, 2, 20, 64).codes.transpose(2, 3),
+                                                   quant(3, 2, 2, 20, 64).scales.transpose(2, 3))})

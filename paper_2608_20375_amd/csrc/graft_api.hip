@@ -225,7 +225,7 @@ int check_walked(const graft_rows &r, int dtype, int rows, int dim, const char *
   if (rc != GRAFT_OK || rows <= 1) return rc;
   if (r.row_stride < dim)
     return fail(GRAFT_ERR_INVALID_ARG, "%s: %s's rows overlap", who, name);
-  if (r.row_stride > (1 << 22) || r.scale_row_stride > (1 << 22))
+  if (r.row_stride > (1 << 22) || (dtype == GRAFT_E4M3 && r.scale_row_stride > (1 << 22)))
     return fail(GRAFT_ERR_UNSUPPORTED, "%s: %s's rows are more than 2^22 elements apart", who, name);
   return GRAFT_OK;
 }

@@ -56,6 +56,19 @@ def test_entry_points_refuse_rows_written_twice():
     assert write(dst=rows(True, plane_stride=0), n_planes=1) == NO_GPU
 
 
+def test_scale_strides_of_other_types_are_ignored():
+    L, f = G.lib(), Fake()
+    attend = lambda **kw: L.graft_tree_attention(f.h, C.byref(attention(**kw)), None)
+    for stride in (1 << 40, -1):
+        far = rows(scale_row_stride=stride, scale_head_stride=stride, scale_batch_stride=stride)
+        for name in ("q", "k", "v", "cache_k", "cache_v", "shared_k", "shared_v", "out"):
+            assert attend(**{name: far}) == NO_GPU, (name, stride)
+    codes = dict(cache_dtype=3, cache_k=rows(True), cache_v=rows(True), shared_k=rows(True), shared_v=rows(True))
+    for name in ("cache_k", "cache_v", "shared_k", "shared_v"):
+        assert attend(**{**codes, name: rows(True, scale_row_stride=(1 << 22) + 1)}) == 2, name
+        assert attend(**{**codes, name: rows(True, scale_row_stride=1 << 22)}) == NO_GPU, name
+
+
 def test_binding_refuses_tensors_written_twice():
     ctx = context()
     for out in (bf(1, 8, 4, 64).expand(2, 8, 4, 64), bf(2, 1, 4, 64).expand(2, 8, 4, 64),

@@ -255,10 +255,20 @@ def _plain(t, dtype, shape):
     return -1
 
 
+_INT32_MAX = 2 ** 31 - 1
+
+
+def _fits(n, name):
+    """n, which the library takes as a 32-bit number: ctypes would drop the bits above."""
+    if n > _INT32_MAX:
+        raise ValueError("%s has an extent of %d, past 2^31 - 1" % (name, n))
+    return n
+
+
 def _batch_of(t, name):
     if not isinstance(t, torch.Tensor) or t.dim() < 1:
         raise ValueError("%s must be a tensor whose first extent is the batch" % name)
-    return int(t.shape[0])
+    return _fits(int(t.shape[0]), name)
 
 
 def _stream():
@@ -734,7 +744,7 @@ class Context:
             quant, s = isinstance(x, QuantRows), x.shape
             if (len(s) == n + 2 and s[-1] == dim and s[-2] == heads and (n == 1 or s[0] >= lead[0])
                     and (quant or (x.dtype is dtype and y.dtype is dtype))):
-                return s[n - 1], quant
+                return _fits(s[n - 1], name), quant
         kinds = set()
         for t in pair:
             if not isinstance(t, (torch.Tensor, QuantRows)):
@@ -750,7 +760,7 @@ class Context:
             kinds.add(quant)
         if len(kinds) != 1 or pair[0].shape[len(lead) - 1] != pair[1].shape[len(lead) - 1]:
             raise ValueError("%s: keys and values must agree in type and rows" % name)
-        return pair[0].shape[len(lead) - 1], kinds.pop()
+        return _fits(pair[0].shape[len(lead) - 1], name), kinds.pop()
 
     def tree_attention(self, q, k, v, n_nodes, mask=None, cache=None, cache_len=None, shared=None,
                        scale=None, with_root=False, out=None, lse=None, workspace=None):
@@ -803,6 +813,8 @@ class Context:
         shape = q.shape
         B, S, Hq, D = shape
         H, N = k.shape[2], self.dims.max_nodes
+        _fits(max(shape), "q")
+        _fits(H, "k")
         W = (N + 63) // 64
         if k.shape != (B, S, H, D) or v.shape != (B, S, H, D):
             _need(k, "k", B, S, H, D)
@@ -923,6 +935,7 @@ class Context:
             if len(t.shape) != 5 or min(t.shape) < 1:
                 raise ValueError("%s must be [planes, batch, rows, heads, dim], got %s"
                                  % (name, list(t.shape)))
+            _fits(max(t.shape), name)
         batch = _batch_of(n_rows, "n_rows")
         P, _, _, H, D = src.shape
         for name, t in (("src", src), ("dst", dst)):
@@ -932,7 +945,7 @@ class Context:
                                  % (name, P, batch, H, D, list(s)))
         _apart(dst, "dst")
         i32, one = torch.int32, (batch,)
-        entries = rows.shape[1] if isinstance(rows, torch.Tensor) and rows.dim() == 2 else 0
+        entries = _fits(rows.shape[1], "rows") if isinstance(rows, torch.Tensor) and rows.dim() == 2 else 0
         p_n, p_start, p_list = self._args(
             (("src", src), ("dst", dst)),
             ("n_rows", n_rows, i32, one, one),

@@ -94,3 +94,31 @@ def test_binding_refuses_tensors_written_twice():
     with pytest.raises(TypeError, match="CUDA"):
         ctx.cache_write(**{**w, "dst": G.QuantRows(quant(3, 2, 2, 20, 64).codes.transpose(2, 3),
                                                    quant(3, 2, 2, 20, 64).scales.transpose(2, 3))})
+
+
+def test_binding_refuses_extents_past_32_bits():
+    """The library's sizes are 32-bit numbers: 2^32 + 9 rows must not become 9, nor 2^32 none."""
+    ctx = context()
+    for n in (2 ** 31, 2 ** 32, 2 ** 32 + 9):
+        far = lambda *lead: bf(*[1] * len(lead), 2, 64).expand(*lead, 2, 64)
+        every = lambda *lead: G.QuantRows(torch.zeros(1, dtype=torch.uint8).expand(*lead, 2, 64),
+                                          torch.zeros(1, dtype=torch.uint8).expand(*lead, 2))
+        for kw in (dict(cache=(far(2, n), far(2, n))), dict(shared=(far(n), far(n))),
+                   dict(cache=(every(2, n), every(2, n)), shared=None),
+                   dict(cache=(far(2, n), torch.nn.Parameter(far(2, n))), shared=None),
+                   dict(q=bf(1).expand(2, n, 4, 64), k=far(2, n), v=far(2, n)),
+                   dict(q=bf(1).expand(2, 8, n, 64)),
+                   dict(k=bf(1).expand(2, 8, n, 64), v=bf(1).expand(2, 8, n, 64)),
+                   ):
+            with pytest.raises(ValueError, match="past 2"):
+                ctx.tree_attention(**block(**kw))
+        w = dict(dst=quant(3, 2, 20, 2, 64), src=bf(3, 2, 9, 2, 64), n_rows=i32(2), rows=i32(2, 4), start=i32(2))
+        for kw in (dict(src=far(3, 2, n)), dict(dst=every(3, 2, n)), dict(rows=i32(1, 1).expand(2, n)),
+                   dict(n_rows=i32(1).expand(n)), dict(src=far(n, 2, 9), dst=every(n, 2, 20))):
+            with pytest.raises(ValueError, match="past 2"):
+                ctx.cache_write(**{**w, **kw})
+        with pytest.raises(ValueError, match="past 2"):
+            ctx.cache_read(every(3, 2, n), i32(2), out=bf(3, 2, 9, 2, 64))
+        with pytest.raises(ValueError, match="past 2"):
+            ctx.accept_sampled(i32(1).expand(n), i32(2, 32), i32(2, 32), bf(2, 100), bf(2, 8, 100),
+                               torch.zeros(2, 4, dtype=torch.float64))

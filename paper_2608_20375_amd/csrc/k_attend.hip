@@ -463,11 +463,9 @@ __device__ __forceinline__ void wide_part(const AttendArgs &a, const Item &it, u
   bool bad = false, unused;
   const int per_seq = a.slots * a.group;
   const int live = packed ? 0 : __builtin_amdgcn_readfirstlane(slots_of(a, b, &bad));
-  const bool speaks = it.tile_row == 0 && it.part == 0 && kvh == 0 && tid == 0;
-  if (!packed && it.tile_row * kRowTile >= live * a.group) {
-    if (bad && speaks) atomicOr(a.error_flag, kErrBlockSizes);
-    return;
-  }
+  const int len = packed ? 0 : __builtin_amdgcn_readfirstlane(len_of(a, b, &bad));
+  if (bad && it.tile_row == 0 && it.part == 0 && kvh == 0 && tid == 0) atomicOr(a.error_flag, kErrBlockSizes);
+  if (!packed && it.tile_row * kRowTile >= live * a.group) return;
   int row = it.tile_row * kRowTile + wave * 32 + col;
   int rb = b;
   if (packed) {
@@ -481,8 +479,6 @@ __device__ __forceinline__ void wide_part(const AttendArgs &a, const Item &it, u
   if (packed && !__syncthreads_or(valid)) return;
   const bool busy = __ballot(valid) != 0;
 
-  const int len = packed ? 0 : __builtin_amdgcn_readfirstlane(len_of(a, b, &bad));
-  if (bad && speaks) atomicOr(a.error_flag, kErrBlockSizes);
   const Tiles n = tiles_of(a, packed, len, live);
   const Part part = part_of(n, it.part);
   const int t0 = part.first, t1 = part.last;

@@ -309,6 +309,9 @@ GRAFT_API int graft_commit_accepted(graft_ctx *ctx, int32_t batch, const int32_t
 /* cache, the sampled walk, and the cache's rows (plain or quantised).          */
 /* ------------------------------------------------------------------------ */
 
+/* A call below whose rows, keys or batch need more than 2^24 - 1 workgroups of 256 threads in one
+ * launch is refused with GRAFT_ERR_UNSUPPORTED before anything is launched. */
+
 /* Element types of the calls below. */
 #define GRAFT_F32 0
 #define GRAFT_BF16 1

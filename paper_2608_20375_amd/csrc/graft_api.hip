@@ -278,7 +278,7 @@ int check_attention(const graft_ctx *ctx, const graft_attention *a, bool pointer
   return rc;
 }
 
-int check_move(const graft_ctx *ctx, const graft_cache_move *m, const char *who) {
+int check_move(const graft_ctx *ctx, const graft_cache_move *m, bool write, const char *who) {
   if (!ctx || !m || !m->n_rows) return fail(GRAFT_ERR_INVALID_ARG, "%s: NULL argument", who);
   if (m->batch < 1 || m->batch > ctx->dims.max_batch)
     return fail(GRAFT_ERR_INVALID_ARG, "%s: batch %d outside 1..%d", who, m->batch,
@@ -296,10 +296,9 @@ int check_move(const graft_ctx *ctx, const graft_cache_move *m, const char *who)
   if (m->src_rows > (1 << 30) || m->dst_rows > (1 << 30) || m->list_len > (1 << 30) ||
       m->n_planes > (1 << 28) || m->heads > (1 << 28))
     return fail(GRAFT_ERR_UNSUPPORTED, "%s: more than 2^30 rows or 2^28 planes or heads", who);
-  // workgroups of 256 columns, at most 32 a head, and of at least 4 rows
-  const int64_t cols = static_cast<int64_t>(m->n_planes) * m->heads * 32;
-  const int64_t rows = std::max(m->src_rows, std::max(m->dst_rows, m->list_len + 1));
-  if (cols > (1 << 28) || (cols / 256 + 1) * (rows / 4 + 1) > (int64_t{1} << 31) / m->batch - 1)
+  // threads of a row, at most 32 a head, are counted in 32 bits too
+  if (static_cast<int64_t>(m->n_planes) * m->heads > (1 << 23) ||
+      graft::cache_move_blocks(*m, write) > graft::kMaxBlocks)
     return fail(GRAFT_ERR_UNSUPPORTED, "%s: too many rows to move in one call", who);
   return check_device(ctx, who);
 }
@@ -619,9 +618,12 @@ int graft_tree_attention_workspace(graft_ctx *ctx, const graft_attention *a, int
 int graft_tree_attention(graft_ctx *ctx, const graft_attention *a, graft_stream_t stream) {
   const char *who = "graft_tree_attention";
   int rc = check_attention(ctx, a, true, who);
-  if (rc == GRAFT_OK) rc = check_device(ctx, who);
   if (rc != GRAFT_OK) return rc;
   const graft::AttendPlan p = graft::attend_plan(*a);
+  if (p.blocks > graft::kMaxBlocks || p.merge_blocks > graft::kMaxBlocks)
+    return fail(GRAFT_ERR_UNSUPPORTED, "%s: too many query rows and keys for one call", who);
+  rc = check_device(ctx, who);
+  if (rc != GRAFT_OK) return rc;
   if (p.bytes > 0 && (!a->workspace || (reinterpret_cast<uintptr_t>(a->workspace) & 15u) != 0 ||
                       a->workspace_bytes < p.bytes))
     return fail(GRAFT_ERR_INVALID_ARG,
@@ -667,6 +669,8 @@ int graft_accept_sampled(graft_ctx *ctx, int32_t batch, const int32_t *n_nodes,
   if (at % type_bytes(t->dtype) != 0 || reinterpret_cast<uintptr_t>(t->uniform) % 8 != 0)
     return fail(GRAFT_ERR_INVALID_ARG, "%s: misaligned logits or uniform", who);
   if (V > (1 << 30)) return fail(GRAFT_ERR_UNSUPPORTED, "%s: vocab over 2^30", who);
+  if (static_cast<int64_t>(batch) * graft::sample_plan(ctx->dims, batch, t->dtype).splits > graft::kMaxBlocks)
+    return fail(GRAFT_ERR_UNSUPPORTED, "%s: batch %d is too large for one call", who, batch);
   if (update_history && !ctx->has_history)
     return fail(GRAFT_ERR_INVALID_ARG, "%s: no history ring (graft_set_history)", who);
   const int64_t need = graft::sample_bytes(ctx->dims, batch);
@@ -693,7 +697,7 @@ int graft_cache_write(graft_ctx *ctx, const graft_cache_move *m, graft_stream_t 
     return fail(GRAFT_ERR_INVALID_ARG, "%s: list_len %d", who, m->list_len);
   if (m && m->with_root && !m->list)
     return fail(GRAFT_ERR_INVALID_ARG, "%s: with_root needs a list", who);
-  const int rc = check_move(ctx, m, who);
+  const int rc = check_move(ctx, m, true, who);
   if (rc != GRAFT_OK) return rc;
   const hipError_t e = graft::launch_cache_write(ctx, *m, reinterpret_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, who);
@@ -707,7 +711,7 @@ int graft_cache_read(graft_ctx *ctx, const graft_cache_move *m, graft_stream_t s
                 m->dst_dtype);
   if (m && (m->list || m->with_root || m->list_len != 0))
     return fail(GRAFT_ERR_INVALID_ARG, "%s: takes no list and no root", who);
-  const int rc = check_move(ctx, m, who);
+  const int rc = check_move(ctx, m, false, who);
   if (rc != GRAFT_OK) return rc;
   const hipError_t e = graft::launch_cache_read(ctx, *m, reinterpret_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, who);

@@ -286,6 +286,7 @@ struct AttendPlan {
   int shared_splits;  // parts of the shared prefix then
   int parts;          // splits + shared_splits
   int64_t bytes;      // workspace
+  int64_t blocks, merge_blocks;   // workgroups of the two launches
 };
 AttendPlan attend_plan(const graft_attention &a);
 hipError_t launch_attend(graft_ctx *ctx, const graft_attention &a, const AttendPlan &p,
@@ -305,8 +306,11 @@ hipError_t launch_accept_sampled(graft_ctx *ctx, int batch, const int32_t *n_nod
                                  const graft_target_logits *t, int32_t *acc_len,
                                  int32_t *acc_nodes, int32_t *bonus, float *logp,
                                  int update_history, void *workspace, hipStream_t stream);
+int64_t cache_move_blocks(const graft_cache_move &m, bool write);   // workgroups of its launch
 hipError_t launch_cache_write(graft_ctx *ctx, const graft_cache_move &m, hipStream_t stream);
 hipError_t launch_cache_read(graft_ctx *ctx, const graft_cache_move &m, hipStream_t stream);
+// Workgroups of 256 threads that a launch holds: it counts its threads in 32 bits.
+constexpr int64_t kMaxBlocks = (int64_t{1} << 24) - 1;
 // Bits of a context's error flag set by these (1, 2 and 4 are the round's).
 constexpr uint32_t kErrBlockSizes = 8u, kErrTargetRow = 16u, kErrCacheRow = 32u;
 hipError_t launch_synth_targets(graft_ctx *ctx, int batch, uint64_t seed,

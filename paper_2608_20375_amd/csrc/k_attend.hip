@@ -1119,6 +1119,10 @@ AttendPlan attend_plan(const graft_attention &a) {
   p.splits = cut(units, most, p.few ? 4096 : 1024, own_pass ? 32 : kMaxParts);
   p.parts = p.splits + p.shared_splits;
   const int64_t all = static_cast<int64_t>(a.batch) * a.slots * a.q_heads;
+  const int64_t outer = p.few ? a.batch : static_cast<int64_t>(a.batch) * a.kv_heads;
+  const int64_t groups = ((outer | 1) * p.splits + 7) / 8 * 8 * (p.few ? a.kv_heads : 1);
+  p.blocks = static_cast<int64_t>(a.kv_heads) * p.shared_tiles * p.shared_splits + groups * p.row_tiles;
+  p.merge_blocks = p.parts > 1 ? (all + kAttWaves - 1) / kAttWaves : 0;
   p.bytes = p.parts > 1 ? p.parts * all * (a.head_dim * int64_t{4} + 8) : 0;
   return p;
 }
@@ -1168,9 +1172,7 @@ hipError_t launch_attend(graft_ctx *ctx, const graft_attention &d, const AttendP
   a.parts = p.parts;
   a.shared_items = p.shared_tiles * p.shared_splits * d.kv_heads;
   a.c = d.scale * 1.4426950408889634f;
-  const int64_t outer = p.few ? d.batch : static_cast<int64_t>(d.batch) * d.kv_heads;
-  const int64_t groups = ((outer | 1) * p.splits + 7) / 8 * 8 * (p.few ? d.kv_heads : 1);
-  const dim3 grid(static_cast<unsigned>(a.shared_items + groups * p.row_tiles)), block(kAttThreads);
+  const dim3 grid(static_cast<unsigned>(p.blocks)), block(kAttThreads);
   auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };
   auto pick = [&](auto few, auto dp) {
     constexpr int F = decltype(few)::value;
@@ -1188,7 +1190,7 @@ hipError_t launch_attend(graft_ctx *ctx, const graft_attention &d, const AttendP
   else width(std::integral_constant<int, 0>{});
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.parts <= 1) return e;
-  const dim3 mgrid(static_cast<unsigned>((a.rows_all + kAttWaves - 1) / kAttWaves));
+  const dim3 mgrid(static_cast<unsigned>(p.merge_blocks));
   if (d.dtype == GRAFT_F16) hipLaunchKernelGGL(merge_parts_kernel<F16>, mgrid, block, 0, stream, a);
   else hipLaunchKernelGGL(merge_parts_kernel<Bf16>, mgrid, block, 0, stream, a);
   return hipGetLastError();

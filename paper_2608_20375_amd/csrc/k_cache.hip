@@ -211,15 +211,19 @@ move_kernel(MoveArgs a) {
   }
 }
 
-hipError_t launch_move(graft_ctx *ctx, const graft_cache_move &m, Move mode, int most,
-                       hipStream_t stream) {
-  if (most < 1) return hipSuccess;
+Move mode_of(const graft_cache_move &m, bool write) {
+  if (write) return m.dst_dtype == GRAFT_E4M3 ? Move::kQuantise : Move::kCopy;
+  return m.dst_dtype == GRAFT_F32 ? Move::kRead32 : Move::kRead16;
+}
+// All of a call's arguments but the context's; blocks: the workgroups of its launch.
+MoveArgs plan_move(const graft_cache_move &m, bool write, int64_t *blocks) {
+  const Move mode = mode_of(m, write);
+  const int most = !write ? m.dst_rows : m.list ? m.list_len + (m.with_root ? 1 : 0) : m.src_rows;
   MoveArgs a{};
   a.src = m.src;
   a.dst = m.dst;
   a.n_rows = m.n_rows;
   a.start = m.start;
-  const bool write = mode == Move::kCopy || mode == Move::kQuantise;
   a.list = write ? m.list : nullptr;
   a.list_len = m.list_len;
   a.root = a.list && m.with_root ? 1 : 0;
@@ -235,9 +239,16 @@ hipError_t launch_move(graft_ctx *ctx, const graft_cache_move &m, Move mode, int
   a.col_blocks = (a.cols + kMoveThreads - 1) / kMoveThreads;
   const int per = a.at_once * kMoveRows;
   a.row_blocks = (most + per - 1) / per;
+  *blocks = static_cast<int64_t>(a.col_blocks) * a.row_blocks * m.batch;
+  return a;
+}
+
+hipError_t launch_move(graft_ctx *ctx, const graft_cache_move &m, bool write, hipStream_t stream) {
+  int64_t blocks;
+  MoveArgs a = plan_move(m, write, &blocks);
   a.error_flag = ctx->error_flag;
-  const dim3 grid(static_cast<unsigned>(a.col_blocks) * a.row_blocks * m.batch), block(kMoveThreads);
-  switch (mode) {
+  const dim3 grid(static_cast<unsigned>(blocks)), block(kMoveThreads);
+  switch (mode_of(m, write)) {
     case Move::kCopy: hipLaunchKernelGGL(move_kernel<Move::kCopy>, grid, block, 0, stream, a); break;
     case Move::kQuantise: hipLaunchKernelGGL(move_kernel<Move::kQuantise>, grid, block, 0, stream, a); break;
     case Move::kRead16: hipLaunchKernelGGL(move_kernel<Move::kRead16>, grid, block, 0, stream, a); break;
@@ -248,14 +259,18 @@ hipError_t launch_move(graft_ctx *ctx, const graft_cache_move &m, Move mode, int
 
 }  // namespace
 
+int64_t cache_move_blocks(const graft_cache_move &m, bool write) {
+  int64_t blocks;
+  plan_move(m, write, &blocks);
+  return blocks;
+}
+
 hipError_t launch_cache_write(graft_ctx *ctx, const graft_cache_move &m, hipStream_t stream) {
-  const int most = m.list ? m.list_len + (m.with_root ? 1 : 0) : m.src_rows;
-  return launch_move(ctx, m, m.dst_dtype == GRAFT_E4M3 ? Move::kQuantise : Move::kCopy, most, stream);
+  return launch_move(ctx, m, true, stream);
 }
 
 hipError_t launch_cache_read(graft_ctx *ctx, const graft_cache_move &m, hipStream_t stream) {
-  return launch_move(ctx, m, m.dst_dtype == GRAFT_F32 ? Move::kRead32 : Move::kRead16, m.dst_rows,
-                     stream);
+  return launch_move(ctx, m, false, stream);
 }
 
 }  // namespace graft

@@ -122,3 +122,29 @@ def test_binding_refuses_extents_past_32_bits():
         with pytest.raises(ValueError, match="past 2"):
             ctx.accept_sampled(i32(1).expand(n), i32(2, 32), i32(2, 32), bf(2, 100), bf(2, 8, 100),
                                torch.zeros(2, 4, dtype=torch.float64))
+
+
+def test_calls_past_a_launch_are_refused():
+    """A launch counts its threads in 32 bits: 2^24 - 1 workgroups of 256."""
+    L, f = G.lib(), Fake(batch=1 << 24, L=1, N=8)
+    attend = lambda **kw: L.graft_tree_attention(f.h, C.byref(attention(**{**big, **kw})), None)
+    # single tokens: a workgroup a sequence and key head, sequences in an odd number, then eights
+    big = dict(slots=1, with_root=1, q_heads=8, kv_heads=8, shared_len=0, workspace_bytes=1 << 60, out=rows(),
+               batch=(1 << 21) - 16)
+    assert attend() == NO_GPU and attend(batch=1 << 21) == 2 and attend(batch=1 << 24) == 2
+    # four rows of the merge a workgroup; the shared prefix has a pass of its own
+    big.update(slots=8, with_root=0, q_heads=8, kv_heads=1, shared_len=5, batch=(1 << 20) - 1)
+    assert attend() == NO_GPU and attend(batch=1 << 20) == 2
+    t = G.TargetLogits(1, 1 << 20, 100, 0, 0, 0, 0, 0, 1 << 20)
+    p = 1 << 20
+    walk = lambda batch: L.graft_accept_sampled(f.h, batch, p, p, p, C.byref(t), p, p, p, None, 0, p, 1 << 60, None)
+    assert walk((1 << 24) - 1) == NO_GPU and walk(1 << 24) == 2
+    m = dict(batch=1, n_planes=1, heads=1, head_dim=128, list=0, list_len=0, with_root=0)
+    write = lambda **kw: L.graft_cache_write(f.h, C.byref(move(**{**m, **kw})), None)
+    # 16 threads a row, four rows each: 64 rows a workgroup
+    assert write(src_rows=1 << 30) == 2 and write(src_rows=(1 << 30) - 64) == NO_GPU
+    assert write(src_rows=1 << 20, batch=1 << 10) == 2 and write(src_rows=1 << 20, batch=1 << 9) == NO_GPU
+    back = dict(src_dtype=3, dst_dtype=1, src=rows(True), dst=rows())
+    read = lambda **kw: L.graft_cache_read(f.h, C.byref(move(**{**m, **back, **kw})), None)
+    assert read(dst_rows=1 << 30) == 2 and read(dst_rows=(1 << 30) - 64) == NO_GPU
+    assert read(dst_rows=1 << 30, dst_dtype=0) == 2 and read(dst_rows=1 << 28, dst_dtype=0) == NO_GPU

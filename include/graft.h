@@ -365,7 +365,7 @@ typedef struct {
     int32_t head_dim;            /* a multiple of 16, 16..128 */
     int32_t dtype;               /* q, k, v, out: GRAFT_BF16 or GRAFT_F16 */
     int32_t cache_dtype;         /* cache and shared prefix: dtype, or GRAFT_E4M3 with BF16 */
-    float scale;                 /* finite, > 0 */
+    float scale;                 /* > 0, at most 1e38 */
     graft_rows q, k, v;          /* [batch, slots, q_heads or kv_heads, head_dim] */
     const int32_t *n_nodes;      /* [batch] */
     const uint64_t *mask;        /* [batch, max_nodes, ceil(max_nodes/64)] or NULL (chain) */
@@ -397,7 +397,8 @@ GRAFT_API int graft_tree_attention(graft_ctx *ctx, const graft_attention *a /* h
 /* The target model's logits for the sampled walk.  Row of the root of sequence
  * b: root + b * root_stride; of node i < node_rows: node + b *
  * node_batch_stride + i * node_row_stride; vocab elements each, strides in
- * elements, any alignment that the type has. */
+ * elements, any alignment that the type has; with several node rows they are at least vocab
+ * apart. */
 typedef struct {
     int32_t dtype;               /* GRAFT_F32, GRAFT_BF16 or GRAFT_F16 */
     const void *root;

@@ -253,6 +253,7 @@ int check_attention(const graft_ctx *ctx, const graft_attention *a, bool pointer
                 a->cache_dtype, a->dtype);
   if (!std::isfinite(a->scale) || !(a->scale > 0.0f))
     return fail(GRAFT_ERR_INVALID_ARG, "%s: scale must be positive and finite", who);
+  if (a->scale > 1e38f) return fail(GRAFT_ERR_UNSUPPORTED, "%s: scale over 1e38", who);   // times log2 e
   if (a->cache_rows < 0 || a->shared_len < 0)
     return fail(GRAFT_ERR_INVALID_ARG, "%s: cache_rows and shared_len must not be negative", who);
   if (a->cache_rows > (1 << 30) || a->shared_len > (1 << 30))

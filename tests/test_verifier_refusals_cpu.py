@@ -69,6 +69,14 @@ def test_scale_strides_of_other_types_are_ignored():
         assert attend(**{**codes, name: rows(True, scale_row_stride=1 << 22)}) == NO_GPU, name
 
 
+def test_scales_past_the_exponent_are_refused():
+    """scale log2 e would be infinite, and every result NaN."""
+    L, f = G.lib(), Fake()
+    attend = lambda s: L.graft_tree_attention(f.h, C.byref(attention(scale=s)), None)
+    assert attend(1e38) == NO_GPU and attend(1e-38) == NO_GPU
+    assert attend(2.4e38) == 2 and attend(3.4e38) == 2
+
+
 def test_binding_refuses_tensors_written_twice():
     ctx = context()
     for out in (bf(1, 8, 4, 64).expand(2, 8, 4, 64), bf(2, 1, 4, 64).expand(2, 8, 4, 64),

@@ -813,8 +813,7 @@ class Context:
         shape = q.shape
         B, S, Hq, D = shape
         H, N = k.shape[2], self.dims.max_nodes
-        _fits(max(shape), "q")
-        _fits(H, "k")
+        _fits(B | S | Hq | D | H, "q or k")      # the largest's bits are in it
         W = (N + 63) // 64
         if k.shape != (B, S, H, D) or v.shape != (B, S, H, D):
             _need(k, "k", B, S, H, D)
@@ -935,7 +934,6 @@ class Context:
             if len(t.shape) != 5 or min(t.shape) < 1:
                 raise ValueError("%s must be [planes, batch, rows, heads, dim], got %s"
                                  % (name, list(t.shape)))
-            _fits(max(t.shape), name)
         batch = _batch_of(n_rows, "n_rows")
         P, _, _, H, D = src.shape
         for name, t in (("src", src), ("dst", dst)):
@@ -943,6 +941,8 @@ class Context:
             if s[0] != P or s[1] < batch or s[3] != H or s[4] != D:
                 raise ValueError("%s must be [%d, >=%d, rows, %d, %d], got %s"
                                  % (name, P, batch, H, D, list(s)))
+        src_rows, dst_rows = src.shape[2], dst.shape[2]
+        _fits(P | H | D | src_rows | dst_rows, "src or dst")      # the largest's bits are in it
         _apart(dst, "dst")
         i32, one = torch.int32, (batch,)
         entries = _fits(rows.shape[1], "rows") if isinstance(rows, torch.Tensor) and rows.dim() == 2 else 0
@@ -953,7 +953,7 @@ class Context:
             ("rows", rows, i32, (one, (1,)), (batch, entries) if entries else None))
         kind = lambda t: 3 if isinstance(t, QuantRows) else _DTYPES.get(t.dtype, -1)
         return CacheMove(batch, P, H, D, kind(src), kind(dst), _rows(src, 4, "src"),
-                         _rows(dst, 4, "dst"), src.shape[2], dst.shape[2], p_n, p_start, p_list,
+                         _rows(dst, 4, "dst"), src_rows, dst_rows, p_n, p_start, p_list,
                          entries, 1 if with_root else 0)
 
     def cache_write(self, dst, src, n_rows, rows=None, start=None, with_root=False):

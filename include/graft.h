@@ -347,6 +347,7 @@ typedef struct {
  * Query head h reads key/value head h / (q_heads / kv_heads):
  *   out[b, i, h] = sum_j p_j v_j,  p = softmax_j(scale q_i . k_j),
  *   lse[b, i, h] = log sum_j exp(scale q_i . k_j)  (natural logarithm).
+ * A score times scale log2 e has to be finite in fp32, whatever its size.
  * A slot that sees nothing gets zeros and an lse of -inf.  Keys and values of
  * slots it does not see never reach it, whatever they hold.  Rows of out and
  * lse from slot S_b on are left as they were.

@@ -26,12 +26,13 @@
 // next tile's loads in flight in registers meanwhile, two LDS buffers, one barrier a
 // tile.  For blocks with many rows: a wave's tile is 1024 cycles of matrix products, about
 // 1500 of vector work (the exponentials 512 of them) and 320 of LDS reads, the registers
-// (238 of 256 at 128 columns) leave two waves a SIMD to overlap them, and 5000 to 5800 cycles
-// pass for the two.  64 trees of up to 512 nodes over 4096 e4m3 rows and 1024 shared ones:
-// 1400 us, 858 TFLOP/s; 16 of up to 256 nodes over 4096 bf16 rows: 176 us, 648 TFLOP/s.
+// (248 of 256 at 128 columns, all of them for codes) leave two waves a SIMD to overlap them, and
+// 5000 to 5800 cycles pass for the two.  64 trees of up to 512 nodes over 4096 e4m3 rows and 1024
+// shared ones: 1400 us, 858 TFLOP/s; 16 of up to 256 nodes over 4096 bf16 rows: 176 us, 648 TFLOP/s
+// (fp16: 184); chains instead of trees the same.  Short runs, at lower clocks, take a tenth longer.
 // One LDS buffer and two barriers for a third wave would spill 300 to 400 bytes; sequences in
-// the order of their work, or the long ones in parts of an even length, change nothing (1566
-// against 1531 us, 210 against 200): the chip is full until near the end.
+// the order of their work, or the long ones in parts of an even length, change nothing (short
+// runs in turn: 1566 against 1531 us, 210 against 200): the chip is full until near the end.
 // narrow_part: 16 or 32 rows a workgroup; every wave walks 32-key tiles of its own (four
 // waves, four times the keys in flight), keys from memory straight into fragments, the
 // values through a stretch of LDS of the wave's own, no barriers; the four waves' sums
@@ -108,7 +109,8 @@ struct Bf16 {
 };
 struct F16 {
   static constexpr uint32_t kExp = 0x7C00u;
-  // 2^15 at most, of 65504.  16 trees of up to 256 nodes: 210 us, unlifted with kSlack 8 205.
+  // 2^15 at most, of 65504.  16 trees of up to 256 nodes: 210 us, unlifted with kSlack 8 205
+  // (in turn, short runs).
   static constexpr float kSlack = 3.0f, kLift = 12.0f;
   static __device__ __forceinline__ f32x16 mfma(const u32x4 &a, const u32x4 &b, const f32x16 &c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a),
@@ -1087,6 +1089,16 @@ Side side(const graft_rows &r, int bytes, int dim, int rows) {
 
 }  // namespace
 
+// The narrow walk up to 32 rows of a sequence and key head.  us narrow and wide, in a graph,
+// 8 key heads of 128 over up to 4096 rows:
+//   rows                    8          16          24          32
+//   1 sequence, bf16     21.5 20.6   22.5 19.9   25.3 20.0   26.8 19.9
+//   32 sequences, bf16   66.6 67.0   73.0 67.7   97.8 69.4  103.4 70.4
+//   32 sequences, e4m3   50.9 73.6   57.4 74.6   83.4 75.6   88.6 76.5
+// One token of 20 and 32 heads a key head over 16384 and 700 rows 28.6 29.5 and 16.3 15.9, e4m3 26.9
+// 30.7 and 15.4 16.9; 64 tokens of 8 over up to 2048 e4m3 rows 49.5 73.8.  So up to 16 rows the
+// narrow walk wins or is near; from 17 to 32 it wins for single tokens of few key heads over
+// codes, and trees there would be faster in the wide one.
 AttendPlan attend_plan(const graft_attention &a) {
   AttendPlan p{};
   const int group = a.q_heads / a.kv_heads;
@@ -1181,6 +1193,8 @@ hipError_t launch_attend(graft_ctx *ctx, const graft_attention &d, const AttendP
     else if (q8) run(attend_kernel<Bf16, true, D, F>);
     else run(attend_kernel<Bf16, false, D, F>);
   };
+  // heads of other sizes run as 64 or 128 columns: 16 trees of up to 256 nodes 109 and 112 us at 32
+  // and 64 numbers, 170, 171, 173 and 176 at 80, 96, 112 and 128
   auto width = [&](auto few) {
     if (d.head_dim > 64) pick(few, std::integral_constant<int, 128>{});
     else pick(few, std::integral_constant<int, 64>{});

@@ -31,9 +31,9 @@
 // rows of 151936 words 23 us before any walk has ended, of which the instructions alone
 // are 11.  The vector registers (190 for 16-bit logits) leave two waves a SIMD; held to
 // 168 or 128 they spill: a sixth and a half more time for the 128 walks.
-// Whole calls: 43 to 67 us for one walk of 32000 words and up to 8 levels, 63 to 83 for 5 of
-// 70001 fp32 words, 200 for 64 of 128256, 316 to 365 for 128 of 151936 words and up to 32
-// levels, as far as the walks go.
+// Whole calls, as far as the walks go: 38 to 60 us for one walk of 32000 words and up to 8 levels, 63
+// to 92 for 5 of 70001 fp32 words, 193 to 207 for 64 of 128256 (fp16 as bf16), 365 to 403 for 128 of
+// 151936 words and up to 32 levels.
 #include "graft_internal.h"
 
 namespace graft {
@@ -43,8 +43,8 @@ constexpr int kSampThreads = 256;
 constexpr int kSampWaves = kSampThreads / kWave;
 constexpr int kRuns = 4;                 // runs of a flight: vectors of a lane in flight
 constexpr int kGroups = 4;               // flights of a row at most: kGroups a lane
-// Waves of a launch, about: 128 walks of 151936 words take 341, 316 and 340 us for 4096, 8192
-// and 16384.
+// Waves of a launch, about: the same 128 walks of 151936 words take 341, 316 and 340 us for 4096,
+// 8192 and 16384.
 constexpr int64_t kSampTarget = 8192;
 constexpr int kSampTree = 4;             // tree slots a lane loads ahead
 constexpr int kStopped = -2;             // a walk that has ended; -1 is the root

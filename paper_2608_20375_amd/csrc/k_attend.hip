@@ -304,7 +304,8 @@ __device__ __forceinline__ uint64_t seen_word(const AttendArgs &a, int rb, int s
 struct Ref {
   float c, off, at;
 };
-constexpr float kNoRef = 3.0e38f;    // off without a reference: any score is above it, -inf gives 0
+// off without a reference, fp32's largest: any score is above it, -inf gives 0
+constexpr float kNoRef = 3.40282347e38f;
 template <typename T>
 __device__ __forceinline__ Ref ref_of(float m, float c) {
   const float size = fabsf(m * c);

@@ -87,3 +87,28 @@ def test_scores_of_any_size(kind, power, nodes, sign):
             for h in range(2):
                 assert ((out[b, i, h] - want).abs() <= 1.01 * tol).all(), (b, i, h)
                 assert abs(lse[b, i, h] - z) <= 2.0 ** -16 + z.abs() * 2.0 ** -22, (b, i, h)
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("nodes", [0, 40])
+def test_the_largest_scores(nodes, sign):
+    """Scores of 1.25 2^127, all alike, whose product with log2 e is just inside fp32: a row is the
+    mean of the values it sees, rounded once with probabilities that are equal and exact."""
+    print("largest", nodes, sign, flush=True)
+    c = make(2, nodes, [300, 20], 0, 2, 1, 64, "bfloat16", False, 1, chain=True, n=[nodes, nodes])
+    c["q"].zero_()
+    c["q"][..., 0] = sign * 1.25 * 2.0 ** 63
+    for k in (c["k"], c["cache"][0]):
+        k.zero_()
+        k[..., 0] = 2.0 ** 64
+    ctx = context(c)
+    out, lse, _ = call(ctx, c, scale=1.0)
+    ctx.close()
+    out, lse, eps = out.cpu().double(), lse.cpu().double(), torch.finfo(c["dt"]).eps
+    for b in range(2):
+        for i in range(nodes + 1):
+            v = torch.cat([c["cache"][1][b, :int(c["lens"][b]), 0], c["v"][b, :i + 1, 0]]).double()
+            want, tol = v.mean(0), 1024 * 2.0 ** -24 * v.abs().mean(0)
+            assert ((out[b, i] - want).abs() <= 1.01 * (tol + eps / 2 * want.abs())).all(), (b, i)
+            z = sign * 1.25 * 2.0 ** 127
+            assert (lse[b, i] - z).abs().max() <= abs(z) * 2.0 ** -22, (b, i)

@@ -268,7 +268,8 @@ def _fits(n, name):
 def _batch_of(t, name):
     if not isinstance(t, torch.Tensor) or t.dim() < 1:
         raise ValueError("%s must be a tensor whose first extent is the batch" % name)
-    return _fits(int(t.shape[0]), name)
+    n = t.shape[0]
+    return n if n <= _INT32_MAX else _fits(n, name)
 
 
 def _stream():
@@ -354,8 +355,6 @@ def _apart(t, name):
     """Raises unless every number of a tensor or QuantRows that is written has a place of its own:
     in the order of their size, each stride passes what the smaller ones span."""
     for x in (t.codes, t.scales) if isinstance(t, QuantRows) else (t,):
-        if x.is_contiguous():
-            continue
         span = 1
         for stride, n in sorted((a, b) for a, b in zip(x.stride(), x.shape) if b > 1):
             if stride < span:
@@ -744,7 +743,8 @@ class Context:
             quant, s = isinstance(x, QuantRows), x.shape
             if (len(s) == n + 2 and s[-1] == dim and s[-2] == heads and (n == 1 or s[0] >= lead[0])
                     and (quant or (x.dtype is dtype and y.dtype is dtype))):
-                return _fits(s[n - 1], name), quant
+                if s[n - 1] <= _INT32_MAX:
+                    return s[n - 1], quant
         kinds = set()
         for t in pair:
             if not isinstance(t, (torch.Tensor, QuantRows)):
@@ -813,14 +813,15 @@ class Context:
         shape = q.shape
         B, S, Hq, D = shape
         H, N = k.shape[2], self.dims.max_nodes
-        _fits(B | S | Hq | D | H, "q or k")      # the largest's bits are in it
+        if B | S | Hq | D | H > _INT32_MAX:      # the largest's bits are in it
+            _fits(max(B, S, Hq, D, H), "q or k")
         W = (N + 63) // 64
         if k.shape != (B, S, H, D) or v.shape != (B, S, H, D):
             _need(k, "k", B, S, H, D)
             _need(v, "v", B, S, H, D)
         if out is not None and not (isinstance(out, torch.Tensor) and out.shape == shape):
             _need(out, "out", B, S, Hq, D)
-        if out is not None:
+        if out is not None and not out.is_contiguous():
             _apart(out, "out")
         if n_nodes is None:
             raise ValueError("n_nodes is required")
@@ -942,10 +943,13 @@ class Context:
                 raise ValueError("%s must be [%d, >=%d, rows, %d, %d], got %s"
                                  % (name, P, batch, H, D, list(s)))
         src_rows, dst_rows = src.shape[2], dst.shape[2]
-        _fits(P | H | D | src_rows | dst_rows, "src or dst")      # the largest's bits are in it
-        _apart(dst, "dst")
+        entries = rows.shape[1] if isinstance(rows, torch.Tensor) and rows.dim() == 2 else 0
+        if P | H | D | src_rows | dst_rows | entries > _INT32_MAX:      # the largest's bits are in it
+            _fits(max(P, H, D, src_rows, dst_rows, entries), "src, dst or rows")
+        to = dst.codes if isinstance(dst, QuantRows) else dst
+        if not to.is_contiguous() or to is not dst and not dst.scales.is_contiguous():
+            _apart(dst, "dst")
         i32, one = torch.int32, (batch,)
-        entries = _fits(rows.shape[1], "rows") if isinstance(rows, torch.Tensor) and rows.dim() == 2 else 0
         p_n, p_start, p_list = self._args(
             (("src", src), ("dst", dst)),
             ("n_rows", n_rows, i32, one, one),

@@ -487,6 +487,139 @@ GRAFT_API int graft_cache_write(graft_ctx *ctx, const graft_cache_move *m /* hos
 GRAFT_API int graft_cache_read(graft_ctx *ctx, const graft_cache_move *m /* host */,
                                graft_stream_t stream);
 
+/* ------------------------------------------------------------------------ */
+/* The same step over a cache in pages: keys and values are written with       */
+/* their position rotation, attended to, and compacted after the acceptance.   */
+/* ------------------------------------------------------------------------ */
+
+/* Where a sequence's rows are in a pool of pages: row r of sequence b is row r %
+ * page_rows of page table[b * table_stride + r / page_rows].  Pages are the entries of
+ * the pool's graft_rows along batch_stride, so keys and values of any layout fit; a
+ * head's rows side by side in a page (row_stride = head_dim) read fastest.  Entries of
+ * pages that a call does not need are not looked at. */
+typedef struct {
+    const int32_t *table;        /* [batch, table_len] page numbers in 0..pages - 1 */
+    int64_t table_stride;        /* >= 0, elements */
+    int32_t table_len;           /* table_len * page_rows <= 2^30 */
+    int32_t pages;               /* 1..2^30 */
+    int32_t page_rows;           /* 1..2^20 */
+} graft_page_table;
+
+/* A block's queries, keys and values on their way into the attention. */
+typedef struct {
+    int32_t batch;               /* 1..max_batch */
+    int32_t slots;               /* rows of q, q_out, k, v a sequence: 1..2^24 */
+    int32_t q_heads;             /* 0: no queries; at most 1024, as kv_heads */
+    int32_t kv_heads;
+    int32_t head_dim;            /* a multiple of 16, 16..128 */
+    int32_t rot_dim;             /* numbers of a head that are rotated: a multiple of 16, 0..head_dim */
+    int32_t interleaved;         /* pairs (2f, 2f + 1) if not 0, else (f, f + rot_dim / 2) */
+    int32_t dtype;               /* q, q_out, k, v: GRAFT_BF16 or GRAFT_F16 */
+    int32_t cache_dtype;         /* dtype, or GRAFT_E4M3 with BF16 */
+    graft_rows q, q_out;         /* [batch, slots, q_heads, head_dim]; q_out may be q itself */
+    graft_rows k, v;             /* [batch, slots, kv_heads, head_dim] */
+    graft_rows cache_k, cache_v; /* [pages, page_rows, kv_heads, head_dim] of one layer */
+    graft_page_table pages;
+    const int32_t *n_rows;       /* [batch] rows of each sequence, or NULL: slots */
+    const int32_t *start;        /* [batch] cache row of slot 0, or NULL: 0 */
+    const int32_t *positions;    /* [axes, batch, slots], or NULL: start[b] + slot on every axis */
+    int32_t axes;                /* 1..8 (ignored without positions) */
+    const int32_t *axis;         /* [rot_dim / 2] axis of each pair in 0..axes - 1, or NULL: 0 */
+    const double *freq;          /* [rot_dim / 2] radians a position (rot_dim 0: not used) */
+} graft_paged_rows;
+
+/* Rotates the block's queries and keys and appends keys and values to the pages.
+ * Slot i < n_rows[b] of sequence b goes to cache row start[b] + i.  Pair f = (x, y) of a
+ * query or key head becomes (x cos a - y sin a, y cos a + x sin a) with a =
+ * positions[axis[f], b, i] * freq[f] (several axes: time, height and width of a picture's
+ * tokens, say).  The angle is formed and reduced in fp64, so far positions lose nothing;
+ * its sine and cosine and the pair are fp32, rounded once to the type that is stored.
+ * Codes are those of graft_cache_write, made from the rotated keys' fp32 numbers.
+ * Rows of q_out, and of the cache, that no slot goes to are left as they were.
+ * n_rows is clamped to 0 .. slots.  Slots whose cache row is outside the table, or whose
+ * page is outside 0 .. pages - 1, write no key and value; these, an n_rows that was
+ * clamped and an axis outside 0 .. axes - 1 (taken as 0) are reported by
+ * graft_get_device_status.  Two slots that go to one place leave one of both there.
+ * No overlap of what is written with anything else, but q_out with q where both are the
+ * same rows; a stride of what is written below head_dim is refused. */
+GRAFT_API int graft_paged_write(graft_ctx *ctx, const graft_paged_rows *r /* host */,
+                                graft_stream_t stream);
+
+/* Attention of a block over pages.  Sequence b has cache_len[b] rows before the block,
+ * whose S_b = n_nodes[b] + (with_root != 0) slots are its rows behind them (as
+ * graft_paged_write left them with start = cache_len): slot 0 is the root with with_root,
+ * the tree's nodes follow; with n_nodes NULL a sequence has `slots` slots.  A slot sees
+ *   - in the block what it sees in graft_tree_attention: itself, its ancestors (mask) and
+ *     the root, or with mask NULL the slots up to its own;
+ *   - the rows before the block.
+ * With a window > 0 a slot at position p (cache_len[b] + the slots that it sees - 1: its depth
+ * in the tree, or its number in a chain) sees only the rows before the block, and
+ * without a mask also the slots, r with r > p - window or r < sinks.  In the block a mask
+ * alone decides, so with one the window must hold a path: window > L.
+ *   out[b, i, h] = sum_j p_j v_j,  p = softmax_j(scale q_i . k_j), h's key head being
+ *   h / (q_heads / kv_heads); lse as in graft_tree_attention.
+ * What a slot does not see never reaches it, whatever it holds; a slot that sees nothing
+ * gets zeros and an lse of -inf.  Rows of out and lse from slot S_b on are left as they were.
+ * Numbers and roundings are those of graft_tree_attention. */
+typedef struct {
+    int32_t batch;               /* 1..max_batch */
+    int32_t slots;               /* 1..2^20; with a mask at most max_nodes + 1 (root), max_nodes */
+    int32_t with_root;
+    int32_t q_heads, kv_heads;   /* q_heads a multiple of kv_heads, at most 1024 */
+    int32_t head_dim;            /* a multiple of 16, 16..128 */
+    int32_t dtype;               /* q, out: GRAFT_BF16 or GRAFT_F16 */
+    int32_t cache_dtype;         /* dtype, or GRAFT_E4M3 with BF16 */
+    float scale;                 /* > 0, at most 1e38 */
+    int32_t window;              /* >= 0; 0: none */
+    int32_t sinks;               /* >= 0 (ignored without a window) */
+    graft_rows q;                /* [batch, slots, q_heads, head_dim] */
+    const int32_t *n_nodes;      /* [batch] or NULL */
+    const uint64_t *mask;        /* [batch, max_nodes, ceil(max_nodes/64)] or NULL (chain) */
+    graft_rows cache_k, cache_v; /* [pages, page_rows, kv_heads, head_dim] of one layer */
+    graft_page_table pages;      /* table_len * page_rows >= slots */
+    const int32_t *cache_len;    /* [batch] */
+    graft_rows out;              /* [batch, slots, q_heads, head_dim]; no overlap with inputs or
+                                    of its rows */
+    float *lse;                  /* [batch, slots, q_heads] or NULL */
+    void *workspace;             /* 16-byte aligned, graft_paged_attention_workspace bytes */
+    int64_t workspace_bytes;
+} graft_paged_attention_desc;
+
+/* *bytes (host) receives the workspace that graft_paged_attention needs for these sizes
+ * (pointers in *a are not looked at); it may be 0. */
+GRAFT_API int graft_paged_attention_workspace(graft_ctx *ctx, const graft_paged_attention_desc *a /* host */,
+                                              int64_t *bytes /* host */);
+
+/* The attention above on `stream`.  The workspace belongs to the call until its work is done
+ * and needs no clearing.  n_nodes[b] outside 0 .. slots - with_root and a block that ends
+ * outside the table are clamped and reported by graft_get_device_status; so are pages
+ * outside 0 .. pages - 1, whose rows are seen by nobody. */
+GRAFT_API int graft_paged_attention(graft_ctx *ctx, const graft_paged_attention_desc *a /* host */,
+                                    graft_stream_t stream);
+
+/* The accepted path's rows of a block in pages. */
+typedef struct {
+    int32_t batch;               /* 1..max_batch */
+    int32_t n_planes;            /* e.g. layers x {key, value} */
+    int32_t heads, head_dim;     /* head_dim a multiple of 16, 16..128 */
+    int32_t dtype;               /* GRAFT_BF16, GRAFT_F16 or GRAFT_E4M3 */
+    graft_rows rows;             /* [n_planes, pages, page_rows, heads, head_dim] */
+    graft_page_table pages;
+    const int32_t *start;        /* [batch] cache row of the block's slot 0, or NULL: 0 */
+    const int32_t *acc_len;      /* [batch] */
+    const int32_t *acc_nodes;    /* [batch, L] as graft_accept writes it */
+    int32_t with_root;           /* slot 0 is the root, which stays */
+} graft_paged_path;
+
+/* Moves the accepted path's rows up to the front of the block: cache row start[b] + r +
+ * acc_nodes[b, i] to start[b] + r + i for i < acc_len[b] (clamped to 0 .. L), r = 1 with
+ * with_root, else 0, in every plane; other rows are untouched.  With node indices that
+ * increase along the path, as graft_accept's do, every row is read before it is written
+ * over.  Node indices outside 0 .. max_nodes - 1, rows outside the table and pages outside
+ * 0 .. pages - 1 are skipped and reported by graft_get_device_status. */
+GRAFT_API int graft_paged_commit(graft_ctx *ctx, const graft_paged_path *p /* host */,
+                                 graft_stream_t stream);
+
 /* Synchronizes `stream` and reports data errors the kernels detected since
  * the last call (token ids outside [0, V), for example): GRAFT_OK or
  * GRAFT_ERR_DEVICE_DATA; the flag is then cleared. */

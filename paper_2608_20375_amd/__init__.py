@@ -12,7 +12,7 @@ import os
 
 import torch
 
-__all__ = ["Context", "QuantRows", "TreeBuffers", "TdesTrainer", "TdesHyper", "saba_fit", "read_stream", "lib",
+__all__ = ["Context", "QuantRows", "paged_cache", "TreeBuffers", "TdesTrainer", "TdesHyper", "saba_fit", "read_stream", "lib",
            "library_path", "GraftError", "EXPORTED_SYMBOLS"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -28,7 +28,8 @@ EXPORTED_SYMBOLS = (
     "graft_tdes_param_count", "graft_tdes_step", "graft_tdes_device_status", "graft_saba_fit",
     "graft_read_stream", "graft_tree_attention", "graft_tree_attention_workspace",
     "graft_accept_sampled", "graft_accept_sampled_workspace", "graft_cache_write",
-    "graft_cache_read",
+    "graft_cache_read", "graft_paged_write", "graft_paged_attention", "graft_paged_attention_workspace",
+    "graft_paged_commit",
 )
 
 READ_STREAM_SINK_WORDS = 4096
@@ -143,6 +144,35 @@ class CacheMove(C.Structure):
                 ("list_len", C.c_int32), ("with_root", C.c_int32)]
 
 
+class PageTable(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("table_stride", C.c_int64), ("table_len", C.c_int32),
+                ("pages", C.c_int32), ("page_rows", C.c_int32)]
+
+
+class PagedRows(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("batch", "slots", "q_heads", "kv_heads", "head_dim", "rot_dim",
+                                          "interleaved", "dtype", "cache_dtype")]
+                + [(n, Rows) for n in ("q", "q_out", "k", "v", "cache_k", "cache_v")]
+                + [("pages", PageTable), ("n_rows", C.c_void_p), ("start", C.c_void_p),
+                   ("positions", C.c_void_p), ("axes", C.c_int32), ("axis", C.c_void_p),
+                   ("freq", C.c_void_p)])
+
+
+class PagedAttention(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("batch", "slots", "with_root", "q_heads", "kv_heads", "head_dim",
+                                          "dtype", "cache_dtype")]
+                + [("scale", C.c_float), ("window", C.c_int32), ("sinks", C.c_int32), ("q", Rows),
+                   ("n_nodes", C.c_void_p), ("mask", C.c_void_p), ("cache_k", Rows), ("cache_v", Rows),
+                   ("pages", PageTable), ("cache_len", C.c_void_p), ("out", Rows), ("lse", C.c_void_p),
+                   ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)])
+
+
+class PagedPath(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("n_planes", C.c_int32), ("heads", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int32), ("rows", Rows), ("pages", PageTable), ("start", C.c_void_p),
+                ("acc_len", C.c_void_p), ("acc_nodes", C.c_void_p), ("with_root", C.c_int32)]
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -194,6 +224,10 @@ def lib():
                                            vp, vp, i32, vp, i64, vp]
         L.graft_cache_write.argtypes = [vp, C.POINTER(CacheMove), vp]
         L.graft_cache_read.argtypes = [vp, C.POINTER(CacheMove), vp]
+        L.graft_paged_write.argtypes = [vp, C.POINTER(PagedRows), vp]
+        L.graft_paged_attention_workspace.argtypes = [vp, C.POINTER(PagedAttention), C.POINTER(i64)]
+        L.graft_paged_attention.argtypes = [vp, C.POINTER(PagedAttention), vp]
+        L.graft_paged_commit.argtypes = [vp, C.POINTER(PagedPath), vp]
         L.graft_status_string.argtypes = [C.c_int]
         L.graft_status_string.restype = C.c_char_p
         L.graft_last_error.argtypes = []
@@ -207,7 +241,8 @@ def lib():
                   "graft_tdes_step", "graft_tdes_device_status", "graft_saba_fit",
                   "graft_read_stream", "graft_tree_attention", "graft_tree_attention_workspace",
                   "graft_accept_sampled", "graft_accept_sampled_workspace", "graft_cache_write",
-                  "graft_cache_read"):
+                  "graft_cache_read", "graft_paged_write", "graft_paged_attention",
+                  "graft_paged_attention_workspace", "graft_paged_commit"):
             getattr(L, n).restype = C.c_int
         _lib = L
     return _lib
@@ -330,6 +365,22 @@ class QuantRows:
     def __getitem__(self, index):
         """A view by leading indices: codes[index], scales[index]."""
         return QuantRows(self.codes[index], self.scales[index])
+
+
+def paged_cache(pages, page_rows, heads, dim, dtype=torch.bfloat16, planes=None, device=None):
+    """An unwritten pool of pages [pages, page_rows, heads, dim] (planes given: [planes, ...], layers x
+    {key, value}, say) whose memory holds a head's rows of a page side by side, the order
+    that the attention reads fastest.  dtype: bfloat16, float16, or float8_e4m3fn for
+    QuantRows."""
+    dev = device or torch.device("cuda", torch.cuda.current_device())
+    lead = () if planes is None else (planes,)
+    if dtype == torch.float8_e4m3fn:
+        codes = torch.empty(*lead, pages, heads, page_rows, dim, dtype=torch.uint8, device=dev)
+        scales = torch.empty(*lead, pages, heads, page_rows, dtype=torch.uint8, device=dev)
+        return QuantRows(codes.transpose(-2, -3), scales.transpose(-1, -2))
+    if dtype not in (torch.bfloat16, torch.float16):
+        raise TypeError("dtype must be bfloat16, float16 or float8_e4m3fn")
+    return torch.empty(*lead, pages, heads, page_rows, dim, dtype=dtype, device=dev).transpose(-2, -3)
 
 
 def _rows(t, n, name):
@@ -981,6 +1032,227 @@ class Context:
         m = self._move(src, out, n_rows, start, None, False)
         _check(lib().graft_cache_read(self._h, C.byref(m), _stream()), "graft_cache_read")
         return out
+
+    def _pages(self, cache, name, heads, dim, dtype):
+        """(keys, values, quantised) of a layer's pages [pages, page_rows, heads, dim]."""
+        if not isinstance(cache, (tuple, list)) or len(cache) != 2:
+            raise ValueError("%s must be a pair of keys and values" % name)
+        k, v = cache
+        for t in (k, v):
+            if not isinstance(t, (torch.Tensor, QuantRows)):
+                raise TypeError("%s must hold tensors or QuantRows" % name)
+        quant, s = isinstance(k, QuantRows), k.shape
+        if isinstance(v, QuantRows) != quant or v.shape != s:
+            raise ValueError("%s: keys and values must agree in type and shape" % name)
+        if len(s) != 4 or s[2] != heads or s[3] != dim or s[0] < 1 or s[1] < 1:
+            raise ValueError("%s must be [pages, page_rows, %d, %d], got %s" % (name, heads, dim, list(s)))
+        if not quant and (k.dtype is not dtype or v.dtype is not dtype):
+            raise TypeError("%s must be %s or QuantRows, got %s and %s" % (name, dtype, k.dtype, v.dtype))
+        if s[0] | s[1] > _INT32_MAX:
+            _fits(max(s[0], s[1]), name)
+        return k, v, quant
+
+    def _table(self, page_table, batch):
+        """Extents of a page table [batch or more, pages of a sequence], for _args."""
+        if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
+            raise ValueError("page_table must be [batch, pages of a sequence]")
+        n = page_table.shape[1]
+        if n > _INT32_MAX:
+            _fits(n, "page_table")
+        return ("page_table", page_table, torch.int32, ((batch,), (1,)), (batch, n))
+
+    def paged_write(self, cache, page_table, k, v, n_rows=None, start=None, q=None, q_out=None, freq=None,
+                    positions=None, axis=None, interleaved=False):
+        """Rotates a block's queries and keys and appends keys and values to pages
+        (graft_paged_write).  cache: a pair of [pages, page_rows, kv_heads, dim] keys and
+        values of one layer, tensors of k's type or QuantRows (bfloat16 rows), paged_cache's
+        for one; page_table [batch, n] int32: row r of sequence b is row r % page_rows
+        of page page_table[b, r // page_rows].  k, v [batch, slots, kv_heads, dim] and q
+        [batch, slots, q_heads, dim], bfloat16 or float16: slot i < n_rows[b] (None: all)
+        goes to row start[b] + i (None: 0).  freq [rot / 2] float64, radians a position,
+        rotates the first rot numbers of every head of q and k, in pairs (f, f + rot / 2)
+        or, interleaved, (2f, 2f + 1); None rotates nothing.  positions [axes, batch,
+        slots] or [batch, slots] int32 (None: start + i), axis [rot / 2] int32 the axis of
+        each pair (None: the first).  Returns q_out (None without q; allocated as
+        zeros when None; q itself rotates in place)."""
+        for name, t in (("k", k), ("v", v), ("q", q)):
+            if t is not None or name != "q":
+                if not isinstance(t, torch.Tensor) or t.dim() != 4 or min(t.shape) < 1:
+                    raise ValueError("%s must be [batch, slots, heads, dim]" % name)
+        B, S, H, D = k.shape
+        if v.shape != k.shape:
+            _need(v, "v", B, S, H, D)
+        Hq = 0
+        if q is not None:
+            Hq = q.shape[2]
+            if q.shape != (B, S, Hq, D):
+                _need(q, "q", B, S, Hq, D)
+        elif q_out is not None:
+            raise ValueError("q_out needs q")
+        if B | S | H | Hq | D > _INT32_MAX:
+            _fits(max(B, S, H, Hq, D), "q or k")
+        if k.dtype not in (torch.bfloat16, torch.float16):
+            raise TypeError("k must be bfloat16 or float16")
+        for name, t in (("v", v), ("q", q), ("q_out", q_out)):
+            if t is not None and (not isinstance(t, torch.Tensor) or t.dtype != k.dtype):
+                raise TypeError("%s must be a tensor of %s" % (name, k.dtype))
+        if q_out is not None and q_out is not q:
+            if q_out.shape != q.shape:
+                _need(q_out, "q_out", B, S, Hq, D)
+        if q_out is not None and not q_out.is_contiguous():
+            _apart(q_out, "q_out")
+        ck, cv, quant = self._pages(cache, "cache", H, D, k.dtype)
+        for t, name in ((ck, "cache keys"), (cv, "cache values")):
+            _apart(t, name)
+        F, axes = 0, 1
+        if freq is not None:
+            if not isinstance(freq, torch.Tensor) or freq.dim() != 1:
+                raise ValueError("freq must be [rot / 2]")
+            F = freq.shape[0]
+            if F < 1 or 2 * F > D:
+                raise ValueError("freq must have 1..%d entries, got %d" % (D // 2, F))
+        elif positions is not None or axis is not None:
+            raise ValueError("positions and axis need freq")
+        if positions is not None:
+            if not isinstance(positions, torch.Tensor) or positions.dim() not in (2, 3):
+                raise ValueError("positions must be [axes, batch, slots] or [batch, slots]")
+            if positions.dim() == 2:
+                positions = positions[None]
+            axes = positions.shape[0]
+        elif axis is not None:
+            raise ValueError("axis needs positions")
+        dtype, one, i32 = _DTYPES[k.dtype], (B,), torch.int32
+        p_table, p_n, p_start, p_pos, p_axis, p_freq = self._args(
+            (("k", k), ("v", v), ("q", q), ("q_out", q_out), ("cache keys", ck), ("cache values", cv)),
+            self._table(page_table, B),
+            ("n_rows", n_rows, i32, one, one),
+            ("start", start, i32, one, one),
+            ("positions", positions, i32, ((1,), B, S), (axes, B, S)),
+            ("axis", axis, i32, (F,), (F,)),
+            ("freq", freq, torch.float64, (F,), (F,)))
+        if q is not None and q_out is None:
+            q_out = torch.zeros_like(q, memory_format=torch.contiguous_format)
+        n = page_table.shape[1]
+        a = PagedRows(B, S, Hq, H, D, 2 * F, 1 if interleaved else 0, dtype, 3 if quant else dtype)
+        if Hq:
+            a.q, a.q_out = _rows(q, 3, "q"), _rows(q_out, 3, "q_out")
+        a.k, a.v, a.cache_k, a.cache_v = (_rows(k, 3, "k"), _rows(v, 3, "v"), _rows(ck, 3, "cache"),
+                                          _rows(cv, 3, "cache"))
+        a.pages = PageTable(p_table, n, n, ck.shape[0], ck.shape[1])
+        a.n_rows, a.start, a.positions, a.axes, a.axis, a.freq = p_n, p_start, p_pos, axes, p_axis, p_freq
+        _check(lib().graft_paged_write(self._h, C.byref(a), _stream()), "graft_paged_write")
+        return q_out
+
+    def paged_attention(self, q, cache, page_table, cache_len, n_nodes=None, mask=None, scale=None,
+                        window=None, sinks=0, with_root=False, out=None, lse=None, workspace=None):
+        """Attention of a block over pages (graft_paged_attention): q [batch, slots, q_heads,
+        dim], bfloat16 or float16; cache and page_table as in paged_write, the block's own
+        rows being rows cache_len[b] + slot (as paged_write leaves them with
+        start=cache_len).  n_nodes[b] (+ 1 with_root) slots are used, None: all.  mask
+        [batch, max_nodes, words] int64 as build_tree writes it, or None for a chain.
+        window: a slot at position p sees rows past p - window, and the first `sinks`
+        ones; None: all.  scale defaults to dim ** -0.5.  Writes out (allocated as zeros
+        when None) up to each sequence's slots and, when given, lse [batch, slots, q_heads]
+        float32; returns out.  workspace: uint8, at least paged_attention_workspace
+        bytes; allocated when None."""
+        a, out = self._paged(q, cache, page_table, cache_len, n_nodes, mask, scale, window, sinks, with_root,
+                             out, lse)
+        L = lib()
+        need = C.c_int64()
+        _check(L.graft_paged_attention_workspace(self._h, C.byref(a), C.byref(need)),
+               "graft_paged_attention_workspace")
+        workspace = self._workspace(workspace, need.value, q.device)
+        if workspace is not None:
+            a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
+        _check(L.graft_paged_attention(self._h, C.byref(a), _stream()), "graft_paged_attention")
+        return out
+
+    def paged_attention_workspace(self, q, cache, page_table, cache_len, n_nodes=None, mask=None, scale=None,
+                                  window=None, sinks=0, with_root=False, out=None, lse=None):
+        """Bytes of workspace that paged_attention needs for these arguments."""
+        a, _ = self._paged(q, cache, page_table, cache_len, n_nodes, mask, scale, window, sinks, with_root,
+                           out, lse)
+        need = C.c_int64()
+        _check(lib().graft_paged_attention_workspace(self._h, C.byref(a), C.byref(need)),
+               "graft_paged_attention_workspace")
+        return need.value
+
+    def _paged(self, q, cache, page_table, cache_len, n_nodes, mask, scale, window, sinks, with_root, out,
+               lse):
+        if not isinstance(q, torch.Tensor) or q.dim() != 4 or min(q.shape) < 1:
+            raise ValueError("q must be [batch, slots, heads, dim]")
+        if q.dtype not in (torch.bfloat16, torch.float16):
+            raise TypeError("q must be bfloat16 or float16")
+        if cache_len is None:
+            raise ValueError("cache_len is required")
+        shape = q.shape
+        B, S, Hq, D = shape
+        if B | S | Hq | D > _INT32_MAX:
+            _fits(max(B, S, Hq, D), "q")
+        if out is not None:
+            if not (isinstance(out, torch.Tensor) and out.shape == shape):
+                _need(out, "out", B, S, Hq, D)
+            if out.dtype is not q.dtype:
+                raise TypeError("out must be %s" % q.dtype)
+            if not out.is_contiguous():
+                _apart(out, "out")
+        if window is None:
+            window = 0
+        elif not 1 <= window <= _INT32_MAX:
+            raise ValueError("window must be 1..2^31 - 1 or None")
+        if not 0 <= sinks <= _INT32_MAX:
+            raise ValueError("sinks must be 0..2^31 - 1")
+        first = cache[0] if isinstance(cache, (tuple, list)) and len(cache) == 2 else None
+        H = first.shape[2] if isinstance(first, (torch.Tensor, QuantRows)) and len(first.shape) == 4 else 1
+        ck, cv, quant = self._pages(cache, "cache", H, D, q.dtype)
+        N = self.dims.max_nodes
+        W = (N + 63) // 64
+        one, i32 = (B,), torch.int32
+        p_table, p_len, p_n, p_mask, p_lse = self._args(
+            (("q", q), ("out", out), ("cache keys", ck), ("cache values", cv)),
+            self._table(page_table, B),
+            ("cache_len", cache_len, i32, one, one),
+            ("n_nodes", n_nodes, i32, one, one),
+            ("mask", mask, torch.int64, (one, N, W), (B, N, W)),
+            ("lse", lse, torch.float32, (B, S, Hq), (B, S, Hq)))
+        if out is None:
+            out = torch.zeros_like(q, memory_format=torch.contiguous_format)
+        dtype, n = _DTYPES[q.dtype], page_table.shape[1]
+        a = PagedAttention(B, S, 1 if with_root else 0, Hq, H, D, dtype, 3 if quant else dtype,
+                           float(D ** -0.5 if scale is None else scale), window, sinks, _rows(q, 3, "q"), p_n,
+                           p_mask, _rows(ck, 3, "cache"), _rows(cv, 3, "cache"),
+                           PageTable(p_table, n, n, ck.shape[0], ck.shape[1]), p_len, _rows(out, 3, "out"), p_lse)
+        return a, out
+
+    def paged_commit(self, cache, page_table, start, acc_len, acc_nodes, with_root=False):
+        """Moves the accepted path's rows up to the front of the block in the pages
+        (graft_paged_commit): cache [planes, pages, page_rows, heads, dim], a tensor or
+        QuantRows; row start[b] + r + acc_nodes[b, i] goes to start[b] + r + i for i <
+        acc_len[b], r = 1 with_root.  start None: 0.  Returns cache."""
+        if not isinstance(cache, (torch.Tensor, QuantRows)):
+            raise TypeError("cache must be a tensor or QuantRows")
+        if len(cache.shape) != 5 or min(cache.shape) < 1:
+            raise ValueError("cache must be [planes, pages, page_rows, heads, dim], got %s" % list(cache.shape))
+        batch = _batch_of(acc_len, "acc_len")
+        P, pages, rows, H, D = cache.shape
+        if P | pages | rows | H | D > _INT32_MAX:
+            _fits(max(P, pages, rows, H, D), "cache")
+        _apart(cache, "cache")
+        kind = 3 if isinstance(cache, QuantRows) else _DTYPES.get(cache.dtype, -1)
+        L, one, i32 = self.dims.num_pos, (batch,), torch.int32
+        if acc_nodes is None:
+            raise ValueError("acc_nodes is required")
+        p_table, p_start, p_acc, p_nodes = self._args(
+            (("cache", cache),),
+            self._table(page_table, batch),
+            ("start", start, i32, (one,), one),
+            ("acc_len", acc_len, i32, (one,), one),
+            ("acc_nodes", acc_nodes, i32, (one, L), (batch, L)))
+        n = page_table.shape[1]
+        a = PagedPath(batch, P, H, D, kind, _rows(cache, 4, "cache"), PageTable(p_table, n, n, pages, rows),
+                      p_start, p_acc, p_nodes, 1 if with_root else 0)
+        _check(lib().graft_paged_commit(self._h, C.byref(a), _stream()), "graft_paged_commit")
+        return cache
 
     def profile_begin(self, max_calls: int):
         _check(lib().graft_profile_begin(self._h, int(max_calls)), "graft_profile_begin")

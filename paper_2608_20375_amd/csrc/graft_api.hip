@@ -304,6 +304,158 @@ int check_move(const graft_ctx *ctx, const graft_cache_move *m, bool write, cons
   return check_device(ctx, who);
 }
 
+// A page table; rows: the fewest that it has to hold.
+int check_pages(const graft_page_table &t, bool pointers, int rows, const char *who) {
+  if (t.pages < 1 || t.page_rows < 1 || t.table_len < 1 || t.table_stride < 0)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: pages, page_rows and table_len must be positive, table_stride not negative",
+                who);
+  if (t.pages > (1 << 30) || t.page_rows > (1 << 20) ||
+      static_cast<int64_t>(t.table_len) * t.page_rows > (int64_t{1} << 30))
+    return fail(GRAFT_ERR_UNSUPPORTED, "%s: more than 2^30 pages, 2^20 rows a page or 2^30 rows a sequence", who);
+  if (static_cast<int64_t>(t.table_len) * t.page_rows < rows)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: a table of %d pages of %d rows holds no block of %d", who, t.table_len,
+                t.page_rows, rows);
+  if (pointers && !t.table) return fail(GRAFT_ERR_INVALID_ARG, "%s: a page table is required", who);
+  return GRAFT_OK;
+}
+
+// A page's rows: offsets inside a page are 32-bit numbers.
+int check_page(const graft_rows &r, int dtype, int rows, int heads, int dim, const char *who, const char *name) {
+  const int rc = check_rows(r, dtype, true, who, name);
+  if (rc != GRAFT_OK) return rc;
+  const int64_t most = int64_t{1} << 30;
+  const int64_t rs = rows > 1 ? r.row_stride : 0, hs = heads > 1 ? r.head_stride : 0;
+  if (rs > most || hs > most || (rows - 1) * rs + (heads - 1) * hs + dim > most)
+    return fail(GRAFT_ERR_UNSUPPORTED, "%s: a page of %s spans more than 2^30 elements", who, name);
+  if (dtype == GRAFT_E4M3) {
+    const int64_t ss = rows > 1 ? r.scale_row_stride : 0, sh = heads > 1 ? r.scale_head_stride : 0;
+    if (ss > most || sh > most || (rows - 1) * ss + (heads - 1) * sh > most)
+      return fail(GRAFT_ERR_UNSUPPORTED, "%s: a page of %s's scales spans more than 2^30 bytes", who, name);
+  }
+  return GRAFT_OK;
+}
+
+int check_heads(int q_heads, int kv_heads, int head_dim, const char *who) {
+  if (kv_heads < 1 || q_heads < 0)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: q_heads %d, kv_heads %d", who, q_heads, kv_heads);
+  if (q_heads > 1024 || kv_heads > 1024)
+    return fail(GRAFT_ERR_UNSUPPORTED, "%s: more than 1024 heads", who);
+  if (head_dim < 16 || head_dim % 16 != 0)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: head_dim %d must be a multiple of 16", who, head_dim);
+  if (head_dim > 128) return fail(GRAFT_ERR_UNSUPPORTED, "%s: head_dim %d > 128", who, head_dim);
+  return GRAFT_OK;
+}
+
+int check_types(int dtype, int cache_dtype, const char *who) {
+  if (dtype != GRAFT_BF16 && dtype != GRAFT_F16)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: dtype %d is neither bf16 (1) nor fp16 (2)", who, dtype);
+  if (cache_dtype != dtype && !(cache_dtype == GRAFT_E4M3 && dtype == GRAFT_BF16))
+    return fail(GRAFT_ERR_UNSUPPORTED, "%s: a cache of type %d with rows of type %d", who, cache_dtype, dtype);
+  return GRAFT_OK;
+}
+
+int check_paged_rows(const graft_ctx *ctx, const graft_paged_rows *r, const char *who) {
+  if (!ctx || !r) return fail(GRAFT_ERR_INVALID_ARG, "%s: NULL argument", who);
+  if (r->batch < 1 || r->batch > ctx->dims.max_batch)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: batch %d outside 1..%d", who, r->batch, ctx->dims.max_batch);
+  if (r->slots < 1) return fail(GRAFT_ERR_INVALID_ARG, "%s: slots %d must be positive", who, r->slots);
+  if (r->slots > (1 << 24)) return fail(GRAFT_ERR_UNSUPPORTED, "%s: slots %d > 2^24", who, r->slots);
+  int rc = check_heads(r->q_heads, r->kv_heads, r->head_dim, who);
+  if (rc == GRAFT_OK) rc = check_types(r->dtype, r->cache_dtype, who);
+  if (rc != GRAFT_OK) return rc;
+  if (r->rot_dim < 0 || r->rot_dim > r->head_dim || r->rot_dim % 16 != 0)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: rot_dim %d must be a multiple of 16 in 0..head_dim", who, r->rot_dim);
+  if (r->rot_dim > 0) {
+    if (!r->freq || reinterpret_cast<uintptr_t>(r->freq) % 8 != 0)
+      return fail(GRAFT_ERR_INVALID_ARG, "%s: a rotation needs freq, 8-byte aligned", who);
+    if (r->positions && (r->axes < 1 || r->axes > 8))
+      return fail(GRAFT_ERR_INVALID_ARG, "%s: axes %d outside 1..8", who, r->axes);
+    if (r->axis && !r->positions)
+      return fail(GRAFT_ERR_INVALID_ARG, "%s: axis needs positions", who);
+  }
+  rc = check_pages(r->pages, true, 1, who);
+  if (rc == GRAFT_OK && r->q_heads > 0) {
+    rc = check_rows(r->q, r->dtype, true, who, "q");
+    if (rc == GRAFT_OK)
+      rc = check_written(r->q_out, r->dtype, {1, r->batch, r->slots, r->q_heads}, r->head_dim, who, "q_out");
+  }
+  if (rc == GRAFT_OK) rc = check_rows(r->k, r->dtype, true, who, "k");
+  if (rc == GRAFT_OK) rc = check_rows(r->v, r->dtype, true, who, "v");
+  const int64_t entries[4] = {1, r->pages.pages, r->pages.page_rows, r->kv_heads};
+  if (rc == GRAFT_OK) rc = check_written(r->cache_k, r->cache_dtype, entries, r->head_dim, who, "cache_k");
+  if (rc == GRAFT_OK) rc = check_written(r->cache_v, r->cache_dtype, entries, r->head_dim, who, "cache_v");
+  if (rc == GRAFT_OK)
+    rc = check_page(r->cache_k, r->cache_dtype, r->pages.page_rows, r->kv_heads, r->head_dim, who, "cache_k");
+  if (rc == GRAFT_OK)
+    rc = check_page(r->cache_v, r->cache_dtype, r->pages.page_rows, r->kv_heads, r->head_dim, who, "cache_v");
+  if (rc == GRAFT_OK && graft::paged_write_blocks(*r) > graft::kMaxBlocks)
+    return fail(GRAFT_ERR_UNSUPPORTED, "%s: too many rows for one call", who);
+  return rc;
+}
+
+int check_paged(const graft_ctx *ctx, const graft_paged_attention_desc *a, bool pointers, const char *who) {
+  if (!ctx || !a) return fail(GRAFT_ERR_INVALID_ARG, "%s: NULL argument", who);
+  const graft_dims &d = ctx->dims;
+  if (a->batch < 1 || a->batch > d.max_batch)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: batch %d outside 1..%d", who, a->batch, d.max_batch);
+  if (a->slots < 1) return fail(GRAFT_ERR_INVALID_ARG, "%s: slots %d must be positive", who, a->slots);
+  if (a->slots > (1 << 20)) return fail(GRAFT_ERR_UNSUPPORTED, "%s: slots %d > 2^20", who, a->slots);
+  int rc = check_heads(a->q_heads, a->kv_heads, a->head_dim, who);
+  if (rc == GRAFT_OK) rc = check_types(a->dtype, a->cache_dtype, who);
+  if (rc != GRAFT_OK) return rc;
+  if (a->q_heads < 1 || a->q_heads % a->kv_heads != 0)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: q_heads %d must be a positive multiple of kv_heads %d", who, a->q_heads,
+                a->kv_heads);
+  if (!std::isfinite(a->scale) || !(a->scale > 0.0f))
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: scale must be positive and finite", who);
+  if (a->scale > 1e38f) return fail(GRAFT_ERR_UNSUPPORTED, "%s: scale over 1e38", who);   // times log2 e
+  if (a->window < 0 || a->sinks < 0)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: window and sinks must not be negative", who);
+  if (static_cast<int64_t>(a->batch) * a->slots * a->q_heads > (int64_t{1} << 30))
+    return fail(GRAFT_ERR_UNSUPPORTED, "%s: more than 2^30 query rows", who);
+  rc = check_pages(a->pages, pointers, a->slots, who);
+  if (rc != GRAFT_OK || !pointers) return rc;
+  if (a->mask) {
+    const int most = d.max_nodes + (a->with_root ? 1 : 0);
+    if (a->slots > most)
+      return fail(GRAFT_ERR_INVALID_ARG, "%s: slots %d with a mask outside 1..%d", who, a->slots, most);
+    if (a->window > 0 && a->window <= d.num_pos)
+      return fail(GRAFT_ERR_INVALID_ARG, "%s: a window of %d does not hold a path of %d nodes", who, a->window,
+                  d.num_pos);
+  }
+  if (!a->cache_len) return fail(GRAFT_ERR_INVALID_ARG, "%s: cache_len is required", who);
+  rc = check_rows(a->q, a->dtype, true, who, "q");
+  if (rc == GRAFT_OK)
+    rc = check_written(a->out, a->dtype, {1, a->batch, a->slots, a->q_heads}, a->head_dim, who, "out");
+  if (rc == GRAFT_OK)
+    rc = check_page(a->cache_k, a->cache_dtype, a->pages.page_rows, a->kv_heads, a->head_dim, who, "cache_k");
+  if (rc == GRAFT_OK)
+    rc = check_page(a->cache_v, a->cache_dtype, a->pages.page_rows, a->kv_heads, a->head_dim, who, "cache_v");
+  return rc;
+}
+
+int check_path(const graft_ctx *ctx, const graft_paged_path *p, const char *who) {
+  if (!ctx || !p || !p->acc_len || !p->acc_nodes) return fail(GRAFT_ERR_INVALID_ARG, "%s: NULL argument", who);
+  if (p->batch < 1 || p->batch > ctx->dims.max_batch)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: batch %d outside 1..%d", who, p->batch, ctx->dims.max_batch);
+  if (p->n_planes < 1 || p->heads < 1)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: n_planes and heads must be positive", who);
+  if (p->n_planes > (1 << 20)) return fail(GRAFT_ERR_UNSUPPORTED, "%s: more than 2^20 planes", who);
+  int rc = check_heads(0, p->heads, p->head_dim, who);
+  if (rc != GRAFT_OK) return rc;
+  if (p->dtype != GRAFT_BF16 && p->dtype != GRAFT_F16 && p->dtype != GRAFT_E4M3)
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: dtype %d is none of bf16 (1), fp16 (2), e4m3 (3)", who, p->dtype);
+  rc = check_pages(p->pages, true, 1, who);
+  if (rc == GRAFT_OK)
+    rc = check_written(p->rows, p->dtype, {p->n_planes, p->pages.pages, p->pages.page_rows, p->heads}, p->head_dim, who,
+                       "rows");
+  if (rc == GRAFT_OK)
+    rc = check_page(p->rows, p->dtype, p->pages.page_rows, p->heads, p->head_dim, who, "rows");
+  if (rc == GRAFT_OK && graft::paged_commit_blocks(*p) > graft::kMaxBlocks)
+    return fail(GRAFT_ERR_UNSUPPORTED, "%s: too many rows to move in one call", who);
+  return rc;
+}
+
 }  // namespace
 
 extern "C" {
@@ -715,6 +867,52 @@ int graft_cache_read(graft_ctx *ctx, const graft_cache_move *m, graft_stream_t s
   const int rc = check_move(ctx, m, false, who);
   if (rc != GRAFT_OK) return rc;
   const hipError_t e = graft::launch_cache_read(ctx, *m, reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, who);
+  return GRAFT_OK;
+}
+
+int graft_paged_write(graft_ctx *ctx, const graft_paged_rows *r, graft_stream_t stream) {
+  const char *who = "graft_paged_write";
+  int rc = check_paged_rows(ctx, r, who);
+  if (rc == GRAFT_OK) rc = check_device(ctx, who);
+  if (rc != GRAFT_OK) return rc;
+  const hipError_t e = graft::launch_paged_write(ctx, *r, reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, who);
+  return GRAFT_OK;
+}
+
+int graft_paged_attention_workspace(graft_ctx *ctx, const graft_paged_attention_desc *a, int64_t *bytes) {
+  if (!bytes) return fail(GRAFT_ERR_INVALID_ARG, "graft_paged_attention_workspace: NULL argument");
+  const int rc = check_paged(ctx, a, false, "graft_paged_attention_workspace");
+  if (rc != GRAFT_OK) return rc;
+  *bytes = graft::paged_plan(*a).bytes;
+  return GRAFT_OK;
+}
+
+int graft_paged_attention(graft_ctx *ctx, const graft_paged_attention_desc *a, graft_stream_t stream) {
+  const char *who = "graft_paged_attention";
+  int rc = check_paged(ctx, a, true, who);
+  if (rc != GRAFT_OK) return rc;
+  const graft::PagedPlan p = graft::paged_plan(*a);
+  if (p.blocks > graft::kMaxBlocks || p.merge_blocks > graft::kMaxBlocks)
+    return fail(GRAFT_ERR_UNSUPPORTED, "%s: too many query rows and keys for one call", who);
+  rc = check_device(ctx, who);
+  if (rc != GRAFT_OK) return rc;
+  if (p.bytes > 0 && (!a->workspace || (reinterpret_cast<uintptr_t>(a->workspace) & 15u) != 0 ||
+                      a->workspace_bytes < p.bytes))
+    return fail(GRAFT_ERR_INVALID_ARG, "%s: needs a 16-byte aligned workspace of %lld bytes", who,
+                static_cast<long long>(p.bytes));
+  const hipError_t e = graft::launch_paged_attend(ctx, *a, p, reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, who);
+  return GRAFT_OK;
+}
+
+int graft_paged_commit(graft_ctx *ctx, const graft_paged_path *p, graft_stream_t stream) {
+  const char *who = "graft_paged_commit";
+  int rc = check_path(ctx, p, who);
+  if (rc == GRAFT_OK) rc = check_device(ctx, who);
+  if (rc != GRAFT_OK) return rc;
+  const hipError_t e = graft::launch_paged_commit(ctx, *p, reinterpret_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, who);
   return GRAFT_OK;
 }

@@ -312,7 +312,21 @@ hipError_t launch_cache_read(graft_ctx *ctx, const graft_cache_move &m, hipStrea
 // Workgroups of 256 threads that a launch holds: it counts its threads in 32 bits.
 constexpr int64_t kMaxBlocks = (int64_t{1} << 24) - 1;
 // Bits of a context's error flag set by these (1, 2 and 4 are the round's).
-constexpr uint32_t kErrBlockSizes = 8u, kErrTargetRow = 16u, kErrCacheRow = 32u;
+constexpr uint32_t kErrBlockSizes = 8u, kErrTargetRow = 16u, kErrCacheRow = 32u, kErrPage = 64u;
+// Rows in pages: the table as the kernels use it, the paged attention's cut, and the launches.
+struct PageMap;
+PageMap page_map(const graft_page_table &t);
+struct PagedPlan {
+  int64_t bytes;                  // workspace
+  int64_t blocks, merge_blocks;   // workgroups of the two launches
+};
+PagedPlan paged_plan(const graft_paged_attention_desc &a);
+hipError_t launch_paged_attend(graft_ctx *ctx, const graft_paged_attention_desc &a, const PagedPlan &p,
+                               hipStream_t stream);
+int64_t paged_write_blocks(const graft_paged_rows &r);
+hipError_t launch_paged_write(graft_ctx *ctx, const graft_paged_rows &r, hipStream_t stream);
+int64_t paged_commit_blocks(const graft_paged_path &p);
+hipError_t launch_paged_commit(graft_ctx *ctx, const graft_paged_path &p, hipStream_t stream);
 hipError_t launch_synth_targets(graft_ctx *ctx, int batch, uint64_t seed,
                                 const int32_t *root_token, const int32_t *n_nodes,
                                 const int32_t *tokens, const int32_t *parents,

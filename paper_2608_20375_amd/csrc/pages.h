@@ -1,0 +1,59 @@
+// pages.h -- rows in pages: which page holds a sequence's row, and which keys a tile of rows of
+// the paged attention walks.  Integers alone, the same for the kernels and for a host program
+// that includes this.
+#pragma once
+
+#include <stdint.h>
+
+namespace graft {
+
+// Row r < 2^31 is in entry r / page_rows of its sequence's table.  With 2^(l-1) < page_rows <= 2^l
+// the quotient is (r * mul) >> (31 + l), mul = ceil(2^(31 + l) / page_rows) <= 2^32 - 1: the
+// product is off by r * e, e < page_rows <= 2^l, so by less than 2^(31 + l).
+struct PageMap {
+  const int32_t *table;
+  int64_t table_stride;
+  int32_t table_len, pages, page_rows;
+  uint32_t mul;
+  int32_t shift;
+  __host__ __device__ __forceinline__ int entry(uint32_t r) const {
+    return static_cast<int>((static_cast<uint64_t>(r) * mul) >> shift);
+  }
+  __host__ __device__ __forceinline__ int rows() const { return table_len * page_rows; }
+};
+inline void set_division(PageMap &m) {
+  int l = 0;
+  while ((int64_t{1} << l) < m.page_rows) ++l;
+  m.shift = 31 + l;
+  m.mul = static_cast<uint32_t>(((uint64_t{1} << m.shift) + m.page_rows - 1) / m.page_rows);
+}
+
+// The keys that a tile of query rows may see, rows [0, sinks) and [low, end), in tiles of `keys`
+// keys that begin at multiples of it: the first n0 tiles, then n1 from tile `first` on.
+struct Span {
+  int n0, first, n1;
+  __host__ __device__ __forceinline__ int all() const { return n0 + n1; }
+  __host__ __device__ __forceinline__ int at(int t) const { return t < n0 ? t : first + t - n0; }
+};
+__host__ __device__ __forceinline__ Span span_of(int low, int sinks, int end, int keys) {
+  low = low < 0 ? 0 : low > end ? end : low;
+  const int s = sinks < end ? sinks : end;
+  const int a = (s + keys - 1) / keys, b = low / keys;
+  Span w;
+  w.n0 = a < b ? a : 0;
+  w.first = a < b ? b : 0;
+  w.n1 = (end + keys - 1) / keys - w.first;
+  return w;
+}
+
+// The first row that a window at position p shows.
+__host__ __device__ __forceinline__ int window_low(int p, int window) {
+  return window > 0 && p - window + 1 > 0 ? p - window + 1 : 0;
+}
+
+// The lowest n of 64 bits.
+__host__ __device__ __forceinline__ uint64_t low_bits(int n) {
+  return n <= 0 ? 0 : n >= 64 ? ~0ull : (1ull << n) - 1;
+}
+
+}  // namespace graft

@@ -344,7 +344,7 @@ def _context(s):
             s["cache"] = G.QuantRows(s["codes"], s["scales"])
     depth = case["most"] if case["kind"] == "commit" else 16
     batch = max(case["batch"], s["pages"]) if case["kind"] == "write" else case["batch"]
-    return G.Context(batch, depth, 64, 1, max(depth, min(1024, case["slots"] - 1)))
+    return G.Context(batch, depth, 64, 1, max(1, min(1024, case["slots"] - 1)))
 
 
 # ---------------------------------------------------------------------------

@@ -317,6 +317,10 @@ constexpr uint32_t kErrBlockSizes = 8u, kErrTargetRow = 16u, kErrCacheRow = 32u,
 struct PageMap;
 PageMap page_map(const graft_page_table &t);
 struct PagedPlan {
+  int few;            // a sequence's rows fit one tile of 16 (1) or 32 (2): the narrow walk
+  int row_tiles;      // tiles of 128 rows of a sequence and key head
+  int splits;         // parts of a row tile's keys at most
+  int min_rounds;     // rounds (narrow: of four 32-key tiles, wide: a 64-key tile) of a part at least
   int64_t bytes;                  // workspace
   int64_t blocks, merge_blocks;   // workgroups of the two launches
 };

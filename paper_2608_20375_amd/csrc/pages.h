@@ -51,6 +51,33 @@ __host__ __device__ __forceinline__ int window_low(int p, int window) {
   return window > 0 && p - window + 1 > 0 ? p - window + 1 : 0;
 }
 
+// What slots s0 .. s1 of a block of n slots walk, which lies behind `base` rows: the tiles, the rows'
+// end, and the rows that every slot sees (those before clear_end that are from clear_low on, or
+// among the sinks).  A chain's slot i is at position base + i; a masked one's position is at least
+// base - 1 (it may see nothing) and at most base + n - 1.  per: tiles of a part, in rounds of
+// `turns` tiles, at least min_rounds of them; parts: how many parts there are, at most `splits`.
+struct RowTile {
+  Span span;
+  int end, clear_low, clear_end, per, parts;
+};
+__host__ __device__ __forceinline__ RowTile row_tile(int base, int n, int s0, int s1, bool masked, int window,
+                                                     int sinks, int keys, int turns, int splits, int min_rounds) {
+  RowTile t;
+  t.end = masked ? base + n : base + s1 + 1;
+  t.span = span_of(window_low(base + (masked ? -1 : s0), window), window > 0 ? sinks : 0, t.end, keys);
+  t.clear_low = window_low(base + (masked ? n - 1 : s1), window);
+  t.clear_end = masked ? base : base + s0 + 1;
+  const int rounds = (t.span.all() + turns - 1) / turns, even = (rounds + splits - 1) / splits;
+  t.per = (even > min_rounds ? even : min_rounds) * turns;
+  t.parts = (t.span.all() + t.per - 1) / t.per;
+  return t;
+}
+
+// Whether every slot of the tile sees all rows j .. j + keys - 1.
+__host__ __device__ __forceinline__ bool is_clear(const RowTile &t, int j, int keys, int sinks) {
+  return j + keys <= t.clear_end && (j >= t.clear_low || j + keys <= sinks);
+}
+
 // The lowest n of 64 bits.
 __host__ __device__ __forceinline__ uint64_t low_bits(int n) {
   return n <= 0 ? 0 : n >= 64 ? ~0ull : (1ull << n) - 1;

@@ -894,7 +894,7 @@ int graft_paged_attention(graft_ctx *ctx, const graft_paged_attention_desc *a, g
   int rc = check_paged(ctx, a, true, who);
   if (rc != GRAFT_OK) return rc;
   const graft::PagedPlan p = graft::paged_plan(*a);
-  if (p.blocks > graft::kMaxBlocks || p.merge_blocks > graft::kMaxBlocks)
+  if (!p.fits || p.blocks > graft::kMaxBlocks || p.merge_blocks > graft::kMaxBlocks)
     return fail(GRAFT_ERR_UNSUPPORTED, "%s: too many query rows and keys for one call", who);
   rc = check_device(ctx, who);
   if (rc != GRAFT_OK) return rc;

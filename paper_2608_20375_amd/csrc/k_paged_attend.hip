@@ -31,7 +31,7 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kWideRows = 128, kWideKeys = 64;    // wide_part
 constexpr int kFewRows = 32, kFewKeys = 32;       // narrow_part; keys of one wave's tile
-constexpr int kMaxParts = 64;                     // one a lane of the merge
+constexpr int kMaxPieces = 128;                   // of a row's keys: four a lane of the merge
 
 struct Pool {                 // keys or values of one layer; bytes
   const char *p;
@@ -55,9 +55,20 @@ struct PagedArgs {
   int64_t rows_all;       // batch * slots * q_heads
   int32_t batch, slots, root, q_heads, kv_heads, group, dim;
   int32_t n_max, words, window, sinks;
-  int32_t row_tiles, splits, min_rounds;
+  int32_t tile_rows, row_tiles;   // rows of a row tile, and how many a sequence and key head has
+  int32_t groups;         // that share all rounds; 0: a workgroup for each row tile's whole walk
+  int32_t *share;         // rounds of a group, then [batch] each sequence's first round
   float c;
 };
+
+// The arguments, read again where they are used: what a loop does not use would otherwise be kept over
+// it in scalar registers, which spill into vector ones, lane by lane.
+typedef const __attribute__((address_space(4))) PagedArgs Late;
+__device__ __forceinline__ const PagedArgs &late() {
+  Late *p = (Late *)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const PagedArgs *)p;
+}
 
 // Slots and cache length of sequence b as the kernels use them.
 struct Sizes {
@@ -136,64 +147,82 @@ __device__ __forceinline__ Spot spot_at(const PagedArgs &a, int page, int j, int
   s.page = s.bad ? 0 : page;
   return s;
 }
-__device__ __forceinline__ const char *row_at(const char *head, int64_t page_bytes, uint32_t row_bytes, int page, uint32_t off) {
-  return head + page * page_bytes + static_cast<uint64_t>(off * row_bytes);
+// Bytes from a head's first row in page 0.
+__device__ __forceinline__ int64_t row_at(const Pool &p, const Spot &s) {
+  return s.page * p.page + static_cast<uint64_t>(s.off * p.row);
+}
+__device__ __forceinline__ int64_t scale_at(const Pool &p, const Spot &s) {
+  return s.page * p.s_page + static_cast<uint64_t>(s.off * p.s_row);
 }
 __device__ __forceinline__ u32x4 take16(const char *p) { return *reinterpret_cast<const u32x4 *>(p); }
+__device__ __forceinline__ u32x4 stream16(const char *p) {
+  return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p));
+}
+
+__device__ __forceinline__ int64_t read_lane64(int64_t x, int lane) {
+  const uint64_t u = static_cast<uint64_t>(x);
+  const uint32_t lo = __builtin_amdgcn_readlane(static_cast<uint32_t>(u), lane);
+  const uint32_t hi = __builtin_amdgcn_readlane(static_cast<uint32_t>(u >> 32), lane);
+  return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
+}
 
 // Both 16-lane rows' values of a lane's column: x of lane col (+ 32) and of lane col + 16 (+ 32).
 __device__ __forceinline__ u32x2 both_rows(uint32_t x) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(x, x, false, false));
 }
+// Lanes 8 .. 15 of every 16 get y of lanes 0 .. 7, the others keep x; and the other way round.
+__device__ __forceinline__ uint32_t upper_from(uint32_t x, uint32_t y) {
+  return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(static_cast<int>(x), static_cast<int>(y), 0x128, 0xF, 0xC, false));
+}
+__device__ __forceinline__ uint32_t lower_from(uint32_t x, uint32_t y) {
+  return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(static_cast<int>(x), static_cast<int>(y), 0x128, 0xF, 0x3, false));
+}
+// The x of keys 8 u + lane % 8, u < 4, where lane l holds key l % 32's.
+__device__ __forceinline__ u32x4 of_eights(uint32_t x) {
+  const u32x2 r = both_rows(x);
+  return u32x4{upper_from(r.x, r.x), lower_from(r.x, r.x), upper_from(r.y, r.y), lower_from(r.y, r.y)};
+}
+
+// Waits for all memory operations.  With a store in flight the compiler takes loads to come back in any
+// order, and every wait for one of them to be a wait for all: a loop that keeps loads in flight begins without.
+__device__ __forceinline__ void drain() { __builtin_amdgcn_s_waitcnt(0x0F70); }
 
 // Four numbers of the values' row of key j, for rows that see infinite or NaN ones.
 template <typename T, bool Q8>
 __device__ __forceinline__ u32x2 four_at(const PagedArgs &a, const char *v_head, const uint8_t *vs_head, const Spot &s, int x) {
-  const char *p = row_at(v_head, a.v.page, a.v.row, s.page, s.off);
+  const char *p = v_head + row_at(a.v, s);
   if (!Q8) return *reinterpret_cast<const u32x2 *>(p + 2 * x);
-  const uint32_t unit = vs_head[s.page * a.v.s_page + static_cast<uint64_t>(s.off * a.v.s_row)];
+  const uint32_t unit = vs_head[scale_at(a.v, s)];
   return widen(*reinterpret_cast<const uint32_t *>(p + x), unit_of(unit));
 }
-
-struct Item {
-  int b, kvh, tile_row, part;
-};
 
 // Rows of a row in the outputs.
 __device__ __forceinline__ void finish(const PagedArgs &a, int64_t all, float m, float l, float at) {
   a.lse[all] = l == 0.0f ? -INFINITY : (m * a.c + (__log2f(l) - at)) * 0.69314718055994531f;
 }
 
-// 16 or 32 rows a workgroup, all of a sequence's and key head's: every wave walks 32-key tiles of
+// 16 or 32 rows, all of a sequence's and key head's, over tiles t0 .. t1 - 1: every wave walks 32-key tiles of
 // its own, keys from memory straight into fragments, values through a stretch of LDS of the wave's
 // own, no barriers; the waves' sums are joined at the end.
-template <typename T, bool Q8, bool FULL, int DP, int QT>
-__device__ __forceinline__ void narrow_part(const PagedArgs &a, const Item &it, u32x4 *lds) {
+// part: where in the workspace the sums go, or -1: they are all there is.
+template <typename T, bool Q8, bool HOT, int DP, int QT>
+__device__ __forceinline__ void narrow_part(const PagedArgs &a, int b, int kvh, int live, int len, const RowTile &tile, int t0,
+                                            int t1, int part, u32x4 *lds) {
   constexpr int C = DP / 8, kSteps = DP / 32, kDTiles = DP / 16;
   constexpr int kLoads = Q8 ? DP / 64 : kSteps;         // 16-byte loads of a lane and 16 keys
   constexpr int kBytes = Q8 ? 1 : 2;
   constexpr int kPad = DP + 4;                          // floats of a row when the waves are joined
-  const int tid = threadIdx.x, lane = lane_id();
-  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));     // a piece's own: what follows from it is not kept over all pieces
+  const int lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int quarter = lane >> 4, col = lane & 15;
-  const int b = it.b, kvh = it.kvh;
   u32x4 *s_v = lds + wave * kFewKeys * C;
 
-  const Sizes sz = sizes_of(a, b);
-  const int live = __builtin_amdgcn_readfirstlane(sz.n), len = __builtin_amdgcn_readfirstlane(sz.len);
-  if (sz.bad && it.part == 0 && kvh == 0 && tid == 0) atomicOr(a.error_flag, kErrBlockSizes);
-  if (live == 0) return;
-  const RowTile tile = row_tile(len, live, 0, live - 1, a.mask != nullptr, a.window, a.sinks, kFewKeys, kWaves, a.splits, a.min_rounds);
-  if (it.part >= tile.parts) return;
-  const bool alone = tile.parts == 1;
-  const int t0 = it.part * tile.per, t1 = std::min(t0 + tile.per, tile.span.all());
-
   // slot and query head of row i
-  const int rows = live * a.group;
-  auto place = [&](int i, int *slot, int *head) {
-    const int row = i < rows ? i : rows - 1;
-    *slot = row / a.group;
-    *head = kvh * a.group + row - *slot * a.group;
+  auto place = [&](const PagedArgs &z, int i, int *slot, int *head) {
+    const int rows = live * z.group, row = i < rows ? i : rows - 1;
+    *slot = row / z.group;
+    *head = kvh * z.group + row - *slot * z.group;
     return i < rows;
   };
 
@@ -201,16 +230,17 @@ __device__ __forceinline__ void narrow_part(const PagedArgs &a, const Item &it, 
   // load brings are two steps' 8.
   auto k_chunk = [&](int s) { return Q8 ? 2 * (4 * (s / 2) + quarter) + s % 2 : 4 * s + quarter; };
   u32x4 rq[QT][kSteps];
-  View view[QT];
+  {
+    const PagedArgs &z = late();
 #pragma unroll
-  for (int q = 0; q < QT; ++q) {
-    int slot, head;
-    place(q * 16 + col, &slot, &head);
-    view[q] = view_of(a, b, slot, len, live);
-    const char *qp = a.q + b * a.q_batch + slot * a.q_slot + head * a.q_head;
+    for (int q = 0; q < QT; ++q) {
+      int slot, head;
+      place(z, q * 16 + col, &slot, &head);
+      const char *qp = z.q + b * z.q_batch + slot * z.q_slot + head * z.q_head;
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s)
-      rq[q][s] = k_chunk(s) * 8 < a.dim ? take16(qp + k_chunk(s) * 16) : u32x4{0, 0, 0, 0};
+      for (int s = 0; s < kSteps; ++s)
+        rq[q][s] = HOT || k_chunk(s) * 8 < z.dim ? take16(qp + k_chunk(s) * 16) : u32x4{0, 0, 0, 0};
+    }
   }
 
   const int32_t *table = a.pages.table + b * a.pages.table_stride;
@@ -218,44 +248,142 @@ __device__ __forceinline__ void narrow_part(const PagedArgs &a, const Item &it, 
   const uint8_t *ks_head = a.k.s + kvh * a.k.s_head, *vs_head = a.v.s + kvh * a.v.s_head;
   const int mine = lane & 31;                           // the key of a tile whose page this lane looks up
 
+  // Loads of a tile.  A cache line is 128 bytes, and a load of 16 rows of 64 would bring each line
+  // for one half of it, the other coming 16 loads later: so a load takes whole lines of 8 rows, lane
+  // (quarter, col) chunk quarter + 4 (col / 8) of row 8 u + col % 8.  The values go to LDS as they
+  // come; two loads' keys change halves (col's and col + 8's) to be rows col of chunks quarter
+  // and quarter + 4.  Rows of 64 bytes are taken 16 at a time.  Keys are read once: the loads are
+  // non-temporal (random 4 KB pieces are read at 6.6 TB/s so, at 5.8 without).
+  constexpr bool kLines = kLoads > 1;
+  constexpr int kSets = kLines ? 4 : 2, kEach = kLines ? kLoads / 2 : 1;   // rows of a lane, loads of a row
+  const int mine_ch = kLines ? quarter + (col >> 3) * 4 : quarter, mine_row = kLines ? col & 7 : col;
   struct Held {                                         // a tile on its way
-    u32x4 rk[2][kLoads], rv[2][kLoads];                 // rows col and 16 + col
-    uint32_t sk, sv;                                    // scales of row `mine`
+    u32x4 rk[kSets][kEach], rv[kSets][kEach];
+    uint32_t sk[2], sv[2];                              // scales of rows col and 16 + col
     int j;                                              // first key
     uint32_t bad;                                       // keys on pages that there are none of
-  } x;
-  int ahead = t0 + wave, next = 0;                      // the tile to load next, this lane's page of it
-  if (ahead < t1) next = entry_at(a, table, tile.span.at(ahead) * kFewKeys + mine, tile.end);
-  auto fetch = [&]() {
-    if (ahead >= t1) return;
-    x.j = tile.span.at(ahead) * kFewKeys;
-    const Spot s = spot_at(a, next, x.j + mine, tile.end);
-    x.bad = static_cast<uint32_t>(__ballot(s.bad));
-    const u32x2 page = both_rows(static_cast<uint32_t>(s.page)), off = both_rows(s.off);
+  };
+  // The loads are made in every step, past the end of the last tile's again: a load that is only made
+  // sometimes would have to be waited for with all those before it.
+  //
+  // HOT: pages of 16 rows or a multiple, so that a tile's halves lie in a page each, and keys and values
+  // at the same places of their pools.  Lanes 0 .. 31 work out where the first half begins, the others the
+  // second; a lane's own rows are at offsets that never change.
+  uint32_t lane_off[2] = {0, 0}, scale_off = 0;
+  if (HOT) {
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
-      const char *p = row_at(k_head, a.k.page, a.k.row, static_cast<int>(page[kt]), off[kt]);
+    for (int s = 0; s < 2; ++s) lane_off[s] = (8 * s + mine_row) * a.k.row + mine_ch * 16;
+    scale_off = col * a.k.s_row;
+  }
+  const int64_t to_v = v_head - k_head, to_vs = vs_head - ks_head;
+  int ahead = t0 + wave;                                // the tile to load next
+  int next = 0;                                         // this lane's page of it
+  uint32_t next_off = 0;                                // and row there
+  auto tile_at = [&](int t) { return tile.span.at(t < t1 ? t : t1 - 1) * kFewKeys; };
+  auto look_up = [&](int t) {
+    const int j = tile_at(t);
+    if (HOT) {
+      const uint32_t r = lane < 32 || j + 16 >= tile.end ? j : j + 16;
+      const int e = a.pages.entry(r);
+      next_off = r - e * a.pages.page_rows;
+      next = table[e];
+    } else {
+      next = entry_at(a, table, j + mine, tile.end);
+    }
+  };
+  look_up(ahead);
+  // where the next tile's rows are: worked out before the last loads are waited for
+  struct Where {
+    const char *k[2];
+    const uint8_t *s[2];
+    int64_t at;
+    int64_t s_at;
+    int j;
+    uint32_t bad;
+  };
+  auto find = [&](Where &w) {
+    w.j = tile_at(ahead);
+    if (HOT) {
+      Spot s;
+      s.bad = static_cast<uint32_t>(next) >= static_cast<uint32_t>(a.pages.pages);
+      s.page = s.bad ? 0 : next;
+      s.off = next_off;
+      const uint64_t bad = __ballot(s.bad);
+      w.bad = (bad & 1 ? 0xFFFFu : 0u) | (bad >> 63 ? 0xFFFF0000u : 0u);
+      const int64_t at = row_at(a.k, s), s_at = Q8 ? scale_at(a.k, s) : 0;
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const int at = (4 * i + quarter) * 16;
-        x.rk[kt][i] = take16(p + (FULL || at < kBytes * a.dim ? at : 0));
+      for (int kt = 0; kt < 2; ++kt) {
+        w.k[kt] = k_head + read_lane64(at, 32 * kt);
+        w.s[kt] = Q8 ? ks_head + read_lane64(s_at, 32 * kt) : nullptr;
+      }
+    } else {
+      const Spot s = spot_at(a, next, w.j + mine, tile.end);
+      w.bad = static_cast<uint32_t>(__ballot(s.bad));
+      w.k[0] = k_head + row_at(a.k, s);                 // this lane's
+      w.at = row_at(a.v, s);
+      if (Q8) {
+        w.s[0] = ks_head + scale_at(a.k, s);
+        w.s_at = scale_at(a.v, s);
       }
     }
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
-      const char *p = row_at(v_head, a.v.page, a.v.row, static_cast<int>(page[kt]), off[kt]);
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const int at = (4 * i + quarter) * 16;
-        x.rv[kt][i] = take16(p + (FULL || at < kBytes * a.dim ? at : 0));
-      }
-    }
-    if (Q8) {
-      x.sk = ks_head[s.page * a.k.s_page + static_cast<uint64_t>(s.off * a.k.s_row)];
-      x.sv = vs_head[s.page * a.v.s_page + static_cast<uint64_t>(s.off * a.v.s_row)];
-    }
+    look_up(ahead + kWaves);
     ahead += kWaves;
-    if (ahead < t1) next = entry_at(a, table, tile.span.at(ahead) * kFewKeys + mine, tile.end);
+  };
+  // a side's loads: `p` is where key `mine` lies
+  auto side = [&](const char *p, u32x4 (&r)[kSets][kEach]) {
+    const uint64_t at = reinterpret_cast<uint64_t>(p);
+    const uint32_t lo = static_cast<uint32_t>(at), hi = static_cast<uint32_t>(at >> 32);
+    u32x4 l4, h4;
+    if (kLines) {
+      l4 = of_eights(lo);
+      h4 = of_eights(hi);
+    } else {
+      const u32x2 l2 = both_rows(lo), h2 = both_rows(hi);
+      l4 = u32x4{l2.x, l2.y, 0, 0};
+      h4 = u32x4{h2.x, h2.y, 0, 0};
+    }
+#pragma unroll
+    for (int u = 0; u < kSets; ++u) {
+      const char *q = reinterpret_cast<const char *>(static_cast<uint64_t>(h4[u]) << 32 | l4[u]);
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const int c0 = (8 * i + mine_ch) * 16;
+        r[u][i] = stream16(q + (c0 < kBytes * a.dim ? c0 : 0));
+      }
+    }
+  };
+  // The next tile's keys, and then its values, into the registers that are free of the last ones.
+  auto fetch_keys = [&](Held &x, const Where &w) {
+    x.j = w.j;
+    x.bad = w.bad;
+    if (HOT) {
+#pragma unroll
+      for (int kt = 0; kt < 2 && Q8; ++kt) {
+        x.sk[kt] = w.s[kt][scale_off];
+        x.sv[kt] = (w.s[kt] + to_vs)[scale_off];
+      }
+#pragma unroll
+      for (int u = 0; u < kSets; ++u)
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) x.rk[u][i] = stream16(w.k[kLines ? u / 2 : u] + lane_off[kLines ? u % 2 : 0] + 128 * i);
+    } else {
+      if (Q8) {
+        x.sk[0] = *w.s[0];                              // of row `mine`
+        x.sv[0] = vs_head[w.s_at];
+      }
+      side(w.k[0], x.rk);
+    }
+  };
+  auto fetch_values = [&](Held &x, const Where &w) {
+    if (HOT) {
+#pragma unroll
+      for (int u = 0; u < kSets; ++u)
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+          x.rv[u][i] = stream16(w.k[kLines ? u / 2 : u] + to_v + lane_off[kLines ? u % 2 : 0] + 128 * i);
+    } else {
+      side(v_head + w.at, x.rv);
+    }
   };
 
   f32x4 o[QT][kDTiles];
@@ -270,58 +398,78 @@ __device__ __forceinline__ void narrow_part(const PagedArgs &a, const Item &it, 
     for (int d = 0; d < kDTiles; ++d) o[q][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
 
-  fetch();
-  for (int t = t0 + wave; t < t1; t += kWaves) {
+  auto step = [&](Held &x) {
     const int j = x.j;
     const uint32_t bad = x.bad;
     const bool clear = bad == 0 && is_clear(tile, j, kFewKeys, a.sinks);
-    if (bad != 0 && lane == 0) atomicOr(a.error_flag, kErrPage);
+    Where w;
+    find(w);
+    __builtin_amdgcn_sched_barrier(0);
+    uint32_t unit_k[2] = {x.sk[0], x.sk[1]}, unit_v[2] = {x.sv[0], x.sv[1]};
+    if (Q8 && !HOT) {
+      const u32x2 sk = both_rows(x.sk[0]), sv = both_rows(x.sv[0]);
+      unit_k[0] = sk.x;
+      unit_k[1] = sk.y;
+      unit_v[0] = sv.x;
+      unit_v[1] = sv.y;
+    }
     f32x4 s[QT][2];
 #pragma unroll
     for (int q = 0; q < QT; ++q) s[q][0] = s[q][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    const u32x2 sk = Q8 ? both_rows(x.sk) : u32x2{0, 0}, sv = Q8 ? both_rows(x.sv) : u32x2{0, 0};
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
-      const float uk = unit_of(sk[kt]);
+      const float uk = Q8 ? unit_of(unit_k[kt]) : 0.0f;
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
+        u32x4 r = x.rk[kt][0];
+        if (kLines) {
+          const u32x4 &lo = x.rk[2 * kt][i / 2], &hi = x.rk[2 * kt + 1][i / 2];
+#pragma unroll
+          for (int y = 0; y < 4; ++y) r[y] = i % 2 == 0 ? upper_from(lo[y], hi[y]) : lower_from(hi[y], lo[y]);
+        }
         u32x4 f[2];
         if (Q8) {
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
-            const u32x2 z = widen(x.rk[kt][i][y], uk);
+            const u32x2 z = widen(r[y], uk);
             f[y / 2][2 * (y % 2)] = z.x;
             f[y / 2][2 * (y % 2) + 1] = z.y;
           }
         } else {
-          f[0] = x.rk[kt][i];
+          f[0] = r;
         }
         // past the head's numbers the queries hold zeros, which an infinite key would not leave so
-        if (!FULL && (4 * i + quarter) * 16 >= kBytes * a.dim) f[0] = f[1] = u32x4{0, 0, 0, 0};
+        if (!HOT && (4 * i + quarter) * 16 >= kBytes * a.dim) f[0] = f[1] = u32x4{0, 0, 0, 0};
 #pragma unroll
         for (int y = 0; y < (Q8 ? 2 : 1); ++y)
 #pragma unroll
           for (int q = 0; q < QT; ++q) s[q][kt] = T::mfma(f[y], rq[q][Q8 ? 2 * i + y : i], s[q][kt]);
       }
     }
+    fetch_keys(x, w);
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
-      const int r = 16 * kt + col;
-      const float uv = unit_of(sv[kt]);
+    for (int u = 0; u < kSets; ++u) {
+      const int r = (kLines ? 8 : 16) * u + mine_row;
+      float uv = 0.0f;
+      if (Q8) {
+        const uint32_t z = unit_v[kLines ? u / 2 : u];
+        uv = unit_of(!kLines ? z : u % 2 == 0 ? upper_from(z, z) : lower_from(z, z));
+      }
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
+      for (int i = 0; i < kEach; ++i) {
+        const int c0 = 8 * i + mine_ch;
         if (Q8) {
           u32x4 f[2];
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
-            const u32x2 z = widen(x.rv[kt][i][y], uv);
+            const u32x2 z = widen(x.rv[u][i][y], uv);
             f[y / 2][2 * (y % 2)] = z.x;
             f[y / 2][2 * (y % 2) + 1] = z.y;
           }
-          s_v[v_at<C>(r, 2 * (4 * i + quarter))] = f[0];
-          s_v[v_at<C>(r, 2 * (4 * i + quarter) + 1)] = f[1];
+          s_v[v_at<C>(r, 2 * c0)] = f[0];
+          s_v[v_at<C>(r, 2 * c0 + 1)] = f[1];
         } else {
-          s_v[v_at<C>(r, 4 * i + quarter)] = x.rv[kt][i];
+          s_v[v_at<C>(r, c0)] = x.rv[u][i];
         }
       }
     }
@@ -329,6 +477,8 @@ __device__ __forceinline__ void narrow_part(const PagedArgs &a, const Item &it, 
     bool odd = false;
     uint32_t seen[QT];
     if (__builtin_expect(!clear, 0)) {
+      const PagedArgs &z = late();
+      if (bad != 0 && lane == 0) atomicOr(z.error_flag, kErrPage);
 #pragma unroll 1
       for (int i = lane; i < kFewKeys * C; i += kWave) {
         u32x4 w = s_v[i];
@@ -339,14 +489,17 @@ __device__ __forceinline__ void narrow_part(const PagedArgs &a, const Item &it, 
       }
 #pragma unroll
       for (int q = 0; q < QT; ++q) {
-        seen[q] = static_cast<uint32_t>(seen_bits(a, b, view[q], j, len, live)) & ~bad;
+        int slot, head;
+        place(z, q * 16 + col, &slot, &head);
+        seen[q] = static_cast<uint32_t>(seen_bits(z, b, view_of(z, b, slot, len, live), j, len, live)) & ~bad;
         const uint32_t bits = seen[q] >> (4 * quarter);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
           s[q][i / 4][i % 4] = (bits >> (16 * (i / 4) + i % 4)) & 1u ? s[q][i / 4][i % 4] : -INFINITY;
       }
+      drain();
     }
-    fetch();
+    fetch_values(x, w);
     // The tile's scores into the running sums, its values being in LDS.  The wave's LDS
     // operations are done in order.
     u32x4 p[QT];
@@ -385,28 +538,41 @@ __device__ __forceinline__ void narrow_part(const PagedArgs &a, const Item &it, 
     }
     __builtin_amdgcn_wave_barrier();
     if (__builtin_expect(__ballot(odd) != 0, 0)) {
+      const PagedArgs &z = late();
+      const char *v_at0 = z.v.p + kvh * z.v.head;
+      const uint8_t *vs_at0 = z.v.s + kvh * z.v.s_head;
 #pragma unroll 1
       for (int y = 0; y < kFewKeys && j + y < tile.end; ++y) {
-        const Spot sp = spot_at(a, entry_at(a, table, j + y, tile.end), j + y, tile.end);
+        const Spot sp = spot_at(z, entry_at(z, z.pages.table + b * z.pages.table_stride, j + y, tile.end), j + y, tile.end);
 #pragma unroll
         for (int q = 0; q < QT; ++q)
 #pragma unroll
           for (int d = 0; d < kDTiles; ++d) {
             const int c0 = d * 16 + 4 * quarter;
             u32x2 w{0, 0};
-            if (((seen[q] >> y) & 1) && c0 < a.dim) w = four_at<T, Q8>(a, v_head, vs_head, sp, c0);
+            if (((seen[q] >> y) & 1) && c0 < z.dim) w = four_at<T, Q8>(z, v_at0, vs_at0, sp, c0);
 #pragma unroll
-            for (int z = 0; z < 4; ++z) {
-              const uint16_t n = static_cast<uint16_t>(w[z / 2] >> (16 * (z & 1)));
-              o[q][d][z] += (n & T::kExp) == T::kExp ? T::number(n) : 0.0f;
+            for (int h = 0; h < 4; ++h) {
+              const uint16_t n = static_cast<uint16_t>(w[h / 2] >> (16 * (h & 1)));
+              o[q][d][h] += (n & T::kExp) == T::kExp ? T::number(n) : 0.0f;
             }
           }
       }
     }
+  };
+  Held x;
+  drain();
+  {
+    Where w;
+    find(w);
+    fetch_keys(x, w);
+    fetch_values(x, w);
   }
+  for (int t = t0 + wave; t < t1; t += kWaves) step(x);
 
   // The four waves' rows: each leaves its own with its maximum and sum, then every thread
   // joins 4 numbers of a row, the waves in order.
+  const PagedArgs &z = late();
   float *s_o = reinterpret_cast<float *>(lds);
   float *s_m = s_o + kWaves * 16 * kPad, *s_l = s_m + kWaves * 16;
 #pragma unroll
@@ -424,39 +590,205 @@ __device__ __forceinline__ void narrow_part(const PagedArgs &a, const Item &it, 
     for (int u = tid; u < 16 * (DP / 4); u += kThreads) {
       const int r = u / (DP / 4), c0 = (u % (DP / 4)) * 4;
       int slot, head;
-      if (!place(q * 16 + r, &slot, &head) || c0 >= a.dim) continue;
+      if (!place(z, q * 16 + r, &slot, &head) || c0 >= z.dim) continue;
       float top = s_m[r];
 #pragma unroll
       for (int i = 1; i < kWaves; ++i) top = fmaxf(top, s_m[i * 16 + r]);
-      const Ref now = ref_of<T>(top, a.c);
+      const Ref now = ref_of<T>(top, z.c);
       f32x4 sum{0.0f, 0.0f, 0.0f, 0.0f};
       float total = 0.0f;
 #pragma unroll
       for (int i = 0; i < kWaves; ++i) {
         const float mi = s_m[i * 16 + r];
-        const float f = mi == top ? 1.0f : factor(mi, ref_of<T>(mi, a.c).at, top, now, a.c);
+        const float f = mi == top ? 1.0f : factor(mi, ref_of<T>(mi, z.c).at, top, now, z.c);
         total += s_l[i * 16 + r] * f;
         sum += *reinterpret_cast<const f32x4 *>(s_o + (i * 16 + r) * kPad + c0) * f;
       }
-      const int64_t all = (static_cast<int64_t>(b) * a.slots + slot) * a.q_heads + head;
-      if (!alone) {
-        const int64_t at = it.part * a.rows_all + all;
-        if (c0 == 0) a.part_ml[at] = f32x2{top, total};
-        *reinterpret_cast<f32x4 *>(a.part_o + at * a.dim + c0) = sum;
+      const int64_t all = (static_cast<int64_t>(b) * z.slots + slot) * z.q_heads + head;
+      if (part >= 0) {
+        const int64_t at = part * static_cast<int64_t>(16 * QT) + q * 16 + r;
+        if (c0 == 0) z.part_ml[at] = f32x2{top, total};
+        *reinterpret_cast<f32x4 *>(z.part_o + at * z.dim + c0) = sum;
       } else {
         const float inv = total > 0.0f || total != total ? 1.0f / total : 0.0f;
-        *reinterpret_cast<u32x2 *>(a.out + b * a.o_batch + slot * a.o_slot + head * a.o_head + 2 * c0) =
+        *reinterpret_cast<u32x2 *>(z.out + b * z.o_batch + slot * z.o_slot + head * z.o_head + 2 * c0) =
             u32x2{T::pack(sum.x * inv, sum.y * inv), T::pack(sum.z * inv, sum.w * inv)};
-        if (a.lse && c0 == 0) finish(a, all, top, total, now.at);
+        if (z.lse && c0 == 0) finish(z, all, top, total, now.at);
       }
     }
   }
 }
 
+// A sequence's row tile, and the rounds that it takes for each of its key heads: of four 32-key tiles
+// in the narrow walk, of a 64-key tile of the last row tile in the wide one.
+template <bool WIDE>
+__device__ __forceinline__ RowTile tile_of(const PagedArgs &a, int n, int len, int tile_row) {
+  const int first = tile_row * a.tile_rows, rows = n * a.group;
+  return row_tile(len, n, WIDE ? first / a.group : 0, WIDE ? (std::min(first + a.tile_rows, rows) - 1) / a.group : n - 1,
+                  a.mask != nullptr, a.window, a.sinks, WIDE ? kWideKeys : kFewKeys);
+}
+template <bool WIDE>
+__device__ __forceinline__ int rounds_of(const PagedArgs &a, int n, int len) {
+  if (n == 0) return 0;
+  const int tiles = tile_of<WIDE>(a, n, len, WIDE ? (n * a.group - 1) / a.tile_rows : 0).span.all();
+  return WIDE ? tiles : (tiles + kWaves - 1) / kWaves;
+}
+// The workgroup of a group and row tile: a group's follow each other on one XCD (workgroups go round
+// all 8), whose L2 then holds the keys that they share.
+__device__ __forceinline__ int block_of(int group, int tile_row, int row_tiles) {
+  return ((group >> 3) * row_tiles + tile_row) * 8 + (group & 7);
+}
+
+// How all rounds are shared.  A thread's sequences are c of them from tid * c on; sums over the workgroup.
+struct Sum {
+  int before, all, most;      // in front of the thread's, all, and the largest of `most`
+};
+__device__ __forceinline__ Sum sum_over(int mine, int most, int *s_sum) {
+  const int tid = threadIdx.x, wave = tid / kWave, upto = wave_incl_scan(mine);
+#pragma unroll
+  for (int k = 1; k < kWave; k <<= 1) most = std::max(most, static_cast<int>(xor_lane(static_cast<uint32_t>(most), k)));
+  __syncthreads();
+  if (lane_id() == kWave - 1) {
+    s_sum[wave] = upto;
+    s_sum[kWaves + wave] = most;
+  }
+  __syncthreads();
+  Sum s{upto - mine, 0, 0};
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    s.before += w < wave ? s_sum[w] : 0;
+    s.all += s_sum[w];
+    s.most = std::max(s.most, s_sum[kWaves + w]);
+  }
+  // the same in all threads: scalars, so that the walk's tables stay scalar
+  s.all = __builtin_amdgcn_readfirstlane(s.all);
+  s.most = __builtin_amdgcn_readfirstlane(s.most);
+  return s;
+}
+template <bool WIDE>
+__device__ __forceinline__ Sum all_rounds(const PagedArgs &a, int b0, int b1, int *s_sum) {
+  int sum = 0, most = 0;
+  for (int b = b0; b < b1; ++b) {
+    const Sizes s = sizes_of(a, b);
+    const int r = rounds_of<WIDE>(a, s.n, s.len);
+    if (s.bad && blockIdx.x == 0) atomicOr(a.error_flag, kErrBlockSizes);
+    sum += r * a.kv_heads;
+    most = std::max(most, r);
+  }
+  return sum_over(sum, most, s_sum);
+}
+
+// The narrow walk's workgroups share all rounds of (sequence, key head, round) evenly, in that order,
+// whatever the sequences' lengths: the chip is full until the end.  A workgroup's first piece may be the
+// end of a (sequence, key head), its last one a begin: these two go to the workspace, whole ones to the
+// outputs.  Every workgroup adds up the rounds in front of its own.
+template <typename Piece>
+__device__ __forceinline__ void share_rounds(const PagedArgs &a, int *s_sum, Piece piece) {
+  const int tid = threadIdx.x, group = blockIdx.x, groups = gridDim.x;
+  const int c = (a.batch + kThreads - 1) / kThreads, b0 = tid * c, b1 = std::min(b0 + c, a.batch);
+  const Sum sum = all_rounds<false>(a, b0, b1, s_sum);
+  const int per = std::max((sum.all + groups - 1) / groups, (sum.most + kMaxPieces - 2) / (kMaxPieces - 1));
+  const int first = group * per, last = std::min(first + per, sum.all);
+  __syncthreads();
+  // where the workgroup's first round is, and for the merge where each sequence begins
+  for (int b = b0, at = sum.before; b < b1; ++b) {
+    const Sizes s = sizes_of(a, b);
+    const int r = rounds_of<false>(a, s.n, s.len);
+    if (group == 0) a.share[1 + b] = at;
+    if (first >= at && first < at + r * a.kv_heads) {
+      s_sum[0] = b;
+      s_sum[1] = at;
+    }
+    at += r * a.kv_heads;
+  }
+  if (group == 0 && tid == 0) a.share[0] = per;
+  __syncthreads();
+  if (first >= last) return;
+  int b = __builtin_amdgcn_readfirstlane(s_sum[0]), begin = __builtin_amdgcn_readfirstlane(s_sum[1]);
+  for (int at = first; at < last;) {
+    const Sizes s = sizes_of(a, b);
+    const int n = __builtin_amdgcn_readfirstlane(s.n), len = __builtin_amdgcn_readfirstlane(s.len);
+    const int r = rounds_of<false>(a, n, len), end = begin + r * a.kv_heads;
+    const RowTile tile = tile_of<false>(a, n, len, 0);
+    while (at < last && at < end) {
+      const int kvh = (at - begin) / r, unit = begin + kvh * r, stop = std::min(unit + r, last);
+      const bool whole = unit >= first && unit + r <= last;
+      const int part = whole ? -1 : 2 * group + (unit >= first ? 1 : 0);
+      __syncthreads();
+      piece(b, kvh, n, len, tile, (at - unit) * kWaves, std::min((stop - unit) * kWaves, tile.span.all()), part);
+      at = stop;
+    }
+    begin = end;
+    ++b;
+  }
+}
+
+// In the wide walk a (sequence, key head) of r rounds is cut into ceil(r / per) even pieces, each a group
+// of workgroups, one for every row tile; a row tile's own tiles are cut in that proportion.  A lone piece
+// goes to the outputs.  per is the least for which there are groups for all pieces.  (Shared as in the
+// narrow walk, two pieces a workgroup begin and end there, and a begin costs three latencies.)
+__device__ __forceinline__ int pieces_of(int rounds, int per) { return (rounds + per - 1) / per; }
+template <typename Piece>
+__device__ __forceinline__ void cut_rounds(const PagedArgs &a, int group, int tile_row, int *s_sum, Piece piece) {
+  const int tid = threadIdx.x;
+  const int c = (a.batch + kThreads - 1) / kThreads, b0 = tid * c, b1 = std::min(b0 + c, a.batch);
+  const Sum sum = all_rounds<true>(a, b0, b1, s_sum);
+  const int spare = std::max(a.groups - a.batch * a.kv_heads, 1);
+  const int per = std::max(std::max((sum.all + spare - 1) / spare, (sum.most + kMaxPieces - 1) / kMaxPieces), 1);
+  int mine = 0;
+  for (int b = b0; b < b1; ++b) {
+    const Sizes s = sizes_of(a, b);
+    mine += pieces_of(rounds_of<true>(a, s.n, s.len), per) * a.kv_heads;
+  }
+  const Sum count = sum_over(mine, 0, s_sum);
+  __syncthreads();
+  for (int b = b0, at = count.before; b < b1; ++b) {
+    const Sizes s = sizes_of(a, b);
+    const int p = pieces_of(rounds_of<true>(a, s.n, s.len), per) * a.kv_heads;
+    if (blockIdx.x == 0) a.share[1 + b] = at;
+    if (group >= at && group < at + p) {
+      s_sum[0] = b;
+      s_sum[1] = at;
+    }
+    at += p;
+  }
+  if (blockIdx.x == 0 && tid == 0) a.share[0] = per;
+  __syncthreads();
+  if (group >= count.all) return;
+  const int b = __builtin_amdgcn_readfirstlane(s_sum[0]), begin = __builtin_amdgcn_readfirstlane(s_sum[1]);
+  const Sizes s = sizes_of(a, b);
+  const int n = __builtin_amdgcn_readfirstlane(s.n), len = __builtin_amdgcn_readfirstlane(s.len);
+  if (tile_row * a.tile_rows >= n * a.group) return;
+  const RowTile tile = tile_of<true>(a, n, len, tile_row);
+  const int pieces = pieces_of(rounds_of<true>(a, n, len), per), kvh = (group - begin) / pieces, p = group - begin - kvh * pieces;
+  const int all = tile.span.all(), t0 = cut_at(all, pieces, p), t1 = cut_at(all, pieces, p + 1);
+  __syncthreads();
+  if (t0 < t1) piece(b, kvh, n, len, tile, t0, t1, pieces == 1 ? -1 : static_cast<int>(blockIdx.x));
+}
+
 // 128 rows a workgroup, 32 a wave; 64-key tiles in LDS for all four waves, the next tile's loads
 // in flight in registers meanwhile, two LDS buffers, one barrier a tile.
-template <typename T, bool Q8, bool FULL, int DP>
-__device__ __forceinline__ void wide_part(const PagedArgs &a, const Item &it, u32x4 *lds) {
+// N products whose fragments are read kAhead products before they are used.  Left to itself the compiler
+// reads a fragment right in front of its product, and the wave waits for LDS every time (8 pieces of 1024
+// slots 355 us; 370, 348, 343, 344 and 346 with fragments 1, 2, 3, 4 and 6 products ahead).
+constexpr int kAhead = 3;
+template <int N, typename Read, typename Product>
+__device__ __forceinline__ void pipelined(Read read, Product product) {
+  u32x4 f[kAhead];
+#pragma unroll
+  for (int n = 0; n < kAhead; ++n) f[n] = read(n);
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    product(n, f[n % kAhead]);
+    if (n + kAhead < N) f[n % kAhead] = read(n + kAhead);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
+template <typename T, bool Q8, bool HOT, int DP>
+__device__ __forceinline__ void wide_part(const PagedArgs &a, int b, int kvh, int live, int len, int tile_row, const RowTile &tile,
+                                          int t0, int t1, int part, u32x4 *lds) {
   constexpr int C = DP / 8;                             // 16-byte chunks of a row in LDS
   constexpr int kSteps = DP / 16, kDTiles = DP / 32;
   constexpr int kBuf = kWideKeys * C;                   // a buffer of keys, or of values
@@ -465,63 +797,85 @@ __device__ __forceinline__ void wide_part(const PagedArgs &a, const Item &it, u3
   constexpr int kStep = kThreads / kPer, kUnits = kWideKeys / kStep;
   u32x4 *s_k = lds, *s_v = lds + 2 * kBuf;
 
-  const int tid = threadIdx.x, lane = lane_id();
-  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));     // a piece's own, as in narrow_part
+  const int lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int h = lane >> 5, col = lane & 31;
-  const int b = it.b, kvh = it.kvh;
 
-  const Sizes sz = sizes_of(a, b);
-  const int live = __builtin_amdgcn_readfirstlane(sz.n), len = __builtin_amdgcn_readfirstlane(sz.len);
-  if (sz.bad && it.tile_row == 0 && it.part == 0 && kvh == 0 && tid == 0) atomicOr(a.error_flag, kErrBlockSizes);
-  const int rows = live * a.group, first = it.tile_row * kWideRows;
-  if (first >= rows) return;
-  const RowTile tile = row_tile(len, live, first / a.group, (std::min(first + kWideRows, rows) - 1) / a.group, a.mask != nullptr,
-                                a.window, a.sinks, kWideKeys, 1, a.splits, a.min_rounds);
-  if (it.part >= tile.parts) return;
-  const bool alone = tile.parts == 1;
-  const int t0 = it.part * tile.per, t1 = std::min(t0 + tile.per, tile.span.all());
-
-  const bool valid = first + wave * 32 + col < rows;
-  const int row = valid ? first + wave * 32 + col : rows - 1;
+  const int rows = live * a.group, local = wave * 32 + col, first = tile_row * a.tile_rows;
+  const bool valid = local < a.tile_rows && first + local < rows;
+  const int row = valid ? first + local : rows - 1;
   const int slot = row / a.group, head = kvh * a.group + row - slot * a.group;
   const bool busy = __ballot(valid) != 0;
-  const View view = view_of(a, b, slot, len, live);
 
   const int32_t *table = a.pages.table + b * a.pages.table_stride;
   const char *k_head = a.k.p + kvh * a.k.head, *v_head = a.v.p + kvh * a.v.head;
   const uint8_t *ks_head = a.k.s + kvh * a.k.s_head, *vs_head = a.v.s + kvh * a.v.s_head;
 
-  // a thread's share of a tile: 16 bytes of rows r0, r0 + kStep, ...
+  // A thread's share of a tile: 16 bytes of rows r0, r0 + kStep, ...  Lane l works out where key l lies.
+  // HOT: a wave's rows of a unit lie in one page, in 16 rows from a multiple of 16 on; in the last tile
+  // they may be the page's rows behind the end, or 16 rows with the last one again.
   const int r0 = tid / kPer, ch = tid % kPer;
-  const int at16 = FULL || ch * 16 < kBytes * a.dim ? ch * 16 : 0;
+  const int at16 = HOT || ch * 16 < kBytes * a.dim ? ch * 16 : 0;
+  constexpr int kWaveRows = kWave / kPer;
+  const uint32_t lane_off = (lane / kPer + (wave * kWaveRows & 15)) * a.k.row + ch * 16;
+  const int64_t to_v = v_head - k_head, to_vs = vs_head - ks_head;
   u32x4 rk[kUnits], rv[kUnits];
   uint32_t sk = 0, sv = 0;                              // scales of key `lane`
-  int held_j = 0, next = entry_at(a, table, tile.span.at(t0) * kWideKeys + lane, tile.end);
+  int held_j = 0, next = 0;
+  uint32_t next_off = 0;
   uint64_t held_bad = 0;
+  auto look_up = [&](int t) {
+    const int j = tile.span.at(t) * kWideKeys + lane;
+    const uint32_t r = j < tile.end ? j : HOT ? (tile.end - 1) & ~15 : tile.end - 1;
+    const int e = a.pages.entry(r);
+    next_off = r - e * a.pages.page_rows;
+    next = table[e];
+  };
+  look_up(t0);
   auto load = [&](int t) {
     held_j = tile.span.at(t) * kWideKeys;
-    const Spot s = spot_at(a, next, held_j + lane, tile.end);
+    Spot s;
+    s.bad = static_cast<uint32_t>(next) >= static_cast<uint32_t>(a.pages.pages);
+    s.page = s.bad ? 0 : next;
+    s.off = next_off;
     held_bad = __ballot(s.bad);
+    if (HOT) {
+      const int64_t at = row_at(a.k, s);
 #pragma unroll
-    for (int i = 0; i < kUnits; ++i) {
-      const int from = 4 * (r0 + i * kStep);
-      const int page = __builtin_amdgcn_ds_bpermute(from, s.page);
-      const uint32_t off = static_cast<uint32_t>(__builtin_amdgcn_ds_bpermute(from, static_cast<int>(s.off)));
-      rk[i] = take16(row_at(k_head, a.k.page, a.k.row, page, off) + at16);
-      rv[i] = take16(row_at(v_head, a.v.page, a.v.row, page, off) + at16);
+      for (int i = 0; i < kUnits; ++i) {
+        const char *p = k_head + read_lane64(at, (wave * kWaveRows & ~15) + i * kStep);
+        rk[i] = take16(p + lane_off);
+        rv[i] = take16(p + to_v + lane_off);
+      }
+      if (Q8) {
+        const uint8_t *p = ks_head + scale_at(a.k, s);
+        sk = *p;
+        sv = p[to_vs];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i) {
+        const int from = 4 * (r0 + i * kStep);
+        Spot r;
+        r.page = __builtin_amdgcn_ds_bpermute(from, s.page);
+        r.off = static_cast<uint32_t>(__builtin_amdgcn_ds_bpermute(from, static_cast<int>(s.off)));
+        rk[i] = take16(k_head + row_at(a.k, r) + at16);
+        rv[i] = take16(v_head + row_at(a.v, r) + at16);
+      }
+      if (Q8) {
+        sk = ks_head[scale_at(a.k, s)];
+        sv = vs_head[scale_at(a.v, s)];
+      }
     }
-    if (Q8) {
-      sk = ks_head[s.page * a.k.s_page + static_cast<uint64_t>(s.off * a.k.s_row)];
-      sv = vs_head[s.page * a.v.s_page + static_cast<uint64_t>(s.off * a.v.s_row)];
-    }
-    if (t + 1 < t1) next = entry_at(a, table, tile.span.at(t + 1) * kWideKeys + lane, tile.end);
+    look_up(t + 1 < t1 ? t + 1 : t);
   };
   // Stores the share; true if a value is infinite or NaN where not all rows see the keys (stored
   // as 0 then).
   auto store = [&](int buf, bool clear) {
     bool odd = false;
     u32x4 *k = s_k + buf * kBuf, *v = s_v + buf * kBuf;
-    const bool past = !FULL && ch * 16 >= kBytes * a.dim;
+    const bool past = !HOT && ch * 16 >= kBytes * a.dim;
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
       const int r = r0 + i * kStep;
@@ -568,7 +922,7 @@ __device__ __forceinline__ void wide_part(const PagedArgs &a, const Item &it, u3
 
   // the queries: the right operand of S^T = K Q^T
   u32x4 rq[kSteps];
-  const char *qp = a.q + b * a.q_batch + slot * a.q_slot + head * a.q_head;
+  const char *qp = late().q + b * late().q_batch + slot * late().q_slot + head * late().q_head;
 #pragma unroll
   for (int s = 0; s < kSteps; ++s) rq[s] = s * 16 < a.dim ? take16(qp + s * 32 + h * 16) : u32x4{0, 0, 0, 0};
 #pragma unroll
@@ -581,7 +935,7 @@ __device__ __forceinline__ void wide_part(const PagedArgs &a, const Item &it, u3
     const int buf = (t - t0) & 1, j = held_j;
     const uint64_t bad = held_bad;
     const bool clear = bad == 0 && is_clear(tile, j, kWideKeys, a.sinks);
-    if (bad != 0 && tid == 0) atomicOr(a.error_flag, kErrPage);
+    if (__builtin_expect(bad != 0, 0) && tid == 0) atomicOr(late().error_flag, kErrPage);
     const bool odd = store(buf, clear);
     if (t + 1 < t1) load(t + 1);
     bool any_odd = false;
@@ -594,14 +948,12 @@ __device__ __forceinline__ void wide_part(const PagedArgs &a, const Item &it, u3
     for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[kt][i] = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kSteps; ++i)
-#pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
-        s[kt] = T::mfma(k[k_at<C>(kt * 32 + col, 2 * i + h)], rq[i], s[kt]);
+    pipelined<2 * kSteps>([&](int n) { return k[k_at<C>(n % 2 * 32 + col, n / 2 * 2 + h)]; },
+                          [&](int n, const u32x4 &f) { s[n % 2] = T::mfma(f, rq[n / 2], s[n % 2]); });
     uint64_t seen = ~0ull;
     if (__builtin_expect(!clear, 0)) {
-      seen = seen_bits(a, b, view, j, len, live) & ~bad;
+      const PagedArgs &z = late();
+      seen = seen_bits(z, b, view_of(z, b, slot, len, live), j, len, live) & ~bad;
       const uint64_t bits = seen >> (4 * h);
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt) {
@@ -612,26 +964,27 @@ __device__ __forceinline__ void wide_part(const PagedArgs &a, const Item &it, u3
     }
     u32x4 p[4];
     softmax_step<T, 2>(st, s, p, a.c);
-#pragma unroll
-    for (int d = 0; d < kDTiles; ++d) {
-#pragma unroll
-      for (int g = 0; g < 4; ++g) st.o[d] = T::mfma(v_fragment<C>(v, d, g, lane), p[g], st.o[d]);
-    }
+    // four tiles of columns in turn: a product does not wait for the one before it
+    pipelined<4 * kDTiles>([&](int n) { return v_fragment<C>(v, n % kDTiles, n / kDTiles, lane); },
+                           [&](int n, const u32x4 &f) { st.o[n % kDTiles] = T::mfma(f, p[n / kDTiles], st.o[n % kDTiles]); });
     if (__builtin_expect(any_odd, 0)) {
+      const PagedArgs &z = late();
+      const char *v_at0 = z.v.p + kvh * z.v.head;
+      const uint8_t *vs_at0 = z.v.s + kvh * z.v.s_head;
 #pragma unroll 1
       for (int y = 0; y < kWideKeys && j + y < tile.end; ++y) {
-        const Spot sp = spot_at(a, entry_at(a, table, j + y, tile.end), j + y, tile.end);
+        const Spot sp = spot_at(z, entry_at(z, z.pages.table + b * z.pages.table_stride, j + y, tile.end), j + y, tile.end);
 #pragma unroll
         for (int d = 0; d < kDTiles; ++d)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int c0 = d * 32 + 8 * i + 4 * h;
             u32x2 w{0, 0};
-            if (((seen >> y) & 1) && c0 < a.dim) w = four_at<T, Q8>(a, v_head, vs_head, sp, c0);
+            if (((seen >> y) & 1) && c0 < z.dim) w = four_at<T, Q8>(z, v_at0, vs_at0, sp, c0);
 #pragma unroll
-            for (int z = 0; z < 4; ++z) {
-              const uint16_t n = static_cast<uint16_t>(w[z / 2] >> (16 * (z & 1)));
-              st.o[d][4 * i + z] += (n & T::kExp) == T::kExp ? T::number(n) : 0.0f;
+            for (int x = 0; x < 4; ++x) {
+              const uint16_t n = static_cast<uint16_t>(w[x / 2] >> (16 * (x & 1)));
+              st.o[d][4 * i + x] += (n & T::kExp) == T::kExp ? T::number(n) : 0.0f;
             }
           }
       }
@@ -640,111 +993,144 @@ __device__ __forceinline__ void wide_part(const PagedArgs &a, const Item &it, u3
 
   st.l = half_sum(st.l);
   if (!valid) return;
-  const int64_t all = (static_cast<int64_t>(b) * a.slots + slot) * a.q_heads + head;
-  if (!alone) {
-    const int64_t at = it.part * a.rows_all + all;
-    if (h == 0) a.part_ml[at] = f32x2{st.m, st.l};
-    float *po = a.part_o + at * a.dim;
+  const PagedArgs &z = late();
+  const int64_t all = (static_cast<int64_t>(b) * z.slots + slot) * z.q_heads + head;
+  if (part >= 0) {
+    const int64_t at = part * static_cast<int64_t>(kWideRows) + local;
+    if (h == 0) z.part_ml[at] = f32x2{st.m, st.l};
+    float *po = z.part_o + at * z.dim;
 #pragma unroll
     for (int d = 0; d < kDTiles; ++d)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int x = d * 32 + 8 * i + 4 * h;
-        if (x < a.dim)
+        if (x < z.dim)
           *reinterpret_cast<f32x4 *>(po + x) =
               f32x4{st.o[d][4 * i], st.o[d][4 * i + 1], st.o[d][4 * i + 2], st.o[d][4 * i + 3]};
       }
     return;
   }
   const float inv = st.l > 0.0f || st.l != st.l ? 1.0f / st.l : 0.0f;
-  char *op = a.out + b * a.o_batch + slot * a.o_slot + head * a.o_head;
+  char *op = z.out + b * z.o_batch + slot * z.o_slot + head * z.o_head;
 #pragma unroll
   for (int d = 0; d < kDTiles; ++d)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int x = d * 32 + 8 * i + 4 * h;
-      if (x < a.dim)
+      if (x < z.dim)
         *reinterpret_cast<u32x2 *>(op + 2 * x) =
             u32x2{T::pack(st.o[d][4 * i] * inv, st.o[d][4 * i + 1] * inv),
                   T::pack(st.o[d][4 * i + 2] * inv, st.o[d][4 * i + 3] * inv)};
     }
-  if (a.lse && h == 0) finish(a, all, st.m, st.l, ref_of<T>(st.m, a.c).at);
+  if (z.lse && h == 0) finish(z, all, st.m, st.l, ref_of<T>(st.m, z.c).at);
 }
 
-// QT = 0: the wide walk; else the narrow one, 16 QT rows.  FULL: heads of DP numbers; the others' loads
-// past a head's end go to its begin, which takes addresses of their own and registers.
-template <typename T, bool Q8, bool FULL, int DP, int QT>
-__global__ void __launch_bounds__(kThreads, QT == 1 || (QT == 2 && DP == 64) ? 3 : 2)
+// QT = 0: the wide walk; else the narrow one, 16 QT rows.  HOT: heads of DP numbers and
+// pages of 16 rows or a multiple.  Others' loads past a head's end go to its begin, and every row
+// has an address of its own: more registers and vector work.
+template <typename T, bool Q8, bool HOT, int DP, int QT>
+__global__ void __launch_bounds__(kThreads, 2)
 paged_attend_kernel(PagedArgs a) {
   constexpr int kNarrow = (kWaves * 16 * (DP + 4) + 2 * kWaves * 16 + 3) / 4;   // joining the waves
   constexpr int kValues = kWaves * kFewKeys * (DP / 8);
   __shared__ __align__(16) u32x4 lds[QT == 0 ? 4 * kWideKeys * (DP / 8) : (kNarrow > kValues ? kNarrow : kValues)];
-  // Workgroups go round the 8 XCDs.  Wide: the row tiles of a (part, sequence, key head) follow each
-  // other on one, whose L2 then holds their keys.  The others go by an odd number (one may be empty),
-  // so that a sequence's parts fall on all XCDs; parts that short sequences leave empty come last.
-  const int i = blockIdx.x, outer = a.batch * a.kv_heads, odd = outer | 1;
-  Item it;
-  int g = i;
-  it.tile_row = 0;
-  if (QT == 0) {
-    const int j = i >> 3;
-    g = (j / a.row_tiles) * 8 + (i & 7);
-    it.tile_row = j % a.row_tiles;
+  int *s_sum = reinterpret_cast<int *>(lds);
+  if constexpr (QT > 0) {
+    share_rounds(a, s_sum, [&](int b, int kvh, int n, int len, const RowTile &tile, int t0, int t1, int part) {
+      narrow_part<T, Q8, HOT, DP, QT>(a, b, kvh, n, len, tile, t0, t1, part, lds);
+    });
+  } else {
+    const int i = blockIdx.x, j = i >> 3, tile_row = j % a.row_tiles, g = (j / a.row_tiles) * 8 + (i & 7);   // block_of
+    auto piece = [&](int b, int kvh, int n, int len, const RowTile &tile, int t0, int t1, int part) {
+      wide_part<T, Q8, HOT, DP>(a, b, kvh, n, len, tile_row, tile, t0, t1, part, lds);
+    };
+    if (a.groups > 0) {
+      cut_rounds(a, g, tile_row, s_sum, piece);
+      return;
+    }
+    if (g >= a.batch * a.kv_heads) return;
+    const int b = g / a.kv_heads, kvh = g - b * a.kv_heads;
+    const Sizes s = sizes_of(a, b);
+    const int n = __builtin_amdgcn_readfirstlane(s.n), len = __builtin_amdgcn_readfirstlane(s.len);
+    if (s.bad && tile_row == 0 && kvh == 0 && threadIdx.x == 0) atomicOr(a.error_flag, kErrBlockSizes);
+    if (tile_row * a.tile_rows >= n * a.group) return;
+    const RowTile tile = tile_of<true>(a, n, len, tile_row);
+    piece(b, kvh, n, len, tile, 0, tile.span.all(), -1);
   }
-  it.part = g / odd;
-  const int o = g - it.part * odd;
-  it.b = o / a.kv_heads;
-  it.kvh = o - it.b * a.kv_heads;
-  if (it.part >= a.splits || o >= outer) return;
-  if (QT == 0) wide_part<T, Q8, FULL, DP>(a, it, lds);
-  else narrow_part<T, Q8, FULL, DP, QT == 0 ? 1 : QT>(a, it, lds);
 }
 
-// Joins the parts of a row: a wave each, one part a lane for the statistics, two
-// numbers a lane for the row.
+// Joins the pieces of a row: 32 lanes each, four pieces a lane for the statistics, four numbers a lane
+// for the row.
 template <typename T, bool WIDE>
 __global__ void __launch_bounds__(kThreads)
 merge_pages_kernel(PagedArgs a) {
-  const int lane = lane_id();
-  const int64_t r = static_cast<int64_t>(blockIdx.x) * kWaves + threadIdx.x / kWave;
+  const int lane = lane_id(), l32 = lane & 31;
+  const int64_t r = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + threadIdx.x / 32;
   if (r >= a.rows_all) return;
   const int64_t bs = r / a.q_heads;
-  const int head = static_cast<int>(r - bs * a.q_heads);
-  const int b = static_cast<int>(bs / a.slots), slot = static_cast<int>(bs - static_cast<int64_t>(b) * a.slots);
+  const int head = static_cast<int>(r - bs * a.q_heads), b = static_cast<int>(bs / a.slots);
+  const int slot = static_cast<int>(bs - static_cast<int64_t>(b) * a.slots);
   const Sizes sz = sizes_of(a, b);
   if (slot >= sz.n) return;
-  int s0 = 0, s1 = sz.n - 1;
+  const int kvh = head / a.group, row = slot * a.group + head - kvh * a.group, tile_row = WIDE ? row / a.tile_rows : 0;
+  const int rounds = rounds_of<WIDE>(a, sz.n, sz.len), per = a.share[0];
+  int g0, pieces;
   if (WIDE) {
-    const int rows = sz.n * a.group, first = (slot * a.group + head % a.group) / kWideRows * kWideRows;
-    s0 = first / a.group;
-    s1 = (std::min(first + kWideRows, rows) - 1) / a.group;
+    pieces = pieces_of(rounds, per);
+    g0 = a.share[1 + b] + kvh * pieces;
+  } else {
+    const int unit = a.share[1 + b] + kvh * rounds;
+    g0 = unit / per;
+    pieces = (unit + rounds - 1) / per - g0 + 1;
   }
-  const RowTile tile = row_tile(sz.len, sz.n, s0, s1, a.mask != nullptr, a.window, a.sinks, WIDE ? kWideKeys : kFewKeys,
-                                WIDE ? 1 : kWaves, a.splits, a.min_rounds);
-  if (tile.parts == 1) return;                             // its only part wrote the row
-  const f32x2 ml = lane < tile.parts ? a.part_ml[lane * a.rows_all + r] : f32x2{-INFINITY, 0.0f};
-  float top = ml.x;
+  if (pieces == 1) return;                                  // the only one wrote the row
+  const int tiles = WIDE ? tile_of<true>(a, sz.n, sz.len, tile_row).span.all() : 0, local = row - tile_row * a.tile_rows;
+  // where piece p's sums are; narrow: the first one is its group's last piece, the others are first ones
+  auto at = [&](int p) {
+    return WIDE ? static_cast<int64_t>(block_of(g0 + p, tile_row, a.row_tiles)) * kWideRows + local
+                : static_cast<int64_t>(2 * (g0 + p) + (p == 0 ? 1 : 0)) * a.tile_rows + local;
+  };
+  // a piece that cut_at leaves nothing was not written
+  auto some = [&](int p) { return p < pieces && (!WIDE || cut_at(tiles, pieces, p) < cut_at(tiles, pieces, p + 1)); };
+  f32x2 ml[4];
+  float top = -INFINITY;
 #pragma unroll
-  for (int k = 1; k < kWave; k <<= 1) top = fmaxf(top, __uint_as_float(xor_lane(__float_as_uint(top), k)));
-  // 0 for a part without keys that the row sees
+  for (int k = 0; k < 4; ++k) {
+    const int p = l32 + 32 * k;
+    ml[k] = 32 * k < pieces && some(p) ? a.part_ml[at(p)] : f32x2{-INFINITY, 0.0f};
+    top = fmaxf(top, ml[k].x);
+  }
+#pragma unroll
+  for (int k = 1; k < 32; k <<= 1) top = fmaxf(top, __uint_as_float(xor_lane(__float_as_uint(top), k)));
+  // 0 for a piece without keys that the row sees
   const Ref now = ref_of<T>(top, a.c);
-  const float w = ml.x == top && top != -INFINITY ? 1.0f : factor(ml.x, ref_of<T>(ml.x, a.c).at, top, now, a.c);
-  float l = w * ml.y;
+  float w[4], l = 0.0f;
 #pragma unroll
-  for (int k = 1; k < kWave; k <<= 1) l += __uint_as_float(xor_lane(__float_as_uint(l), k));
-  const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-  float x = 0.0f, y = 0.0f;
-  if (lane * 2 < a.dim) {
-    for (int p = 0; p < tile.parts; ++p) {
-      const f32x2 v = *reinterpret_cast<const f32x2 *>(a.part_o + (p * a.rows_all + r) * a.dim + lane * 2);
-      const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), p));
-      x = __builtin_fmaf(f, v.x, x);
-      y = __builtin_fmaf(f, v.y, y);
-    }
-    *reinterpret_cast<uint32_t *>(a.out + b * a.o_batch + slot * a.o_slot + head * a.o_head + lane * 4) =
-        T::pack(x * inv, y * inv);
+  for (int k = 0; k < 4; ++k) {
+    w[k] = ml[k].x == top && top != -INFINITY ? 1.0f : factor(ml[k].x, ref_of<T>(ml[k].x, a.c).at, top, now, a.c);
+    l += w[k] * ml[k].y;
   }
-  if (a.lse && lane == 0) finish(a, r, top, l, now.at);
+#pragma unroll
+  for (int k = 1; k < 32; k <<= 1) l += __uint_as_float(xor_lane(__float_as_uint(l), k));
+  const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+  f32x4 x{0.0f, 0.0f, 0.0f, 0.0f};
+  const bool mine = l32 * 4 < a.dim;
+  const float *o = a.part_o + (mine ? l32 * 4 : 0);
+  for (int p0 = 0; p0 < pieces; p0 += 4) {
+    f32x4 v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const f32x4 *>(o + at(std::min(p0 + k, pieces - 1)) * a.dim);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int p = p0 + k;
+      const float f = __shfl(p < 32 ? w[0] : p < 64 ? w[1] : p < 96 ? w[2] : w[3], (lane & 32) + (p & 31));
+      if (p < pieces && f != 0.0f) x += v[k] * f;           // what was not written has no weight
+    }
+  }
+  if (mine)
+    *reinterpret_cast<u32x2 *>(a.out + b * a.o_batch + slot * a.o_slot + head * a.o_head + l32 * 8) =
+        u32x2{T::pack(x.x * inv, x.y * inv), T::pack(x.z * inv, x.w * inv)};
+  if (a.lse && l32 == 0) finish(a, r, top, l, now.at);
 }
 
 Pool pool_of(const graft_rows &r, int bytes) {
@@ -765,23 +1151,37 @@ Pool pool_of(const graft_rows &r, int bytes) {
 PagedPlan paged_plan(const graft_paged_attention_desc &a) {
   PagedPlan p{};
   const int group = a.q_heads / a.kv_heads;
-  const int64_t rows = static_cast<int64_t>(a.slots) * group;
+  const int64_t rows = static_cast<int64_t>(a.slots) * group, outer = static_cast<int64_t>(a.batch) * a.kv_heads;
   p.few = rows <= 16 ? 1 : rows <= kFewRows ? 2 : 0;
   p.row_tiles = p.few ? 1 : static_cast<int>((rows + kWideRows - 1) / kWideRows);
-  const int64_t outer = static_cast<int64_t>(a.batch) * a.kv_heads, units = outer * p.row_tiles;
+  // row tiles of one size, whole waves: 260 rows are three tiles of three waves, not two of four and a rest
+  p.tile_rows = p.few ? 16 * p.few : static_cast<int>((rows + 32 * p.row_tiles - 1) / (32 * p.row_tiles) * 32);
+  p.row_tiles = p.few ? 1 : static_cast<int>((rows + p.tile_rows - 1) / p.tile_rows);
   // keys of a round: of the narrow walk's four waves, or a tile of the wide one
   const int keys = p.few ? kFewKeys * kWaves : kWideKeys;
   int64_t most = static_cast<int64_t>(a.pages.table_len) * a.pages.page_rows;
   if (a.window > 0) most = std::min<int64_t>(most, static_cast<int64_t>(a.window) + a.sinks + a.slots + 2 * keys);
-  const int64_t rounds = (most + keys - 1) / keys;
-  p.min_rounds = p.few ? 1 : 4;
-  int64_t s = ((p.few ? 4096 : 1024) + units - 1) / units;
-  s = std::min(s, (rounds + p.min_rounds - 1) / p.min_rounds);
-  p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(s, kMaxParts)));
-  const int64_t all = static_cast<int64_t>(a.batch) * a.slots * a.q_heads;
-  p.blocks = ((outer | 1) * p.splits + 7) / 8 * 8 * p.row_tiles;
-  p.merge_blocks = p.splits > 1 ? (all + kWaves - 1) / kWaves : 0;
-  p.bytes = p.splits > 1 ? p.splits * all * (a.head_dim * int64_t{4} + 8) : 0;
+  const int64_t rounds = (most + keys - 1) / keys, all = static_cast<int64_t>(a.batch) * a.slots * a.q_heads;
+  p.fits = outer * rounds < (int64_t{1} << 31);
+  if (p.few) {
+    // as many as the registers let run at once
+    p.groups = static_cast<int>(std::min<int64_t>(outer * rounds, a.cache_dtype == GRAFT_E4M3 ? 768 : 512));
+    p.blocks = p.groups;
+  } else if (outer * p.row_tiles < 1024 && rounds > 1) {
+    // a group for every (sequence, key head), and what is left of the workgroups for more pieces (16 trees
+    // of up to 64 nodes: 122, 117, 103, 115 and 117 us with 512, 640, 768, 1024 and 1536 workgroups)
+    const int64_t some = std::max<int64_t>(768 / p.row_tiles, outer + 8) / 8 * 8;
+    p.groups = static_cast<int>(std::min<int64_t>((outer * rounds + 7) / 8 * 8, some));
+    p.blocks = static_cast<int64_t>(p.groups) * p.row_tiles;
+  } else {
+    p.fits = true;
+    p.blocks = (outer + 7) / 8 * 8 * p.row_tiles;
+    return p;
+  }
+  p.merge_blocks = rounds > 1 ? (all + kThreads / 32 - 1) / (kThreads / 32) : 0;
+  p.part_rows = p.blocks * (p.few ? 2 * p.tile_rows : kWideRows);
+  p.share_at = p.part_rows * (a.head_dim * int64_t{4} + 8);
+  p.bytes = p.share_at + (a.batch + int64_t{1}) * 4;
   return p;
 }
 
@@ -807,7 +1207,8 @@ hipError_t launch_paged_attend(graft_ctx *ctx, const graft_paged_attention_desc 
   a.error_flag = ctx->error_flag;
   a.rows_all = static_cast<int64_t>(d.batch) * d.slots * d.q_heads;
   a.part_o = static_cast<float *>(d.workspace);
-  a.part_ml = p.splits > 1 ? reinterpret_cast<f32x2 *>(a.part_o + p.splits * a.rows_all * d.head_dim) : nullptr;
+  a.part_ml = p.bytes > 0 ? reinterpret_cast<f32x2 *>(a.part_o + p.part_rows * d.head_dim) : nullptr;
+  a.share = p.bytes > 0 ? reinterpret_cast<int32_t *>(static_cast<char *>(d.workspace) + p.share_at) : nullptr;
   a.batch = d.batch;
   a.slots = d.slots;
   a.root = d.with_root ? 1 : 0;
@@ -819,9 +1220,9 @@ hipError_t launch_paged_attend(graft_ctx *ctx, const graft_paged_attention_desc 
   a.words = (ctx->dims.max_nodes + 63) / 64;
   a.window = d.window;
   a.sinks = d.window > 0 ? d.sinks : 0;
+  a.tile_rows = p.tile_rows;
   a.row_tiles = p.row_tiles;
-  a.splits = p.splits;
-  a.min_rounds = p.min_rounds;
+  a.groups = p.groups;
   a.c = d.scale * 1.4426950408889634f;
   const dim3 grid(static_cast<unsigned>(p.blocks)), block(kThreads);
   auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };
@@ -837,16 +1238,18 @@ hipError_t launch_paged_attend(graft_ctx *ctx, const graft_paged_attention_desc 
   auto width = [&](auto few) {
     constexpr std::integral_constant<int, 64> k64{};
     constexpr std::integral_constant<int, 128> k128{};
-    if (d.head_dim == 128) pick(few, k128, std::true_type{});
+    const bool even = d.pages.page_rows % 16 == 0 && a.k.page == a.v.page && a.k.row == a.v.row && a.k.head == a.v.head &&
+                      (!q8 || (a.k.s_page == a.v.s_page && a.k.s_row == a.v.s_row && a.k.s_head == a.v.s_head));
+    if (d.head_dim == 128 && even) pick(few, k128, std::true_type{});
     else if (d.head_dim > 64) pick(few, k128, std::false_type{});
-    else if (d.head_dim == 64) pick(few, k64, std::true_type{});
+    else if (d.head_dim == 64 && even) pick(few, k64, std::true_type{});
     else pick(few, k64, std::false_type{});
   };
   if (p.few == 1) width(std::integral_constant<int, 1>{});
   else if (p.few == 2) width(std::integral_constant<int, 2>{});
   else width(std::integral_constant<int, 0>{});
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.splits <= 1) return e;
+  if (e != hipSuccess || p.merge_blocks == 0) return e;
   const dim3 mgrid(static_cast<unsigned>(p.merge_blocks));
   auto merge = [&](auto kernel) { hipLaunchKernelGGL(kernel, mgrid, block, 0, stream, a); };
   if (d.dtype == GRAFT_F16) {

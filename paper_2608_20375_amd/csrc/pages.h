@@ -54,23 +54,24 @@ __host__ __device__ __forceinline__ int window_low(int p, int window) {
 // What slots s0 .. s1 of a block of n slots walk, which lies behind `base` rows: the tiles, the rows'
 // end, and the rows that every slot sees (those before clear_end that are from clear_low on, or
 // among the sinks).  A chain's slot i is at position base + i; a masked one's position is at least
-// base - 1 (it may see nothing) and at most base + n - 1.  per: tiles of a part, in rounds of
-// `turns` tiles, at least min_rounds of them; parts: how many parts there are, at most `splits`.
+// base - 1 (it may see nothing) and at most base + n - 1.
 struct RowTile {
   Span span;
-  int end, clear_low, clear_end, per, parts;
+  int end, clear_low, clear_end;
 };
 __host__ __device__ __forceinline__ RowTile row_tile(int base, int n, int s0, int s1, bool masked, int window,
-                                                     int sinks, int keys, int turns, int splits, int min_rounds) {
+                                                     int sinks, int keys) {
   RowTile t;
   t.end = masked ? base + n : base + s1 + 1;
   t.span = span_of(window_low(base + (masked ? -1 : s0), window), window > 0 ? sinks : 0, t.end, keys);
   t.clear_low = window_low(base + (masked ? n - 1 : s1), window);
   t.clear_end = masked ? base : base + s0 + 1;
-  const int rounds = (t.span.all() + turns - 1) / turns, even = (rounds + splits - 1) / splits;
-  t.per = (even > min_rounds ? even : min_rounds) * turns;
-  t.parts = (t.span.all() + t.per - 1) / t.per;
   return t;
+}
+
+// Where piece p of `pieces` begins among a row tile's n tiles.
+__host__ __device__ __forceinline__ int cut_at(int n, int pieces, int p) {
+  return static_cast<int>(static_cast<int64_t>(n) * p / pieces);
 }
 
 // Whether every slot of the tile sees all rows j .. j + keys - 1.

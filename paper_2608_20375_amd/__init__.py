@@ -1033,12 +1033,12 @@ class Context:
         _check(lib().graft_cache_read(self._h, C.byref(m), _stream()), "graft_cache_read")
         return out
 
-    def _pages(self, cache, name, heads, dim, dtype):
-        """(keys, values, quantised) of a layer's pages [pages, page_rows, heads, dim]."""
+    def _pages(self, cache, name, heads, dim, dtype, written=False):
+        """(keys, values, quantised, their Rows) of a layer's pages [pages, page_rows, heads, dim]."""
         if not isinstance(cache, (tuple, list)) or len(cache) != 2:
             raise ValueError("%s must be a pair of keys and values" % name)
         k, v = cache
-        for t in (k, v):
+        for t in cache:
             if not isinstance(t, (torch.Tensor, QuantRows)):
                 raise TypeError("%s must hold tensors or QuantRows" % name)
         quant, s = isinstance(k, QuantRows), k.shape
@@ -1050,7 +1050,14 @@ class Context:
             raise TypeError("%s must be %s or QuantRows, got %s and %s" % (name, dtype, k.dtype, v.dtype))
         if s[0] | s[1] > _INT32_MAX:
             _fits(max(s[0], s[1]), name)
-        return k, v, quant
+        if written:
+            for t in cache:
+                # paged_cache's layout, a place for every number, is seen at a glance
+                x = t.codes if quant else t
+                if x.stride() != (s[1] * heads * dim, dim, s[1] * dim, 1) or (
+                        quant and t.scales.stride() != (s[1] * heads, 1, s[1])):
+                    _apart(t, name)
+        return k, v, quant, _rows(k, 3, name), _rows(v, 3, name)
 
     def _table(self, page_table, batch):
         """Extents of a page table [batch or more, pages of a sequence], for _args."""
@@ -1075,15 +1082,16 @@ class Context:
         slots] or [batch, slots] int32 (None: start + i), axis [rot / 2] int32 the axis of
         each pair (None: the first).  Returns q_out (None without q; allocated as
         zeros when None; q itself rotates in place)."""
-        for name, t in (("k", k), ("v", v), ("q", q)):
-            if t is not None or name != "q":
-                if not isinstance(t, torch.Tensor) or t.dim() != 4 or min(t.shape) < 1:
-                    raise ValueError("%s must be [batch, slots, heads, dim]" % name)
-        B, S, H, D = k.shape
-        if v.shape != k.shape:
+        if not isinstance(k, torch.Tensor) or k.dim() != 4 or min(k.shape) < 1:
+            raise ValueError("k must be [batch, slots, heads, dim]")
+        shape, kind = k.shape, k.dtype
+        B, S, H, D = shape
+        if not isinstance(v, torch.Tensor) or v.shape != shape:
             _need(v, "v", B, S, H, D)
         Hq = 0
         if q is not None:
+            if not isinstance(q, torch.Tensor) or q.dim() != 4 or q.shape[2] < 1:
+                raise ValueError("q must be [batch, slots, heads, dim]")
             Hq = q.shape[2]
             if q.shape != (B, S, Hq, D):
                 _need(q, "q", B, S, Hq, D)
@@ -1091,19 +1099,18 @@ class Context:
             raise ValueError("q_out needs q")
         if B | S | H | Hq | D > _INT32_MAX:
             _fits(max(B, S, H, Hq, D), "q or k")
-        if k.dtype not in (torch.bfloat16, torch.float16):
+        if kind is not torch.bfloat16 and kind is not torch.float16:
             raise TypeError("k must be bfloat16 or float16")
-        for name, t in (("v", v), ("q", q), ("q_out", q_out)):
-            if t is not None and (not isinstance(t, torch.Tensor) or t.dtype != k.dtype):
-                raise TypeError("%s must be a tensor of %s" % (name, k.dtype))
-        if q_out is not None and q_out is not q:
+        if v.dtype is not kind or (q is not None and q.dtype is not kind):
+            raise TypeError("v and q must be %s" % kind)
+        if q_out is not None:
+            if not isinstance(q_out, torch.Tensor) or q_out.dtype is not kind:
+                raise TypeError("q_out must be a tensor of %s" % kind)
             if q_out.shape != q.shape:
                 _need(q_out, "q_out", B, S, Hq, D)
-        if q_out is not None and not q_out.is_contiguous():
-            _apart(q_out, "q_out")
-        ck, cv, quant = self._pages(cache, "cache", H, D, k.dtype)
-        for t, name in ((ck, "cache keys"), (cv, "cache values")):
-            _apart(t, name)
+            if not q_out.is_contiguous():
+                _apart(q_out, "q_out")
+        ck, cv, quant, rk, rv = self._pages(cache, "cache", H, D, kind, True)
         F, axes = 0, 1
         if freq is not None:
             if not isinstance(freq, torch.Tensor) or freq.dim() != 1:
@@ -1121,7 +1128,7 @@ class Context:
             axes = positions.shape[0]
         elif axis is not None:
             raise ValueError("axis needs positions")
-        dtype, one, i32 = _DTYPES[k.dtype], (B,), torch.int32
+        dtype, one, i32 = _DTYPES[kind], (B,), torch.int32
         p_table, p_n, p_start, p_pos, p_axis, p_freq = self._args(
             (("k", k), ("v", v), ("q", q), ("q_out", q_out), ("cache keys", ck), ("cache values", cv)),
             self._table(page_table, B),
@@ -1136,8 +1143,7 @@ class Context:
         a = PagedRows(B, S, Hq, H, D, 2 * F, 1 if interleaved else 0, dtype, 3 if quant else dtype)
         if Hq:
             a.q, a.q_out = _rows(q, 3, "q"), _rows(q_out, 3, "q_out")
-        a.k, a.v, a.cache_k, a.cache_v = (_rows(k, 3, "k"), _rows(v, 3, "v"), _rows(ck, 3, "cache"),
-                                          _rows(cv, 3, "cache"))
+        a.k, a.v, a.cache_k, a.cache_v = _rows(k, 3, "k"), _rows(v, 3, "v"), rk, rv
         a.pages = PageTable(p_table, n, n, ck.shape[0], ck.shape[1])
         a.n_rows, a.start, a.positions, a.axes, a.axis, a.freq = p_n, p_start, p_pos, axes, p_axis, p_freq
         _check(lib().graft_paged_write(self._h, C.byref(a), _stream()), "graft_paged_write")
@@ -1204,7 +1210,7 @@ class Context:
             raise ValueError("sinks must be 0..2^31 - 1")
         first = cache[0] if isinstance(cache, (tuple, list)) and len(cache) == 2 else None
         H = first.shape[2] if isinstance(first, (torch.Tensor, QuantRows)) and len(first.shape) == 4 else 1
-        ck, cv, quant = self._pages(cache, "cache", H, D, q.dtype)
+        ck, cv, quant, rk, rv = self._pages(cache, "cache", H, D, q.dtype)
         N = self.dims.max_nodes
         W = (N + 63) // 64
         one, i32 = (B,), torch.int32
@@ -1220,8 +1226,7 @@ class Context:
         dtype, n = _DTYPES[q.dtype], page_table.shape[1]
         a = PagedAttention(B, S, 1 if with_root else 0, Hq, H, D, dtype, 3 if quant else dtype,
                            float(D ** -0.5 if scale is None else scale), window, sinks, _rows(q, 3, "q"), p_n,
-                           p_mask, _rows(ck, 3, "cache"), _rows(cv, 3, "cache"),
-                           PageTable(p_table, n, n, ck.shape[0], ck.shape[1]), p_len, _rows(out, 3, "out"), p_lse)
+                           p_mask, rk, rv, PageTable(p_table, n, n, ck.shape[0], ck.shape[1]), p_len, _rows(out, 3, "out"), p_lse)
         return a, out
 
     def paged_commit(self, cache, page_table, start, acc_len, acc_nodes, with_root=False):

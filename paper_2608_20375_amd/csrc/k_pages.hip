@@ -20,7 +20,8 @@ namespace graft {
 namespace {
 
 constexpr int kPageThreads = 256;
-constexpr int kPageRows = 4;      // rows a thread loads before it stores any
+constexpr int kPageRows = 2;      // rows a thread loads before it stores any
+constexpr int kMostThreads = 1024;
 constexpr int kPathGroup = 16;    // rows of the path in registers at a time
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
@@ -42,7 +43,7 @@ struct WriteArgs {
   const double *freq;
   int32_t batch, slots, q_heads, kv_heads, dim, half, pair_step, axes;   // half: rot_dim / 2
   int32_t lanes, cols;                  // lanes of a head; of a row
-  int32_t at_once, col_blocks, row_blocks;
+  int32_t at_once, threads, col_blocks, row_blocks;
   uint32_t *error_flag;
 };
 
@@ -97,9 +98,13 @@ __device__ __forceinline__ uint64_t encode(const float *x, int e) {
   return static_cast<uint64_t>(out[1]) << 32 | out[0];
 }
 
+__device__ __forceinline__ u32x4 load_once(const char *p) {
+  return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p));
+}
+
 // HALF: fp16 numbers, else bf16.  Q8: e4m3 pages.
 template <bool HALF, bool Q8>
-__global__ void __launch_bounds__(kPageThreads)
+__global__ void __launch_bounds__(kMostThreads)
 write_kernel(WriteArgs a) {
   extern __shared__ f32x2 turns[];        // [rows of the workgroup][half]
   int blk = blockIdx.x;
@@ -114,17 +119,19 @@ write_kernel(WriteArgs a) {
   if (row0 >= n) return;
 
   const int sub = a.at_once > 1 ? threadIdx.x / a.cols : 0;
-  const int col = a.at_once > 1 ? threadIdx.x - sub * a.cols : cb * kPageThreads + threadIdx.x;
+  const int col = a.at_once > 1 ? threadIdx.x - sub * a.cols : cb * blockDim.x + threadIdx.x;
   const int unit = col & (a.lanes - 1), hd = col / a.lanes;
   const bool mine = sub < a.at_once && col < a.cols && unit * 16 < a.dim;
   const bool is_q = hd < a.q_heads, is_k = !is_q && hd < a.q_heads + a.kv_heads;
   const int head = is_q ? hd : is_k ? hd - a.q_heads : hd - a.q_heads - a.kv_heads;
   const bool turned = (is_q || is_k) && unit * 8 < a.half;
-  // numbers at c0.. and c1.., eight each
-  const int c0 = turned && a.pair_step == 1 ? unit * 8 : unit * 16;
-  const int c1 = turned && a.pair_step == 1 ? c0 + a.half : c0 + 8;
-  const Place &from = is_q ? a.q : is_k ? a.k : a.v;
-  const char *src = from.p + b * from.batch + head * from.head;
+  // A thread's eight numbers each at c0.. and c1..: a piece of either half of what is rotated, or of
+  // either half of the rest, so that a head's lanes read neighbouring 16 bytes.
+  const int part = is_q || is_k ? 2 * a.half : 0, mid = turned ? a.half : (a.dim - part) / 2;
+  const int c0 = turned ? unit * 8 : part + (unit - part / 16) * 8, c1 = c0 + mid;
+  const char *src = is_q ? a.q.p + b * a.q.batch + head * a.q.head
+                         : is_k ? a.k.p + b * a.k.batch + head * a.k.head : a.v.p + b * a.v.batch + head * a.v.head;
+  const int64_t src_row = is_q ? a.q.row : is_k ? a.k.row : a.v.row;
 
   u32x4 lo[kPageRows], hi[kPageRows];
   int page[kPageRows], off[kPageRows];
@@ -134,26 +141,29 @@ write_kernel(WriteArgs a) {
     const int i = row0 + sub + x * a.at_once;
     ok[x] = mine && i < n;
     lo[x] = hi[x] = u32x4{0, 0, 0, 0};
-    page[x] = off[x] = 0;
     if (ok[x]) {
-      lo[x] = *reinterpret_cast<const u32x4 *>(src + i * from.row + c0 * 2);
-      hi[x] = *reinterpret_cast<const u32x4 *>(src + i * from.row + c1 * 2);
-      if (!is_q) {
-        const int64_t r = static_cast<int64_t>(first) + i;
-        bool good = r >= 0 && r < a.pages.rows();
-        const int entry = a.pages.entry(good ? static_cast<uint32_t>(r) : 0u);
-        off[x] = good ? static_cast<int>(r) - entry * a.pages.page_rows : 0;
-        page[x] = good ? a.pages.table[b * a.pages.table_stride + entry] : -1;
-        good = page[x] >= 0 && page[x] < a.pages.pages;
-        if (!good) atomicOr(a.error_flag, kErrPage);
-        ok[x] = good;
-      }
+      lo[x] = load_once(src + i * src_row + c0 * 2);
+      hi[x] = load_once(src + i * src_row + c1 * 2);
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < kPageRows; ++x) {
+    page[x] = off[x] = 0;
+    if (ok[x] && !is_q) {
+      const int64_t r = static_cast<int64_t>(first) + row0 + sub + x * a.at_once;
+      bool good = r >= 0 && r < a.pages.rows();
+      const int entry = a.pages.entry(good ? static_cast<uint32_t>(r) : 0u);
+      off[x] = good ? static_cast<int>(r) - entry * a.pages.page_rows : 0;
+      page[x] = good ? a.pages.table[b * a.pages.table_stride + entry] : -1;
+      good = page[x] >= 0 && page[x] < a.pages.pages;
+      if (!good) atomicOr(a.error_flag, kErrPage);
+      ok[x] = good;
     }
   }
 
   if (a.half > 0) {
     const int rows = n - row0 < span ? n - row0 : span;
-    for (int u = threadIdx.x; u < rows * a.half; u += kPageThreads) {
+    for (int u = threadIdx.x; u < rows * a.half; u += blockDim.x) {
       const int r = u / a.half, f = u - r * a.half;
       int64_t pos = static_cast<int64_t>(first) + row0 + r;
       if (a.positions) {
@@ -173,16 +183,18 @@ write_kernel(WriteArgs a) {
   for (int x = 0; x < kPageRows; ++x) {
     const int r = sub + x * a.at_once, i = row0 + r;
     float u[8], w[8];                     // what goes to c0.. and c1..
+    if (turned || (Q8 && !is_q)) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      u[2 * j] = lower<HALF>(lo[x][j]);
-      u[2 * j + 1] = upper<HALF>(lo[x][j]);
-      w[2 * j] = lower<HALF>(hi[x][j]);
-      w[2 * j + 1] = upper<HALF>(hi[x][j]);
+      for (int j = 0; j < 4; ++j) {
+        u[2 * j] = lower<HALF>(lo[x][j]);
+        u[2 * j + 1] = upper<HALF>(lo[x][j]);
+        w[2 * j] = lower<HALF>(hi[x][j]);
+        w[2 * j + 1] = upper<HALF>(hi[x][j]);
+      }
     }
     if (turned && ok[x]) {
-      const f32x2 *t = turns + r * a.half + unit * 8;
       if (a.pair_step == 1) {
+        const f32x2 *t = turns + r * a.half + c0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const f32x2 cs = t[j];
@@ -193,7 +205,7 @@ write_kernel(WriteArgs a) {
       } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const f32x2 cs = t[j];
+          const f32x2 cs = turns[r * a.half + (j < 4 ? c0 : c1) / 2 + j % 4];
           float *z = j < 4 ? u + 2 * j : w + 2 * (j - 4);
           const float p = z[0], s = z[1];
           z[0] = p * cs.x - s * cs.y;
@@ -217,8 +229,8 @@ write_kernel(WriteArgs a) {
       int e = static_cast<int>(m >> 23) - 135 + ((m & 0x7FFFFFu) > 0x600000u ? 1 : 0);
       e = e < -118 ? -118 : e;
       if (ok[x]) {
-        const Place &to = is_k ? a.cache_k : a.cache_v;
-        char *d = to.p + page[x] * to.batch + off[x] * to.row + head * to.head;
+        char *d = is_k ? a.cache_k.p + page[x] * a.cache_k.batch + off[x] * a.cache_k.row + head * a.cache_k.head
+                       : a.cache_v.p + page[x] * a.cache_v.batch + off[x] * a.cache_v.row + head * a.cache_v.head;
         *reinterpret_cast<uint64_t *>(d + c0) = encode(u, e);
         *reinterpret_cast<uint64_t *>(d + c1) = encode(w, e);
         if (unit == 0) {
@@ -235,9 +247,9 @@ write_kernel(WriteArgs a) {
           hi[x][j] = pack<HALF>(w[2 * j], w[2 * j + 1]);
         }
       }
-      const Place &to = is_q ? a.q_out : is_k ? a.cache_k : a.cache_v;
-      char *d = is_q ? to.p + b * to.batch + i * to.row + head * to.head
-                     : to.p + page[x] * to.batch + off[x] * to.row + head * to.head;
+      char *d = is_q ? a.q_out.p + b * a.q_out.batch + i * a.q_out.row + head * a.q_out.head
+                : is_k ? a.cache_k.p + page[x] * a.cache_k.batch + off[x] * a.cache_k.row + head * a.cache_k.head
+                       : a.cache_v.p + page[x] * a.cache_v.batch + off[x] * a.cache_v.row + head * a.cache_v.head;
       *reinterpret_cast<u32x4 *>(d + c0 * 2) = lo[x];
       *reinterpret_cast<u32x4 *>(d + c1 * 2) = hi[x];
     }
@@ -306,7 +318,7 @@ path_kernel(PathArgs a) {
 #pragma unroll
     for (int k = 0; k < kPathGroup; ++k) {
       if (((moves >> g) >> k) & 1) {
-        if (active) v[k] = *reinterpret_cast<const u32x4 *>(p + uniform64(at_s, g + k));
+        if (active) v[k] = load_once(p + uniform64(at_s, g + k));
         if (scales) w[k] = s[uniform64(sc_s, g + k)];
       }
     }
@@ -359,8 +371,11 @@ WriteArgs plan_write(const graft_paged_rows &r, int64_t *blocks) {
   a.lanes = 1;
   while (a.lanes < r.head_dim / 16) a.lanes *= 2;
   a.cols = (r.q_heads + 2 * r.kv_heads) * a.lanes;
-  a.at_once = a.cols < kPageThreads ? kPageThreads / a.cols : 1;
-  a.col_blocks = (a.cols + kPageThreads - 1) / kPageThreads;
+  // a row's columns in one workgroup, whose angles they share, where they fit: whole waves, or several
+  // rows of up to 256 columns
+  a.at_once = a.cols <= kPageThreads ? kPageThreads / a.cols : 1;
+  a.threads = a.cols <= kPageThreads ? kPageThreads : a.cols <= kMostThreads ? (a.cols + kWave - 1) / kWave * kWave : 512;
+  a.col_blocks = (a.cols + a.threads - 1) / a.threads;
   const int span = a.at_once * kPageRows;
   a.row_blocks = (r.slots + span - 1) / span;
   *blocks = static_cast<int64_t>(a.col_blocks) * a.row_blocks * r.batch;
@@ -409,15 +424,15 @@ PageMap page_map(const graft_page_table &t) {
 
 int64_t paged_write_blocks(const graft_paged_rows &r) {
   int64_t blocks;
-  plan_write(r, &blocks);
-  return blocks;
+  const WriteArgs a = plan_write(r, &blocks);
+  return blocks * ((a.threads + 255) / 256);   // a launch counts its threads
 }
 
 hipError_t launch_paged_write(graft_ctx *ctx, const graft_paged_rows &r, hipStream_t stream) {
   int64_t blocks;
   WriteArgs a = plan_write(r, &blocks);
   a.error_flag = ctx->error_flag;
-  const dim3 grid(static_cast<unsigned>(blocks)), block(kPageThreads);
+  const dim3 grid(static_cast<unsigned>(blocks)), block(static_cast<unsigned>(a.threads));
   const size_t lds = static_cast<size_t>(a.at_once) * kPageRows * a.half * sizeof(f32x2);   // 32 KB at most
   if (r.cache_dtype == GRAFT_E4M3) hipLaunchKernelGGL((write_kernel<false, true>), grid, block, lds, stream, a);
   else if (r.dtype == GRAFT_F16) hipLaunchKernelGGL((write_kernel<true, false>), grid, block, lds, stream, a);

@@ -59,6 +59,46 @@ int main() {
           for (int r = 0; r < end; ++r)
             if ((r < sinks || r >= low) && !in[r]) fail("missing", r, low, sinks);
         }
+  // a row tile's tiles against each of its slots' rows: all in, and in a clear tile all seen by all
+  for (int base = 0; base <= 200; base += 9)
+    for (int n : {1, 2, 7, 40, 70})
+      for (int s0 = 0; s0 < n; s0 += 1 + n / 3)
+        for (int s1 = s0; s1 < n; s1 += 1 + n / 4)
+          for (int window : {0, 1, 5, 64, 100, 0x7FFFFFFF})
+            for (int sinks : {0, 3, 40, 0x7FFFFFFF})
+              for (bool masked : {false, true})
+                for (int keys : {32, 64}) {
+                  const RowTile t = row_tile(base, n, s0, s1, masked, window, sinks, keys);
+                  auto holds = [&](int r) {
+                    for (int i = 0; i < t.span.all(); ++i)
+                      if (r / keys == t.span.at(i)) return true;
+                    return false;
+                  };
+                  for (int slot = s0; slot <= s1; ++slot)
+                    // a masked slot's position: any from base - 1 to base + slot
+                    for (int place = masked ? -1 : slot; place <= slot; ++place)
+                      for (int r = 0; r < base + n; ++r) {
+                        const bool near = window == 0 || r > static_cast<int64_t>(base) + place - window || r < sinks;
+                        const bool sees = r < base ? near : !masked && r <= base + slot && near;
+                        if (sees && !holds(r)) fail("row not walked", base, slot, r);
+                        const int j = r / keys * keys;
+                        if (!sees && is_clear(t, j, keys, window > 0 ? sinks : 0) && place <= n - 1)
+                          fail("tile not clear", base, slot, r);
+                      }
+                  if (masked)
+                    for (int r = base; r < base + n; ++r)
+                      if (!holds(r)) fail("slot not walked", base, n, r);
+                }
+  // pieces are in order, without gaps, and as even as whole tiles allow
+  for (int n = 0; n <= 300; n += 7)
+    for (int pieces = 1; pieces <= 128; ++pieces) {
+      if (cut_at(n, pieces, 0) != 0 || cut_at(n, pieces, pieces) != n) fail("ends", n, pieces, 0);
+      for (int p = 0; p < pieces; ++p) {
+        const int d = cut_at(n, pieces, p + 1) - cut_at(n, pieces, p);
+        if (d < n / pieces || d > (n + pieces - 1) / pieces) fail("piece", n, pieces, p);
+      }
+    }
+  if (cut_at(1 << 25, 128, 127) != (1 << 25) / 128 * 127) fail("cut_at", 0, 0, 0);
   if (low_bits(-5) != 0 || low_bits(0) != 0 || low_bits(1) != 1 || low_bits(63) != ~0ull >> 1 ||
       low_bits(64) != ~0ull || low_bits(1000) != ~0ull)
     fail("low_bits", 0, 0, 0);

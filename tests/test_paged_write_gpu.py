@@ -283,3 +283,67 @@ def test_pages_past_32_bit_offsets():
         assert torch.equal(p[pages - 1, page - 2:], x[0, :2]) and torch.equal(p[pages - 2, :2], x[0, 2:])
         assert int(torch.count_nonzero(p[:pages - 2])) == 0
     ctx.close()
+
+
+def test_calls_on_side_streams_and_in_graphs():
+    """Writes to pages of their own on two streams at once; a captured write follows its inputs' memory."""
+    rng = np.random.default_rng(6)
+    D, page = 64, 16
+    freq = dev(10.0 ** -np.linspace(0, 4, 32))
+    runs = []
+    for i in range(2):
+        ctx = G.Context(2, 4, 64, 1, 8)
+        kv = tuple(torch.zeros(6, page, 2, D, dtype=BF, device="cuda") for _ in range(2))
+        x = [block(rng, 2, 20, h, D, BF).cuda() for h in (2, 2, 4)]
+        t = dev(rng.permutation(6).astype(np.int32).reshape(2, 3))
+        start = dev(np.array([3 + i, 20], np.int32))
+        runs.append((ctx, kv, x, t, start, torch.zeros_like(x[2]), torch.cuda.Stream()))
+    call = lambda r: r[0].paged_write(r[1], r[3], r[2][0], r[2][1], start=r[4], q=r[2][2], q_out=r[5], freq=freq)
+    torch.cuda.synchronize()
+    for r in runs:
+        with torch.cuda.stream(r[6]):
+            call(r)
+    torch.cuda.synchronize()
+    for r in runs:
+        got = [x.clone() for x in (*r[1], r[5])]
+        for x in (*r[1], r[5]):
+            x.zero_()
+        call(r)
+        assert all(torch.equal(a, b) for a, b in zip(got, (*r[1], r[5]))) and got[0].abs().sum() > 0
+    r = runs[0]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call(r)
+    for s in ([0, 5], [28, 1], [9, 9]):
+        r[4].copy_(dev(np.array(s, np.int32)))
+        r[2][0].copy_(block(rng, 2, 20, 2, D, BF))
+        for x in (*r[1], r[5]):
+            x.zero_()
+        call(r)
+        eager = [x.clone() for x in (*r[1], r[5])]
+        for x in (*r[1], r[5]):
+            x.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(eager, (*r[1], r[5])))
+    for r in runs:
+        assert r[0].device_status() == 0
+        r[0].close()
+
+
+def test_codes_match_the_contiguous_cache():
+    """Rows that are not rotated get the codes and scales of cache_write."""
+    rng = np.random.default_rng(8)
+    k = block(rng, 2, 21, 3, 80, BF, 3.0).cuda()
+    ctx = G.Context(2, 4, 64, 1, 8)
+    flat = G.QuantRows.empty(1, 2, 24, 3, 80)
+    n = dev(np.array([21, 10], np.int32))
+    ctx.cache_write(flat, k[None], n)
+    kp, vp = (G.paged_cache(6, 8, 3, 80, Q8) for _ in range(2))
+    ctx.paged_write((kp, vp), dev(np.array([[5, 0, 3], [1, 2, 4]], np.int32)), k, k, n)
+    for b, pages in ((0, (5, 0, 3)), (1, (1, 2, 4))):
+        m = int(n[b])
+        for p in (kp, vp):
+            for x, y in ((p.codes, flat.codes), (p.scales, flat.scales)):
+                assert torch.equal(torch.cat([x[i] for i in pages])[:m], y[0, b, :m])
+    ctx.close()

@@ -320,7 +320,6 @@ struct PagedPlan {
   int few;            // a sequence's rows fit one tile of 16 (1) or 32 (2): the narrow walk
   int tile_rows;      // rows of a row tile (wide: 32, 64, 96 or 128)
   int row_tiles;      // of a sequence and key head
-  int groups;         // that share all rounds, each a workgroup for every row tile; 0: not shared
   bool fits;          // all rounds are counted in 32 bits
   int64_t part_rows;  // rows of pieces in the workspace
   int64_t share_at;   // how the rounds are shared, in the workspace

@@ -55,9 +55,9 @@ struct PagedArgs {
   int64_t rows_all;       // batch * slots * q_heads
   int32_t batch, slots, root, q_heads, kv_heads, group, dim;
   int32_t n_max, words, window, sinks;
-  int32_t tile_rows, row_tiles;   // rows of a row tile, and how many a sequence and key head has
-  int32_t groups;         // that share all rounds; 0: a workgroup for each row tile's whole walk
-  int32_t *share;         // rounds of a group, then [batch] each sequence's first round
+  int32_t tile_rows, row_tiles;   // rows of the narrow walk's tile; most row tiles of a sequence and key head
+  int32_t cut;            // wide: rounds are shared; 0: a workgroup for each row tile's whole walk
+  int32_t *share;         // rounds of a workgroup, then [batch] each sequence's first round or workgroup
   float c;
 };
 
@@ -619,63 +619,99 @@ __device__ __forceinline__ void narrow_part(const PagedArgs &a, int b, int kvh, 
   }
 }
 
-// A sequence's row tile, and the rounds that it takes for each of its key heads: of four 32-key tiles
-// in the narrow walk, of a 64-key tile of the last row tile in the wide one.
+// The row tiles of a sequence's query rows of a key head: the narrow walk's one; of the wide one's as few
+// as 128 rows each allow, all of one size in whole waves (260 rows are three tiles of three waves, not two
+// of four and a rest).
+__device__ __forceinline__ int row_tiles_of(int rows) { return (rows + kWideRows - 1) / kWideRows; }
+__device__ __forceinline__ int height_of(int rows) {
+  const int waves = 32 * row_tiles_of(rows);
+  return (rows + waves - 1) / waves * 32;
+}
 template <bool WIDE>
 __device__ __forceinline__ RowTile tile_of(const PagedArgs &a, int n, int len, int tile_row) {
-  const int first = tile_row * a.tile_rows, rows = n * a.group;
-  return row_tile(len, n, WIDE ? first / a.group : 0, WIDE ? (std::min(first + a.tile_rows, rows) - 1) / a.group : n - 1,
+  const int rows = n * a.group, height = WIDE ? height_of(rows) : 0, first = tile_row * height;
+  return row_tile(len, n, WIDE ? first / a.group : 0, WIDE ? (std::min(first + height, rows) - 1) / a.group : n - 1,
                   a.mask != nullptr, a.window, a.sinks, WIDE ? kWideKeys : kFewKeys);
 }
+// The rounds that it takes for each of its key heads: of four 32-key tiles in the narrow walk, of a
+// 64-key tile of the last row tile in the wide one.
 template <bool WIDE>
 __device__ __forceinline__ int rounds_of(const PagedArgs &a, int n, int len) {
   if (n == 0) return 0;
-  const int tiles = tile_of<WIDE>(a, n, len, WIDE ? (n * a.group - 1) / a.tile_rows : 0).span.all();
+  const int tiles = tile_of<WIDE>(a, n, len, WIDE ? row_tiles_of(n * a.group) - 1 : 0).span.all();
   return WIDE ? tiles : (tiles + kWaves - 1) / kWaves;
 }
-// The workgroup of a group and row tile: a group's follow each other on one XCD (workgroups go round
-// all 8), whose L2 then holds the keys that they share.
-__device__ __forceinline__ int block_of(int group, int tile_row, int row_tiles) {
-  return ((group >> 3) * row_tiles + tile_row) * 8 + (group & 7);
+// A sequence's workgroups in the wide walk, units (pieces of key heads) x row tiles: a unit's row tiles
+// follow each other on one XCD (workgroups go round all 8), whose L2 then holds the keys that they share.
+// Eights of units, and what is left in the same way.
+struct Item {
+  int unit, tile_row;
+};
+__device__ __forceinline__ Item item_at(int at, int units, int row_tiles) {
+  const int eight = at / (8 * row_tiles), base = 8 * eight, wide = std::min(8, units - base), x = at - base * row_tiles;
+  const int r = x / wide;
+  return Item{base + x - r * wide, r};
+}
+__device__ __forceinline__ int place_of(int unit, int tile_row, int units, int row_tiles) {
+  const int base = unit & ~7, wide = std::min(8, units - base);
+  return base * row_tiles + tile_row * wide + unit - base;
 }
 
 // How all rounds are shared.  A thread's sequences are c of them from tid * c on; sums over the workgroup.
+template <int N>
 struct Sum {
-  int before, all, most;      // in front of the thread's, all, and the largest of `most`
+  int before[N], all[N], most;      // in front of the thread's, all, and the largest of `most`
 };
-__device__ __forceinline__ Sum sum_over(int mine, int most, int *s_sum) {
-  const int tid = threadIdx.x, wave = tid / kWave, upto = wave_incl_scan(mine);
+template <int N>
+__device__ __forceinline__ Sum<N> sum_over(const int (&mine)[N], int most, int *s_sum) {
+  const int wave = threadIdx.x / kWave;
+  Sum<N> s;
+#pragma unroll
+  for (int i = 0; i < N; ++i) s.before[i] = wave_incl_scan(mine[i]);
 #pragma unroll
   for (int k = 1; k < kWave; k <<= 1) most = std::max(most, static_cast<int>(xor_lane(static_cast<uint32_t>(most), k)));
   __syncthreads();
   if (lane_id() == kWave - 1) {
-    s_sum[wave] = upto;
-    s_sum[kWaves + wave] = most;
+#pragma unroll
+    for (int i = 0; i < N; ++i) s_sum[wave * (N + 1) + i] = s.before[i];
+    s_sum[wave * (N + 1) + N] = most;
   }
   __syncthreads();
-  Sum s{upto - mine, 0, 0};
+  s.most = 0;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    s.before += w < wave ? s_sum[w] : 0;
-    s.all += s_sum[w];
-    s.most = std::max(s.most, s_sum[kWaves + w]);
+  for (int i = 0; i < N; ++i) {
+    s.before[i] -= mine[i];
+    s.all[i] = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const int x = s_sum[w * (N + 1) + i];
+      s.before[i] += w < wave ? x : 0;
+      s.all[i] += x;
+    }
+    // the same in all threads: scalars, so that the walk's tables stay scalar
+    s.all[i] = __builtin_amdgcn_readfirstlane(s.all[i]);
   }
-  // the same in all threads: scalars, so that the walk's tables stay scalar
-  s.all = __builtin_amdgcn_readfirstlane(s.all);
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) s.most = std::max(s.most, s_sum[w * (N + 1) + N]);
   s.most = __builtin_amdgcn_readfirstlane(s.most);
+  __syncthreads();
   return s;
 }
+// A sequence's share: slots, length, rounds of a walk, and walks (key heads and, in the wide walk, row tiles).
+struct Share {
+  int n, len, rounds, walks;
+};
 template <bool WIDE>
-__device__ __forceinline__ Sum all_rounds(const PagedArgs &a, int b0, int b1, int *s_sum) {
-  int sum = 0, most = 0;
-  for (int b = b0; b < b1; ++b) {
-    const Sizes s = sizes_of(a, b);
-    const int r = rounds_of<WIDE>(a, s.n, s.len);
-    if (s.bad && blockIdx.x == 0) atomicOr(a.error_flag, kErrBlockSizes);
-    sum += r * a.kv_heads;
-    most = std::max(most, r);
-  }
-  return sum_over(sum, most, s_sum);
+__device__ __forceinline__ Share share_of(const PagedArgs &a, int b) {
+  const Sizes s = sizes_of(a, b);
+  if (s.bad && blockIdx.x == 0) atomicOr(a.error_flag, kErrBlockSizes);
+  return Share{s.n, s.len, rounds_of<WIDE>(a, s.n, s.len), a.kv_heads * (WIDE ? row_tiles_of(s.n * a.group) : 1)};
+}
+// of(b, share) for the thread's sequences; the first of them, and up to 256 the only one, is `first`.
+template <bool WIDE, typename Of>
+__device__ __forceinline__ void each_share(const PagedArgs &a, int b0, int b1, const Share &first, Of of) {
+  if (b0 < b1) of(b0, first);
+  for (int b = b0 + 1; b < b1; ++b) of(b, share_of<WIDE>(a, b));
 }
 
 // The narrow walk's workgroups share all rounds of (sequence, key head, round) evenly, in that order,
@@ -686,28 +722,33 @@ template <typename Piece>
 __device__ __forceinline__ void share_rounds(const PagedArgs &a, int *s_sum, Piece piece) {
   const int tid = threadIdx.x, group = blockIdx.x, groups = gridDim.x;
   const int c = (a.batch + kThreads - 1) / kThreads, b0 = tid * c, b1 = std::min(b0 + c, a.batch);
-  const Sum sum = all_rounds<false>(a, b0, b1, s_sum);
-  const int per = std::max((sum.all + groups - 1) / groups, (sum.most + kMaxPieces - 2) / (kMaxPieces - 1));
-  const int first = group * per, last = std::min(first + per, sum.all);
-  __syncthreads();
+  const Share mine = b0 < b1 ? share_of<false>(a, b0) : Share{0, 0, 0, 0};
+  int rounds[1] = {0}, most = 0;
+  each_share<false>(a, b0, b1, mine, [&](int, const Share &s) {
+    rounds[0] += s.rounds * s.walks;
+    most = std::max(most, s.rounds);
+  });
+  const Sum<1> sum = sum_over(rounds, most, s_sum);
+  const int per = std::max((sum.all[0] + groups - 1) / groups, (sum.most + kMaxPieces - 2) / (kMaxPieces - 1));
+  const int first = group * per, last = std::min(first + per, sum.all[0]);
   // where the workgroup's first round is, and for the merge where each sequence begins
-  for (int b = b0, at = sum.before; b < b1; ++b) {
-    const Sizes s = sizes_of(a, b);
-    const int r = rounds_of<false>(a, s.n, s.len);
-    if (group == 0) a.share[1 + b] = at;
-    if (first >= at && first < at + r * a.kv_heads) {
+  int next = sum.before[0];
+  each_share<false>(a, b0, b1, mine, [&](int b, const Share &s) {
+    if (group == 0) a.share[1 + b] = next;
+    if (first >= next && first < next + s.rounds * s.walks) {
       s_sum[0] = b;
-      s_sum[1] = at;
+      s_sum[1] = next;
+      s_sum[2] = s.n;
+      s_sum[3] = s.len;
     }
-    at += r * a.kv_heads;
-  }
+    next += s.rounds * s.walks;
+  });
   if (group == 0 && tid == 0) a.share[0] = per;
   __syncthreads();
   if (first >= last) return;
   int b = __builtin_amdgcn_readfirstlane(s_sum[0]), begin = __builtin_amdgcn_readfirstlane(s_sum[1]);
-  for (int at = first; at < last;) {
-    const Sizes s = sizes_of(a, b);
-    const int n = __builtin_amdgcn_readfirstlane(s.n), len = __builtin_amdgcn_readfirstlane(s.len);
+  int n = __builtin_amdgcn_readfirstlane(s_sum[2]), len = __builtin_amdgcn_readfirstlane(s_sum[3]);
+  for (int at = first;;) {
     const int r = rounds_of<false>(a, n, len), end = begin + r * a.kv_heads;
     const RowTile tile = tile_of<false>(a, n, len, 0);
     while (at < last && at < end) {
@@ -718,52 +759,104 @@ __device__ __forceinline__ void share_rounds(const PagedArgs &a, int *s_sum, Pie
       piece(b, kvh, n, len, tile, (at - unit) * kWaves, std::min((stop - unit) * kWaves, tile.span.all()), part);
       at = stop;
     }
+    if (at >= last) return;
     begin = end;
     ++b;
+    const Sizes s = sizes_of(a, b);
+    n = __builtin_amdgcn_readfirstlane(s.n);
+    len = __builtin_amdgcn_readfirstlane(s.len);
   }
 }
 
-// In the wide walk a (sequence, key head) of r rounds is cut into ceil(r / per) even pieces, each a group
-// of workgroups, one for every row tile; a row tile's own tiles are cut in that proportion.  A lone piece
-// goes to the outputs.  per is the least for which there are groups for all pieces.  (Shared as in the
-// narrow walk, two pieces a workgroup begin and end there, and a begin costs three latencies.)
+// In the wide walk a (sequence, key head) of r rounds is cut into ceil(r / per) even pieces, each a unit
+// with a workgroup for every row tile; a row tile's own tiles are cut in that proportion.  A lone piece
+// goes to the outputs.  per is the least of four for which there are workgroups for all, from the rounds
+// of a workgroup if nothing were rounded up to what does when everything is.  (Shared as in the narrow
+// walk, two pieces a workgroup begin and end there, and a begin costs three latencies.)
 __device__ __forceinline__ int pieces_of(int rounds, int per) { return (rounds + per - 1) / per; }
-template <typename Piece>
-__device__ __forceinline__ void cut_rounds(const PagedArgs &a, int group, int tile_row, int *s_sum, Piece piece) {
-  const int tid = threadIdx.x;
+struct Wide {             // what a workgroup of the wide walk does, if t0 < t1
+  int b, kvh, n, len, tile_row, t0, t1, part;
+  RowTile tile;
+};
+__device__ __forceinline__ Wide cut_rounds(const PagedArgs &a, int *s_sum) {
+  constexpr int kTries = 4;
+  const int tid = threadIdx.x, me = blockIdx.x, groups = gridDim.x;
   const int c = (a.batch + kThreads - 1) / kThreads, b0 = tid * c, b1 = std::min(b0 + c, a.batch);
-  const Sum sum = all_rounds<true>(a, b0, b1, s_sum);
-  const int spare = std::max(a.groups - a.batch * a.kv_heads, 1);
-  const int per = std::max(std::max((sum.all + spare - 1) / spare, (sum.most + kMaxPieces - 1) / kMaxPieces), 1);
-  int mine = 0;
-  for (int b = b0; b < b1; ++b) {
-    const Sizes s = sizes_of(a, b);
-    mine += pieces_of(rounds_of<true>(a, s.n, s.len), per) * a.kv_heads;
-  }
-  const Sum count = sum_over(mine, 0, s_sum);
-  __syncthreads();
-  for (int b = b0, at = count.before; b < b1; ++b) {
-    const Sizes s = sizes_of(a, b);
-    const int p = pieces_of(rounds_of<true>(a, s.n, s.len), per) * a.kv_heads;
-    if (blockIdx.x == 0) a.share[1 + b] = at;
-    if (group >= at && group < at + p) {
-      s_sum[0] = b;
-      s_sum[1] = at;
+  const Share mine = b0 < b1 ? share_of<true>(a, b0) : Share{0, 0, 0, 0};
+  int work[2] = {0, 0}, most = 0;
+  each_share<true>(a, b0, b1, mine, [&](int, const Share &s) {
+    work[0] += s.rounds * s.walks;
+    work[1] += s.walks;
+    most = std::max(most, s.rounds);
+  });
+  const Sum<2> sum = sum_over(work, most, s_sum);
+  const int spare = std::max(groups - sum.all[1], 1);
+  const int lo = std::max(std::max((sum.all[0] + groups - 1) / groups, (sum.most + kMaxPieces - 1) / kMaxPieces), 1);
+  const int hi = std::max(std::min((sum.all[0] + spare - 1) / spare, sum.most), lo);
+  int tried[kTries] = {};
+  each_share<true>(a, b0, b1, mine, [&](int, const Share &s) {
+#pragma unroll
+    for (int k = 0; k < kTries; ++k) tried[k] += pieces_of(s.rounds, lo + (hi - lo) * k / (kTries - 1)) * s.walks;
+  });
+  const Sum<kTries> counts = sum_over(tried, 0, s_sum);
+  int per = hi, count = counts.all[kTries - 1], next = counts.before[kTries - 1];
+#pragma unroll
+  for (int k = kTries - 2; k >= 0; --k) {
+    if (counts.all[k] <= groups) {
+      per = lo + (hi - lo) * k / (kTries - 1);
+      count = counts.all[k];
+      next = counts.before[k];
     }
-    at += p;
   }
-  if (blockIdx.x == 0 && tid == 0) a.share[0] = per;
+  each_share<true>(a, b0, b1, mine, [&](int b, const Share &s) {
+    const int p = pieces_of(s.rounds, per) * s.walks;
+    if (me == 0) a.share[1 + b] = next;
+    if (me >= next && me < next + p) {
+      s_sum[0] = b;
+      s_sum[1] = next;
+      s_sum[2] = s.n;
+      s_sum[3] = s.len;
+    }
+    next += p;
+  });
+  if (me == 0 && tid == 0) a.share[0] = per;
+  Wide w;
+  w.t0 = w.t1 = 0;
+  if (me >= count) return w;
   __syncthreads();
-  if (group >= count.all) return;
-  const int b = __builtin_amdgcn_readfirstlane(s_sum[0]), begin = __builtin_amdgcn_readfirstlane(s_sum[1]);
-  const Sizes s = sizes_of(a, b);
-  const int n = __builtin_amdgcn_readfirstlane(s.n), len = __builtin_amdgcn_readfirstlane(s.len);
-  if (tile_row * a.tile_rows >= n * a.group) return;
-  const RowTile tile = tile_of<true>(a, n, len, tile_row);
-  const int pieces = pieces_of(rounds_of<true>(a, n, len), per), kvh = (group - begin) / pieces, p = group - begin - kvh * pieces;
-  const int all = tile.span.all(), t0 = cut_at(all, pieces, p), t1 = cut_at(all, pieces, p + 1);
+  w.b = __builtin_amdgcn_readfirstlane(s_sum[0]);
+  w.n = __builtin_amdgcn_readfirstlane(s_sum[2]);
+  w.len = __builtin_amdgcn_readfirstlane(s_sum[3]);
+  const int begin = __builtin_amdgcn_readfirstlane(s_sum[1]), pieces = pieces_of(rounds_of<true>(a, w.n, w.len), per);
+  const Item item = item_at(me - begin, pieces * a.kv_heads, row_tiles_of(w.n * a.group));
+  const int p = item.unit % pieces;
+  w.kvh = item.unit / pieces;
+  w.tile_row = item.tile_row;
+  w.tile = tile_of<true>(a, w.n, w.len, item.tile_row);
+  const int all = w.tile.span.all();
+  w.t0 = cut_at(all, pieces, p);
+  w.t1 = cut_at(all, pieces, p + 1);
+  w.part = pieces == 1 ? -1 : me;
   __syncthreads();
-  if (t0 < t1) piece(b, kvh, n, len, tile, t0, t1, pieces == 1 ? -1 : static_cast<int>(blockIdx.x));
+  return w;
+}
+// A workgroup for each row tile's whole walk.
+__device__ __forceinline__ Wide whole_walk(const PagedArgs &a) {
+  const Item item = item_at(blockIdx.x, a.batch * a.kv_heads, a.row_tiles);
+  Wide w;
+  w.t0 = w.t1 = 0;
+  w.tile_row = item.tile_row;
+  w.b = item.unit / a.kv_heads;
+  w.kvh = item.unit - w.b * a.kv_heads;
+  const Sizes s = sizes_of(a, w.b);
+  if (s.bad && item.tile_row == 0 && w.kvh == 0 && threadIdx.x == 0) atomicOr(a.error_flag, kErrBlockSizes);
+  w.n = __builtin_amdgcn_readfirstlane(s.n);
+  w.len = __builtin_amdgcn_readfirstlane(s.len);
+  if (item.tile_row >= row_tiles_of(w.n * a.group)) return w;
+  w.tile = tile_of<true>(a, w.n, w.len, item.tile_row);
+  w.t1 = w.tile.span.all();
+  w.part = -1;
+  return w;
 }
 
 // 128 rows a workgroup, 32 a wave; 64-key tiles in LDS for all four waves, the next tile's loads
@@ -802,8 +895,8 @@ __device__ __forceinline__ void wide_part(const PagedArgs &a, int b, int kvh, in
   const int lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int h = lane >> 5, col = lane & 31;
 
-  const int rows = live * a.group, local = wave * 32 + col, first = tile_row * a.tile_rows;
-  const bool valid = local < a.tile_rows && first + local < rows;
+  const int rows = live * a.group, local = wave * 32 + col, height = height_of(rows), first = tile_row * height;
+  const bool valid = local < height && first + local < rows;
   const int row = valid ? first + local : rows - 1;
   const int slot = row / a.group, head = kvh * a.group + row - slot * a.group;
   const bool busy = __ballot(valid) != 0;
@@ -925,12 +1018,12 @@ __device__ __forceinline__ void wide_part(const PagedArgs &a, int b, int kvh, in
   const char *qp = late().q + b * late().q_batch + slot * late().q_slot + head * late().q_head;
 #pragma unroll
   for (int s = 0; s < kSteps; ++s) rq[s] = s * 16 < a.dim ? take16(qp + s * 32 + h * 16) : u32x4{0, 0, 0, 0};
+  load(t0);
 #pragma unroll
   for (int s = 0; s < kSteps; ++s) settle(rq[s]);
 
   Sums<DP> st;
   st.clear(a.c);
-  load(t0);
   for (int t = t0; t < t1; ++t) {
     const int buf = (t - t0) & 1, j = held_j;
     const uint64_t bad = held_bad;
@@ -948,8 +1041,12 @@ __device__ __forceinline__ void wide_part(const PagedArgs &a, int b, int kvh, in
     for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[kt][i] = 0.0f;
+    // products go first, so that the other wave of the SIMD does its vector work in their time (with the
+    // sum made early: 8 pieces of 1024 slots 341 -> 334 us, 16 trees of up to 64 nodes 91 -> 85)
+    __builtin_amdgcn_s_setprio(1);
     pipelined<2 * kSteps>([&](int n) { return k[k_at<C>(n % 2 * 32 + col, n / 2 * 2 + h)]; },
                           [&](int n, const u32x4 &f) { s[n % 2] = T::mfma(f, rq[n / 2], s[n % 2]); });
+    __builtin_amdgcn_s_setprio(0);
     uint64_t seen = ~0ull;
     if (__builtin_expect(!clear, 0)) {
       const PagedArgs &z = late();
@@ -964,9 +1061,13 @@ __device__ __forceinline__ void wide_part(const PagedArgs &a, int b, int kvh, in
     }
     u32x4 p[4];
     softmax_step<T, 2>(st, s, p, a.c);
+    // the sum is made here: made where it is next needed, 32 probabilities would be kept over the products
+    asm volatile("" : "+v"(st.l));
+    __builtin_amdgcn_s_setprio(1);
     // four tiles of columns in turn: a product does not wait for the one before it
     pipelined<4 * kDTiles>([&](int n) { return v_fragment<C>(v, n % kDTiles, n / kDTiles, lane); },
                            [&](int n, const u32x4 &f) { st.o[n % kDTiles] = T::mfma(f, p[n / kDTiles], st.o[n % kDTiles]); });
+    __builtin_amdgcn_s_setprio(0);
     if (__builtin_expect(any_odd, 0)) {
       const PagedArgs &z = late();
       const char *v_at0 = z.v.p + kvh * z.v.head;
@@ -1040,22 +1141,8 @@ paged_attend_kernel(PagedArgs a) {
       narrow_part<T, Q8, HOT, DP, QT>(a, b, kvh, n, len, tile, t0, t1, part, lds);
     });
   } else {
-    const int i = blockIdx.x, j = i >> 3, tile_row = j % a.row_tiles, g = (j / a.row_tiles) * 8 + (i & 7);   // block_of
-    auto piece = [&](int b, int kvh, int n, int len, const RowTile &tile, int t0, int t1, int part) {
-      wide_part<T, Q8, HOT, DP>(a, b, kvh, n, len, tile_row, tile, t0, t1, part, lds);
-    };
-    if (a.groups > 0) {
-      cut_rounds(a, g, tile_row, s_sum, piece);
-      return;
-    }
-    if (g >= a.batch * a.kv_heads) return;
-    const int b = g / a.kv_heads, kvh = g - b * a.kv_heads;
-    const Sizes s = sizes_of(a, b);
-    const int n = __builtin_amdgcn_readfirstlane(s.n), len = __builtin_amdgcn_readfirstlane(s.len);
-    if (s.bad && tile_row == 0 && kvh == 0 && threadIdx.x == 0) atomicOr(a.error_flag, kErrBlockSizes);
-    if (tile_row * a.tile_rows >= n * a.group) return;
-    const RowTile tile = tile_of<true>(a, n, len, tile_row);
-    piece(b, kvh, n, len, tile, 0, tile.span.all(), -1);
+    const Wide w = a.cut ? cut_rounds(a, s_sum) : whole_walk(a);
+    if (w.t0 < w.t1) wide_part<T, Q8, HOT, DP>(a, w.b, w.kvh, w.n, w.len, w.tile_row, w.tile, w.t0, w.t1, w.part, lds);
   }
 }
 
@@ -1072,22 +1159,24 @@ merge_pages_kernel(PagedArgs a) {
   const int slot = static_cast<int>(bs - static_cast<int64_t>(b) * a.slots);
   const Sizes sz = sizes_of(a, b);
   if (slot >= sz.n) return;
-  const int kvh = head / a.group, row = slot * a.group + head - kvh * a.group, tile_row = WIDE ? row / a.tile_rows : 0;
+  const int kvh = head / a.group, row = slot * a.group + head - kvh * a.group;
+  const int height = WIDE ? height_of(sz.n * a.group) : a.tile_rows, tile_row = row / height, local = row - tile_row * height;
+  const int row_tiles = row_tiles_of(sz.n * a.group);
   const int rounds = rounds_of<WIDE>(a, sz.n, sz.len), per = a.share[0];
   int g0, pieces;
   if (WIDE) {
     pieces = pieces_of(rounds, per);
-    g0 = a.share[1 + b] + kvh * pieces;
+    g0 = kvh * pieces;                                        // the first unit
   } else {
     const int unit = a.share[1 + b] + kvh * rounds;
     g0 = unit / per;
     pieces = (unit + rounds - 1) / per - g0 + 1;
   }
   if (pieces == 1) return;                                  // the only one wrote the row
-  const int tiles = WIDE ? tile_of<true>(a, sz.n, sz.len, tile_row).span.all() : 0, local = row - tile_row * a.tile_rows;
+  const int tiles = WIDE ? tile_of<true>(a, sz.n, sz.len, tile_row).span.all() : 0;
   // where piece p's sums are; narrow: the first one is its group's last piece, the others are first ones
   auto at = [&](int p) {
-    return WIDE ? static_cast<int64_t>(block_of(g0 + p, tile_row, a.row_tiles)) * kWideRows + local
+    return WIDE ? static_cast<int64_t>(a.share[1 + b] + place_of(g0 + p, tile_row, pieces * a.kv_heads, row_tiles)) * kWideRows + local
                 : static_cast<int64_t>(2 * (g0 + p) + (p == 0 ? 1 : 0)) * a.tile_rows + local;
   };
   // a piece that cut_at leaves nothing was not written
@@ -1154,28 +1243,23 @@ PagedPlan paged_plan(const graft_paged_attention_desc &a) {
   const int64_t rows = static_cast<int64_t>(a.slots) * group, outer = static_cast<int64_t>(a.batch) * a.kv_heads;
   p.few = rows <= 16 ? 1 : rows <= kFewRows ? 2 : 0;
   p.row_tiles = p.few ? 1 : static_cast<int>((rows + kWideRows - 1) / kWideRows);
-  // row tiles of one size, whole waves: 260 rows are three tiles of three waves, not two of four and a rest
-  p.tile_rows = p.few ? 16 * p.few : static_cast<int>((rows + 32 * p.row_tiles - 1) / (32 * p.row_tiles) * 32);
-  p.row_tiles = p.few ? 1 : static_cast<int>((rows + p.tile_rows - 1) / p.tile_rows);
+  p.tile_rows = p.few ? 16 * p.few : kWideRows;
   // keys of a round: of the narrow walk's four waves, or a tile of the wide one
   const int keys = p.few ? kFewKeys * kWaves : kWideKeys;
   int64_t most = static_cast<int64_t>(a.pages.table_len) * a.pages.page_rows;
   if (a.window > 0) most = std::min<int64_t>(most, static_cast<int64_t>(a.window) + a.sinks + a.slots + 2 * keys);
   const int64_t rounds = (most + keys - 1) / keys, all = static_cast<int64_t>(a.batch) * a.slots * a.q_heads;
-  p.fits = outer * rounds < (int64_t{1} << 31);
+  p.fits = outer * p.row_tiles * rounds < (int64_t{1} << 31);
   if (p.few) {
     // as many as the registers let run at once
-    p.groups = static_cast<int>(std::min<int64_t>(outer * rounds, a.cache_dtype == GRAFT_E4M3 ? 768 : 512));
-    p.blocks = p.groups;
+    p.blocks = std::min<int64_t>(outer * rounds, a.cache_dtype == GRAFT_E4M3 ? 768 : 512);
   } else if (outer * p.row_tiles < 1024 && rounds > 1) {
-    // a group for every (sequence, key head), and what is left of the workgroups for more pieces (16 trees
-    // of up to 64 nodes: 122, 117, 103, 115 and 117 us with 512, 640, 768, 1024 and 1536 workgroups)
-    const int64_t some = std::max<int64_t>(768 / p.row_tiles, outer + 8) / 8 * 8;
-    p.groups = static_cast<int>(std::min<int64_t>((outer * rounds + 7) / 8 * 8, some));
-    p.blocks = static_cast<int64_t>(p.groups) * p.row_tiles;
+    // two a CU, which is what registers and LDS let run at once, but one for every row tile at least (16
+    // trees of up to 64 nodes: 91, 106, 112 and 111 us with 512, 640, 768 and 1024)
+    p.blocks = std::min<int64_t>(outer * p.row_tiles * rounds, std::max<int64_t>(512, outer * p.row_tiles));
   } else {
     p.fits = true;
-    p.blocks = (outer + 7) / 8 * 8 * p.row_tiles;
+    p.blocks = outer * p.row_tiles;
     return p;
   }
   p.merge_blocks = rounds > 1 ? (all + kThreads / 32 - 1) / (kThreads / 32) : 0;
@@ -1222,7 +1306,7 @@ hipError_t launch_paged_attend(graft_ctx *ctx, const graft_paged_attention_desc 
   a.sinks = d.window > 0 ? d.sinks : 0;
   a.tile_rows = p.tile_rows;
   a.row_tiles = p.row_tiles;
-  a.groups = p.groups;
+  a.cut = !p.few && p.bytes > 0 ? 1 : 0;
   a.c = d.scale * 1.4426950408889634f;
   const dim3 grid(static_cast<unsigned>(p.blocks)), block(kThreads);
   auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };

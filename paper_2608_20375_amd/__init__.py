@@ -174,11 +174,21 @@ class PagedPath(C.Structure):
                 ("acc_len", C.c_void_p), ("acc_nodes", C.c_void_p), ("with_root", C.c_int32)]
 
 
-# The two descriptors that a layer's step passes, packed in one go: at small batches the step waits
-# for the host (a write of one token 17.8 -> 16.0 us of it, against structures of structures).
-_PACK_ROWS = struct.Struct("@9i62qiii3qi2q")
-_PACK_ATTENTION = struct.Struct("@8ifii34qiii14q")
-assert _PACK_ROWS.size == C.sizeof(PagedRows) and _PACK_ATTENTION.size == C.sizeof(PagedAttention)
+# The descriptors that a layer's step passes, packed in one go: at small batches the step waits for the
+# host, and structures of structures take 2 to 3 us of a call (of a commit's 10.4 us, an attention's 18.5).
+# A graft_rows without scales is its address and three strides, one with them twice that; pads are zeros.
+def _packing(form, size):
+    """[of 16-bit caches, of quantised ones]; R: a graft_rows without scales, C: the cache's."""
+    plain, quant = "q8x3q40x", "q8x4q8x3q"
+    packings = [struct.Struct("@" + form.replace("R", plain).replace("C", c)) for c in (plain, quant)]
+    assert all(p.size == C.sizeof(size) for p in packings)
+    return packings
+
+
+_PACK_ROWS = _packing("9iRRRRCCqqiii4xqqqiqq", PagedRows)
+_PACK_ATTENTION = _packing("8ifiiRqqCCqqiii4xqRqqq", PagedAttention)
+_PACK_PATH = [struct.Struct("@5i%sqqiii4xqqqi4x" % c) for c in ("5q40x", "10q")]   # with planes
+_NO_ROWS = (0,) * 8
 
 
 def library_path() -> str:
@@ -235,7 +245,7 @@ def lib():
         L.graft_paged_write.argtypes = [vp, vp, vp]                 # packed descriptors
         L.graft_paged_attention_workspace.argtypes = [vp, vp, C.POINTER(i64)]
         L.graft_paged_attention.argtypes = [vp, vp, vp]
-        L.graft_paged_commit.argtypes = [vp, C.POINTER(PagedPath), vp]
+        L.graft_paged_commit.argtypes = [vp, vp, vp]
         L.graft_status_string.argtypes = [C.c_int]
         L.graft_status_string.restype = C.c_char_p
         L.graft_last_error.argtypes = []
@@ -410,24 +420,12 @@ def _rows(t, n, name):
     return Rows(*at, t.scales.data_ptr(), *lead, *[s[i] if e[i] > 1 else 0 for i in range(n)])
 
 
-_NONE = (0,) * 10
-
-
-def _flat_rows(t, name):
-    """The ten numbers of a graft_rows, as _rows, of a tensor or QuantRows with three extents."""
-    quant = isinstance(t, QuantRows)
-    x = t.codes if quant else t
-    a, b, c, d = x.stride()
-    e = x.shape
-    if d != 1 and e[3] > 1:
+def _row_at(t, batch, slots, heads, dim, name):
+    """Address and strides of a block's rows; strides of extents with one entry are 0."""
+    a, b, c, d = t.stride()
+    if d != 1 and dim > 1:
         raise ValueError("%s must have unit stride along its last dimension" % name)
-    if 1 in e:
-        a, b, c = a if e[0] > 1 else 0, b if e[1] > 1 else 0, c if e[2] > 1 else 0
-    if not quant:
-        return x.data_ptr(), 0, a, b, c, 0, 0, 0, 0, 0
-    i, j, k = t.scales.stride()
-    return (x.data_ptr(), 0, a, b, c, t.scales.data_ptr(), 0, i if e[0] > 1 else 0, j if e[1] > 1 else 0,
-            k if e[2] > 1 else 0)
+    return t.data_ptr(), a if batch > 1 else 0, b if slots > 1 else 0, c if heads > 1 else 0
 
 
 def _at(t, dtype, shape, dev):
@@ -1072,7 +1070,7 @@ class Context:
         return out
 
     def _pages(self, cache, name, heads, dim, dtype, written=False):
-        """(keys, values, quantised, their rows' numbers) of a layer's pages [pages, page_rows, heads, dim]."""
+        """(keys, values, quantised, addresses and strides) of a layer's pages [pages, page_rows, heads, dim]."""
         if not isinstance(cache, (tuple, list)) or len(cache) != 2:
             raise ValueError("%s must be a pair of keys and values" % name)
         k, v = cache
@@ -1086,16 +1084,25 @@ class Context:
             raise ValueError("%s must be [pages, page_rows, %d, %d], got %s" % (name, heads, dim, list(s)))
         if not quant and (k.dtype is not dtype or v.dtype is not dtype):
             raise TypeError("%s must be %s or QuantRows, got %s and %s" % (name, dtype, k.dtype, v.dtype))
-        if s[0] | s[1] > _INT32_MAX:
-            _fits(max(s[0], s[1]), name)
-        if written:
-            for t in cache:
-                # paged_cache's layout, a place for every number, is seen at a glance
-                x = t.codes if quant else t
-                if x.stride() != (s[1] * heads * dim, dim, s[1] * dim, 1) or (
-                        quant and t.scales.stride() != (s[1] * heads, 1, s[1])):
-                    _apart(t, name)
-        return k, v, quant, _flat_rows(k, name), _flat_rows(v, name)
+        pages, rows = s[0], s[1]
+        if pages | rows > _INT32_MAX:
+            _fits(max(pages, rows), name)
+        at = ()
+        for t in cache:
+            x = t.codes if quant else t
+            st = x.stride()
+            if st[3] != 1 and dim > 1:
+                raise ValueError("%s must have unit stride along its last dimension" % name)
+            # paged_cache's layout, a place for every number, is seen at a glance
+            if written and (st != (rows * heads * dim, dim, rows * dim, 1) or (
+                    quant and t.scales.stride() != (rows * heads, 1, rows))):
+                _apart(t, name)
+            at += (x.data_ptr(), st[0] if pages > 1 else 0, st[1] if rows > 1 else 0, st[2] if heads > 1 else 0)
+            if quant:
+                st = t.scales.stride()
+                at += (t.scales.data_ptr(), st[0] if pages > 1 else 0, st[1] if rows > 1 else 0,
+                       st[2] if heads > 1 else 0)
+        return k, v, quant, at
 
     def _table(self, page_table, batch):
         """Extents of a page table [batch or more, pages of a sequence], for _args."""
@@ -1120,10 +1127,11 @@ class Context:
         slots] or [batch, slots] int32 (None: start + i), axis [rot / 2] int32 the axis of
         each pair (None: the first).  Returns q_out (None without q; allocated as
         zeros when None; q itself rotates in place)."""
-        if not isinstance(k, torch.Tensor) or k.dim() != 4 or min(k.shape) < 1:
+        shape = k.shape if isinstance(k, torch.Tensor) else ()
+        if len(shape) != 4 or min(shape) < 1:
             raise ValueError("k must be [batch, slots, heads, dim]")
-        shape, kind = k.shape, k.dtype
         B, S, H, D = shape
+        kind = k.dtype
         if not isinstance(v, torch.Tensor) or v.shape != shape:
             _need(v, "v", B, S, H, D)
         Hq = 0
@@ -1148,7 +1156,7 @@ class Context:
                 _need(q_out, "q_out", B, S, Hq, D)
             if not q_out.is_contiguous():
                 _apart(q_out, "q_out")
-        ck, cv, quant, rk, rv = self._pages(cache, "cache", H, D, kind, True)
+        ck, cv, quant, pools = self._pages(cache, "cache", H, D, kind, True)
         F, axes = 0, 1
         if freq is not None:
             if not isinstance(freq, torch.Tensor) or freq.dim() != 1:
@@ -1167,13 +1175,15 @@ class Context:
         elif axis is not None:
             raise ValueError("axis needs positions")
         dtype, one, i32, dev = _DTYPES[kind], (B,), torch.int32, self._device
-        others = (k, v, q, q_out, ck.codes if quant else ck, cv.codes if quant else cv)
         table = self._table(page_table, B)
-        at = (_at(page_table, i32, table[4], dev), _at(n_rows, i32, one, dev), _at(start, i32, one, dev),
-              _at(positions, i32, (axes, B, S), dev), _at(axis, i32, (F,), dev),
-              _at(freq, torch.float64, (F,), dev))
-        if min(at) < 0 or not self._all_here(others):
-            at = [p or 0 for p in self._args(
+        p_table, p_n, p_start = _at(page_table, i32, table[4], dev), _at(n_rows, i32, one, dev), _at(start, i32, one, dev)
+        p_pos, p_axis, p_freq = 0, 0, 0
+        if F:
+            p_pos, p_axis = _at(positions, i32, (axes, B, S), dev), _at(axis, i32, (F,), dev)
+            p_freq = _at(freq, torch.float64, (F,), dev)
+        if (p_table < 0 or p_n < 0 or p_start < 0 or p_pos < 0 or p_axis < 0 or p_freq < 0
+                or not self._all_here((k, v, q, q_out, ck, cv))):
+            p_table, p_n, p_start, p_pos, p_axis, p_freq = [p or 0 for p in self._args(
                 (("k", k), ("v", v), ("q", q), ("q_out", q_out), ("cache keys", ck), ("cache values", cv)),
                 table,
                 ("n_rows", n_rows, i32, one, one),
@@ -1181,14 +1191,16 @@ class Context:
                 ("positions", positions, i32, ((1,), B, S), (axes, B, S)),
                 ("axis", axis, i32, (F,), (F,)),
                 ("freq", freq, torch.float64, (F,), (F,)))]
-        if q is not None and q_out is None:
-            q_out = torch.zeros_like(q, memory_format=torch.contiguous_format)
-        n, s = page_table.shape[1], ck.shape
-        desc = _PACK_ROWS.pack(
-            B, S, Hq, H, D, 2 * F, 1 if interleaved else 0, dtype, 3 if quant else dtype,
-            *(_flat_rows(q, "q") if Hq else _NONE), *(_flat_rows(q_out, "q_out") if Hq else _NONE),
-            *_flat_rows(k, "k"), *_flat_rows(v, "v"), *rk, *rv, at[0], n, n, s[0], s[1], at[1], at[2], at[3],
-            axes, at[4], at[5])
+        queries = _NO_ROWS
+        if Hq:
+            if q_out is None:
+                q_out = torch.zeros_like(q, memory_format=torch.contiguous_format)
+            queries = _row_at(q, B, S, Hq, D, "q") + _row_at(q_out, B, S, Hq, D, "q_out")
+        n, pool = page_table.shape[1], ck.shape
+        desc = _PACK_ROWS[quant].pack(
+            B, S, Hq, H, D, 2 * F, 1 if interleaved else 0, dtype, 3 if quant else dtype, *queries,
+            *_row_at(k, B, S, H, D, "k"), *_row_at(v, B, S, H, D, "v"), *pools, p_table, n, n, pool[0], pool[1],
+            p_n, p_start, p_pos, axes, p_axis, p_freq)
         _check(lib().graft_paged_write(self._h, desc, _stream()), "graft_paged_write")
         return q_out
 
@@ -1196,7 +1208,7 @@ class Context:
         """Whether all that are given are on the context's device, and that is the current one."""
         dev = self._device
         for t in tensors:
-            if t is not None and t.get_device() != dev:
+            if t is not None and (t.codes if isinstance(t, QuantRows) else t).get_device() != dev:
                 return False
         return torch.cuda.current_device() == dev
 
@@ -1216,11 +1228,11 @@ class Context:
                                 out, lse)
         L = lib()
         need = C.c_int64()
-        _check(L.graft_paged_attention_workspace(self._h, desc(0, 0), C.byref(need)),
-               "graft_paged_attention_workspace")
+        _check(L.graft_paged_attention_workspace(self._h, desc, C.byref(need)), "graft_paged_attention_workspace")
         workspace = self._workspace(workspace, need.value, q.device)
-        a = desc(0, 0) if workspace is None else desc(workspace.data_ptr(), workspace.numel())
-        _check(L.graft_paged_attention(self._h, a, _stream()), "graft_paged_attention")
+        if workspace is not None:
+            desc = desc[:-16] + struct.pack("qq", workspace.data_ptr(), workspace.numel())
+        _check(L.graft_paged_attention(self._h, desc, _stream()), "graft_paged_attention")
         return out
 
     def paged_attention_workspace(self, q, cache, page_table, cache_len, n_nodes=None, mask=None, scale=None,
@@ -1229,27 +1241,29 @@ class Context:
         desc, _ = self._paged(q, cache, page_table, cache_len, n_nodes, mask, scale, window, sinks, with_root,
                               out, lse)
         need = C.c_int64()
-        _check(lib().graft_paged_attention_workspace(self._h, desc(0, 0), C.byref(need)),
+        _check(lib().graft_paged_attention_workspace(self._h, desc, C.byref(need)),
                "graft_paged_attention_workspace")
         return need.value
 
     def _paged(self, q, cache, page_table, cache_len, n_nodes, mask, scale, window, sinks, with_root, out,
                lse):
-        if not isinstance(q, torch.Tensor) or q.dim() != 4 or min(q.shape) < 1:
+        """(its descriptor without a workspace, out)"""
+        shape = q.shape if isinstance(q, torch.Tensor) else ()
+        if len(shape) != 4 or min(shape) < 1:
             raise ValueError("q must be [batch, slots, heads, dim]")
-        if q.dtype not in (torch.bfloat16, torch.float16):
+        kind = q.dtype
+        if kind is not torch.bfloat16 and kind is not torch.float16:
             raise TypeError("q must be bfloat16 or float16")
         if cache_len is None:
             raise ValueError("cache_len is required")
-        shape = q.shape
         B, S, Hq, D = shape
         if B | S | Hq | D > _INT32_MAX:
             _fits(max(B, S, Hq, D), "q")
         if out is not None:
             if not (isinstance(out, torch.Tensor) and out.shape == shape):
                 _need(out, "out", B, S, Hq, D)
-            if out.dtype is not q.dtype:
-                raise TypeError("out must be %s" % q.dtype)
+            if out.dtype is not kind:
+                raise TypeError("out must be %s" % kind)
             if not out.is_contiguous():
                 _apart(out, "out")
         if window is None:
@@ -1260,15 +1274,17 @@ class Context:
             raise ValueError("sinks must be 0..2^31 - 1")
         first = cache[0] if isinstance(cache, (tuple, list)) and len(cache) == 2 else None
         H = first.shape[2] if isinstance(first, (torch.Tensor, QuantRows)) and len(first.shape) == 4 else 1
-        ck, cv, quant, rk, rv = self._pages(cache, "cache", H, D, q.dtype)
+        ck, cv, quant, pools = self._pages(cache, "cache", H, D, kind)
         N = self.dims.max_nodes
         W = (N + 63) // 64
         one, i32, dev = (B,), torch.int32, self._device
         table = self._table(page_table, B)
-        at = (_at(page_table, i32, table[4], dev), _at(cache_len, i32, one, dev), _at(n_nodes, i32, one, dev),
-              _at(mask, torch.int64, (B, N, W), dev), _at(lse, torch.float32, (B, S, Hq), dev))
-        if min(at) < 0 or not self._all_here((q, out, ck.codes if quant else ck, cv.codes if quant else cv)):
-            at = [p or 0 for p in self._args(
+        p_table, p_len, p_n = (_at(page_table, i32, table[4], dev), _at(cache_len, i32, one, dev),
+                               _at(n_nodes, i32, one, dev))
+        p_mask, p_lse = _at(mask, torch.int64, (B, N, W), dev), _at(lse, torch.float32, (B, S, Hq), dev)
+        if (p_table < 0 or p_len < 0 or p_n < 0 or p_mask < 0 or p_lse < 0
+                or not self._all_here((q, out, ck, cv))):
+            p_table, p_len, p_n, p_mask, p_lse = [p or 0 for p in self._args(
                 (("q", q), ("out", out), ("cache keys", ck), ("cache values", cv)),
                 table,
                 ("cache_len", cache_len, i32, one, one),
@@ -1277,11 +1293,12 @@ class Context:
                 ("lse", lse, torch.float32, (B, S, Hq), (B, S, Hq)))]
         if out is None:
             out = torch.zeros_like(q, memory_format=torch.contiguous_format)
-        dtype, n, s = _DTYPES[q.dtype], page_table.shape[1], ck.shape
-        fields = (B, S, 1 if with_root else 0, Hq, H, D, dtype, 3 if quant else dtype,
-                  float(D ** -0.5 if scale is None else scale), window, sinks, *_flat_rows(q, "q"), at[2], at[3], *rk,
-                  *rv, at[0], n, n, s[0], s[1], at[1], *_flat_rows(out, "out"), at[4])
-        return lambda *workspace: _PACK_ATTENTION.pack(*fields, *workspace), out
+        dtype, n, pool = _DTYPES[kind], page_table.shape[1], ck.shape
+        desc = _PACK_ATTENTION[quant].pack(
+            B, S, 1 if with_root else 0, Hq, H, D, dtype, 3 if quant else dtype,
+            float(D ** -0.5 if scale is None else scale), window, sinks, *_row_at(q, B, S, Hq, D, "q"), p_n, p_mask,
+            *pools, p_table, n, n, pool[0], pool[1], p_len, *_row_at(out, B, S, Hq, D, "out"), p_lse, 0, 0)
+        return desc, out
 
     def paged_commit(self, cache, page_table, start, acc_len, acc_nodes, with_root=False):
         """Moves the accepted path's rows up to the front of the block in the pages
@@ -1296,21 +1313,38 @@ class Context:
         P, pages, rows, H, D = cache.shape
         if P | pages | rows | H | D > _INT32_MAX:
             _fits(max(P, pages, rows, H, D), "cache")
-        _apart(cache, "cache")
-        kind = 3 if isinstance(cache, QuantRows) else _DTYPES.get(cache.dtype, -1)
-        L, one, i32 = self.dims.num_pos, (batch,), torch.int32
+        quant = isinstance(cache, QuantRows)
+        x = cache.codes if quant else cache
+        st = x.stride()
+        if st[4] != 1 and D > 1:
+            raise ValueError("cache must have unit stride along its last dimension")
+        # paged_cache's layout, a place for every number, is seen at a glance
+        if st != (pages * rows * H * D, rows * H * D, D, rows * D, 1) or (
+                quant and cache.scales.stride() != (pages * rows * H, rows * H, 1, rows)):
+            _apart(cache, "cache")
         if acc_nodes is None:
             raise ValueError("acc_nodes is required")
-        p_table, p_start, p_acc, p_nodes = self._args(
-            (("cache", cache),),
-            self._table(page_table, batch),
-            ("start", start, i32, (one,), one),
-            ("acc_len", acc_len, i32, (one,), one),
-            ("acc_nodes", acc_nodes, i32, (one, L), (batch, L)))
+        L, one, i32, dev = self.dims.num_pos, (batch,), torch.int32, self._device
+        table = self._table(page_table, batch)
+        p_table, p_start = _at(page_table, i32, table[4], dev), _at(start, i32, one, dev)
+        p_acc, p_nodes = _at(acc_len, i32, one, dev), _at(acc_nodes, i32, (batch, L), dev)
+        if p_table < 0 or p_start < 0 or p_acc < 0 or p_nodes < 0 or not self._all_here((cache,)):
+            p_table, p_start, p_acc, p_nodes = [p or 0 for p in self._args(
+                (("cache", cache),),
+                table,
+                ("start", start, i32, (one,), one),
+                ("acc_len", acc_len, i32, (one,), one),
+                ("acc_nodes", acc_nodes, i32, (one, L), (batch, L)))]
+        at = (x.data_ptr(), st[1] if pages > 1 else 0, st[2] if rows > 1 else 0, st[3] if H > 1 else 0)
+        if quant:
+            sc = cache.scales.stride()
+            at += (cache.scales.data_ptr(), sc[0] if P > 1 else 0, sc[1] if pages > 1 else 0,
+                   sc[2] if rows > 1 else 0, sc[3] if H > 1 else 0)
         n = page_table.shape[1]
-        a = PagedPath(batch, P, H, D, kind, _rows(cache, 4, "cache"), PageTable(p_table, n, n, pages, rows),
-                      p_start, p_acc, p_nodes, 1 if with_root else 0)
-        _check(lib().graft_paged_commit(self._h, C.byref(a), _stream()), "graft_paged_commit")
+        desc = _PACK_PATH[quant].pack(
+            batch, P, H, D, 3 if quant else _DTYPES.get(cache.dtype, -1), at[0], st[0] if P > 1 else 0, *at[1:],
+            p_table, n, n, pages, rows, p_start, p_acc, p_nodes, 1 if with_root else 0)
+        _check(lib().graft_paged_commit(self._h, desc, _stream()), "graft_paged_commit")
         return cache
 
     def profile_begin(self, max_calls: int):

@@ -52,7 +52,6 @@ struct PagedArgs {
   float *part_o;          // [parts][batch * slots * q_heads][head_dim], unnormalised
   f32x2 *part_ml;         // [parts][batch * slots * q_heads] reference, sum
   uint32_t *error_flag;
-  int64_t rows_all;       // batch * slots * q_heads
   int32_t batch, slots, root, q_heads, kv_heads, group, dim;
   int32_t n_max, words, window, sinks;
   int32_t tile_rows, row_tiles;   // rows of the narrow walk's tile; most row tiles of a sequence and key head
@@ -1151,14 +1150,15 @@ paged_attend_kernel(PagedArgs a) {
 template <typename T, bool WIDE>
 __global__ void __launch_bounds__(kThreads)
 merge_pages_kernel(PagedArgs a) {
+  constexpr int kHeads = kThreads / 32;
   const int lane = lane_id(), l32 = lane & 31;
-  const int64_t r = static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + threadIdx.x / 32;
-  if (r >= a.rows_all) return;
-  const int64_t bs = r / a.q_heads;
-  const int head = static_cast<int>(r - bs * a.q_heads), b = static_cast<int>(bs / a.slots);
-  const int slot = static_cast<int>(bs - static_cast<int64_t>(b) * a.slots);
+  const int head_blocks = (a.q_heads + kHeads - 1) / kHeads, bs = blockIdx.x / head_blocks;
+  const int b = bs / a.slots, slot = bs - b * a.slots;
   const Sizes sz = sizes_of(a, b);
   if (slot >= sz.n) return;
+  const int head = (blockIdx.x - bs * head_blocks) * kHeads + threadIdx.x / 32;
+  if (head >= a.q_heads) return;
+  const int64_t r = static_cast<int64_t>(bs) * a.q_heads + head;
   const int kvh = head / a.group, row = slot * a.group + head - kvh * a.group;
   const int height = WIDE ? height_of(sz.n * a.group) : a.tile_rows, tile_row = row / height, local = row - tile_row * height;
   const int row_tiles = row_tiles_of(sz.n * a.group);
@@ -1179,8 +1179,8 @@ merge_pages_kernel(PagedArgs a) {
     return WIDE ? static_cast<int64_t>(a.share[1 + b] + place_of(g0 + p, tile_row, pieces * a.kv_heads, row_tiles)) * kWideRows + local
                 : static_cast<int64_t>(2 * (g0 + p) + (p == 0 ? 1 : 0)) * a.tile_rows + local;
   };
-  // a piece that cut_at leaves nothing was not written
-  auto some = [&](int p) { return p < pieces && (!WIDE || cut_at(tiles, pieces, p) < cut_at(tiles, pieces, p + 1)); };
+  // a piece that cut_at leaves nothing, there being fewer tiles than pieces, was not written
+  auto some = [&](int p) { return p < pieces && (!WIDE || tiles >= pieces || cut_at(tiles, pieces, p) < cut_at(tiles, pieces, p + 1)); };
   f32x2 ml[4];
   float top = -INFINITY;
 #pragma unroll
@@ -1248,7 +1248,7 @@ PagedPlan paged_plan(const graft_paged_attention_desc &a) {
   const int keys = p.few ? kFewKeys * kWaves : kWideKeys;
   int64_t most = static_cast<int64_t>(a.pages.table_len) * a.pages.page_rows;
   if (a.window > 0) most = std::min<int64_t>(most, static_cast<int64_t>(a.window) + a.sinks + a.slots + 2 * keys);
-  const int64_t rounds = (most + keys - 1) / keys, all = static_cast<int64_t>(a.batch) * a.slots * a.q_heads;
+  const int64_t rounds = (most + keys - 1) / keys;
   p.fits = outer * p.row_tiles * rounds < (int64_t{1} << 31);
   if (p.few) {
     // as many as the registers let run at once
@@ -1262,7 +1262,8 @@ PagedPlan paged_plan(const graft_paged_attention_desc &a) {
     p.blocks = outer * p.row_tiles;
     return p;
   }
-  p.merge_blocks = rounds > 1 ? (all + kThreads / 32 - 1) / (kThreads / 32) : 0;
+  constexpr int kHeads = kThreads / 32;                     // of a workgroup of the merge
+  p.merge_blocks = rounds > 1 ? static_cast<int64_t>(a.batch) * a.slots * ((a.q_heads + int64_t{kHeads} - 1) / kHeads) : 0;
   p.part_rows = p.blocks * (p.few ? 2 * p.tile_rows : kWideRows);
   p.share_at = p.part_rows * (a.head_dim * int64_t{4} + 8);
   p.bytes = p.share_at + (a.batch + int64_t{1}) * 4;
@@ -1289,7 +1290,6 @@ hipError_t launch_paged_attend(graft_ctx *ctx, const graft_paged_attention_desc 
   a.mask = d.mask;
   a.lse = d.lse;
   a.error_flag = ctx->error_flag;
-  a.rows_all = static_cast<int64_t>(d.batch) * d.slots * d.q_heads;
   a.part_o = static_cast<float *>(d.workspace);
   a.part_ml = p.bytes > 0 ? reinterpret_cast<f32x2 *>(a.part_o + p.part_rows * d.head_dim) : nullptr;
   a.share = p.bytes > 0 ? reinterpret_cast<int32_t *>(static_cast<char *>(d.workspace) + p.share_at) : nullptr;

@@ -318,8 +318,8 @@ struct PageMap;
 PageMap page_map(const graft_page_table &t);
 struct PagedPlan {
   int few;            // a sequence's rows fit one tile of 16 (1) or 32 (2): the narrow walk
-  int tile_rows;      // rows of a row tile (wide: 32, 64, 96 or 128)
-  int row_tiles;      // of a sequence and key head
+  int tile_rows;      // most rows of a row tile
+  int row_tiles;      // most of a sequence and key head
   bool fits;          // all rounds are counted in 32 bits
   int64_t part_rows;  // rows of pieces in the workspace
   int64_t share_at;   // how the rounds are shared, in the workspace

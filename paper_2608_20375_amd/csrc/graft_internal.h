@@ -278,7 +278,7 @@ hipError_t launch_commit(graft_ctx *ctx, int batch, const int32_t *acc_len,
                          int64_t db, int64_t dr, hipStream_t stream);
 // The draft block's attention: how a call is cut into workgroups, and its launches.
 struct AttendPlan {
-  int few;            // a sequence's rows fit one tile of 16 (1) or 32 (2): the narrow walk
+  bool few;           // a sequence's rows fit one tile of 16: the narrow walk
   int row_tiles;      // tiles of (slot, head of the group) rows of one sequence: of 128, or 16 few
   int splits;         // parts of a sequence's keys at most
   int min_tiles;      // tiles (narrow: rounds of four tiles) of a part at least
@@ -317,7 +317,7 @@ constexpr uint32_t kErrBlockSizes = 8u, kErrTargetRow = 16u, kErrCacheRow = 32u,
 struct PageMap;
 PageMap page_map(const graft_page_table &t);
 struct PagedPlan {
-  int few;            // a sequence's rows fit one tile of 16 (1) or 32 (2): the narrow walk
+  bool few;           // a sequence's rows fit one tile of 16: the narrow walk
   int tile_rows;      // most rows of a row tile
   int row_tiles;      // most of a sequence and key head
   bool fits;          // all rounds are counted in 32 bits

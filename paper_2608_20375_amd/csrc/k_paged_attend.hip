@@ -14,6 +14,17 @@
 // offset inside a page 32.  Rows past a tile's end are loaded from its last row again, rows of
 // pages that the pool does not have from page 0: both are hidden.
 //
+// Two walks.  Up to 16 rows a key head (single tokens, short chains) keys are read once and a
+// wave's own: narrow_part, bound by memory.  More rows share keys through LDS: wide_part, bound by
+// matrix, vector, LDS and load work that two waves a SIMD do not quite overlap.  Rounds of either are
+// shared over the chip whatever the sequences' lengths, and merge_pages_kernel joins what was cut.
+// Measured (in a graph, 32/8 heads of 128, the join included): 64 tokens over up to 8192 e4m3 rows 125 us
+// for 584 MB (4.7 TB/s), over bf16 rows 194 us for 1158 MB (6.0 TB/s); 32 windows of 4096 over up to
+// 16384 rows 97 us for 504 MB (5.2 TB/s; plain reads of as large pieces reach 5.8, 6.6 non-temporal); 16
+// trees of up to 64 nodes over up to 4096 rows 82 us for 30 GFLOP and 167 MB; 8 pieces of 1024 prompt
+// rows, windows of 2048, 335 us for 257 GFLOP (766 TFLOP/s); one token over 700 rows 13 us, two launches
+// and their dependent loads.
+//
 // Hidden keys.  A tile whose keys all query rows see (most of them) takes no masks.  In the others
 // a score that a row does not see becomes -inf, and infinite and NaN values are stored as 0, since
 // 0 times them is NaN; where there were any, what the rows that see them get is added after.
@@ -30,7 +41,8 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kWideRows = 128, kWideKeys = 64;    // wide_part
-constexpr int kFewRows = 32, kFewKeys = 32;       // narrow_part; keys of one wave's tile
+constexpr int kFewRows = 16, kFewKeys = 32;       // narrow_part; keys of one wave's tile
+constexpr int kWideBlocks = 512;                  // two a CU
 constexpr int kMaxPieces = 128;                   // of a row's keys: four a lane of the merge
 
 struct Pool {                 // keys or values of one layer; bytes
@@ -200,11 +212,14 @@ __device__ __forceinline__ void finish(const PagedArgs &a, int64_t all, float m,
   a.lse[all] = l == 0.0f ? -INFINITY : (m * a.c + (__log2f(l) - at)) * 0.69314718055994531f;
 }
 
-// 16 or 32 rows, all of a sequence's and key head's, over tiles t0 .. t1 - 1: every wave walks 32-key tiles of
+// Up to 16 rows, all of a sequence's and key head's, over tiles t0 .. t1 - 1: every wave walks 32-key tiles of
 // its own, keys from memory straight into fragments, values through a stretch of LDS of the wave's
-// own, no barriers; the waves' sums are joined at the end.
+// own, no barriers; the waves' sums are joined at the end.  A tile is in flight while the one before it is
+// worked on.  The loads alone, with nothing done to what they bring, take 107 of the 125 us of 64
+// tokens over e4m3 rows and 90 of the 97 of the windows; two tiles in flight and 3 or 4 waves a SIMD gained
+// nothing.
 // part: where in the workspace the sums go, or -1: they are all there is.
-template <typename T, bool Q8, bool HOT, int DP, int QT>
+template <typename T, bool Q8, bool HOT, int DP>
 __device__ __forceinline__ void narrow_part(const PagedArgs &a, int b, int kvh, int live, int len, const RowTile &tile, int t0,
                                             int t1, int part, u32x4 *lds) {
   constexpr int C = DP / 8, kSteps = DP / 32, kDTiles = DP / 16;
@@ -228,18 +243,15 @@ __device__ __forceinline__ void narrow_part(const PagedArgs &a, int b, int kvh, 
   // Contracted entries 8 of a step are chunk k_chunk(step) of a row: the 16 codes that one
   // load brings are two steps' 8.
   auto k_chunk = [&](int s) { return Q8 ? 2 * (4 * (s / 2) + quarter) + s % 2 : 4 * s + quarter; };
-  u32x4 rq[QT][kSteps];
+  u32x4 rq[kSteps];
   {
     const PagedArgs &z = late();
+    int slot, head;
+    place(z, col, &slot, &head);
+    const char *qp = z.q + b * z.q_batch + slot * z.q_slot + head * z.q_head;
 #pragma unroll
-    for (int q = 0; q < QT; ++q) {
-      int slot, head;
-      place(z, q * 16 + col, &slot, &head);
-      const char *qp = z.q + b * z.q_batch + slot * z.q_slot + head * z.q_head;
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s)
-        rq[q][s] = HOT || k_chunk(s) * 8 < z.dim ? take16(qp + k_chunk(s) * 16) : u32x4{0, 0, 0, 0};
-    }
+    for (int s = 0; s < kSteps; ++s)
+      rq[s] = HOT || k_chunk(s) * 8 < z.dim ? take16(qp + k_chunk(s) * 16) : u32x4{0, 0, 0, 0};
   }
 
   const int32_t *table = a.pages.table + b * a.pages.table_stride;
@@ -249,10 +261,10 @@ __device__ __forceinline__ void narrow_part(const PagedArgs &a, int b, int kvh, 
 
   // Loads of a tile.  A cache line is 128 bytes, and a load of 16 rows of 64 would bring each line
   // for one half of it, the other coming 16 loads later: so a load takes whole lines of 8 rows, lane
-  // (quarter, col) chunk quarter + 4 (col / 8) of row 8 u + col % 8.  The values go to LDS as they
-  // come; two loads' keys change halves (col's and col + 8's) to be rows col of chunks quarter
-  // and quarter + 4.  Rows of 64 bytes are taken 16 at a time.  Keys are read once: the loads are
-  // non-temporal (random 4 KB pieces are read at 6.6 TB/s so, at 5.8 without).
+  // (quarter, col) chunk quarter + 4 (col / 8) of row 8 u + col % 8 (the windows 103 -> 96 us).  The
+  // values go to LDS as they come; two loads' keys change halves (col's and col + 8's) to be rows col
+  // of chunks quarter and quarter + 4.  Rows of 64 bytes are taken 16 at a time.  Keys are read once:
+  // the loads are non-temporal (random 4 KB pieces are read at 6.6 TB/s so, at 5.8 without).
   constexpr bool kLines = kLoads > 1;
   constexpr int kSets = kLines ? 4 : 2, kEach = kLines ? kLoads / 2 : 1;   // rows of a lane, loads of a row
   const int mine_ch = kLines ? quarter + (col >> 3) * 4 : quarter, mine_row = kLines ? col & 7 : col;
@@ -385,17 +397,14 @@ __device__ __forceinline__ void narrow_part(const PagedArgs &a, int b, int kvh, 
     }
   };
 
-  f32x4 o[QT][kDTiles];
-  float m[QT], l[QT];
-  Ref ref[QT];                  // of m
+  f32x4 o[kDTiles];
+  float m, l;
+  Ref ref;                      // of m
+  m = -INFINITY;
+  l = 0.0f;
+  ref = ref_of<T>(m, a.c);
 #pragma unroll
-  for (int q = 0; q < QT; ++q) {
-    m[q] = -INFINITY;
-    l[q] = 0.0f;
-    ref[q] = ref_of<T>(m[q], a.c);
-#pragma unroll
-    for (int d = 0; d < kDTiles; ++d) o[q][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  }
+  for (int d = 0; d < kDTiles; ++d) o[d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
   auto step = [&](Held &x) {
     const int j = x.j;
@@ -412,9 +421,7 @@ __device__ __forceinline__ void narrow_part(const PagedArgs &a, int b, int kvh, 
       unit_v[0] = sv.x;
       unit_v[1] = sv.y;
     }
-    f32x4 s[QT][2];
-#pragma unroll
-    for (int q = 0; q < QT; ++q) s[q][0] = s[q][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    f32x4 s[2] = {f32x4{0.0f, 0.0f, 0.0f, 0.0f}, f32x4{0.0f, 0.0f, 0.0f, 0.0f}};
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
       const float uk = Q8 ? unit_of(unit_k[kt]) : 0.0f;
@@ -441,8 +448,7 @@ __device__ __forceinline__ void narrow_part(const PagedArgs &a, int b, int kvh, 
         if (!HOT && (4 * i + quarter) * 16 >= kBytes * a.dim) f[0] = f[1] = u32x4{0, 0, 0, 0};
 #pragma unroll
         for (int y = 0; y < (Q8 ? 2 : 1); ++y)
-#pragma unroll
-          for (int q = 0; q < QT; ++q) s[q][kt] = T::mfma(f[y], rq[q][Q8 ? 2 * i + y : i], s[q][kt]);
+          s[kt] = T::mfma(f[y], rq[Q8 ? 2 * i + y : i], s[kt]);
       }
     }
     fetch_keys(x, w);
@@ -474,7 +480,7 @@ __device__ __forceinline__ void narrow_part(const PagedArgs &a, int b, int kvh, 
     }
     // before the next tile's loads take their registers
     bool odd = false;
-    uint32_t seen[QT];
+    uint32_t seen = 0;
     if (__builtin_expect(!clear, 0)) {
       const PagedArgs &z = late();
       if (bad != 0 && lane == 0) atomicOr(z.error_flag, kErrPage);
@@ -486,44 +492,37 @@ __device__ __forceinline__ void narrow_part(const PagedArgs &a, int b, int kvh, 
           odd = true;
         }
       }
+      int slot, head;
+      place(z, col, &slot, &head);
+      seen = static_cast<uint32_t>(seen_bits(z, b, view_of(z, b, slot, len, live), j, len, live)) & ~bad;
+      const uint32_t bits = seen >> (4 * quarter);
 #pragma unroll
-      for (int q = 0; q < QT; ++q) {
-        int slot, head;
-        place(z, q * 16 + col, &slot, &head);
-        seen[q] = static_cast<uint32_t>(seen_bits(z, b, view_of(z, b, slot, len, live), j, len, live)) & ~bad;
-        const uint32_t bits = seen[q] >> (4 * quarter);
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          s[q][i / 4][i % 4] = (bits >> (16 * (i / 4) + i % 4)) & 1u ? s[q][i / 4][i % 4] : -INFINITY;
-      }
+      for (int i = 0; i < 8; ++i)
+        s[i / 4][i % 4] = (bits >> (16 * (i / 4) + i % 4)) & 1u ? s[i / 4][i % 4] : -INFINITY;
       drain();
     }
     fetch_values(x, w);
     // The tile's scores into the running sums, its values being in LDS.  The wave's LDS
     // operations are done in order.
-    u32x4 p[QT];
+    float mx = s[0][0];
 #pragma unroll
-    for (int q = 0; q < QT; ++q) {
-      float mx = s[q][0][0];
+    for (int i = 1; i < 8; ++i) mx = fmaxf(mx, s[i / 4][i % 4]);
+    mx = quarter_max(mx);
+    const bool up = __builtin_fmaf(mx, ref.c, ref.off) > T::kLift + T::kSlack;   // as in softmax_step
+    if (__ballot(up) != 0) {
+      const Ref now = ref_of<T>(up ? mx : m, a.c);
+      const float alpha = up ? factor(m, ref.at, mx, now, a.c) : 1.0f;
+      l *= alpha;
 #pragma unroll
-      for (int i = 1; i < 8; ++i) mx = fmaxf(mx, s[q][i / 4][i % 4]);
-      mx = quarter_max(mx);
-      const bool up = __builtin_fmaf(mx, ref[q].c, ref[q].off) > T::kLift + T::kSlack;   // as in softmax_step
-      if (__ballot(up) != 0) {
-        const Ref now = ref_of<T>(up ? mx : m[q], a.c);
-        const float alpha = up ? factor(m[q], ref[q].at, mx, now, a.c) : 1.0f;
-        l[q] *= alpha;
-#pragma unroll
-        for (int d = 0; d < kDTiles; ++d) o[q][d] *= alpha;
-        m[q] = up ? mx : m[q];
-        ref[q] = now;
-      }
-      float e[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[q][i / 4][i % 4], ref[q].c, ref[q].off));
-      l[q] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-      p[q] = u32x4{T::pack(e[0], e[1]), T::pack(e[2], e[3]), T::pack(e[4], e[5]), T::pack(e[6], e[7])};
+      for (int d = 0; d < kDTiles; ++d) o[d] *= alpha;
+      m = up ? mx : m;
+      ref = now;
     }
+    float e[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 4][i % 4], ref.c, ref.off));
+    l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+    const u32x4 p = u32x4{T::pack(e[0], e[1]), T::pack(e[2], e[3]), T::pack(e[4], e[5]), T::pack(e[6], e[7])};
     __builtin_amdgcn_wave_barrier();
     const int vr = 4 * quarter + (col >> 2);
 #pragma unroll
@@ -532,8 +531,7 @@ __device__ __forceinline__ void narrow_part(const PagedArgs &a, int b, int kvh, 
       const char *vp = reinterpret_cast<const char *>(s_v + v_at<C>(vr, 2 * d + ((col & 3) >> 1))) + (col & 1) * 8;
       const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)(vp)));
       const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)(vp + 16 * C * 16)));
-#pragma unroll
-      for (int q = 0; q < QT; ++q) o[q][d] = T::mfma(u32x4{lo.x, lo.y, hi.x, hi.y}, p[q], o[q][d]);
+      o[d] = T::mfma(u32x4{lo.x, lo.y, hi.x, hi.y}, p, o[d]);
     }
     __builtin_amdgcn_wave_barrier();
     if (__builtin_expect(__ballot(odd) != 0, 0)) {
@@ -544,18 +542,16 @@ __device__ __forceinline__ void narrow_part(const PagedArgs &a, int b, int kvh, 
       for (int y = 0; y < kFewKeys && j + y < tile.end; ++y) {
         const Spot sp = spot_at(z, entry_at(z, z.pages.table + b * z.pages.table_stride, j + y, tile.end), j + y, tile.end);
 #pragma unroll
-        for (int q = 0; q < QT; ++q)
+        for (int d = 0; d < kDTiles; ++d) {
+          const int c0 = d * 16 + 4 * quarter;
+          u32x2 w{0, 0};
+          if (((seen >> y) & 1) && c0 < z.dim) w = four_at<T, Q8>(z, v_at0, vs_at0, sp, c0);
 #pragma unroll
-          for (int d = 0; d < kDTiles; ++d) {
-            const int c0 = d * 16 + 4 * quarter;
-            u32x2 w{0, 0};
-            if (((seen[q] >> y) & 1) && c0 < z.dim) w = four_at<T, Q8>(z, v_at0, vs_at0, sp, c0);
-#pragma unroll
-            for (int h = 0; h < 4; ++h) {
-              const uint16_t n = static_cast<uint16_t>(w[h / 2] >> (16 * (h & 1)));
-              o[q][d][h] += (n & T::kExp) == T::kExp ? T::number(n) : 0.0f;
-            }
+          for (int h = 0; h < 4; ++h) {
+            const uint16_t n = static_cast<uint16_t>(w[h / 2] >> (16 * (h & 1)));
+            o[d][h] += (n & T::kExp) == T::kExp ? T::number(n) : 0.0f;
           }
+        }
       }
     }
   };
@@ -574,46 +570,43 @@ __device__ __forceinline__ void narrow_part(const PagedArgs &a, int b, int kvh, 
   const PagedArgs &z = late();
   float *s_o = reinterpret_cast<float *>(lds);
   float *s_m = s_o + kWaves * 16 * kPad, *s_l = s_m + kWaves * 16;
+  __syncthreads();
+  l = quarter_sum(l);
+  if (quarter == 0) {
+    s_m[wave * 16 + col] = m;
+    s_l[wave * 16 + col] = l;
+  }
 #pragma unroll
-  for (int q = 0; q < QT; ++q) {
-    __syncthreads();
-    l[q] = quarter_sum(l[q]);
-    if (quarter == 0) {
-      s_m[wave * 16 + col] = m[q];
-      s_l[wave * 16 + col] = l[q];
+  for (int d = 0; d < kDTiles; ++d)
+    *reinterpret_cast<f32x4 *>(s_o + (wave * 16 + col) * kPad + d * 16 + 4 * quarter) = o[d];
+  __syncthreads();
+  for (int u = tid; u < 16 * (DP / 4); u += kThreads) {
+    const int r = u / (DP / 4), c0 = (u % (DP / 4)) * 4;
+    int slot, head;
+    if (!place(z, r, &slot, &head) || c0 >= z.dim) continue;
+    float top = s_m[r];
+#pragma unroll
+    for (int i = 1; i < kWaves; ++i) top = fmaxf(top, s_m[i * 16 + r]);
+    const Ref now = ref_of<T>(top, z.c);
+    f32x4 sum{0.0f, 0.0f, 0.0f, 0.0f};
+    float total = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+      const float mi = s_m[i * 16 + r];
+      const float f = mi == top ? 1.0f : factor(mi, ref_of<T>(mi, z.c).at, top, now, z.c);
+      total += s_l[i * 16 + r] * f;
+      sum += *reinterpret_cast<const f32x4 *>(s_o + (i * 16 + r) * kPad + c0) * f;
     }
-#pragma unroll
-    for (int d = 0; d < kDTiles; ++d)
-      *reinterpret_cast<f32x4 *>(s_o + (wave * 16 + col) * kPad + d * 16 + 4 * quarter) = o[q][d];
-    __syncthreads();
-    for (int u = tid; u < 16 * (DP / 4); u += kThreads) {
-      const int r = u / (DP / 4), c0 = (u % (DP / 4)) * 4;
-      int slot, head;
-      if (!place(z, q * 16 + r, &slot, &head) || c0 >= z.dim) continue;
-      float top = s_m[r];
-#pragma unroll
-      for (int i = 1; i < kWaves; ++i) top = fmaxf(top, s_m[i * 16 + r]);
-      const Ref now = ref_of<T>(top, z.c);
-      f32x4 sum{0.0f, 0.0f, 0.0f, 0.0f};
-      float total = 0.0f;
-#pragma unroll
-      for (int i = 0; i < kWaves; ++i) {
-        const float mi = s_m[i * 16 + r];
-        const float f = mi == top ? 1.0f : factor(mi, ref_of<T>(mi, z.c).at, top, now, z.c);
-        total += s_l[i * 16 + r] * f;
-        sum += *reinterpret_cast<const f32x4 *>(s_o + (i * 16 + r) * kPad + c0) * f;
-      }
-      const int64_t all = (static_cast<int64_t>(b) * z.slots + slot) * z.q_heads + head;
-      if (part >= 0) {
-        const int64_t at = part * static_cast<int64_t>(16 * QT) + q * 16 + r;
-        if (c0 == 0) z.part_ml[at] = f32x2{top, total};
-        *reinterpret_cast<f32x4 *>(z.part_o + at * z.dim + c0) = sum;
-      } else {
-        const float inv = total > 0.0f || total != total ? 1.0f / total : 0.0f;
-        *reinterpret_cast<u32x2 *>(z.out + b * z.o_batch + slot * z.o_slot + head * z.o_head + 2 * c0) =
-            u32x2{T::pack(sum.x * inv, sum.y * inv), T::pack(sum.z * inv, sum.w * inv)};
-        if (z.lse && c0 == 0) finish(z, all, top, total, now.at);
-      }
+    const int64_t all = (static_cast<int64_t>(b) * z.slots + slot) * z.q_heads + head;
+    if (part >= 0) {
+      const int64_t at = part * static_cast<int64_t>(kFewRows) + r;
+      if (c0 == 0) z.part_ml[at] = f32x2{top, total};
+      *reinterpret_cast<f32x4 *>(z.part_o + at * z.dim + c0) = sum;
+    } else {
+      const float inv = total > 0.0f || total != total ? 1.0f / total : 0.0f;
+      *reinterpret_cast<u32x2 *>(z.out + b * z.o_batch + slot * z.o_slot + head * z.o_head + 2 * c0) =
+          u32x2{T::pack(sum.x * inv, sum.y * inv), T::pack(sum.z * inv, sum.w * inv)};
+      if (z.lse && c0 == 0) finish(z, all, top, total, now.at);
     }
   }
 }
@@ -858,8 +851,6 @@ __device__ __forceinline__ Wide whole_walk(const PagedArgs &a) {
   return w;
 }
 
-// 128 rows a workgroup, 32 a wave; 64-key tiles in LDS for all four waves, the next tile's loads
-// in flight in registers meanwhile, two LDS buffers, one barrier a tile.
 // N products whose fragments are read kAhead products before they are used.  Left to itself the compiler
 // reads a fragment right in front of its product, and the wave waits for LDS every time (8 pieces of 1024
 // slots 355 us; 370, 348, 343, 344 and 346 with fragments 1, 2, 3, 4 and 6 products ahead).
@@ -878,6 +869,11 @@ __device__ __forceinline__ void pipelined(Read read, Product product) {
   }
 }
 
+// 128 rows a workgroup, 32 a wave; 64-key tiles in LDS for all four waves, the next tile's loads
+// in flight in registers meanwhile, two LDS buffers, one barrier a tile.  A step of two waves a SIMD is 2050
+// cycles of matrix work in 4280 (8 pieces of 1024 slots); 1300 of them go by while a wave issues its eight
+// loads behind the barrier, where all waves issue theirs.  Loads straight to LDS, and the next tile's
+// products beside this tile's exponentials, came to the same time within 1%.
 template <typename T, bool Q8, bool HOT, int DP>
 __device__ __forceinline__ void wide_part(const PagedArgs &a, int b, int kvh, int live, int len, int tile_row, const RowTile &tile,
                                           int t0, int t1, int part, u32x4 *lds) {
@@ -1125,19 +1121,19 @@ __device__ __forceinline__ void wide_part(const PagedArgs &a, int b, int kvh, in
   if (z.lse && h == 0) finish(z, all, st.m, st.l, ref_of<T>(st.m, z.c).at);
 }
 
-// QT = 0: the wide walk; else the narrow one, 16 QT rows.  HOT: heads of DP numbers and
+// HOT: heads of DP numbers and
 // pages of 16 rows or a multiple.  Others' loads past a head's end go to its begin, and every row
 // has an address of its own: more registers and vector work.
-template <typename T, bool Q8, bool HOT, int DP, int QT>
+template <typename T, bool Q8, bool HOT, int DP, bool WIDE>
 __global__ void __launch_bounds__(kThreads, 2)
 paged_attend_kernel(PagedArgs a) {
   constexpr int kNarrow = (kWaves * 16 * (DP + 4) + 2 * kWaves * 16 + 3) / 4;   // joining the waves
   constexpr int kValues = kWaves * kFewKeys * (DP / 8);
-  __shared__ __align__(16) u32x4 lds[QT == 0 ? 4 * kWideKeys * (DP / 8) : (kNarrow > kValues ? kNarrow : kValues)];
+  __shared__ __align__(16) u32x4 lds[WIDE ? 4 * kWideKeys * (DP / 8) : (kNarrow > kValues ? kNarrow : kValues)];
   int *s_sum = reinterpret_cast<int *>(lds);
-  if constexpr (QT > 0) {
+  if constexpr (!WIDE) {
     share_rounds(a, s_sum, [&](int b, int kvh, int n, int len, const RowTile &tile, int t0, int t1, int part) {
-      narrow_part<T, Q8, HOT, DP, QT>(a, b, kvh, n, len, tile, t0, t1, part, lds);
+      narrow_part<T, Q8, HOT, DP>(a, b, kvh, n, len, tile, t0, t1, part, lds);
     });
   } else {
     const Wide w = a.cut ? cut_rounds(a, s_sum) : whole_walk(a);
@@ -1146,7 +1142,9 @@ paged_attend_kernel(PagedArgs a) {
 }
 
 // Joins the pieces of a row: 32 lanes each, four pieces a lane for the statistics, four numbers a lane
-// for the row.
+// for the row.  A workgroup has rows of one slot, so that sizes and shares are scalars (16 trees of up to 64
+// nodes, rows of two or three pieces: 16.3 -> 13.4 us).  The rows' first pieces loaded beside the statistics
+// gained 0.1 us for one token and cost the trees 1.
 template <typename T, bool WIDE>
 __global__ void __launch_bounds__(kThreads)
 merge_pages_kernel(PagedArgs a) {
@@ -1241,9 +1239,12 @@ PagedPlan paged_plan(const graft_paged_attention_desc &a) {
   PagedPlan p{};
   const int group = a.q_heads / a.kv_heads;
   const int64_t rows = static_cast<int64_t>(a.slots) * group, outer = static_cast<int64_t>(a.batch) * a.kv_heads;
-  p.few = rows <= 16 ? 1 : rows <= kFewRows ? 2 : 0;
+  // with 17 to 32 rows the wide walk, although half its waves are idle (8, 16 and 64 trees of up to 7 nodes over
+  // up to 4096 rows: 31.6, 49 and 145 us, and 42.7, 55 and 167 with two tiles of 16 rows a wave in the
+  // narrow one; only 64 chains of 8 over e4m3 rows lose, 102 -> 110)
+  p.few = rows <= kFewRows;
   p.row_tiles = p.few ? 1 : static_cast<int>((rows + kWideRows - 1) / kWideRows);
-  p.tile_rows = p.few ? 16 * p.few : kWideRows;
+  p.tile_rows = p.few ? kFewRows : kWideRows;
   // keys of a round: of the narrow walk's four waves, or a tile of the wide one
   const int keys = p.few ? kFewKeys * kWaves : kWideKeys;
   int64_t most = static_cast<int64_t>(a.pages.table_len) * a.pages.page_rows;
@@ -1251,12 +1252,16 @@ PagedPlan paged_plan(const graft_paged_attention_desc &a) {
   const int64_t rounds = (most + keys - 1) / keys;
   p.fits = outer * p.row_tiles * rounds < (int64_t{1} << 31);
   if (p.few) {
-    // as many as the registers let run at once
+    // as many as the registers let run at once (the windows: 95, 94 and 97 us with 256, 512 and 1024
+    // workgroups; e4m3 rows take fewer registers, and 512 and 768 come out alike)
     p.blocks = std::min<int64_t>(outer * rounds, a.cache_dtype == GRAFT_E4M3 ? 768 : 512);
-  } else if (outer * p.row_tiles < 1024 && rounds > 1) {
-    // two a CU, which is what registers and LDS let run at once, but one for every row tile at least (16
-    // trees of up to 64 nodes: 91, 106, 112 and 111 us with 512, 640, 768 and 1024)
-    p.blocks = std::min<int64_t>(outer * p.row_tiles * rounds, std::max<int64_t>(512, outer * p.row_tiles));
+  } else if (outer * p.row_tiles < kWideBlocks && rounds > 1) {
+    // what registers and LDS let run at once (16 trees of up to 64 nodes: 91, 106, 112 and 111 us with 512, 640,
+    // 768 and 1024); row tiles that are that many walk on their own (pieces of 1024 slots over up to 4096
+    // rows: one, 256 row tiles, 123 us cut and 130 whole; two, three and four 175, 240 and 302 cut, 163, 219
+    // and 274 whole; 64 trees of up to 7 nodes 145 and 139; but 32 of up to 32, with half of the row tiles
+    // empty, 97 and 121)
+    p.blocks = std::min<int64_t>(outer * p.row_tiles * rounds, kWideBlocks);
   } else {
     p.fits = true;
     p.blocks = outer * p.row_tiles;
@@ -1310,28 +1315,27 @@ hipError_t launch_paged_attend(graft_ctx *ctx, const graft_paged_attention_desc 
   a.c = d.scale * 1.4426950408889634f;
   const dim3 grid(static_cast<unsigned>(p.blocks)), block(kThreads);
   auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };
-  auto pick = [&](auto few, auto dp, auto full) {
-    constexpr int F = decltype(few)::value;
+  auto pick = [&](auto wide, auto dp, auto full) {
+    constexpr bool W = decltype(wide)::value;
     constexpr int D = decltype(dp)::value;
     constexpr bool A = decltype(full)::value;
-    if (d.dtype == GRAFT_F16) run(paged_attend_kernel<F16, false, A, D, F>);
-    else if (q8) run(paged_attend_kernel<Bf16, true, A, D, F>);
-    else run(paged_attend_kernel<Bf16, false, A, D, F>);
+    if (d.dtype == GRAFT_F16) run(paged_attend_kernel<F16, false, A, D, W>);
+    else if (q8) run(paged_attend_kernel<Bf16, true, A, D, W>);
+    else run(paged_attend_kernel<Bf16, false, A, D, W>);
   };
   // heads of other sizes run as 64 or 128 columns
-  auto width = [&](auto few) {
+  auto width = [&](auto wide) {
     constexpr std::integral_constant<int, 64> k64{};
     constexpr std::integral_constant<int, 128> k128{};
     const bool even = d.pages.page_rows % 16 == 0 && a.k.page == a.v.page && a.k.row == a.v.row && a.k.head == a.v.head &&
                       (!q8 || (a.k.s_page == a.v.s_page && a.k.s_row == a.v.s_row && a.k.s_head == a.v.s_head));
-    if (d.head_dim == 128 && even) pick(few, k128, std::true_type{});
-    else if (d.head_dim > 64) pick(few, k128, std::false_type{});
-    else if (d.head_dim == 64 && even) pick(few, k64, std::true_type{});
-    else pick(few, k64, std::false_type{});
+    if (d.head_dim == 128 && even) pick(wide, k128, std::true_type{});
+    else if (d.head_dim > 64) pick(wide, k128, std::false_type{});
+    else if (d.head_dim == 64 && even) pick(wide, k64, std::true_type{});
+    else pick(wide, k64, std::false_type{});
   };
-  if (p.few == 1) width(std::integral_constant<int, 1>{});
-  else if (p.few == 2) width(std::integral_constant<int, 2>{});
-  else width(std::integral_constant<int, 0>{});
+  if (p.few) width(std::false_type{});
+  else width(std::true_type{});
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.merge_blocks == 0) return e;
   const dim3 mgrid(static_cast<unsigned>(p.merge_blocks));

@@ -40,7 +40,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
-constexpr int kWideRows = 128, kWideKeys = 64;    // wide_part
+constexpr int kWideKeys = 64;                     // wide_part
 constexpr int kFewRows = 16, kFewKeys = 32;       // narrow_part; keys of one wave's tile
 constexpr int kWideBlocks = 512;                  // two a CU
 constexpr int kMaxPieces = 128;                   // of a row's keys: four a lane of the merge
@@ -611,14 +611,7 @@ __device__ __forceinline__ void narrow_part(const PagedArgs &a, int b, int kvh, 
   }
 }
 
-// The row tiles of a sequence's query rows of a key head: the narrow walk's one; of the wide one's as few
-// as 128 rows each allow, all of one size in whole waves (260 rows are three tiles of three waves, not two
-// of four and a rest).
-__device__ __forceinline__ int row_tiles_of(int rows) { return (rows + kWideRows - 1) / kWideRows; }
-__device__ __forceinline__ int height_of(int rows) {
-  const int waves = 32 * row_tiles_of(rows);
-  return (rows + waves - 1) / waves * 32;
-}
+// A sequence's row tile.
 template <bool WIDE>
 __device__ __forceinline__ RowTile tile_of(const PagedArgs &a, int n, int len, int tile_row) {
   const int rows = n * a.group, height = WIDE ? height_of(rows) : 0, first = tile_row * height;
@@ -633,22 +626,6 @@ __device__ __forceinline__ int rounds_of(const PagedArgs &a, int n, int len) {
   const int tiles = tile_of<WIDE>(a, n, len, WIDE ? row_tiles_of(n * a.group) - 1 : 0).span.all();
   return WIDE ? tiles : (tiles + kWaves - 1) / kWaves;
 }
-// A sequence's workgroups in the wide walk, units (pieces of key heads) x row tiles: a unit's row tiles
-// follow each other on one XCD (workgroups go round all 8), whose L2 then holds the keys that they share.
-// Eights of units, and what is left in the same way.
-struct Item {
-  int unit, tile_row;
-};
-__device__ __forceinline__ Item item_at(int at, int units, int row_tiles) {
-  const int eight = at / (8 * row_tiles), base = 8 * eight, wide = std::min(8, units - base), x = at - base * row_tiles;
-  const int r = x / wide;
-  return Item{base + x - r * wide, r};
-}
-__device__ __forceinline__ int place_of(int unit, int tile_row, int units, int row_tiles) {
-  const int base = unit & ~7, wide = std::min(8, units - base);
-  return base * row_tiles + tile_row * wide + unit - base;
-}
-
 // How all rounds are shared.  A thread's sequences are c of them from tid * c on; sums over the workgroup.
 template <int N>
 struct Sum {

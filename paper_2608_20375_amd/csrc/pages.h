@@ -69,6 +69,31 @@ __host__ __device__ __forceinline__ RowTile row_tile(int base, int n, int s0, in
   return t;
 }
 
+constexpr int kWideRows = 128;      // most rows of a row tile of the wide walk
+// The row tiles of a sequence's query rows of a key head: the narrow walk's one; of the wide one's as few
+// as 128 rows each allow, all of one size in whole waves (260 rows are three tiles of three waves, not two
+// of four and a rest).
+__host__ __device__ __forceinline__ int row_tiles_of(int rows) { return (rows + kWideRows - 1) / kWideRows; }
+__host__ __device__ __forceinline__ int height_of(int rows) {
+  const int waves = 32 * row_tiles_of(rows);
+  return (rows + waves - 1) / waves * 32;
+}
+// A sequence's workgroups in the wide walk, units (pieces of key heads) x row tiles: a unit's row tiles
+// follow each other on one XCD (workgroups go round all 8), whose L2 then holds the keys that they share.
+// Eights of units, and what is left in the same way.
+struct Item {
+  int unit, tile_row;
+};
+__host__ __device__ __forceinline__ Item item_at(int at, int units, int row_tiles) {
+  const int eight = at / (8 * row_tiles), base = 8 * eight, wide = (units - base < 8 ? units - base : 8), x = at - base * row_tiles;
+  const int r = x / wide;
+  return Item{base + x - r * wide, r};
+}
+__host__ __device__ __forceinline__ int place_of(int unit, int tile_row, int units, int row_tiles) {
+  const int base = unit & ~7, wide = (units - base < 8 ? units - base : 8);
+  return base * row_tiles + tile_row * wide + unit - base;
+}
+
 // Where piece p of `pieces` begins among a row tile's n tiles.
 __host__ __device__ __forceinline__ int cut_at(int n, int pieces, int p) {
   return static_cast<int>(static_cast<int64_t>(n) * p / pieces);

@@ -278,8 +278,8 @@ hipError_t launch_commit(graft_ctx *ctx, int batch, const int32_t *acc_len,
                          int64_t db, int64_t dr, hipStream_t stream);
 // The draft block's attention: how a call is cut into workgroups, and its launches.
 struct AttendPlan {
-  bool few;           // a sequence's rows fit one tile of 16: the narrow walk
-  int row_tiles;      // tiles of (slot, head of the group) rows of one sequence: of 128, or 16 few
+  int column_tiles;   // narrow walk: a sequence's rows in tiles of 16, 1 or 2 of them; 0: the wide walk
+  int row_tiles;      // tiles of (slot, head of the group) rows of one sequence: of 128, or 16 column_tiles
   int splits;         // parts of a sequence's keys at most
   int min_tiles;      // tiles (narrow: rounds of four tiles) of a part at least
   int shared_tiles;   // row tiles over the whole batch for the shared prefix, 0: no own pass

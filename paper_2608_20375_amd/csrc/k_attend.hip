@@ -858,26 +858,31 @@ Side side(const graft_rows &r, int bytes, int dim, int rows) {
 
 }  // namespace
 
-// The narrow walk up to 32 rows of a sequence and key head.  us narrow and wide, in a graph,
-// 8 key heads of 128 over up to 4096 rows:
+// The narrow walk up to 32 rows of a sequence and key head.  us narrow and wide, in a graph, three
+// input sets in turn, 8 key heads of 128 over up to 4096 rows:
 //   rows                    8          16          24          32
-//   1 sequence, bf16     21.5 20.6   22.5 19.9   25.3 20.0   26.8 19.9
-//   32 sequences, bf16   66.6 67.0   73.0 67.7   97.8 69.4  103.4 70.4
-//   32 sequences, e4m3   50.9 73.6   57.4 74.6   83.4 75.6   88.6 76.5
-// One token of 20 and 32 heads a key head over 16384 and 700 rows 28.6 29.5 and 16.3 15.9, e4m3 26.9
-// 30.7 and 15.4 16.9; 64 tokens of 8 over up to 2048 e4m3 rows 49.5 73.8.  So up to 16 rows the
-// narrow walk wins or is near; from 17 to 32 it wins for single tokens of few key heads over
-// codes, and trees there would be faster in the wide one.
+//   1 sequence, bf16     25.4 21.3   26.8 21.4   28.6 21.4   30.1 21.5
+//   32 sequences, bf16   79.2 79.1   84.0 80.3  102.8 82.6  108.4 83.1
+//   32 sequences, e4m3   57.6 83.3   63.4 84.4   88.1 85.0   93.3 86.1
+// One token of 20 and 32 heads a key head over 16384 rows 27.2 28.8 and 30.2 32.1, e4m3 26.2 30.4 and
+// 29.6 32.7; over 700 rows 15.2 15.8 and 16.6 16.1, e4m3 14.9 16.8 and 15.8 17.2; 64 trees of 7 nodes
+// over up to 4096 e4m3 rows 119 148.  So up to 16 rows the narrow walk wins or is near; from 17 to
+// 32 it wins over codes and for single tokens, and trees over bf16 rows would be faster in the wide one.
+// 17 to 32 rows are one row tile, in two tiles of columns that share every row read.  Two row tiles of 16
+// would read a cache twice: 24 and 32 rows 26.7 and 27.0, 97.5 and 96.5, 72.3 and 72.9 us in the lines
+// above, where there are few workgroups or the second read comes from a cache, but 64 trees of 7 nodes of 4
+// key heads over up to 16384 bf16 rows 294 instead of 268, and beside 4096 shared rows 205 instead of 153.
 AttendPlan attend_plan(const graft_attention &a) {
   AttendPlan p{};
   const int group = a.q_heads / a.kv_heads;
   const int64_t rows = static_cast<int64_t>(a.slots) * group;
-  p.few = rows <= 16 ? 1 : rows <= kFewRows ? 2 : 0;
-  const int tile = p.few ? 16 * p.few : kRowTile;
+  p.column_tiles = rows <= 16 ? 1 : rows <= kFewRows ? 2 : 0;
+  const bool few = p.column_tiles > 0;
+  const int tile = few ? 16 * p.column_tiles : kRowTile;
   p.row_tiles = static_cast<int>((rows + tile - 1) / tile);
   const int64_t units = static_cast<int64_t>(a.batch) * a.kv_heads * p.row_tiles;
   // keys of a tile of the wide walk, or of a round of the narrow one's four waves
-  const int keys = p.few ? kFewKeys * kAttWaves : kKeyTile;
+  const int keys = few ? kFewKeys * kAttWaves : kKeyTile;
   auto tiles = [](int64_t n, int k) { return (n + k - 1) / k; };
   // a pass of its own where sequences share a row tile
   const bool own_pass = a.shared_len > 0 && a.batch > 1 && rows * 2 <= kRowTile;
@@ -885,7 +890,7 @@ AttendPlan attend_plan(const graft_attention &a) {
   // the shortest part: below it a part costs more than it shares (one token over 700 keys
   // 11.4 us, in parts of 4 rounds 12.7; 5 trees of 70 nodes over 1664 keys 24.2 us, in parts of
   // 2 tiles 29.2, of 8 26.8)
-  p.min_tiles = p.few ? 1 : 4;
+  p.min_tiles = few ? 1 : 4;
   auto cut = [&](int64_t n_units, int64_t n_tiles, int64_t want, int64_t cap) {
     int64_t s = (want + n_units - 1) / n_units;
     s = std::min(s, (n_tiles + p.min_tiles - 1) / p.min_tiles);
@@ -897,11 +902,11 @@ AttendPlan attend_plan(const graft_attention &a) {
   }
   // a wide part leaves 512 bytes for each of its rows, which the merge reads: splitting pays
   // only where the chip is not filled (16 trees of up to 256 nodes: 200 us whole, 240 in 4 parts)
-  p.splits = cut(units, most, p.few ? 4096 : 1024, own_pass ? 32 : kMaxParts);
+  p.splits = cut(units, most, few ? 4096 : 1024, own_pass ? 32 : kMaxParts);
   p.parts = p.splits + p.shared_splits;
   const int64_t all = static_cast<int64_t>(a.batch) * a.slots * a.q_heads;
-  const int64_t outer = p.few ? a.batch : static_cast<int64_t>(a.batch) * a.kv_heads;
-  const int64_t groups = ((outer | 1) * p.splits + 7) / 8 * 8 * (p.few ? a.kv_heads : 1);
+  const int64_t outer = few ? a.batch : static_cast<int64_t>(a.batch) * a.kv_heads;
+  const int64_t groups = ((outer | 1) * p.splits + 7) / 8 * 8 * (few ? a.kv_heads : 1);
   p.blocks = static_cast<int64_t>(a.kv_heads) * p.shared_tiles * p.shared_splits + groups * p.row_tiles;
   p.merge_blocks = p.parts > 1 ? (all + kAttWaves - 1) / kAttWaves : 0;
   p.bytes = p.parts > 1 ? p.parts * all * (a.head_dim * int64_t{4} + 8) : 0;
@@ -943,8 +948,8 @@ hipError_t launch_attend(graft_ctx *ctx, const graft_attention &d, const AttendP
   a.words = (ctx->dims.max_nodes + 63) / 64;
   a.cache_rows = d.cache_rows;
   a.shared_len = d.shared_len;
-  a.tile_keys = p.few ? kFewKeys : kKeyTile;
-  a.turns = p.few ? kAttWaves : 1;
+  a.tile_keys = p.column_tiles > 0 ? kFewKeys : kKeyTile;
+  a.turns = p.column_tiles > 0 ? kAttWaves : 1;
   a.row_tiles = p.row_tiles;
   a.splits = p.splits;
   a.min_tiles = p.min_tiles;
@@ -955,8 +960,8 @@ hipError_t launch_attend(graft_ctx *ctx, const graft_attention &d, const AttendP
   a.c = d.scale * 1.4426950408889634f;
   const dim3 grid(static_cast<unsigned>(p.blocks)), block(kAttThreads);
   auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };
-  auto pick = [&](auto few, auto dp) {
-    constexpr int F = decltype(few)::value;
+  auto pick = [&](auto tiles, auto dp) {
+    constexpr int F = decltype(tiles)::value;
     constexpr int D = decltype(dp)::value;
     if (d.dtype == GRAFT_F16) run(attend_kernel<F16, false, D, F>);
     else if (q8) run(attend_kernel<Bf16, true, D, F>);
@@ -964,12 +969,12 @@ hipError_t launch_attend(graft_ctx *ctx, const graft_attention &d, const AttendP
   };
   // heads of other sizes run as 64 or 128 columns: 16 trees of up to 256 nodes 109 and 112 us at 32
   // and 64 numbers, 170, 171, 173 and 176 at 80, 96, 112 and 128
-  auto width = [&](auto few) {
-    if (d.head_dim > 64) pick(few, std::integral_constant<int, 128>{});
-    else pick(few, std::integral_constant<int, 64>{});
+  auto width = [&](auto tiles) {
+    if (d.head_dim > 64) pick(tiles, std::integral_constant<int, 128>{});
+    else pick(tiles, std::integral_constant<int, 64>{});
   };
-  if (p.few == 1) width(std::integral_constant<int, 1>{});
-  else if (p.few == 2) width(std::integral_constant<int, 2>{});
+  if (p.column_tiles == 1) width(std::integral_constant<int, 1>{});
+  else if (p.column_tiles == 2) width(std::integral_constant<int, 2>{});
   else width(std::integral_constant<int, 0>{});
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.parts <= 1) return e;

@@ -496,7 +496,7 @@ GRAFT_API int graft_cache_read(graft_ctx *ctx, const graft_cache_move *m /* host
  * page_rows of page table[b * table_stride + r / page_rows].  Pages are the entries of
  * the pool's graft_rows along batch_stride, so keys and values of any layout fit; a
  * head's rows side by side in a page (row_stride = head_dim) read fastest.  Entries of
- * pages that a call does not need are not looked at. */
+ * pages that a call does not need may hold anything. */
 typedef struct {
     const int32_t *table;        /* [batch, table_len] page numbers in 0..pages - 1 */
     int64_t table_stride;        /* >= 0, elements */
@@ -592,8 +592,9 @@ GRAFT_API int graft_paged_attention_workspace(graft_ctx *ctx, const graft_paged_
 
 /* The attention above on `stream`.  The workspace belongs to the call until its work is done
  * and needs no clearing.  n_nodes[b] outside 0 .. slots - with_root and a block that ends
- * outside the table are clamped and reported by graft_get_device_status; so are pages
- * outside 0 .. pages - 1, whose rows are seen by nobody. */
+ * outside the table are clamped and reported by graft_get_device_status.  Rows of pages outside
+ * 0 .. pages - 1 are seen by nobody, and reported where a slot would see them; pages that a window
+ * has moved past may be gone. */
 GRAFT_API int graft_paged_attention(graft_ctx *ctx, const graft_paged_attention_desc *a /* host */,
                                     graft_stream_t stream);
 

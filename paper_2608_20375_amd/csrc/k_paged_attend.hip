@@ -12,7 +12,9 @@
 // Pages.  A lane looks up the page of a key of its own, a tile ahead, and the others' come by lane
 // exchanges, so pages of any length work and may end inside a tile.  Addresses are 64 bits, an
 // offset inside a page 32.  Rows past a tile's end are loaded from its last row again, rows of
-// pages that the pool does not have from page 0: both are hidden.
+// pages that the pool does not have from page 0: both are hidden.  Tiles also hold rows that no
+// query sees (next to a window, behind the first rows), whose pages may be gone: a page is reported
+// where a query sees a row of it.
 //
 // Two walks.  Up to 16 rows a key head (single tokens, short chains) keys are read once and a
 // wave's own: narrow_part, bound by memory.  More rows share keys through LDS: wide_part, bound by
@@ -483,7 +485,6 @@ __device__ __forceinline__ void narrow_part(const PagedArgs &a, int b, int kvh, 
     uint32_t seen = 0;
     if (__builtin_expect(!clear, 0)) {
       const PagedArgs &z = late();
-      if (bad != 0 && lane == 0) atomicOr(z.error_flag, kErrPage);
 #pragma unroll 1
       for (int i = lane; i < kFewKeys * C; i += kWave) {
         u32x4 w = s_v[i];
@@ -494,7 +495,9 @@ __device__ __forceinline__ void narrow_part(const PagedArgs &a, int b, int kvh, 
       }
       int slot, head;
       place(z, col, &slot, &head);
-      seen = static_cast<uint32_t>(seen_bits(z, b, view_of(z, b, slot, len, live), j, len, live)) & ~bad;
+      seen = static_cast<uint32_t>(seen_bits(z, b, view_of(z, b, slot, len, live), j, len, live));
+      if ((seen & bad) != 0) atomicOr(z.error_flag, kErrPage);
+      seen &= ~bad;
       const uint32_t bits = seen >> (4 * quarter);
 #pragma unroll
       for (int i = 0; i < 8; ++i)
@@ -1000,7 +1003,6 @@ __device__ __forceinline__ void wide_part(const PagedArgs &a, int b, int kvh, in
     const int buf = (t - t0) & 1, j = held_j;
     const uint64_t bad = held_bad;
     const bool clear = bad == 0 && is_clear(tile, j, kWideKeys, a.sinks);
-    if (__builtin_expect(bad != 0, 0) && tid == 0) atomicOr(late().error_flag, kErrPage);
     const bool odd = store(buf, clear);
     if (t + 1 < t1) load(t + 1);
     bool any_odd = false;
@@ -1022,7 +1024,9 @@ __device__ __forceinline__ void wide_part(const PagedArgs &a, int b, int kvh, in
     uint64_t seen = ~0ull;
     if (__builtin_expect(!clear, 0)) {
       const PagedArgs &z = late();
-      seen = seen_bits(z, b, view_of(z, b, slot, len, live), j, len, live) & ~bad;
+      seen = seen_bits(z, b, view_of(z, b, slot, len, live), j, len, live);
+      if ((seen & bad) != 0) atomicOr(z.error_flag, kErrPage);
+      seen &= ~bad;
       const uint64_t bits = seen >> (4 * h);
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt) {

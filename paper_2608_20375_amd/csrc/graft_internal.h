@@ -321,6 +321,8 @@ struct PagedPlan {
   int tile_rows;      // most rows of a row tile
   int row_tiles;      // most of a sequence and key head
   bool fits;          // all rounds are counted in 32 bits
+  bool many;          // the second launch's workgroups go over the rows in turns
+  int64_t joins;      // all rows, in its workgroups
   int64_t part_rows;  // rows of pieces in the workspace
   int64_t share_at;   // how the rounds are shared, in the workspace
   int64_t bytes;                  // workspace

@@ -18,8 +18,9 @@
 //
 // Two walks.  Up to 16 rows a key head (single tokens, short chains) keys are read once and a
 // wave's own: narrow_part, bound by memory.  More rows share keys through LDS: wide_part, bound by
-// matrix, vector, LDS and load work that two waves a SIMD do not quite overlap.  Rounds of either are
-// shared over the chip whatever the sequences' lengths, and merge_pages_kernel joins what was cut.
+// matrix, vector, LDS and load work that two waves a SIMD do not quite overlap.  Rounds of the narrow
+// walk are shared evenly over the chip, of the wide one the longest walks are cut, as the lengths on
+// the device say, and merge_pages_kernel joins what was cut.
 // Measured (in a graph, 32/8 heads of 128, the join included): 64 tokens over up to 8192 e4m3 rows 125 us
 // for 584 MB (4.7 TB/s), over bf16 rows 194 us for 1158 MB (6.0 TB/s); 32 windows of 4096 over up to
 // 16384 rows 97 us for 504 MB (5.2 TB/s; plain reads of as large pieces reach 5.8, 6.6 non-temporal); 16
@@ -45,7 +46,8 @@ constexpr int kWaves = kThreads / kWave;
 constexpr int kWideKeys = 64;                     // wide_part
 constexpr int kFewRows = 16, kFewKeys = 32;       // narrow_part; keys of one wave's tile
 constexpr int kWideBlocks = 512;                  // two a CU
-constexpr int kMaxPieces = 128;                   // of a row's keys: four a lane of the merge
+constexpr int kLongRounds = 64;                   // the fewest that many row tiles' walks are cut for
+constexpr int kMergeBlocks = 4096;                // of a merge that mostly finds nothing to do
 
 struct Pool {                 // keys or values of one layer; bytes
   const char *p;
@@ -68,9 +70,11 @@ struct PagedArgs {
   uint32_t *error_flag;
   int32_t batch, slots, root, q_heads, kv_heads, group, dim;
   int32_t n_max, words, window, sinks;
+  int32_t joins;          // rows of cut walks and others, in the merge's workgroups
   int32_t tile_rows, row_tiles;   // rows of the narrow walk's tile; most row tiles of a sequence and key head
-  int32_t cut;            // wide: rounds are shared; 0: a workgroup for each row tile's whole walk
-  int32_t *share;         // rounds of a workgroup, then [batch] each sequence's first round or workgroup
+  int32_t cut;            // wide: walks may be cut; 0: a workgroup for each row tile's whole walk
+  int32_t *share;         // rounds of a workgroup (0: nothing is to be joined), then [batch] each sequence's first
+                          // round or workgroup
   float c;
 };
 
@@ -634,14 +638,24 @@ template <int N>
 struct Sum {
   int before[N], all[N], most;      // in front of the thread's, all, and the largest of `most`
 };
+// each_wave: all waves have all sequences, and none waits for another.
 template <int N>
-__device__ __forceinline__ Sum<N> sum_over(const int (&mine)[N], int most, int *s_sum) {
+__device__ __forceinline__ Sum<N> sum_over(const int (&mine)[N], int most, int *s_sum, bool each_wave = false) {
   const int wave = threadIdx.x / kWave;
   Sum<N> s;
 #pragma unroll
   for (int i = 0; i < N; ++i) s.before[i] = wave_incl_scan(mine[i]);
 #pragma unroll
   for (int k = 1; k < kWave; k <<= 1) most = std::max(most, static_cast<int>(xor_lane(static_cast<uint32_t>(most), k)));
+  if (each_wave) {
+    s.most = __builtin_amdgcn_readfirstlane(most);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      s.all[i] = static_cast<int>(__builtin_amdgcn_readlane(static_cast<uint32_t>(s.before[i]), kWave - 1));
+      s.before[i] -= mine[i];
+    }
+    return s;
+  }
   __syncthreads();
   if (lane_id() == kWave - 1) {
 #pragma unroll
@@ -742,18 +756,20 @@ __device__ __forceinline__ void share_rounds(const PagedArgs &a, int *s_sum, Pie
 
 // In the wide walk a (sequence, key head) of r rounds is cut into ceil(r / per) even pieces, each a unit
 // with a workgroup for every row tile; a row tile's own tiles are cut in that proportion.  A lone piece
-// goes to the outputs.  per is the least of four for which there are workgroups for all, from the rounds
-// of a workgroup if nothing were rounded up to what does when everything is.  (Shared as in the narrow
-// walk, two pieces a workgroup begin and end there, and a begin costs three latencies.)
-__device__ __forceinline__ int pieces_of(int rounds, int per) { return (rounds + per - 1) / per; }
+// goes to the outputs, the others' sums to the workspace, one place behind the other.  cut_of has what per is.
+// Where not all workgroups run at once those of what is cut come first: they are the longest (64 trees of
+// up to 64 nodes, the last of them over 65,536 rows and the others over 500: 188 us, 240 in order; but three
+// pieces of 400 prompt rows, which all run at once, 102 in order and 113).  (Shared as in the narrow walk, two
+// pieces a workgroup begin and end there, and a begin costs three latencies.)
 struct Wide {             // what a workgroup of the wide walk does, if t0 < t1
   int b, kvh, n, len, tile_row, t0, t1, part;
   RowTile tile;
 };
 __device__ __forceinline__ Wide cut_rounds(const PagedArgs &a, int *s_sum) {
-  constexpr int kTries = 4;
-  const int tid = threadIdx.x, me = blockIdx.x, groups = gridDim.x;
-  const int c = (a.batch + kThreads - 1) / kThreads, b0 = tid * c, b1 = std::min(b0 + c, a.batch);
+  const int tid = threadIdx.x, me = blockIdx.x, groups = std::min<int>(gridDim.x, kWideBlocks);
+  const bool each_wave = a.batch <= kWave;
+  const int c = (a.batch + kThreads - 1) / kThreads, b0 = each_wave ? std::min(lane_id(), a.batch) : tid * c,
+            b1 = std::min(b0 + c, a.batch);
   const Share mine = b0 < b1 ? share_of<true>(a, b0) : Share{0, 0, 0, 0};
   int work[2] = {0, 0}, most = 0;
   each_share<true>(a, b0, b1, mine, [&](int, const Share &s) {
@@ -761,46 +777,50 @@ __device__ __forceinline__ Wide cut_rounds(const PagedArgs &a, int *s_sum) {
     work[1] += s.walks;
     most = std::max(most, s.rounds);
   });
-  const Sum<2> sum = sum_over(work, most, s_sum);
-  const int spare = std::max(groups - sum.all[1], 1);
-  const int lo = std::max(std::max((sum.all[0] + groups - 1) / groups, (sum.most + kMaxPieces - 1) / kMaxPieces), 1);
-  const int hi = std::max(std::min((sum.all[0] + spare - 1) / spare, sum.most), lo);
-  int tried[kTries] = {};
+  const Sum<2> sum = sum_over(work, most, s_sum, each_wave);
+  const Cut cut = cut_of(sum.all[0], sum.all[1], sum.most, groups);
+  int tried[kCutTries] = {};
   each_share<true>(a, b0, b1, mine, [&](int, const Share &s) {
 #pragma unroll
-    for (int k = 0; k < kTries; ++k) tried[k] += pieces_of(s.rounds, lo + (hi - lo) * k / (kTries - 1)) * s.walks;
+    for (int k = 0; k < kCutTries; ++k) tried[k] += pieces_of(s.rounds, cut.at(k)) * s.walks;
   });
-  const Sum<kTries> counts = sum_over(tried, 0, s_sum);
-  int per = hi, count = counts.all[kTries - 1], next = counts.before[kTries - 1];
+  const Sum<kCutTries> counts = sum_over(tried, 0, s_sum, each_wave);
+  int per = cut.hi;
 #pragma unroll
-  for (int k = kTries - 2; k >= 0; --k) {
-    if (counts.all[k] <= groups) {
-      per = lo + (hi - lo) * k / (kTries - 1);
-      count = counts.all[k];
-      next = counts.before[k];
-    }
-  }
-  each_share<true>(a, b0, b1, mine, [&](int b, const Share &s) {
+  for (int k = kCutTries - 2; k >= 0; --k) per = counts.all[k] <= groups ? cut.at(k) : per;
+  int sizes[2] = {0, 0};                                      // workgroups, and those of what is cut
+  each_share<true>(a, b0, b1, mine, [&](int, const Share &s) {
     const int p = pieces_of(s.rounds, per) * s.walks;
-    if (me == 0) a.share[1 + b] = next;
-    if (me >= next && me < next + p) {
+    sizes[0] += p;
+    sizes[1] += s.rounds > per ? p : 0;
+  });
+  const Sum<2> units = sum_over(sizes, 0, s_sum, each_wave);
+  const bool crowded = units.all[0] > groups;
+  int next = units.before[0], place = units.before[1];
+  each_share<true>(a, b0, b1, mine, [&](int b, const Share &s) {
+    const int size = pieces_of(s.rounds, per) * s.walks, from = !crowded ? next : s.rounds > per ? place : units.all[1] + next - place;
+    if (me == 0) a.share[1 + b] = place;
+    if (me >= from && me < from + size) {
       s_sum[0] = b;
-      s_sum[1] = next;
+      s_sum[1] = from;
       s_sum[2] = s.n;
       s_sum[3] = s.len;
+      s_sum[4] = s.rounds > per ? place : -1;
     }
-    next += p;
+    next += size;
+    place += s.rounds > per ? size : 0;
   });
-  if (me == 0 && tid == 0) a.share[0] = per;
+  if (me == 0 && tid == 0) a.share[0] = units.all[1] > 0 ? per : 0;
   Wide w;
   w.t0 = w.t1 = 0;
-  if (me >= count) return w;
+  if (me >= units.all[0]) return w;
   __syncthreads();
   w.b = __builtin_amdgcn_readfirstlane(s_sum[0]);
   w.n = __builtin_amdgcn_readfirstlane(s_sum[2]);
   w.len = __builtin_amdgcn_readfirstlane(s_sum[3]);
-  const int begin = __builtin_amdgcn_readfirstlane(s_sum[1]), pieces = pieces_of(rounds_of<true>(a, w.n, w.len), per);
-  const Item item = item_at(me - begin, pieces * a.kv_heads, row_tiles_of(w.n * a.group));
+  const int from = __builtin_amdgcn_readfirstlane(s_sum[1]), part = __builtin_amdgcn_readfirstlane(s_sum[4]);
+  const int pieces = pieces_of(rounds_of<true>(a, w.n, w.len), per);
+  const Item item = item_at(me - from, pieces * a.kv_heads, row_tiles_of(w.n * a.group));
   const int p = item.unit % pieces;
   w.kvh = item.unit / pieces;
   w.tile_row = item.tile_row;
@@ -808,7 +828,7 @@ __device__ __forceinline__ Wide cut_rounds(const PagedArgs &a, int *s_sum) {
   const int all = w.tile.span.all();
   w.t0 = cut_at(all, pieces, p);
   w.t1 = cut_at(all, pieces, p + 1);
-  w.part = pieces == 1 ? -1 : me;
+  w.part = part < 0 ? -1 : part + me - from;
   __syncthreads();
   return w;
 }
@@ -1127,21 +1147,20 @@ paged_attend_kernel(PagedArgs a) {
 // nodes, rows of two or three pieces: 16.3 -> 13.4 us).  The rows' first pieces loaded beside the statistics
 // gained 0.1 us for one token and cost the trees 1.
 template <typename T, bool WIDE>
-__global__ void __launch_bounds__(kThreads)
-merge_pages_kernel(PagedArgs a) {
+__device__ __forceinline__ void join_rows(const PagedArgs &a, int block, int per) {
   constexpr int kHeads = kThreads / 32;
   const int lane = lane_id(), l32 = lane & 31;
-  const int head_blocks = (a.q_heads + kHeads - 1) / kHeads, bs = blockIdx.x / head_blocks;
+  const int head_blocks = (a.q_heads + kHeads - 1) / kHeads, bs = block / head_blocks;
   const int b = bs / a.slots, slot = bs - b * a.slots;
   const Sizes sz = sizes_of(a, b);
   if (slot >= sz.n) return;
-  const int head = (blockIdx.x - bs * head_blocks) * kHeads + threadIdx.x / 32;
+  const int head = (block - bs * head_blocks) * kHeads + threadIdx.x / 32;
   if (head >= a.q_heads) return;
   const int64_t r = static_cast<int64_t>(bs) * a.q_heads + head;
   const int kvh = head / a.group, row = slot * a.group + head - kvh * a.group;
   const int height = WIDE ? height_of(sz.n * a.group) : a.tile_rows, tile_row = row / height, local = row - tile_row * height;
   const int row_tiles = row_tiles_of(sz.n * a.group);
-  const int rounds = rounds_of<WIDE>(a, sz.n, sz.len), per = a.share[0];
+  const int rounds = rounds_of<WIDE>(a, sz.n, sz.len);
   int g0, pieces;
   if (WIDE) {
     pieces = pieces_of(rounds, per);
@@ -1200,6 +1219,18 @@ merge_pages_kernel(PagedArgs a) {
         u32x2{T::pack(x.x * inv, x.y * inv), T::pack(x.z * inv, x.w * inv)};
   if (a.lse && l32 == 0) finish(a, r, top, l, now.at);
 }
+// MANY: of calls with many row tiles, which mostly cut none.
+template <typename T, bool WIDE, bool MANY>
+__global__ void __launch_bounds__(kThreads)
+merge_pages_kernel(PagedArgs a) {
+  const int per = a.share[0];
+  if (per == 0) return;
+  if constexpr (MANY) {
+    for (int block = blockIdx.x; block < a.joins; block += gridDim.x) join_rows<T, WIDE>(a, block, per);
+  } else {
+    join_rows<T, WIDE>(a, blockIdx.x, per);
+  }
+}
 
 Pool pool_of(const graft_rows &r, int bytes) {
   Pool p;
@@ -1230,27 +1261,32 @@ PagedPlan paged_plan(const graft_paged_attention_desc &a) {
   const int keys = p.few ? kFewKeys * kWaves : kWideKeys;
   int64_t most = static_cast<int64_t>(a.pages.table_len) * a.pages.page_rows;
   if (a.window > 0) most = std::min<int64_t>(most, static_cast<int64_t>(a.window) + a.sinks + a.slots + 2 * keys);
-  const int64_t rounds = (most + keys - 1) / keys;
-  p.fits = outer * p.row_tiles * rounds < (int64_t{1} << 31);
+  const int64_t rounds = (most + keys - 1) / keys, tiles = outer * p.row_tiles;
+  p.fits = tiles * rounds < (int64_t{1} << 31) - 1024;       // sums are rounded up to workgroups
   if (p.few) {
     // as many as the registers let run at once (the windows: 95, 94 and 97 us with 256, 512 and 1024
     // workgroups; e4m3 rows take fewer registers, and 512 and 768 come out alike)
     p.blocks = std::min<int64_t>(outer * rounds, a.cache_dtype == GRAFT_E4M3 ? 768 : 512);
-  } else if (outer * p.row_tiles < kWideBlocks && rounds > 1) {
-    // what registers and LDS let run at once (16 trees of up to 64 nodes: 91, 106, 112 and 111 us with 512, 640,
-    // 768 and 1024); row tiles that are that many walk on their own (pieces of 1024 slots over up to 4096
-    // rows: one, 256 row tiles, 123 us cut and 130 whole; two, three and four 175, 240 and 302 cut, 163, 219
-    // and 274 whole; 64 trees of up to 7 nodes 145 and 139; but 32 of up to 32, with half of the row tiles
-    // empty, 97 and 121)
-    p.blocks = std::min<int64_t>(outer * p.row_tiles * rounds, kWideBlocks);
+  } else if (rounds > 1 && (tiles < kWideBlocks || (rounds > kLongRounds && p.fits && tiles + kWideBlocks <= kMaxBlocks))) {
+    // kWideBlocks is what registers and LDS let run at once (16 trees of up to 64 nodes: 91, 106, 112 and 111 us with
+    // 512, 640, 768 and 1024 pieces); with more row tiles the longest walks are cut, since one long sequence
+    // among short ones would leave the chip to a workgroup for each of its row tiles: over 65,536 rows beside 63 over
+    // 500, trees of up to 7 nodes 104 us, whole 1292, trees of up to 64 nodes 184 and 1434; 64 trees of up to
+    // 32 nodes over up to 4096 rows, half of whose row tiles are empty, 155 and 210.  Where little is cut that
+    // costs the second launch: 64 trees of up to 7 nodes 141 and 136, 8 pieces of 1024 prompt rows 478 and 470.
+    // Walks of up to kLongRounds are short enough to be left whole (one over 4096 rows beside 63 over 500:
+    // 106 cut and 107 whole; 64 trees of up to 7 nodes over up to 300 rows 22.4 and 18.6).
+    p.blocks = std::min(tiles * rounds, std::max<int64_t>(kWideBlocks, tiles + kWideBlocks / 2));
   } else {
     p.fits = true;
-    p.blocks = outer * p.row_tiles;
+    p.blocks = tiles;
     return p;
   }
   constexpr int kHeads = kThreads / 32;                     // of a workgroup of the merge
-  p.merge_blocks = rounds > 1 ? static_cast<int64_t>(a.batch) * a.slots * ((a.q_heads + int64_t{kHeads} - 1) / kHeads) : 0;
-  p.part_rows = p.blocks * (p.few ? 2 * p.tile_rows : kWideRows);
+  p.joins = rounds > 1 ? static_cast<int64_t>(a.batch) * a.slots * ((a.q_heads + int64_t{kHeads} - 1) / kHeads) : 0;
+  p.many = !p.few && p.joins > 2 * kMergeBlocks;
+  p.merge_blocks = p.many ? std::min<int64_t>(p.joins, kMergeBlocks) : p.joins;
+  p.part_rows = p.few ? p.blocks * 2 * p.tile_rows : std::min<int64_t>(p.blocks, kWideBlocks) * kWideRows;
   p.share_at = p.part_rows * (a.head_dim * int64_t{4} + 8);
   p.bytes = p.share_at + (a.batch + int64_t{1}) * 4;
   return p;
@@ -1293,6 +1329,7 @@ hipError_t launch_paged_attend(graft_ctx *ctx, const graft_paged_attention_desc 
   a.tile_rows = p.tile_rows;
   a.row_tiles = p.row_tiles;
   a.cut = !p.few && p.bytes > 0 ? 1 : 0;
+  a.joins = static_cast<int32_t>(p.joins);
   a.c = d.scale * 1.4426950408889634f;
   const dim3 grid(static_cast<unsigned>(p.blocks)), block(kThreads);
   auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };
@@ -1321,13 +1358,14 @@ hipError_t launch_paged_attend(graft_ctx *ctx, const graft_paged_attention_desc 
   if (e != hipSuccess || p.merge_blocks == 0) return e;
   const dim3 mgrid(static_cast<unsigned>(p.merge_blocks));
   auto merge = [&](auto kernel) { hipLaunchKernelGGL(kernel, mgrid, block, 0, stream, a); };
-  if (d.dtype == GRAFT_F16) {
-    if (p.few) merge(merge_pages_kernel<F16, false>);
-    else merge(merge_pages_kernel<F16, true>);
-  } else {
-    if (p.few) merge(merge_pages_kernel<Bf16, false>);
-    else merge(merge_pages_kernel<Bf16, true>);
-  }
+  auto join = [&](auto type) {
+    using T = decltype(type);
+    if (p.few) merge(merge_pages_kernel<T, false, false>);
+    else if (p.many) merge(merge_pages_kernel<T, true, true>);
+    else merge(merge_pages_kernel<T, true, false>);
+  };
+  if (d.dtype == GRAFT_F16) join(F16{});
+  else join(Bf16{});
   return hipGetLastError();
 }
 

@@ -99,6 +99,34 @@ __host__ __device__ __forceinline__ int cut_at(int n, int pieces, int p) {
   return static_cast<int>(static_cast<int64_t>(n) * p / pieces);
 }
 
+// How the wide walk's workgroups share the rounds of all walks (a walk: a row tile's over the keys of its
+// sequence and key head): one of more than `per` rounds is cut into ceil(rounds / per) even pieces.  per is the
+// least of kCutTries between lo and hi for which all walks and pieces run at once, in `groups` workgroups; or hi.
+//   lo: what a workgroup has to do if nothing were rounded up; a join holds kMaxPieces pieces.
+//   hi: what fits into the workgroups that are not needed for walks, whatever is rounded up.  Where these are
+//       less than a quarter hi would be large, and the longest walks would be walked alone: then twice an even share,
+//       and not all run at once.
+// Walks of more than twice an even share are less than groups / 2, and so are the pieces added to
+// them: there are at most max(groups, walks + groups / 2) workgroups, and at most `groups` pieces of cut walks.
+constexpr int kMaxPieces = 128;                   // of a row's keys: four a lane of the merge
+constexpr int kCutTries = 4;
+struct Cut {
+  int lo, hi;
+  __host__ __device__ __forceinline__ int at(int k) const { return lo + (hi - lo) * k / (kCutTries - 1); }
+};
+__host__ __device__ __forceinline__ int pieces_of(int rounds, int per) { return (rounds + per - 1) / per; }
+// all: rounds of all walks; most: of the longest
+__host__ __device__ __forceinline__ Cut cut_of(int all, int walks, int most, int groups) {
+  const int share = pieces_of(all, groups), join = pieces_of(most, kMaxPieces), spare = groups - walks;
+  Cut c;
+  c.lo = share > join ? share : join;
+  c.lo = c.lo > 1 ? c.lo : 1;
+  c.hi = 4 * spare >= groups ? pieces_of(all, spare) : 2 * share;
+  c.hi = c.hi < most ? c.hi : most;
+  c.hi = c.hi > c.lo ? c.hi : c.lo;
+  return c;
+}
+
 // Whether every slot of the tile sees all rows j .. j + keys - 1.
 __host__ __device__ __forceinline__ bool is_clear(const RowTile &t, int j, int keys, int sinks) {
   return j + keys <= t.clear_end && (j >= t.clear_low || j + keys <= sinks);

@@ -1105,21 +1105,28 @@ class Context:
         return k, v, quant, at
 
     def _table(self, page_table, batch):
-        """Extents of a page table [batch or more, pages of a sequence], for _args."""
+        """(address, distance of its rows, pages of a sequence) of a page table [batch or more, n]."""
         if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2:
             raise ValueError("page_table must be [batch, pages of a sequence]")
-        n = page_table.shape[1]
+        if page_table.dtype is not torch.int32:
+            raise TypeError("page_table must be torch.int32, got %s" % page_table.dtype)
+        rows, n = page_table.shape
+        if rows < batch or n < 1:
+            _need(page_table, "page_table", (batch,), (1,))
         if n > _INT32_MAX:
             _fits(n, "page_table")
-        return ("page_table", page_table, torch.int32, ((batch,), (1,)), (batch, n))
+        stride, unit = page_table.stride()
+        if unit != 1 and n > 1:
+            raise ValueError("page_table must have unit stride along its last dimension")
+        return page_table.data_ptr(), stride if batch > 1 else 0, n
 
     def paged_write(self, cache, page_table, k, v, n_rows=None, start=None, q=None, q_out=None, freq=None,
                     positions=None, axis=None, interleaved=False):
         """Rotates a block's queries and keys and appends keys and values to pages
         (graft_paged_write).  cache: a pair of [pages, page_rows, kv_heads, dim] keys and
         values of one layer, tensors of k's type or QuantRows (bfloat16 rows), paged_cache's
-        for one; page_table [batch, n] int32: row r of sequence b is row r % page_rows
-        of page page_table[b, r // page_rows].  k, v [batch, slots, kv_heads, dim] and q
+        for one; page_table [batch, n] int32 (columns of a wider table, too): row r of sequence
+        b is row r % page_rows of page page_table[b, r // page_rows].  k, v [batch, slots, kv_heads, dim] and q
         [batch, slots, q_heads, dim], bfloat16 or float16: slot i < n_rows[b] (None: all)
         goes to row start[b] + i (None: 0).  freq [rot / 2] float64, radians a position,
         rotates the first rot numbers of every head of q and k, in pairs (f, f + rot / 2)
@@ -1175,17 +1182,17 @@ class Context:
         elif axis is not None:
             raise ValueError("axis needs positions")
         dtype, one, i32, dev = _DTYPES[kind], (B,), torch.int32, self._device
-        table = self._table(page_table, B)
-        p_table, p_n, p_start = _at(page_table, i32, table[4], dev), _at(n_rows, i32, one, dev), _at(start, i32, one, dev)
+        table, table_stride, n = self._table(page_table, B)
+        p_n, p_start = _at(n_rows, i32, one, dev), _at(start, i32, one, dev)
         p_pos, p_axis, p_freq = 0, 0, 0
         if F:
             p_pos, p_axis = _at(positions, i32, (axes, B, S), dev), _at(axis, i32, (F,), dev)
             p_freq = _at(freq, torch.float64, (F,), dev)
-        if (p_table < 0 or p_n < 0 or p_start < 0 or p_pos < 0 or p_axis < 0 or p_freq < 0
-                or not self._all_here((k, v, q, q_out, ck, cv))):
-            p_table, p_n, p_start, p_pos, p_axis, p_freq = [p or 0 for p in self._args(
-                (("k", k), ("v", v), ("q", q), ("q_out", q_out), ("cache keys", ck), ("cache values", cv)),
-                table,
+        if (p_n < 0 or p_start < 0 or p_pos < 0 or p_axis < 0 or p_freq < 0
+                or not self._all_here((k, v, q, q_out, ck, cv, page_table))):
+            p_n, p_start, p_pos, p_axis, p_freq = [p or 0 for p in self._args(
+                (("k", k), ("v", v), ("q", q), ("q_out", q_out), ("cache keys", ck), ("cache values", cv),
+                 ("page_table", page_table)),
                 ("n_rows", n_rows, i32, one, one),
                 ("start", start, i32, one, one),
                 ("positions", positions, i32, ((1,), B, S), (axes, B, S)),
@@ -1196,11 +1203,11 @@ class Context:
             if q_out is None:
                 q_out = torch.zeros_like(q, memory_format=torch.contiguous_format)
             queries = _row_at(q, B, S, Hq, D, "q") + _row_at(q_out, B, S, Hq, D, "q_out")
-        n, pool = page_table.shape[1], ck.shape
+        pool = ck.shape
         desc = _PACK_ROWS[quant].pack(
             B, S, Hq, H, D, 2 * F, 1 if interleaved else 0, dtype, 3 if quant else dtype, *queries,
-            *_row_at(k, B, S, H, D, "k"), *_row_at(v, B, S, H, D, "v"), *pools, p_table, n, n, pool[0], pool[1],
-            p_n, p_start, p_pos, axes, p_axis, p_freq)
+            *_row_at(k, B, S, H, D, "k"), *_row_at(v, B, S, H, D, "v"), *pools, table, table_stride, n,
+            pool[0], pool[1], p_n, p_start, p_pos, axes, p_axis, p_freq)
         _check(lib().graft_paged_write(self._h, desc, _stream()), "graft_paged_write")
         return q_out
 
@@ -1278,26 +1285,24 @@ class Context:
         N = self.dims.max_nodes
         W = (N + 63) // 64
         one, i32, dev = (B,), torch.int32, self._device
-        table = self._table(page_table, B)
-        p_table, p_len, p_n = (_at(page_table, i32, table[4], dev), _at(cache_len, i32, one, dev),
-                               _at(n_nodes, i32, one, dev))
+        table, table_stride, n = self._table(page_table, B)
+        p_len, p_n = _at(cache_len, i32, one, dev), _at(n_nodes, i32, one, dev)
         p_mask, p_lse = _at(mask, torch.int64, (B, N, W), dev), _at(lse, torch.float32, (B, S, Hq), dev)
-        if (p_table < 0 or p_len < 0 or p_n < 0 or p_mask < 0 or p_lse < 0
-                or not self._all_here((q, out, ck, cv))):
-            p_table, p_len, p_n, p_mask, p_lse = [p or 0 for p in self._args(
-                (("q", q), ("out", out), ("cache keys", ck), ("cache values", cv)),
-                table,
+        if (p_len < 0 or p_n < 0 or p_mask < 0 or p_lse < 0
+                or not self._all_here((q, out, ck, cv, page_table))):
+            p_len, p_n, p_mask, p_lse = [p or 0 for p in self._args(
+                (("q", q), ("out", out), ("cache keys", ck), ("cache values", cv), ("page_table", page_table)),
                 ("cache_len", cache_len, i32, one, one),
                 ("n_nodes", n_nodes, i32, one, one),
                 ("mask", mask, torch.int64, (one, N, W), (B, N, W)),
                 ("lse", lse, torch.float32, (B, S, Hq), (B, S, Hq)))]
         if out is None:
             out = torch.zeros_like(q, memory_format=torch.contiguous_format)
-        dtype, n, pool = _DTYPES[kind], page_table.shape[1], ck.shape
+        dtype, pool = _DTYPES[kind], ck.shape
         desc = _PACK_ATTENTION[quant].pack(
             B, S, 1 if with_root else 0, Hq, H, D, dtype, 3 if quant else dtype,
             float(D ** -0.5 if scale is None else scale), window, sinks, *_row_at(q, B, S, Hq, D, "q"), p_n, p_mask,
-            *pools, p_table, n, n, pool[0], pool[1], p_len, *_row_at(out, B, S, Hq, D, "out"), p_lse, 0, 0)
+            *pools, table, table_stride, n, pool[0], pool[1], p_len, *_row_at(out, B, S, Hq, D, "out"), p_lse, 0, 0)
         return desc, out
 
     def paged_commit(self, cache, page_table, start, acc_len, acc_nodes, with_root=False):
@@ -1325,13 +1330,12 @@ class Context:
         if acc_nodes is None:
             raise ValueError("acc_nodes is required")
         L, one, i32, dev = self.dims.num_pos, (batch,), torch.int32, self._device
-        table = self._table(page_table, batch)
-        p_table, p_start = _at(page_table, i32, table[4], dev), _at(start, i32, one, dev)
+        table, table_stride, n = self._table(page_table, batch)
+        p_start = _at(start, i32, one, dev)
         p_acc, p_nodes = _at(acc_len, i32, one, dev), _at(acc_nodes, i32, (batch, L), dev)
-        if p_table < 0 or p_start < 0 or p_acc < 0 or p_nodes < 0 or not self._all_here((cache,)):
-            p_table, p_start, p_acc, p_nodes = [p or 0 for p in self._args(
-                (("cache", cache),),
-                table,
+        if p_start < 0 or p_acc < 0 or p_nodes < 0 or not self._all_here((cache, page_table)):
+            p_start, p_acc, p_nodes = [p or 0 for p in self._args(
+                (("cache", cache), ("page_table", page_table)),
                 ("start", start, i32, (one,), one),
                 ("acc_len", acc_len, i32, (one,), one),
                 ("acc_nodes", acc_nodes, i32, (one, L), (batch, L)))]
@@ -1340,10 +1344,9 @@ class Context:
             sc = cache.scales.stride()
             at += (cache.scales.data_ptr(), sc[0] if P > 1 else 0, sc[1] if pages > 1 else 0,
                    sc[2] if rows > 1 else 0, sc[3] if H > 1 else 0)
-        n = page_table.shape[1]
         desc = _PACK_PATH[quant].pack(
             batch, P, H, D, 3 if quant else _DTYPES.get(cache.dtype, -1), at[0], st[0] if P > 1 else 0, *at[1:],
-            p_table, n, n, pages, rows, p_start, p_acc, p_nodes, 1 if with_root else 0)
+            table, table_stride, n, pages, rows, p_start, p_acc, p_nodes, 1 if with_root else 0)
         _check(lib().graft_paged_commit(self._h, desc, _stream()), "graft_paged_commit")
         return cache
 

@@ -21,11 +21,11 @@
 // matrix, vector, LDS and load work that two waves a SIMD do not quite overlap.  Rounds of the narrow
 // walk are shared evenly over the chip, of the wide one the longest walks are cut, as the lengths on
 // the device say, and merge_pages_kernel joins what was cut.
-// Measured (in a graph, 32/8 heads of 128, the join included): 64 tokens over up to 8192 e4m3 rows 125 us
-// for 584 MB (4.7 TB/s), over bf16 rows 194 us for 1158 MB (6.0 TB/s); 32 windows of 4096 over up to
-// 16384 rows 97 us for 504 MB (5.2 TB/s; plain reads of as large pieces reach 5.8, 6.6 non-temporal); 16
-// trees of up to 64 nodes over up to 4096 rows 82 us for 30 GFLOP and 167 MB; 8 pieces of 1024 prompt
-// rows, windows of 2048, 335 us for 257 GFLOP (766 TFLOP/s); one token over 700 rows 13 us, two launches
+// Measured (in a graph, clocks settled, 32/8 heads of 128, the join included): 64 tokens over up to 8192 e4m3
+// rows 109 us for 584 MB (5.4 TB/s), over bf16 rows 195 us for 1158 MB (5.9 TB/s); 32 windows of 4096 over up
+// to 16384 rows 93 us for 504 MB (5.4 TB/s; plain reads of as large pieces reach 5.8, 6.6 non-temporal); 16
+// trees of up to 64 nodes over up to 4096 rows 80 us for 30 GFLOP and 167 MB; 8 pieces of 1024 prompt
+// rows, windows of 2048, 331 us for 257 GFLOP (774 TFLOP/s); one token over 700 rows 13 us, two launches
 // and their dependent loads.
 //
 // Hidden keys.  A tile whose keys all query rows see (most of them) takes no masks.  In the others
@@ -221,8 +221,8 @@ __device__ __forceinline__ void finish(const PagedArgs &a, int64_t all, float m,
 // Up to 16 rows, all of a sequence's and key head's, over tiles t0 .. t1 - 1: every wave walks 32-key tiles of
 // its own, keys from memory straight into fragments, values through a stretch of LDS of the wave's
 // own, no barriers; the waves' sums are joined at the end.  A tile is in flight while the one before it is
-// worked on.  The loads alone, with nothing done to what they bring, take 107 of the 125 us of 64
-// tokens over e4m3 rows and 90 of the 97 of the windows; two tiles in flight and 3 or 4 waves a SIMD gained
+// worked on.  The loads alone, with nothing done to what they bring, take 107 of 125 us of 64
+// tokens over e4m3 rows and 90 of 97 of the windows (before the clocks settle); two tiles in flight and 3 or 4 waves a SIMD gained
 // nothing.
 // part: where in the workspace the sums go, or -1: they are all there is.
 template <typename T, bool Q8, bool HOT, int DP>
@@ -1251,9 +1251,9 @@ PagedPlan paged_plan(const graft_paged_attention_desc &a) {
   PagedPlan p{};
   const int group = a.q_heads / a.kv_heads;
   const int64_t rows = static_cast<int64_t>(a.slots) * group, outer = static_cast<int64_t>(a.batch) * a.kv_heads;
-  // with 17 to 32 rows the wide walk, although half its waves are idle (8, 16 and 64 trees of up to 7 nodes over
-  // up to 4096 rows: 31.6, 49 and 145 us, and 42.7, 55 and 167 with two tiles of 16 rows a wave in the
-  // narrow one; only 64 chains of 8 over e4m3 rows lose, 102 -> 110)
+  // with 17 to 32 rows the wide walk, although three of its four waves have none (8, 16 and 64 trees of up to 7
+  // nodes over up to 4096 rows: 31, 49 and 142 us, and 42.7, 55 and 167 with two tiles of 16 rows a wave in
+  // the narrow one; only 64 chains of 8 over e4m3 rows lose, 102 and 108)
   p.few = rows <= kFewRows;
   p.row_tiles = p.few ? 1 : static_cast<int>((rows + kWideRows - 1) / kWideRows);
   p.tile_rows = p.few ? kFewRows : kWideRows;
@@ -1264,8 +1264,10 @@ PagedPlan paged_plan(const graft_paged_attention_desc &a) {
   const int64_t rounds = (most + keys - 1) / keys, tiles = outer * p.row_tiles;
   p.fits = tiles * rounds < (int64_t{1} << 31) - 1024;       // sums are rounded up to workgroups
   if (p.few) {
-    // as many as the registers let run at once (the windows: 95, 94 and 97 us with 256, 512 and 1024
-    // workgroups; e4m3 rows take fewer registers, and 512 and 768 come out alike)
+    // as many as the registers let run at once, of e4m3 rows three a CU (the windows: 95, 94 and 97 us with 256,
+    // 512 and 1024 workgroups; e4m3 rows with 512 and 768: 64 tokens over 8192 113 and 111, 128 over 2000 83 and 75,
+    // 64 over 500 30 and 26, chains of 4 82 and 76, heads of 64 72 and 65; but 16 tokens over 8192 40 and
+    // 44, one over 65,536 39 and 45, and the general form, two a CU, 118 and 136)
     p.blocks = std::min<int64_t>(outer * rounds, a.cache_dtype == GRAFT_E4M3 ? 768 : 512);
   } else if (rounds > 1 && (tiles < kWideBlocks || (rounds > kLongRounds && p.fits && tiles + kWideBlocks <= kMaxBlocks))) {
     // kWideBlocks is what registers and LDS let run at once (16 trees of up to 64 nodes: 91, 106, 112 and 111 us with

@@ -46,8 +46,8 @@ constexpr int kWaves = kThreads / kWave;
 constexpr int kWideKeys = 64;                     // wide_part
 constexpr int kFewRows = 16, kFewKeys = 32;       // narrow_part; keys of one wave's tile
 constexpr int kWideBlocks = 512;                  // two a CU
-constexpr int kLongRounds = 64;                   // the fewest that many row tiles' walks are cut for
-constexpr int kMergeBlocks = 4096;                // of a merge that mostly finds nothing to do
+constexpr int kLongRounds = 64;                   // of a walk that is left whole where row tiles fill the chip
+constexpr int kMergeBlocks = 4096;                // of a merge of twice as much and more, which mostly finds nothing to do
 
 struct Pool {                 // keys or values of one layer; bytes
   const char *p;
@@ -222,7 +222,8 @@ __device__ __forceinline__ void finish(const PagedArgs &a, int64_t all, float m,
 // its own, keys from memory straight into fragments, values through a stretch of LDS of the wave's
 // own, no barriers; the waves' sums are joined at the end.  A tile is in flight while the one before it is
 // worked on.  The loads alone, with nothing done to what they bring, take 107 of 125 us of 64
-// tokens over e4m3 rows and 90 of 97 of the windows (before the clocks settle); two tiles in flight and 3 or 4 waves a SIMD gained
+// tokens over e4m3 rows and 90 of 97 of the windows (before the clocks settle); two tiles in flight and 3
+// or 4 waves a SIMD gained
 // nothing.
 // part: where in the workspace the sums go, or -1: they are all there is.
 template <typename T, bool Q8, bool HOT, int DP>
